@@ -194,6 +194,104 @@ int fastkv_prefill_attention(const fastkv_shape* shape, const void* q, const voi
                              void* stream);
 
 /*
+ * Paged cache: where the kept entries of Alg. 1 go when decoding continues behind them.  Entry t of sequence b is row
+ * t % page_size of page block_table[b][t / page_size]; K and V pools are [n_pages, n_kv_heads, page_size, head_dim], dense,
+ * 16-byte aligned.  FASTKV_CACHE_BF16: bf16 values.  FASTKV_CACHE_E4M3: 8-bit floating-point codes (4 exponent bits, 3
+ * mantissa bits, largest value 448) that stand for code * scale, with one scale for each page and KV head in
+ * k_scales / v_scales, fp32 [n_pages, n_kv_heads]; scales are powers of two from 2^-64 to 2^120, written by
+ * fastkv_paged_append.  Pages may be shared between sequences for reading; a page that a call appends to belongs to one
+ * sequence.  All pointers are DEVICE memory of the device that is current at the call.
+ */
+enum { FASTKV_CACHE_BF16 = 0, FASTKV_CACHE_E4M3 = 1 };
+enum { FASTKV_ROT_HALVES = 0, FASTKV_ROT_ADJACENT = 1 };
+
+typedef struct fastkv_paged_cache {
+  int32_t batch;             /* B >= 1: rows of block_table                                          */
+  int32_t max_pages;         /* pages a row of block_table has room for                              */
+  int32_t n_pages;           /* pages in the pools                                                   */
+  int32_t page_size;         /* 16, 32, 64 or 128 entries                                            */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128                                                            */
+  int32_t format;            /* FASTKV_CACHE_BF16 | FASTKV_CACHE_E4M3                                */
+  int32_t reserved;          /* 0                                                                    */
+  void* k_pages;
+  void* v_pages;
+  float* k_scales;           /* FASTKV_CACHE_E4M3 only, else NULL                                    */
+  float* v_scales;
+  const int32_t* block_table;/* DEVICE int32 [batch, max_pages]                                      */
+} fastkv_paged_cache;
+
+/*
+ * The rows one fastkv_paged_append call brings.  Sequence b owns rows cu_new[b] .. cu_new[b+1]-1 of the call's
+ * [total] rows (cu_new == NULL: max_new rows each, total == batch * max_new); they become its entries lens[b],
+ * lens[b] + 1, ...
+ *   Source, new tokens (total_src == 0): k, v [total, n_kv_heads, head_dim] and, with n_q_heads > 0, q
+ *     [total, n_q_heads, head_dim], bf16, strides in elements.
+ *   Source, kept rows (total_src > 0): row r of KV head g is row cu_src[b] + idx[g, r] of k and v
+ *     [total_src, n_kv_heads, head_dim], idx int32 [n_kv_heads, total] sequence-local as fastkv_select_kv writes it
+ *     (cu_src == NULL when batch == 1): what fastkv_compact would copy, straight into pages.  No rotation then (the keys
+ *     were rotated before they were scored) and no queries.
+ *   Rotation (rot_dim > 0): the first rot_dim elements of every query and key head, at position pos[r] of its row; pairs
+ *     (i, i + rot_dim / 2) for FASTKV_ROT_HALVES, (2 i, 2 i + 1) for FASTKV_ROT_ADJACENT, angle pos * inv_freq[i]
+ *     (formed in 64 bits).  Positions are independent of slots: the cache holds fewer entries than the prompt had tokens.
+ */
+typedef struct fastkv_new_rows {
+  int32_t total;             /* >= 1                                                                 */
+  int32_t max_new;           /* HOST: most rows any sequence brings (grid sizing, validation)        */
+  int32_t n_q_heads;         /* 0: no queries; else a multiple of n_kv_heads                         */
+  int32_t rot_dim;           /* 0: no rotation; else a multiple of 16, <= head_dim                   */
+  int32_t rot_pairs;         /* FASTKV_ROT_HALVES | FASTKV_ROT_ADJACENT                              */
+  int32_t total_src;         /* 0, or the rows of k / v that idx points into                         */
+  const int32_t* cu_new;     /* DEVICE int32 [batch + 1] or NULL                                     */
+  const int32_t* cu_src;     /* DEVICE int32 [batch + 1] or NULL                                     */
+  int64_t q_stride_tok, q_stride_head;   /* elements; multiples of 8                                 */
+  int64_t k_stride_tok, k_stride_head;
+  int64_t v_stride_tok, v_stride_head;
+} fastkv_new_rows;
+
+/*
+ * Appends `rows` behind the lens[b] entries of every sequence, in one launch.  lens: DEVICE int32 [batch], read only;
+ * new_lens (may be NULL, must not overlap lens): DEVICE int32 [batch], receives lens[b] plus the rows written.
+ * q_out: bf16, dense [total, n_q_heads, head_dim], the rotated queries; may be q itself when q is dense.
+ * Bf16 pages and q_out: rotated in fp32, rounded once.  8-bit pages: a page that had entries keeps its scale unless a new
+ * row needs a larger one (the smallest 2^e with 448 * 2^e >= the largest absolute value), in which case the entries that
+ * were there are re-encoded, code * old / new, rounded to nearest even; a page without entries takes the scale its new rows
+ * need.  Codes are rounded once, from fp32, to nearest even.  Entries behind the new length and pages that no row falls in
+ * are left as they were.
+ * Reported in the status word (FASTKV_ERR_DEVICE_INDEX), never dereferenced: a page id outside the pool, an index outside
+ * its sequence, rows beyond max_new, total or the block table's room; those rows are not written.  The status word is not
+ * cleared by this call.  workspace: 256 bytes (the header), 256-byte aligned.  Calls that write the same sequences must be
+ * ordered.
+ */
+int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* rows, const int32_t* lens, const void* q,
+                        const void* k, const void* v, const int32_t* pos, const float* inv_freq, const int32_t* idx,
+                        void* q_out, int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of q_len new query tokens per sequence over the paged cache (Sec. 3, Sec. 5.3: decoding over the kept entries
+ * and those appended since).  lens: DEVICE int32 [batch], the entries of each sequence, those of the new tokens included;
+ * query token i of sequence b sees entries 0 .. lens[b] - (q_len - 1 - i) - 1:
+ *   out[b, i, h, :] = sum_t softmax_t(scale * <q[b, i, h], K[t, h / G]>) * V[t, h / G, :]
+ * q: bf16, dense [batch, q_len, n_q_heads, head_dim], 16-byte aligned; out: fp32, the same shape; lse (optional): fp32
+ * [batch, q_len, n_q_heads], natural log.  A query that sees no entry gives out 0 and lse -infinity.
+ * max_len and total_len are what the HOST knows of lens (their maximum and sum, or bounds); they size the launch, and
+ * results do not depend on them beyond rounding.  A length beyond the block table's room is cut to it, a page id outside the
+ * pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
+ * workspace: >= fastkv_paged_attn_workspace_bytes for this cache and query, 256-byte aligned; not shared by calls that
+ * may overlap.
+ */
+typedef struct fastkv_query {
+  int32_t n_q_heads;         /* a multiple of the cache's n_kv_heads                                 */
+  int32_t q_len;             /* query tokens per sequence, >= 1                                      */
+  int32_t max_len;           /* HOST: longest length, >= 1                                           */
+  float softmax_scale;       /* 0 => 1/sqrt(head_dim)                                                */
+  int64_t total_len;         /* HOST: sum of lengths; 0 => batch * max_len                           */
+} fastkv_query;
+int fastkv_paged_attn_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_query* query, size_t* bytes);
+int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query, const int32_t* lens, const void* q,
+                      float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Synchronises `stream`, then copies the device status word of `workspace` to the HOST
  * integers *status (a fastkv_status) and *site (which wait or check raised it; 0 if none).
  */
@@ -276,7 +374,7 @@ int fastkv_debug_set(const char* key, int64_t value);
 /*
  * Sum of the device durations (HOST double, milliseconds) and number of launches recorded for one
  * kernel class since the last query (0 scoring kernel, 1 pooling kernel, 2 selection, 3 compaction,
- * 4 decode attention, 5 prefill attention, 6 window scores); waits for the recorded launches and forgets them.  *name receives a static
+ * 4 decode attention, 5 prefill attention, 6 window scores, 7 paged append, 8 paged attention); waits for the recorded launches and forgets them.  *name receives a static
  * string.  Any of the three outputs may be NULL.  No counterpart in the paper (measurement aid).
  */
 int fastkv_debug_kernel_time(int32_t kernel, double* total_ms, int64_t* launches, const char** name);

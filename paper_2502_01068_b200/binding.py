@@ -19,10 +19,13 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_DEVICE_TIMEOUT, E
 POOL_AVG, POOL_MAX = 0, 1
 GROUP_THEN_POOL, POOL_THEN_GROUP = 0, 1
 Q_FULL, Q_WINDOW = 0, 1
+CACHE_BF16, CACHE_E4M3 = 0, 1
+ROT_HALVES, ROT_ADJACENT = 0, 1
 
 EXPORTS = ["fastkv_workspace_bytes", "fastkv_score", "fastkv_select_kv", "fastkv_select_tsp", "fastkv_select",
            "fastkv_compact", "fastkv_decode_attn_workspace_bytes", "fastkv_decode_attn", "fastkv_prefill_workspace_bytes",
-           "fastkv_prefill_attention", "fastkv_device_status", "fastkv_layer_host_arena_bytes",
+           "fastkv_prefill_attention", "fastkv_paged_append", "fastkv_paged_attn_workspace_bytes", "fastkv_paged_attn",
+           "fastkv_device_status", "fastkv_layer_host_arena_bytes",
            "fastkv_layer_host", "fastkv_score_static", "fastkv_score_static_status", "fastkv_debug_set",
            "fastkv_debug_kernel_time",
            "fastkv_status_string", "fastkv_last_error", "fastkv_kernel_launches"]
@@ -58,6 +61,31 @@ class Budget(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int32), ("total", ctypes.c_int32), ("cu_k", ctypes.c_void_p)]
 
 
+class PagedCache(ctypes.Structure):
+    """fastkv_paged_cache"""
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
+
+
+class NewRows(ctypes.Structure):
+    """fastkv_new_rows"""
+    _fields_ = [("total", ctypes.c_int32), ("max_new", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("rot_pairs", ctypes.c_int32), ("total_src", ctypes.c_int32),
+                ("cu_new", ctypes.c_void_p), ("cu_src", ctypes.c_void_p),
+                ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("k_stride_tok", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64)]
+
+
+class Query(ctypes.Structure):
+    """fastkv_query"""
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("q_len", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("total_len", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -89,6 +117,10 @@ def _load():
         lib.fastkv_decode_attn.argtypes = [ps, vp, vp, vp, pb, vp, vp, vp, sz, vp]
         lib.fastkv_prefill_workspace_bytes.argtypes = [ps, ctypes.POINTER(sz)]
         lib.fastkv_prefill_attention.argtypes = [ps, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        pc, pn, pq = ctypes.POINTER(PagedCache), ctypes.POINTER(NewRows), ctypes.POINTER(Query)
+        lib.fastkv_paged_append.argtypes = [pc, pn] + [vp] * 10 + [sz, vp]
+        lib.fastkv_paged_attn_workspace_bytes.argtypes = [pc, pq, ctypes.POINTER(sz)]
+        lib.fastkv_paged_attn.argtypes = [pc, pq, vp, vp, vp, vp, vp, sz, vp]
         lib.fastkv_score_static_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
         lib.fastkv_debug_set.argtypes = [ctypes.c_char_p, ctypes.c_int64]
         lib.fastkv_debug_kernel_time.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_double),
@@ -219,6 +251,99 @@ def fastkv_prefill_attention(shape: Shape, q, k, v, out, scores_kv, scores_tsp, 
     _check(_load().fastkv_prefill_attention(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(out), _p(scores_kv),
                                             _p(scores_tsp), _p(workspace), workspace.numel() * workspace.element_size(),
                                             _stream(stream)), "fastkv_prefill_attention")
+
+
+def _page_format(pages: torch.Tensor) -> int:
+    if pages.dtype in (torch.bfloat16, torch.int16):
+        return CACHE_BF16
+    if pages.dtype in (torch.float8_e4m3fn, torch.uint8):
+        return CACHE_E4M3
+    raise TypeError("pages are bf16 (bfloat16, int16) or 8-bit (float8_e4m3fn, uint8), not %s" % pages.dtype)
+
+
+def make_paged_cache(k_pages, v_pages, block_table, k_scales=None, v_scales=None) -> PagedCache:
+    """Fill a fastkv_paged_cache from its tensors: pools [n_pages, n_kv_heads, page_size, head_dim], block_table int32
+    [batch, max_pages], and for 8-bit pages the scales, fp32 [n_pages, n_kv_heads].  All dense, on one device."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+        raise ValueError("k_pages and v_pages are [n_pages, n_kv_heads, page_size, head_dim], alike")
+    if block_table.dim() != 2 or block_table.dtype != torch.int32:
+        raise ValueError("block_table is int32 [batch, max_pages]")
+    fmt = _page_format(k_pages)
+    for s in (k_scales, v_scales):
+        if (s is not None) != (fmt == CACHE_E4M3):
+            raise ValueError("k_scales and v_scales go with 8-bit pages and only with them")
+        if s is not None and (s.dtype != torch.float32 or s.shape != k_pages.shape[:2]):
+            raise ValueError("scales are float32 [n_pages, n_kv_heads]")
+    parts = [x for x in (k_pages, v_pages, block_table, k_scales, v_scales) if x is not None]
+    if any(not x.is_contiguous() for x in parts) or any(x.device != k_pages.device for x in parts):
+        raise ValueError("the cache's tensors must be dense and on one device")
+    c = PagedCache()
+    c.batch, c.max_pages = block_table.shape
+    c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = k_pages.shape
+    c.format = fmt
+    c.k_pages, c.v_pages, c.block_table = _p(k_pages), _p(v_pages), _p(block_table)
+    c.k_scales, c.v_scales = _p(k_scales), _p(v_scales)
+    c._keep_alive = parts               # the struct only holds addresses: the tensors must outlive it
+    c._device = k_pages.device
+    return c
+
+
+def make_new_rows(*, batch: int, total: int, n_kv_heads: int, head_dim: int, max_new: Optional[int] = None, cu_new=None,
+                  n_q_heads: int = 0, rot_dim: int = 0, rot_pairs: int = ROT_HALVES, total_src: int = 0, cu_src=None,
+                  q_stride_tok: Optional[int] = None, q_stride_head: Optional[int] = None,
+                  k_stride_tok: Optional[int] = None, k_stride_head: Optional[int] = None,
+                  v_stride_tok: Optional[int] = None, v_stride_head: Optional[int] = None) -> NewRows:
+    """Fill a fastkv_new_rows; strides default to dense [rows, heads, head_dim] tensors, max_new to an even share (the whole
+    call when cu_new is given)."""
+    r = NewRows()
+    r.total = total
+    r.max_new = max_new if max_new is not None else (total if cu_new is not None else total // batch)
+    r.n_q_heads, r.rot_dim, r.rot_pairs, r.total_src = n_q_heads, rot_dim, rot_pairs, total_src
+    r.cu_new, r.cu_src = _p(cu_new), _p(cu_src)
+    r._keep_alive = (cu_new, cu_src)    # the struct only holds addresses: the tensors must outlive it
+    r.q_stride_head = head_dim if q_stride_head is None else q_stride_head
+    r.q_stride_tok = n_q_heads * head_dim if q_stride_tok is None else q_stride_tok
+    r.k_stride_head = head_dim if k_stride_head is None else k_stride_head
+    r.k_stride_tok = n_kv_heads * head_dim if k_stride_tok is None else k_stride_tok
+    r.v_stride_head = head_dim if v_stride_head is None else v_stride_head
+    r.v_stride_tok = n_kv_heads * head_dim if v_stride_tok is None else v_stride_tok
+    return r
+
+
+def make_query(*, n_q_heads: int, max_len: int, q_len: int = 1, total_len: int = 0, softmax_scale: float = 0.0) -> Query:
+    """Fill a fastkv_query."""
+    q = Query()
+    q.n_q_heads, q.q_len, q.max_len, q.softmax_scale, q.total_len = n_q_heads, q_len, max_len, softmax_scale, total_len
+    return q
+
+
+def _on_device(cache: PagedCache) -> None:
+    """The library launches on the current device: a cache that lives on another one is refused here."""
+    if cache._device.index != torch.cuda.current_device():
+        raise ValueError("the cache is on %s, the current device is cuda:%d" % (cache._device, torch.cuda.current_device()))
+
+
+def fastkv_paged_append(cache: PagedCache, rows: NewRows, lens, q, k, v, pos, inv_freq, idx, q_out, new_lens, workspace,
+                        stream=None) -> None:
+    """Append rows to the paged cache (new tokens, rotated by their positions, or the rows that idx names); see the header."""
+    _on_device(cache)
+    _check(_load().fastkv_paged_append(cache, rows, _p(lens), _p(q), _p(k), _p(v), _p(pos), _p(inv_freq), _p(idx), _p(q_out),
+                                       _p(new_lens), _p(workspace), workspace.numel() * workspace.element_size(),
+                                       _stream(stream)), "fastkv_paged_append")
+
+
+def fastkv_paged_attn_workspace_bytes(cache: PagedCache, query: Query) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_load().fastkv_paged_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(query), ctypes.byref(n)),
+           "fastkv_paged_attn_workspace_bytes")
+    return int(n.value)
+
+
+def fastkv_paged_attn(cache: PagedCache, query: Query, lens, q, out, lse, workspace, stream=None) -> None:
+    """Attention of query.q_len new tokens per sequence over the paged cache; see the header."""
+    _on_device(cache)
+    _check(_load().fastkv_paged_attn(cache, query, _p(lens), _p(q), _p(out), _p(lse), _p(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream(stream)), "fastkv_paged_attn")
 
 
 def fastkv_device_status(workspace, stream=None):

@@ -11,6 +11,7 @@
 
 #include "compact.cuh"
 #include "decode_attn.cuh"
+#include "paged.cuh"
 #include "prefill_attn.cuh"
 #include "score.cuh"
 #include "select.cuh"
@@ -52,9 +53,9 @@ DebugConfig g_debug;
 
 // ---- optional per-kernel timing ("time_kernels" hook): a pair of events around every launch ----------
 enum KernelId { KID_SCORE = 0, KID_POOL = 1, KID_SELECT = 2, KID_COMPACT = 3, KID_DECODE = 4, KID_PREFILL = 5,
-                KID_WINDOW_SCORES = 6, KID_COUNT = 7 };
+                KID_WINDOW_SCORES = 6, KID_PAGED_APPEND = 7, KID_PAGED_ATTN = 8, KID_COUNT = 9 };
 const char* const kKernelNames[KID_COUNT] = {"score", "pool", "select", "compact", "decode_attn", "prefill_attn",
-                                             "window_scores"};
+                                             "window_scores", "paged_append", "paged_attn"};
 struct KernelTimes {
   bool on = false;
   std::mutex mu;
@@ -802,6 +803,189 @@ int fastkv_prefill_attention(const fastkv_shape* shape, const void* q, const voi
   }
   if (e != cudaSuccess) return cuda_fail(e, "pool_rows_kernel launch");
   ++g_launches;
+  return FASTKV_OK;
+}
+
+// ---- paged cache ------------------------------------------------------------------------------------------
+namespace {
+int check_paged_cache(const fastkv_paged_cache* c) {
+  if (c == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged cache is NULL");
+  if (c->batch < 1 || c->max_pages < 1 || c->n_pages < 1 || c->n_kv_heads < 1)
+    return fail(FASTKV_ERR_INVALID_ARG, "paged cache: batch, max_pages, n_pages and n_kv_heads must be >= 1");
+  if (c->format != FASTKV_CACHE_BF16 && c->format != FASTKV_CACHE_E4M3) return fail(FASTKV_ERR_INVALID_ARG, "paged cache: unknown format");
+  if (c->reserved != 0) return fail(FASTKV_ERR_INVALID_ARG, "paged cache: reserved must be 0");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(FASTKV_ERR_UNSUPPORTED, "paged cache: head_dim must be 64 or 128");
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged cache: page_size must be 16, 32, 64 or 128");
+  if (static_cast<long long>(c->n_pages) * c->n_kv_heads > 0x7fffffffLL)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged cache: more than 2^31 - 1 (page, head) blocks");
+  if (static_cast<long long>(c->max_pages) * c->page_size > 0x7fffffffLL)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged cache: a block-table row holds more than 2^31 - 1 entries");
+  if (!c->k_pages || !c->v_pages || !c->block_table) return fail(FASTKV_ERR_INVALID_ARG, "paged cache: k_pages, v_pages and block_table are required");
+  if (reinterpret_cast<uintptr_t>(c->k_pages) % 16 || reinterpret_cast<uintptr_t>(c->v_pages) % 16)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged cache: the pools must be 16-byte aligned");
+  const bool scaled = c->format == FASTKV_CACHE_E4M3;
+  if (scaled != (c->k_scales != nullptr) || scaled != (c->v_scales != nullptr))
+    return fail(FASTKV_ERR_INVALID_ARG, "paged cache: k_scales and v_scales go with the 8-bit format and only with it");
+  return FASTKV_OK;
+}
+PagedView paged_view(const fastkv_paged_cache& c) {
+  PagedView v;
+  v.batch = c.batch; v.max_pages = c.max_pages; v.n_pages = c.n_pages; v.n_kv_heads = c.n_kv_heads;
+  v.page_log2 = c.page_size == 16 ? 4 : c.page_size == 32 ? 5 : c.page_size == 64 ? 6 : 7;
+  v.k_pages = static_cast<uint8_t*>(c.k_pages); v.v_pages = static_cast<uint8_t*>(c.v_pages);
+  v.k_scales = c.k_scales; v.v_scales = c.v_scales; v.block_table = c.block_table;
+  return v;
+}
+int check_strides(const char* name, int64_t tok, int64_t head, int head_dim, const void* base) {
+  if (tok % 8 || head % 8 || reinterpret_cast<uintptr_t>(base) % 16)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: %s needs a 16-byte aligned base and strides that are multiples of 8 elements", name);
+  if (tok < head_dim || head < head_dim) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: %s strides are smaller than head_dim", name);
+  return FASTKV_OK;
+}
+// One pool as a (column, row of the page, page x head) tensor; boxes of 16 rows x 128 bytes (64 for 8-bit rows of 64).
+int encode_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
+  const cuuint64_t item = e4m3 ? 1 : 2, row = c.head_dim * item;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size),
+                        static_cast<cuuint64_t>(c.n_pages) * c.n_kv_heads};
+  cuuint64_t strides[2] = {row, row * c.page_size};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(row > 128 ? 128 / item : c.head_dim), 16, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  row >= 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+  return FASTKV_OK;
+}
+int check_query(const fastkv_paged_cache* c, const fastkv_query* q) {
+  int rc = check_paged_cache(c);
+  if (rc) return rc;
+  if (q == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged_attn: query is NULL");
+  if (q->n_q_heads < 1 || q->n_q_heads % c->n_kv_heads) return fail(FASTKV_ERR_INVALID_ARG, "paged_attn: n_q_heads must be a positive multiple of n_kv_heads");
+  if (q->q_len < 1 || q->max_len < 1 || q->total_len < 0) return fail(FASTKV_ERR_INVALID_ARG, "paged_attn: need q_len >= 1, max_len >= 1 and total_len >= 0");
+  if (!(q->softmax_scale >= 0.0f) || std::isinf(q->softmax_scale)) return fail(FASTKV_ERR_INVALID_ARG, "softmax_scale must be finite and >= 0");
+  const long long rows = static_cast<long long>(q->q_len) * q->n_q_heads * c->batch;
+  if (rows > 0x7fffffffLL) return fail(FASTKV_ERR_UNSUPPORTED, "paged_attn: more than 2^31 - 1 query rows");
+  return FASTKV_OK;
+}
+PagedAttnPlan plan_of(const fastkv_paged_cache& c, const fastkv_query& q) {
+  const long long total = q.total_len > 0 ? q.total_len : static_cast<long long>(c.batch) * q.max_len;
+  return plan_paged_attn(c.batch, c.n_kv_heads, q.n_q_heads / c.n_kv_heads * q.q_len, c.head_dim, c.format == FASTKV_CACHE_E4M3,
+                         q.max_len, total);
+}
+}  // namespace
+
+int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* rows, const int32_t* lens, const void* q,
+                        const void* k, const void* v, const int32_t* pos, const float* inv_freq, const int32_t* idx,
+                        void* q_out, int32_t* new_lens, void* workspace, size_t workspace_bytes, void* stream_) {
+  int rc = check_paged_cache(cache);
+  if (rc) return rc;
+  if (rows == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: rows is NULL");
+  const fastkv_paged_cache& c = *cache;
+  const fastkv_new_rows& r = *rows;
+  if (!lens || !k || !v) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: lens, k and v are required");
+  if (r.total < 1 || r.max_new < 1 || r.max_new > r.total) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: need 1 <= max_new <= total");
+  if (r.cu_new == nullptr && static_cast<long long>(r.max_new) * c.batch != r.total)
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: without cu_new, total must equal batch * max_new");
+  if (r.n_q_heads < 0 || r.n_q_heads % c.n_kv_heads) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: n_q_heads must be a multiple of n_kv_heads");
+  if ((r.n_q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr))
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: q and q_out go with n_q_heads > 0 and only with it");
+  if (r.rot_dim < 0 || r.rot_dim > c.head_dim) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: rot_dim must be in 0 .. head_dim");
+  if (r.rot_dim % 16) return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: rot_dim must be a multiple of 16");
+  if (r.rot_pairs != FASTKV_ROT_HALVES && r.rot_pairs != FASTKV_ROT_ADJACENT) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: unknown rot_pairs");
+  if ((r.rot_dim > 0) != (pos != nullptr) || (r.rot_dim > 0) != (inv_freq != nullptr))
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: pos and inv_freq go with rot_dim > 0 and only with it");
+  if (reinterpret_cast<uintptr_t>(inv_freq) % 16) return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: inv_freq must be 16-byte aligned");
+  if (r.total_src < 0 || (r.total_src > 0) != (idx != nullptr))
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: idx goes with total_src > 0 and only with it");
+  if (idx != nullptr) {
+    if (r.rot_dim > 0 || q != nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: kept rows are neither rotated nor accompanied by queries");
+    if (c.batch > 1 && r.cu_src == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: cu_src is required with idx when batch > 1");
+  } else if (r.cu_src != nullptr) {
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: cu_src goes with idx");
+  }
+  if (new_lens != nullptr && new_lens < lens + c.batch && lens < new_lens + c.batch)
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_append: new_lens must not overlap lens");
+  if ((rc = check_strides("k", r.k_stride_tok, r.k_stride_head, c.head_dim, k)) ||
+      (rc = check_strides("v", r.v_stride_tok, r.v_stride_head, c.head_dim, v)))
+    return rc;
+  if (q != nullptr) {
+    if ((rc = check_strides("q", r.q_stride_tok, r.q_stride_head, c.head_dim, q))) return rc;
+    if (reinterpret_cast<uintptr_t>(q_out) % 16) return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: q_out must be 16-byte aligned");
+    if (q_out == q && (r.q_stride_head != c.head_dim || r.q_stride_tok != static_cast<int64_t>(r.n_q_heads) * c.head_dim))
+      return fail(FASTKV_ERR_INVALID_ARG, "paged_append: q_out may be q only when q is dense");
+  }
+  if ((rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader)))) return rc;
+  if ((rc = check_device())) return rc;
+  AppendParams p;
+  memset(&p, 0, sizeof p);
+  p.c = paged_view(c);
+  p.total = r.total; p.max_new = r.max_new; p.uniform = r.max_new; p.n_q_heads = r.n_q_heads; p.rot_dim = r.rot_dim;
+  p.adjacent = r.rot_pairs == FASTKV_ROT_ADJACENT; p.total_src = r.total_src;
+  p.lens = lens; p.new_lens = new_lens; p.cu_new = r.cu_new; p.cu_src = r.cu_src; p.idx = idx; p.pos = pos; p.inv_freq = inv_freq;
+  p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
+  p.q_out = static_cast<uint16_t*>(q_out);
+  p.q_tok = r.q_stride_tok; p.q_head = r.q_stride_head; p.k_tok = r.k_stride_tok; p.k_head = r.k_stride_head;
+  p.v_tok = r.v_stride_tok; p.v_head = r.v_stride_head;
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  cudaError_t e;
+  {
+    TimedLaunch timed(KID_PAGED_APPEND, static_cast<cudaStream_t>(stream_));
+    e = launch_paged_append(p, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_));
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "paged_append_kernel launch");
+  ++g_launches;
+  return FASTKV_OK;
+}
+
+int fastkv_paged_attn_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_query* query, size_t* bytes) {
+  int rc = check_query(cache, query);
+  if (rc) return rc;
+  if (bytes == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = round_up(paged_attn_workspace_bytes(plan_of(*cache, *query), cache->batch, cache->n_kv_heads,
+                                               query->n_q_heads / cache->n_kv_heads * query->q_len, cache->head_dim), 256);
+  return FASTKV_OK;
+}
+
+int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query, const int32_t* lens, const void* q,
+                      float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream_) {
+  int rc = check_query(cache, query);
+  if (rc) return rc;
+  if (!lens || !q || !out) return fail(FASTKV_ERR_INVALID_ARG, "paged_attn: lens, q and out are required");
+  if (reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(out) % 16)
+    return fail(FASTKV_ERR_UNSUPPORTED, "paged_attn: q and out must be 16-byte aligned");
+  const fastkv_paged_cache& c = *cache;
+  const PagedAttnPlan plan = plan_of(c, *query);
+  const int G = query->n_q_heads / c.n_kv_heads, rows = G * query->q_len;
+  const size_t need = round_up(paged_attn_workspace_bytes(plan, c.batch, c.n_kv_heads, rows, c.head_dim), 256);
+  if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+  if ((rc = check_device())) return rc;
+  CUtensorMap tmap_k, tmap_v;
+  if ((rc = encode_pool(&tmap_k, c, c.k_pages)) || (rc = encode_pool(&tmap_v, c, c.v_pages))) return rc;
+  PagedAttnParams p;
+  memset(&p, 0, sizeof p);
+  p.c = paged_view(c);
+  p.n_q_heads = query->n_q_heads; p.group = G; p.q_len = query->q_len; p.rows = rows;
+  const float scale = query->softmax_scale > 0.0f ? query->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c.head_dim));
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const size_t parts = static_cast<size_t>(c.batch) * c.n_kv_heads * plan.splits * rows;
+  p.part_ml = reinterpret_cast<float4*>(ws + sizeof(WorkspaceHeader));
+  p.part_o = reinterpret_cast<float*>(ws + sizeof(WorkspaceHeader) + round_up(parts * sizeof(float4), 256));
+  p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+  cudaError_t e;
+  int launched = 0;
+  {
+    TimedLaunch timed(KID_PAGED_ATTN, static_cast<cudaStream_t>(stream_));
+    e = launch_paged_attn(tmap_k, tmap_v, p, plan, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_), &launched);
+  }
+  g_launches += launched;
+  if (e != cudaSuccess) return cuda_fail(e, "paged_attn_kernel launch");
   return FASTKV_OK;
 }
 

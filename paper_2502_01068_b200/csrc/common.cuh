@@ -55,6 +55,12 @@ enum Site : int {
   SITE_ATTN_SFULL = 33,
   SITE_ATTN_PFREE = 34,
   SITE_ATTN_ODONE = 35,
+  SITE_APPEND_INDEX = 36,
+  SITE_APPEND_PAGE = 37,
+  SITE_APPEND_ROWS = 38,
+  SITE_PAGED_WAIT = 39,
+  SITE_PAGED_PAGE = 40,
+  SITE_PAGED_LEN = 41,
 };
 
 // Records `text` as the calling thread's last error (see fastkv_last_error) and returns `status`.

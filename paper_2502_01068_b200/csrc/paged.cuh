@@ -1,0 +1,64 @@
+// Parameter blocks and launchers of the paged cache: appending rows (paged_append.cu) and attention (paged_attn.cu).
+#pragma once
+
+#include "common.cuh"
+#include "paged_index.h"
+
+namespace fastkv {
+
+struct PagedView {
+  int batch, max_pages, n_pages, page_log2, n_kv_heads;
+  uint8_t* k_pages;           // [n_pages][n_kv_heads][page][d]
+  uint8_t* v_pages;
+  float* k_scales;            // [n_pages][n_kv_heads], 8-bit pages only
+  float* v_scales;
+  const int* block_table;     // [batch][max_pages]
+};
+
+struct AppendParams {
+  PagedView c;
+  int total, max_new, uniform, n_q_heads, rot_dim, adjacent, total_src;
+  const int* lens;            // entries before the call
+  int* new_lens;              // entries after it, may be null
+  const int* cu_new;          // may be null (uniform)
+  const int* cu_src;          // gathered rows: source offsets of the sequences, may be null (one sequence)
+  const int* idx;             // gathered rows: [n_kv_heads][total], or null
+  const int* pos;
+  const float* inv_freq;
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* q_out;
+  long long q_tok, q_head, k_tok, k_head, v_tok, v_head;   // strides, elements
+  WorkspaceHeader* hdr;
+  // work split, filled in by the launcher
+  int heads_per_unit, row_heads, row_slices, row_blocks;   // row role
+  int pages_per_seq, job_slices, jobs_per_slice;           // page role (8-bit pages)
+};
+
+cudaError_t launch_paged_append(AppendParams& p, int head_dim, bool e4m3, cudaStream_t stream);
+
+constexpr int kPagedMaxSplits = 64;
+
+struct PagedAttnParams {
+  PagedView c;
+  int n_q_heads, group, q_len, rows, row_tiles, splits;    // rows = group * q_len query rows per (sequence, KV head)
+  float scale_log2;           // softmax scale times log2(e)
+  const int* lens;
+  const uint16_t* q;          // [B][q_len][Hq][d]
+  float* out;                 // [B][q_len][Hq][d]
+  float* lse;                 // [B][q_len][Hq], may be null
+  float4* part_ml;            // [B][Hkv][splits][rows]: (max, sum, reference of the outputs, -)
+  float* part_o;              // [B][Hkv][splits][rows][d]
+  WorkspaceHeader* hdr;
+};
+
+struct PagedAttnPlan {
+  int warps, row_tiles_of_8, row_tiles, splits;
+};
+PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, int head_dim, bool e4m3, int max_len, long long total_len);
+size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int rows, int head_dim);
+cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
+                              int head_dim, bool e4m3, cudaStream_t stream, int* launches);
+
+}  // namespace fastkv
