@@ -843,7 +843,8 @@ int check_strides(const char* name, int64_t tok, int64_t head, int head_dim, con
   if (tok < head_dim || head < head_dim) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: %s strides are smaller than head_dim", name);
   return FASTKV_OK;
 }
-// One pool as a (column, row of the page, page x head) tensor; boxes of 16 rows x 128 bytes (64 for 8-bit rows of 64).
+// One pool as a (column, row of the page, page x head) tensor; boxes of a page's rows (at most 64 in bf16) x 128 bytes (64 for 8-bit
+// rows of 64).
 int encode_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
@@ -852,7 +853,8 @@ int encode_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base)
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size),
                         static_cast<cuuint64_t>(c.n_pages) * c.n_kv_heads};
   cuuint64_t strides[2] = {row, row * c.page_size};
-  cuuint32_t box[3] = {static_cast<cuuint32_t>(row > 128 ? 128 / item : c.head_dim), 16, 1};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(row > 128 ? 128 / item : c.head_dim),
+                       static_cast<cuuint32_t>(paged_box_rows(e4m3, c.page_size)), 1};
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
                   strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -874,8 +876,8 @@ int check_query(const fastkv_paged_cache* c, const fastkv_query* q) {
 }
 PagedAttnPlan plan_of(const fastkv_paged_cache& c, const fastkv_query& q) {
   const long long total = q.total_len > 0 ? q.total_len : static_cast<long long>(c.batch) * q.max_len;
-  return plan_paged_attn(c.batch, c.n_kv_heads, q.n_q_heads / c.n_kv_heads * q.q_len, c.head_dim, c.format == FASTKV_CACHE_E4M3,
-                         q.max_len, total);
+  return plan_paged_attn(c.batch, c.n_kv_heads, q.n_q_heads / c.n_kv_heads * q.q_len, c.format == FASTKV_CACHE_E4M3, q.max_len,
+                         total);
 }
 }  // namespace
 
@@ -946,8 +948,7 @@ int fastkv_paged_attn_workspace_bytes(const fastkv_paged_cache* cache, const fas
   int rc = check_query(cache, query);
   if (rc) return rc;
   if (bytes == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = round_up(paged_attn_workspace_bytes(plan_of(*cache, *query), cache->batch, cache->n_kv_heads,
-                                               query->n_q_heads / cache->n_kv_heads * query->q_len, cache->head_dim), 256);
+  *bytes = round_up(paged_attn_workspace_bytes(plan_of(*cache, *query), cache->batch, cache->n_kv_heads, cache->head_dim), 256);
   return FASTKV_OK;
 }
 
@@ -961,7 +962,7 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   const fastkv_paged_cache& c = *cache;
   const PagedAttnPlan plan = plan_of(c, *query);
   const int G = query->n_q_heads / c.n_kv_heads, rows = G * query->q_len;
-  const size_t need = round_up(paged_attn_workspace_bytes(plan, c.batch, c.n_kv_heads, rows, c.head_dim), 256);
+  const size_t need = round_up(paged_attn_workspace_bytes(plan, c.batch, c.n_kv_heads, c.head_dim), 256);
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
   if ((rc = check_device())) return rc;
   CUtensorMap tmap_k, tmap_v;
@@ -974,9 +975,9 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   p.scale_log2 = scale * 1.4426950408889634f;
   p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const size_t parts = static_cast<size_t>(c.batch) * c.n_kv_heads * plan.splits * rows;
+  p.box_subs = paged_box_rows(c.format == FASTKV_CACHE_E4M3, c.page_size) / 16;
   p.part_ml = reinterpret_cast<float4*>(ws + sizeof(WorkspaceHeader));
-  p.part_o = reinterpret_cast<float*>(ws + sizeof(WorkspaceHeader) + round_up(parts * sizeof(float4), 256));
+  p.part_o = reinterpret_cast<float*>(ws + paged_attn_partials_offset(plan, c.batch, c.n_kv_heads));
   p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
   cudaError_t e;
   int launched = 0;

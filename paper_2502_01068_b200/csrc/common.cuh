@@ -61,6 +61,7 @@ enum Site : int {
   SITE_PAGED_WAIT = 39,
   SITE_PAGED_PAGE = 40,
   SITE_PAGED_LEN = 41,
+  SITE_APPEND_WAIT = 42,
 };
 
 // Records `text` as the calling thread's last error (see fastkv_last_error) and returns `status`.
@@ -214,6 +215,11 @@ __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* map) {
 __device__ __forceinline__ uint64_t l2_policy_evict_first() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t l2_policy_evict_normal() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
   return p;
 }
 __device__ __forceinline__ uint64_t l2_policy_evict_last() {

@@ -32,32 +32,39 @@ struct AppendParams {
   long long q_tok, q_head, k_tok, k_head, v_tok, v_head;   // strides, elements
   WorkspaceHeader* hdr;
   // work split, filled in by the launcher
-  int heads_per_unit, row_heads, row_slices, row_blocks;   // row role
+  int page_blocks, heads_per_unit, row_heads, row_slices;  // row role, behind the page role's blocks
   int pages_per_seq, job_slices, jobs_per_slice;           // page role (8-bit pages)
 };
 
 cudaError_t launch_paged_append(AppendParams& p, int head_dim, bool e4m3, cudaStream_t stream);
 
-constexpr int kPagedMaxSplits = 64;
+constexpr int kPagedMaxPieces = 592;   // pieces of one (sequence, KV head): the CTAs that can share it
 
 struct PagedAttnParams {
   PagedView c;
-  int n_q_heads, group, q_len, rows, row_tiles, splits;    // rows = group * q_len query rows per (sequence, KV head)
+  int n_q_heads, group, q_len, rows;     // rows = group * q_len query rows per (sequence, KV head)
+  int row_tiles, tile_rows;   // tiles the rows are cut into, and rows of a tile (8 or 16)
+  int splits;                 // static launches: CTAs that share a (sequence, KV head, row tile)
+  int balanced, ctas;         // balanced launches: CTAs that share all of them
+  int box_subs;               // 16-entry steps that one TMA box brings
   float scale_log2;           // softmax scale times log2(e)
   const int* lens;
   const uint16_t* q;          // [B][q_len][Hq][d]
   float* out;                 // [B][q_len][Hq][d]
   float* lse;                 // [B][q_len][Hq], may be null
-  float4* part_ml;            // [B][Hkv][splits][rows]: (max, sum, reference of the outputs, -)
-  float* part_o;              // [B][Hkv][splits][rows][d]
+  float4* part_ml;            // [pieces][8]: (max, sum, reference of the outputs, -)
+  float* part_o;              // [pieces][8][d]
   WorkspaceHeader* hdr;
 };
 
 struct PagedAttnPlan {
-  int warps, row_tiles_of_8, row_tiles, splits;
+  int row_tiles_of_8, row_tiles, splits, balanced, ctas;
 };
-PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, int head_dim, bool e4m3, int max_len, long long total_len);
-size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int rows, int head_dim);
+PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len);
+size_t paged_attn_partials_offset(const PagedAttnPlan& plan, int batch, int n_kv_heads);
+size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int head_dim);
+// Entries of a page that one TMA box brings: a chunk's 32 of 8-bit pages when the page has them, else 16.
+inline int paged_box_rows(bool e4m3, int page_size) { return e4m3 && page_size >= 32 ? 32 : 16; }
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
                               int head_dim, bool e4m3, cudaStream_t stream, int* launches);
 

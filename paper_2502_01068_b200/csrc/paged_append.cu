@@ -3,7 +3,7 @@
 // a power-of-two scale for each (page, KV head).
 //
 // Rotation: for pair i of a head's first rot_dim elements, angle a = pos * inv_freq[i],
-//   y1 = x1 cos a - x2 sin a,   y2 = x2 cos a + x1 sin a      (three roundings each in fp32, then the one of the cache).
+//   y1 = x1 cos a - x2 sin a,   y2 = x2 cos a + x1 sin a      (in fp32, one rounding a product and one a sum, then the one of the cache).
 // The angle is formed and reduced in fp64: in fp32 a position of 100 000 leaves 2^-7 of an angle's bits.
 //
 // Eight lanes (four for head_dim 64) handle one row of one head: sixteen elements each, as two 16-byte pieces chosen so
@@ -21,6 +21,7 @@ namespace fastkv {
 
 namespace {
 
+constexpr int kPageStages = 4;         // page role: heads whose rows are on their way or in use
 constexpr int kSmallRows = 8;        // rows per sequence up to which the small role is used
 
 struct Row16 {                       // a lane's sixteen elements of one row: the pieces at `lo` and `hi`
@@ -52,38 +53,54 @@ __device__ __forceinline__ uint32_t rescale_e4m3(uint32_t w, float ratio) {
   return pack_e4m3(f[0] * ratio, f[1] * ratio, f[2] * ratio, f[3] * ratio);
 }
 
-// Where lane j's two pieces start in a head's row, and whether they are rotated.
+// Where lane j's two pieces start in a head's row of `dim` elements, and whether they are rotated.  Halves: the pieces lie half of
+// the rotated part (or half of the rest) apart, which keeps neighbouring lanes on neighbouring 16 bytes.
 struct Pieces {
   int lo, hi;
   bool turned;
 };
-__device__ __forceinline__ Pieces pieces_of(int j, int rot_dim, int adjacent) {
+__device__ __forceinline__ Pieces pieces_of(int j, int dim, int rot_dim, int adjacent) {
   Pieces q;
   q.turned = 16 * j < rot_dim;
-  q.lo = 16 * j;
-  q.hi = 16 * j + 8;
-  if (q.turned && !adjacent) {       // halves: elements i and i + rot_dim / 2
-    q.lo = 8 * j;
-    q.hi = rot_dim / 2 + 8 * j;
+  const int base = q.turned ? 0 : rot_dim, part = q.turned ? rot_dim : dim - rot_dim;
+  q.lo = base + 8 * (j - base / 16);
+  q.hi = q.lo + part / 2;
+  if (q.turned && adjacent) {        // pairs (2 i, 2 i + 1) of sixteen elements in a row
+    q.lo = 16 * j;
+    q.hi = 16 * j + 8;
   }
   return q;
 }
 
-// cos and sin of the eight pairs 8j .. 8j + 7 at position `pos`.  The angle in turns, pos * f / (2 pi), is formed in fp64
-// with the rounding error of the product added back after the whole turns are gone.
+// cos and sin of the eight pairs 8j .. 8j + 7 at position `pos`.  The angle is formed in fp64 in quarter turns, pos * f * 2 / pi,
+// with the rounding error of the product added back after the whole quarters are gone; what is left, at most an eighth of
+// a turn, goes through the Taylor series of sin and cos (to x^13 and x^14: off by 2e-14 and 1e-15, so that the one rounding to
+// fp32 is the right one but for one value in millions).  24 fp64 instructions a pair.
 __device__ __forceinline__ void angles_of(int pos, const float* inv_freq, int j, float (&cs)[8], float (&sn)[8]) {
-  const double kInv2Pi = 0.15915494309189535, kInv2PiLow = -9.839338337591243e-18;
+  const double kQuarters = 0.6366197723675814, kQuartersLow = -3.935735335036497e-17;      // 2 / pi, high and low part
+  const double kHalfPi = 1.5707963267948966;
+  const double kRound = 6755399441055744.0;       // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
   const float4 f0 = *reinterpret_cast<const float4*>(inv_freq + 8 * j), f1 = *reinterpret_cast<const float4*>(inv_freq + 8 * j + 4);
   const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+  const double dpos = static_cast<double>(pos);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const double a = static_cast<double>(pos) * static_cast<double>(f[e]);
-    const double t = a * kInv2Pi;
-    const double r = (t - rint(t)) + (fma(a, kInv2Pi, -t) + a * kInv2PiLow);
-    double s, c;
-    sincospi(2.0 * r, &s, &c);
-    cs[e] = static_cast<float>(c);
-    sn[e] = static_cast<float>(s);
+    const double a = dpos * static_cast<double>(f[e]);
+    const double t = a * kQuarters, whole = t + kRound;
+    const double rest = (t - (whole - kRound)) + fma(a, kQuartersLow, fma(a, kQuarters, -t));
+    const double x = rest * kHalfPi, z = x * x;
+    double s = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+    s = fma(z, s, 1.0 / 362880.0); s = fma(z, s, -1.0 / 5040.0); s = fma(z, s, 1.0 / 120.0); s = fma(z, s, -1.0 / 6.0);
+    s = fma(x * z, s, x);
+    double c = fma(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+    c = fma(z, c, -1.0 / 3628800.0); c = fma(z, c, 1.0 / 40320.0); c = fma(z, c, -1.0 / 720.0); c = fma(z, c, 1.0 / 24.0);
+    c = fma(z, c, -0.5);
+    c = fma(z, c, 1.0);
+    const int quarter = __double2loint(whole);
+    const float fs = static_cast<float>(s), fc = static_cast<float>(c);
+    const float u = (quarter & 1) ? fs : fc, v = (quarter & 1) ? fc : fs;       // |cos|, |sin| of the whole angle
+    cs[e] = ((quarter + 1) & 2) ? -u : u;
+    sn[e] = (quarter & 2) ? -v : v;
   }
 }
 
@@ -103,13 +120,35 @@ __device__ __forceinline__ void unpack(const Row16& r, float (&x)[16]) {
     x[2 * i + 1] = bf_hi(w[i]);
   }
 }
+// Pairs of fp32 products and sums.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ void rotate16(float (&x)[16], const float (&cs)[8], const float (&sn)[8], int adjacent) {
   if (adjacent) {
 #pragma unroll
     for (int m = 0; m < 8; ++m) turn(x[2 * m], x[2 * m + 1], cs[m], sn[m]);
   } else {
 #pragma unroll
-    for (int m = 0; m < 8; ++m) turn(x[m], x[8 + m], cs[m], sn[m]);
+    for (int m = 0; m < 8; m += 2) {              // two pairs at a time
+      const unsigned long long x1 = pair_of(x[m], x[m + 1]), x2 = pair_of(x[8 + m], x[9 + m]);
+      const unsigned long long c = pair_of(cs[m], cs[m + 1]), s = pair_of(sn[m], sn[m + 1]), ns = pair_of(-sn[m], -sn[m + 1]);
+      const unsigned long long y1 = add2(mul2(x1, c), mul2(x2, ns)), y2 = add2(mul2(x2, c), mul2(x1, s));
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(x[m]), "=f"(x[m + 1]) : "l"(y1));
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(x[8 + m]), "=f"(x[9 + m]) : "l"(y2));
+    }
   }
 }
 __device__ __forceinline__ float amax16(const float (&x)[16]) {
@@ -134,10 +173,16 @@ __device__ __forceinline__ void store_codes(uint8_t* row, const Pieces& at, cons
   *reinterpret_cast<uint2*>(row + at.hi) = hi;
 }
 
-// The source row of new row `row` of head h: itself, or the kept row that idx names (-1: none such).
-__device__ __forceinline__ long long source_row(const AppendParams& p, int row, int b, int h) {
-  if (p.idx == nullptr) return row;
-  const int i = p.idx[static_cast<long long>(h) * p.total + row];
+// The source row of new row `row` of head h: itself, or the kept row that idx names (-1: none such).  The index is fetched
+// apart from its use, so that a caller can have it under way before it is needed.  Rotated calls have no indices.
+template <bool kRot>
+__device__ __forceinline__ int fetch_index(const AppendParams& p, int row, int h) {
+  if (kRot || p.idx == nullptr) return row;
+  return p.idx[static_cast<long long>(h) * p.total + row];
+}
+template <bool kRot>
+__device__ __forceinline__ long long source_row(const AppendParams& p, int i, int b) {
+  if (kRot || p.idx == nullptr) return i;
   const int s0 = p.cu_src ? p.cu_src[b] : 0;
   const int L = p.cu_src ? p.cu_src[b + 1] - s0 : p.total_src;
   if (i < 0 || i >= L || s0 < 0 || static_cast<long long>(s0) + i >= p.total_src) {
@@ -161,19 +206,20 @@ __device__ __forceinline__ int owner_of_row(const AppendParams& p, int t) {
 }  // namespace
 
 // Row role: unit u = (slice of heads, token); heads in the order queries, keys, values.
-template <int D, bool kE4M3>
-__device__ void append_rows(const AppendParams& p) {
+template <int D, bool kE4M3, bool kRot>
+__device__ void append_rows(const AppendParams& p, int block) {
   constexpr int GL = D / 16;                      // lanes of a row
-  constexpr int kBatch = 4;                       // rows loaded before the first is used
+  constexpr int kBatch = 4;                        // rows loaded before the first is used
   const int j = threadIdx.x % GL;
-  const long long u = static_cast<long long>(blockIdx.x) * (blockDim.x / GL) + threadIdx.x / GL;
+  const long long u = static_cast<long long>(block) * (blockDim.x / GL) + threadIdx.x / GL;
   if (u >= static_cast<long long>(p.row_slices) * p.total) return;
   const int slice = static_cast<int>(u / p.total), t = static_cast<int>(u - static_cast<long long>(slice) * p.total);
   const int h0 = slice * p.heads_per_unit, h1 = min(h0 + p.heads_per_unit, p.row_heads);
   const int Hq = p.n_q_heads, Hkv = p.c.n_kv_heads;
-  const Pieces turned = pieces_of(j, p.rot_dim, p.adjacent), plain = pieces_of(j, 0, 0);
+  const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
   float cs[8], sn[8];
-  if (turned.turned && h0 < Hq + Hkv) angles_of(p.pos[t], p.inv_freq, j, cs, sn);
+  const bool turns = kRot && turned.turned && h0 < Hq + Hkv;
+  const int pos = turns ? p.pos[t] : 0;
   int b = 0, slot = -1;
   long long page = -1;                            // of bf16 pages: where row t goes; -1: nowhere
   if (!kE4M3 && h1 > Hq) {
@@ -203,13 +249,14 @@ __device__ void append_rows(const AppendParams& p) {
       } else if (!kE4M3 && page >= 0) {
         const bool is_k = h < Hq + Hkv;
         const int g = is_k ? h - Hq : h - Hq - Hkv;
-        const long long src = source_row(p, t, b, g);
+        const long long src = source_row<kRot>(p, fetch_index<kRot>(p, t, g), b);
         if (src < 0) continue;
         have[i] = true;
         if (is_k) raw[i] = load_row(p.k + src * p.k_tok + g * p.k_head, turned);
         else raw[i] = load_row(p.v + src * p.v_tok + g * p.v_head, plain);
       }
     }
+    if (hb == h0 && turns) angles_of(pos, p.inv_freq, j, cs, sn);       // while the first rows are on their way
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (!have[i]) continue;
@@ -222,7 +269,7 @@ __device__ void append_rows(const AppendParams& p) {
         const int g = is_v ? h - Hq - Hkv : h - Hq;
         dst = reinterpret_cast<uint16_t*>(is_v ? p.c.v_pages : p.c.k_pages) + (((page + g) << p.c.page_log2) + in_page) * D;
       }
-      if (!is_v && turned.turned) {
+      if (kRot && !is_v && turned.turned) {
         float x[16];
         unpack(raw[i], x);
         rotate16(x, cs, sn, p.adjacent);
@@ -250,7 +297,7 @@ __device__ void append_small(const AppendParams& p, int block) {
   const int b = static_cast<int>(item / p.pages_per_seq), which = static_cast<int>(item - static_cast<long long>(b) * p.pages_per_seq);
   const bool is_v = job >= Hkv;
   const int g = is_v ? job - Hkv : job;
-  const Pieces at = is_v ? pieces_of(j, 0, 0) : pieces_of(j, p.rot_dim, p.adjacent);
+  const Pieces at = is_v ? pieces_of(j, D, 0, 0) : pieces_of(j, D, p.rot_dim, p.adjacent);
   const int P = 1 << p.c.page_log2;
   int len = 0, lo = 0, hi = 0, row0 = 0;           // slots [lo, hi) of the sequence are this unit's new rows
   long long block_row = -1;
@@ -281,7 +328,7 @@ __device__ void append_small(const AppendParams& p, int block) {
   float x[16];
   auto load = [&](int slot) -> bool {
     const int row = row0 + (slot - len);
-    const long long src = source_row(p, row, b, g);
+    const long long src = source_row<false>(p, fetch_index<false>(p, row, g), b);
     if (src < 0) return false;
     unpack(load_row(base + src * tok, at), x);
     if (at.turned) {
@@ -322,47 +369,125 @@ __device__ void append_small(const AppendParams& p, int block) {
   }
 }
 
-// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads; NS rows per lane group.
-template <int D, int NS>
+__device__ __forceinline__ void bulk_row(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+// The larger of two pairs of bf16 magnitudes (a NaN gives way, as with fmaxf).
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t m, uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b32 a;\n\tabs.bf16x2 a, %2;\n\tmax.bf16x2 %0, %1, a;\n\t}" : "=r"(r) : "r"(m), "r"(w));
+  return r;
+}
+__device__ __forceinline__ float amax_raw(const Row16& r) {
+  uint32_t m = 0;
+  m = max_abs_bf16x2(m, r.lo.x); m = max_abs_bf16x2(m, r.lo.y); m = max_abs_bf16x2(m, r.lo.z); m = max_abs_bf16x2(m, r.lo.w);
+  m = max_abs_bf16x2(m, r.hi.x); m = max_abs_bf16x2(m, r.hi.y); m = max_abs_bf16x2(m, r.hi.z); m = max_abs_bf16x2(m, r.hi.w);
+  return fmaxf(bf_lo(m), bf_hi(m));
+}
+
+// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads.  One thread per row of the page brings the
+// rows of the next heads into shared memory with bulk copies (kPageStages - 1 heads ahead; the threads that compute hold no
+// addresses of theirs); a lane group takes NS rows of a head, and the block meets once per head, over the rows' largest
+// absolute value.
+template <int D, int NS, bool kRot>
 __device__ void append_page(const AppendParams& p, int block) {
   constexpr int GL = D / 16;
-  __shared__ float top[2][16];                    // per warp: largest absolute value of the rows it holds
+  extern __shared__ __align__(128) uint8_t ring[];   // [kPageStages][rows of a round][D] bf16
+  __shared__ uint64_t full[kPageStages];
+  __shared__ uint32_t top[3][4];                  // by round: the bits of the largest absolute value, per head side by side
+  __shared__ uint8_t absent[kPageStages][128];    // gathered rows whose index names no row
+  __shared__ int abort_flag;
   const int P = 1 << p.c.page_log2, Hkv = p.c.n_kv_heads, jobs = 2 * Hkv;
-  const int groups = blockDim.x / GL, j = threadIdx.x % GL, grp = threadIdx.x / GL;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int side = groups > P ? groups / P : 1;   // heads that a small page lets the block take side by side
-  const int mine = grp / P;                       // which of them (0 when side == 1)
+  const int threads = blockDim.x, groups = threads / GL, j = threadIdx.x % GL, grp = threadIdx.x / GL;
+  const int lane = threadIdx.x & 31;
+  const int side = groups > P ? groups / P : 1;   // heads that a small page lets the block take side by side (4 at most)
+  const int mine = grp >> p.c.page_log2;          // which of them (0 when side == 1)
+  const int n_rows = groups * NS;                 // rows of a round
   const int item = block / p.job_slices, slice = block - item * p.job_slices;
   const int b = item / p.pages_per_seq, which = item - b * p.pages_per_seq;
   const int len = p.lens[b];
   RowRange r;
   new_rows_of(p.cu_new, p.uniform, p.total, p.max_new, b, len, p.c.max_pages, p.c.page_log2, &r);
   if (r.count <= 0) return;
-  const int pg = (len >> p.c.page_log2) + which;
-  const int lo = max(len, pg << p.c.page_log2), hi = min(len + r.count, (pg + 1) << p.c.page_log2);
+  const int pg = (len >> p.c.page_log2) + which, slot0 = pg << p.c.page_log2;
+  const int lo = max(len, slot0), hi = min(len + r.count, slot0 + P);
   if (hi <= lo) return;
   const int pid = p.c.block_table[static_cast<long long>(b) * p.c.max_pages + pg];
   if (pool_block(pid, p.c.n_pages, Hkv, 0) < 0) {
     if (threadIdx.x == 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_PAGE);
     return;
   }
-  const int n_old = max(0, min(len - (pg << p.c.page_log2), P));
+  if (threadIdx.x < 4) top[0][threadIdx.x] = 0u;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < kPageStages; ++i) mbar_init(&full[i], n_rows);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  const int n_old = max(0, min(len - slot0, P));
   const int job0 = slice * p.jobs_per_slice, job1 = min(job0 + p.jobs_per_slice, jobs);
-  const Pieces turned = pieces_of(j, p.rot_dim, p.adjacent), plain = pieces_of(j, 0, 0);
-  int in_page[NS], row[NS];
+  const int rounds = (job1 - job0 + side - 1) / side;
+  const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
+
+  // ---- the row this thread brings ----
+  const bool gather = !kRot && p.idx != nullptr;
+  const bool brings = static_cast<int>(threadIdx.x) < n_rows;
+  const int my_side = threadIdx.x >> p.c.page_log2, my_slot = slot0 + (threadIdx.x & (P - 1));
+  const bool my_fresh = brings && my_slot >= lo && my_slot < hi;
+  const int my_row = r.first + (my_slot - len);
+  const int src0 = gather && p.cu_src ? p.cu_src[b] : 0;          // where the sequence's source rows start, and how many
+  const int src_n = gather ? min(p.cu_src ? p.cu_src[b + 1] - src0 : p.total_src, src0 >= 0 ? p.total_src - src0 : 0) : 0;
+  int index = 0;                                  // source row of the round that starts next
+  auto fetch = [&](int k) {
+    const int job = job0 + k * side + my_side, g = job >= Hkv ? job - Hkv : job;
+    if (gather && my_fresh && job < job1) index = p.idx[static_cast<long long>(g) * p.total + my_row];
+  };
+  auto start = [&](int k) {                       // the copies of round k; every bringing thread arrives
+    if (!brings || k >= rounds) return;
+    const int job = job0 + k * side + my_side, st = k % kPageStages;
+    bool take = my_fresh && job < job1;
+    int src = my_row;
+    if (gather && take) {
+      const bool good = index >= 0 && index < src_n;
+      if (!good) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_INDEX);
+      absent[st][threadIdx.x] = !good;
+      take = good;
+      src = src0 + index;
+    }
+    if (take) {
+      const bool is_v = job >= Hkv;
+      const int g = is_v ? job - Hkv : job;
+      const uint16_t* x = is_v ? p.v + g * p.v_head + src * p.v_tok : p.k + g * p.k_head + src * p.k_tok;
+      mbar_arrive_expect_tx(&full[st], D * 2);
+      bulk_row(ring + (static_cast<size_t>(st) * n_rows + threadIdx.x) * (D * 2), x, D * 2, &full[st]);
+    } else {
+      mbar_arrive(&full[st]);
+    }
+    fetch(k + 1);
+  };
+  fetch(0);
+  __syncthreads();                                // barriers and top[0] are set
+#pragma unroll
+  for (int k = 0; k < kPageStages - 1; ++k) start(k);
+
+  // ---- the rows this lane group computes ----
   bool fresh[NS];
   float cs[NS][8], sn[NS][8];
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
-    in_page[n] = grp % P + n * groups;            // side == 1 whenever NS > 1
-    const int slot = (pg << p.c.page_log2) + in_page[n];
-    fresh[n] = in_page[n] < P && slot >= lo && slot < hi;
-    row[n] = r.first + (slot - len);
-    if (fresh[n] && turned.turned && job0 < Hkv) angles_of(p.pos[row[n]], p.inv_freq, j, cs[n], sn[n]);
+    const int slot = slot0 + ((grp + n * groups) & (P - 1));
+    fresh[n] = slot >= lo && slot < hi;
+    if constexpr (kRot)
+      if (fresh[n] && turned.turned && job0 < Hkv) angles_of(p.pos[r.first + (slot - len)], p.inv_freq, j, cs[n], sn[n]);
   }
-  int turnstile = 0;
-  for (int jb = job0; jb < job1; jb += side, turnstile ^= 1) {
-    const int job = jb + mine;
+  bool ok = true;
+  int now = 0;                                    // k % 3
+  for (int k = 0; k < rounds; ++k) {
+    const int st = k % kPageStages;
+    start(k + kPageStages - 1);                   // into the stage that was read before the last meeting
+    const int job = job0 + k * side + mine;
     const bool on = job < job1;
     const bool is_v = job >= Hkv;
     const int g = is_v ? job - Hkv : job;
@@ -370,95 +495,108 @@ __device__ void append_page(const AppendParams& p, int block) {
     const long long block_row = static_cast<long long>(pid) * Hkv + g;
     float* const scales = is_v ? p.c.v_scales : p.c.k_scales;
     const float old_scale = on && n_old > 0 ? scales[block_row] : 0.0f;
+    ok = ok && mbar_wait_bounded(&full[st], (k / kPageStages) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT);
+    Row16 raw[NS];
     float x[NS][16];
-    bool got[NS];
+    bool here[NS];
     float m = 0.0f;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      got[n] = false;
-      if (!on || !fresh[n]) continue;
-      const long long src = source_row(p, row[n], b, g);
-      if (src < 0) continue;
-      got[n] = true;
-      unpack(load_row((is_v ? p.v + g * p.v_head + src * p.v_tok : p.k + g * p.k_head + src * p.k_tok), at), x[n]);
+      const int at_row = grp + n * groups;
+      here[n] = ok && on && fresh[n] && !(gather && absent[st][at_row]);
+      if (!here[n]) continue;
+      raw[n] = load_row(reinterpret_cast<const uint16_t*>(ring + (static_cast<uint32_t>(st) * n_rows + at_row) * (D * 2)), at);
+      if (kRot && !is_v) {
+        unpack(raw[n], x[n]);
+        if (at.turned) rotate16(x[n], cs[n], sn[n], p.adjacent);
+        m = fmaxf(m, amax16(x[n]));
+      } else {
+        m = fmaxf(m, amax_raw(raw[n]));
+      }
     }
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      if (!got[n]) continue;
-      if (at.turned) rotate16(x[n], cs[n], sn[n], p.adjacent);
-      m = fmaxf(m, amax16(x[n]));
-    }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) top[turnstile][warp] = m;
+    // magnitudes order like their bits
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+    const int next = now == 2 ? 0 : now + 1;
+    if (lane == 0 && most != 0u) atomicMax(&top[now][mine], most);
+    if (threadIdx.x < 4) top[next][threadIdx.x] = 0u;          // last read two rounds ago
     __syncthreads();                              // also: every thread has read the old scale
-    const int warps_each = (blockDim.x >> 5) / side, w0 = mine * warps_each;
-    m = 0.0f;
-    for (int w = 0; w < warps_each; ++w) m = fmaxf(m, top[turnstile][w0 + w]);
-    if (!on) continue;
-    int e = scale_exponent(__float_as_uint(m));
+    int e = scale_exponent(top[now][mine]);
+    now = next;
+    if (!on || !ok) continue;
     const int e_old = scale_log2(__float_as_uint(old_scale));
     if (n_old > 0 && e_old > e) e = e_old;
     const float inv = __uint_as_float(pow2_bits(-e));
     uint8_t* const rows = (is_v ? p.c.v_pages : p.c.k_pages) + (block_row << p.c.page_log2) * D;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      if (got[n]) store_codes(rows + in_page[n] * D, at, x[n], inv);
-      if (n_old > 0 && e > e_old && in_page[n] < n_old) {
+      const int in_page = (grp + n * groups) & (P - 1);
+      if (here[n]) {
+        if (!(kRot && !is_v)) unpack(raw[n], x[n]);
+        store_codes(rows + in_page * D, at, x[n], inv);
+      }
+      if (n_old > 0 && e > e_old && in_page < n_old) {
         const float ratio = __uint_as_float(pow2_bits(max(e_old - e, -126)));
-        uint4* w = reinterpret_cast<uint4*>(rows + in_page[n] * D + 16 * j);
+        uint4* w = reinterpret_cast<uint4*>(rows + in_page * D + 16 * j);
         uint4 c = *w;
         c.x = rescale_e4m3(c.x, ratio); c.y = rescale_e4m3(c.y, ratio);
         c.z = rescale_e4m3(c.z, ratio); c.w = rescale_e4m3(c.w, ratio);
         *w = c;
       }
     }
-    if (grp % P == 0 && j == 0) scales[block_row] = __uint_as_float(pow2_bits(e));
+    if ((grp & (P - 1)) == 0 && j == 0) scales[block_row] = __uint_as_float(pow2_bits(e));
   }
+  if (!ok)                                        // a wait gave up: no copy may still be in flight when the block leaves
+    for (int k = max(0, rounds - kPageStages); k < rounds; ++k)
+      mbar_wait_drain(&full[k % kPageStages], (k / kPageStages) & 1, p.hdr, SITE_APPEND_WAIT);
 }
 
-// kPage: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per
-// lane group).  The first row_blocks blocks take the row role.
-template <int D, int kKind>
-__global__ void __launch_bounds__(kKind == 3 ? 512 : 256) paged_append_kernel(const AppendParams p) {
+// kKind: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per lane
+// group).  The blocks from page_blocks on take the row role.
+template <int D, int kKind, bool kRot>
+__global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0) paged_append_kernel(const AppendParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  if (blockIdx.x == 0 && p.new_lens != nullptr) {
+  if (blockIdx.x == 0) {
     for (int b = threadIdx.x; b < p.c.batch; b += blockDim.x) {
       RowRange r;
       const int len = p.lens[b];
       const bool ok = new_rows_of(p.cu_new, p.uniform, p.total, p.max_new, b, len, p.c.max_pages, p.c.page_log2, &r);
-      p.new_lens[b] = max(len, 0) + r.count;
+      if (p.new_lens != nullptr) p.new_lens[b] = max(len, 0) + r.count;
       if (!ok) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_ROWS);
     }
-  } else if (blockIdx.x == 0) {
-    for (int b = threadIdx.x; b < p.c.batch; b += blockDim.x) {
-      RowRange r;
-      if (!new_rows_of(p.cu_new, p.uniform, p.total, p.max_new, b, p.lens[b], p.c.max_pages, p.c.page_log2, &r))
-        raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_ROWS);
-    }
   }
-  const int block = static_cast<int>(blockIdx.x) - p.row_blocks;
-  if (block < 0) {
-    append_rows<D, kKind != 0>(p);
-    return;
-  }
-  if constexpr (kKind == 1) append_small<D>(p, block);
-  if constexpr (kKind == 2) append_page<D, 1>(p, block);
-  if constexpr (kKind == 3) append_page<D, 2>(p, block);
+  // the long blocks of the page role come first, so that the short ones of the row role fill the gaps they leave
+  const int block = static_cast<int>(blockIdx.x);
+  if (block >= p.page_blocks) append_rows<D, kKind != 0, kRot>(p, block - p.page_blocks);
+  else if constexpr (kKind == 1) append_small<D>(p, block);
+  else if constexpr (kKind == 2) append_page<D, 1, kRot>(p, block);
+  else if constexpr (kKind == 3) append_page<D, 2, kRot>(p, block);
 }
 
-template <int D, int kKind>
+template <int D, int kKind, bool kRot>
 static cudaError_t launch_kind(const AppendParams& p, int blocks, int threads, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(threads);
   cfg.stream = stream;
+  if (kKind >= 2) {
+    constexpr int kRowsEach = kKind == 3 ? 2 : 1, kMost = kPageStages * kRowsEach * 32 * (kKind == 3 ? 512 : 256);
+    static PerDeviceOnce configured;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (!configured.done(dev)) {
+      e = cudaFuncSetAttribute(paged_append_kernel<D, kKind, kRot>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+      if (e != cudaSuccess) return e;
+      configured.set(dev);
+    }
+    cfg.dynamicSmemBytes = kPageStages * kRowsEach * 32 * threads;
+  }
   cudaLaunchAttribute attr[1];
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind>, p);
+  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind, kRot>, p);
 }
 
 template <int D>
@@ -468,39 +606,44 @@ static cudaError_t launch_d(AppendParams& p, bool e4m3, cudaStream_t stream) {
   const bool small = p.max_new <= kSmallRows;
   const int per_page = P * GL;                    // lanes that hold a page's rows of one head, one row per lane group
   const int threads = e4m3 && !small && per_page > 512 ? 512 : 256;
-  // Row role: a token's heads are split over as many lane groups as it takes to put about eight blocks on every SM; a
+  // Row role: a token's heads are split over as many lane groups as it takes to put two blocks on every SM (what their registers allow); a
   // long call keeps them together, so that a token's angles are formed once.
   p.row_heads = p.n_q_heads + (e4m3 ? 0 : jobs);
-  const long long groups = static_cast<long long>(kSms) * 8 * (threads / GL);
+  const long long groups = static_cast<long long>(kSms) * 2 * (256 / GL);
   long long hpu = p.row_heads > 0 ? (static_cast<long long>(p.total) * p.row_heads + groups - 1) / groups : 1;
   if (hpu < 1) hpu = 1;
   if (hpu > p.row_heads && p.row_heads > 0) hpu = p.row_heads;
-  p.heads_per_unit = static_cast<int>(hpu);
-  p.row_slices = p.row_heads > 0 ? (p.row_heads + p.heads_per_unit - 1) / p.heads_per_unit : 0;
+  p.row_slices = p.row_heads > 0 ? (p.row_heads + static_cast<int>(hpu) - 1) / static_cast<int>(hpu) : 0;
+  p.heads_per_unit = p.row_slices > 0 ? (p.row_heads + p.row_slices - 1) / p.row_slices : 1;        // alike
   const long long units = static_cast<long long>(p.row_slices) * p.total;
-  p.row_blocks = static_cast<int>((units + threads / GL - 1) / (threads / GL));
-  if (!e4m3) return launch_kind<D, 0>(p, p.row_blocks, threads, stream);
-  // pages a sequence's new rows can touch
-  p.pages_per_seq = (p.max_new + P - 2) / P + 1;
-  const long long items = static_cast<long long>(p.c.batch) * p.pages_per_seq;
-  if (small) {
-    if (p.max_new == 1) p.pages_per_seq = 1;
-    const long long n = static_cast<long long>(p.c.batch) * p.pages_per_seq * jobs;
-    const long long blocks = (n + threads / GL - 1) / (threads / GL);
-    return launch_kind<D, 1>(p, p.row_blocks + static_cast<int>(blocks), threads, stream);
+  const long long row_blocks = (units + threads / GL - 1) / (threads / GL);
+  long long page_blocks = 0;
+  if (e4m3) {
+    // pages a sequence's new rows can touch
+    p.pages_per_seq = p.max_new == 1 ? 1 : (p.max_new + P - 2) / P + 1;
+    const long long items = static_cast<long long>(p.c.batch) * p.pages_per_seq;
+    if (small) {
+      page_blocks = (items * jobs + threads / GL - 1) / (threads / GL);
+    } else {
+      // Page role: a block walks all heads of its page; with fewer pages than the SMs hold blocks, the heads are split over as
+      // many blocks as still run at once.
+      long long slices = 1LL * kSms * (threads == 512 ? 1 : p.rot_dim ? 2 : 3) / items;
+      const int side = per_page < threads ? threads / per_page : 1;
+      if (slices > jobs / side) slices = jobs / side;
+      if (slices < 1) slices = 1;
+      p.jobs_per_slice = static_cast<int>((jobs + slices - 1) / slices);
+      p.jobs_per_slice = (p.jobs_per_slice + side - 1) / side * side;
+      p.job_slices = (jobs + p.jobs_per_slice - 1) / p.jobs_per_slice;
+      page_blocks = items * p.job_slices;
+    }
   }
-  // Page role: a block walks all heads of its page when there are pages enough for about four blocks on every SM.
-  long long slices = (4LL * kSms + items - 1) / items;
-  const int side = per_page < threads ? threads / per_page : 1;
-  if (slices > jobs / side) slices = jobs / side;
-  if (slices < 1) slices = 1;
-  p.jobs_per_slice = static_cast<int>((jobs + slices - 1) / slices);
-  p.jobs_per_slice = (p.jobs_per_slice + side - 1) / side * side;
-  p.job_slices = (jobs + p.jobs_per_slice - 1) / p.jobs_per_slice;
-  const long long blocks = p.row_blocks + items * p.job_slices;
-  if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-  if (per_page > threads) return launch_kind<D, 3>(p, static_cast<int>(blocks), threads, stream);
-  return launch_kind<D, 2>(p, static_cast<int>(blocks), threads, stream);
+  if (page_blocks + row_blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  p.page_blocks = static_cast<int>(page_blocks);
+  const int blocks = static_cast<int>(page_blocks + row_blocks);
+  if (!e4m3) return p.rot_dim ? launch_kind<D, 0, true>(p, blocks, threads, stream) : launch_kind<D, 0, false>(p, blocks, threads, stream);
+  if (small) return launch_kind<D, 1, true>(p, blocks, threads, stream);
+  if (per_page > threads) return p.rot_dim ? launch_kind<D, 3, true>(p, blocks, threads, stream) : launch_kind<D, 3, false>(p, blocks, threads, stream);
+  return p.rot_dim ? launch_kind<D, 2, true>(p, blocks, threads, stream) : launch_kind<D, 2, false>(p, blocks, threads, stream);
 }
 
 cudaError_t launch_paged_append(AppendParams& p, int head_dim, bool e4m3, cudaStream_t stream) {

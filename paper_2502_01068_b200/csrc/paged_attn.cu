@@ -20,13 +20,15 @@
 // against their own running reference R = max(l + v), the sum of exponentials 2^(l - M) against M = max(l) as usual, and
 // out = O / L * 2^(R - M): the weights of the second product stay in (0, 1] whatever the pages' scales are.
 // P goes in as two 16-bit terms (value and rounding remainder), so the result carries fp32-level error.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace fastkv {
 
 namespace {
 
-constexpr int kChunk = 16;          // entries per stage
+constexpr int kSub = 16;            // entries of one step of the second product; a page holds a whole number of them
 constexpr float kShift = 14.0f;     // 8-bit pages: the weights of the second product are 2^14 times too large, so that the
                                     // remainder term of the largest of them is far from fp16's subnormals
 
@@ -38,15 +40,18 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-// D[16x8] += A[16x16] B[16x8], fp32 accumulators.
+// D[16x8] += A[16x16] B[16x8], fp32 accumulators; `first`: D = A B.
 template <bool kHalf>
-__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16(float (&c)[4], bool first, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  const float z0 = first ? 0.0f : c[0], z1 = first ? 0.0f : c[1], z2 = first ? 0.0f : c[2], z3 = first ? 0.0f : c[3];
   if constexpr (kHalf)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
 }
 // Two floats to a pair of 16-bit values (`lo` in the low half), and what the rounding left over.
 template <bool kHalf>
@@ -77,476 +82,689 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
   return r;
 }
 
-template <int D, bool kE4M3, int RT, int kWarps>
+// Four warps per CTA, two CTAs per SM: eight warps that may hold 255 registers each.  The chain from one chunk's logits to its
+// outputs is long and every warp walks it alone, so what counts is how much independent work the compiler can weave into it,
+// and that takes registers.
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+
+template <int D, bool kE4M3, int RT>
 struct PagedCfg {
   static constexpr int kItem = kE4M3 ? 1 : 2;
+  // 8-bit rows go through in chunks of 32 entries: two independent halves, and the work that does not depend on the chunk's size
+  // (waits, shuffles, rescaling) is paid half as often.
+  static constexpr int kSubs = kE4M3 ? 2 : 1;
+  static constexpr int kChunk = kSub * kSubs;                              // entries per stage
   static constexpr int kRowBytes = D * kItem;
   static constexpr int kBoxes = kRowBytes > 128 ? kRowBytes / 128 : 1;     // 128-byte column blocks of a row (or one of 64)
   static constexpr int kBoxRow = kRowBytes / kBoxes;
   static constexpr int kBoxBytes = kChunk * kBoxRow;
   static constexpr int kHalfBytes = kBoxes * kBoxBytes;                    // K (or V) rows of one stage
   static constexpr int kStageBytes = 2 * kHalfBytes;
-  static constexpr int kStages = kE4M3 ? 6 : 3;
+  static constexpr int kStages = kE4M3 ? 2 : 3;   // of 8 KB each for head_dim 128
   static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
   static constexpr int kRows = 8 * RT;
   static constexpr int kMergeBytes = kWarps * kRows * (D * 4 + 16);        // the warps' outputs and (max, sum, reference)
   static constexpr int kSmem = (kRingBytes > kMergeBytes ? kRingBytes : kMergeBytes) + 1024;
 };
 
+// Sum over the block of one value per thread; every thread gets it.  `scratch`: one word per warp.
+template <int kBlock>
+__device__ __forceinline__ long long block_sum(long long x, long long* scratch) {
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+  __syncthreads();
+  long long s = 0;
+#pragma unroll
+  for (int w = 0; w < kBlock / 32; ++w) s += scratch[w];
+  return s;
+}
+
+__device__ __forceinline__ int chunks_of(const PagedAttnParams& p, int b, int chunk_log2) {
+  return (usable_len(p.lens[b], p.c.max_pages, p.c.page_log2) + (1 << chunk_log2) - 1) >> chunk_log2;
+}
+
+// First unit of CTA c when `total` units are dealt evenly to n CTAs.
+__device__ __forceinline__ long long share_begin(long long total, int c, int n) { return total * c / n; }
+
 }  // namespace
 
-template <int D, bool kE4M3, int RT, int kWarps>
-__global__ void __launch_bounds__(32 * kWarps)
+// p.balanced == 0: one segment per CTA, (split of the entries, KV head, row tile, sequence).  p.balanced == 1: the chunks of all
+// (sequence, row tile, KV head) triples in a row are dealt evenly to the grid's CTAs, so that sequences of very different
+// lengths load every SM alike; a CTA walks the segments its share touches.
+template <int D, bool kE4M3, int RT>
+__global__ void __launch_bounds__(kThreads, 2)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedAttnParams p) {
-  using Cfg = PagedCfg<D, kE4M3, RT, kWarps>;
-  constexpr int KS = D / 16, MT = D / 16, kRows = Cfg::kRows, kStages = Cfg::kStages;
+  using Cfg = PagedCfg<D, kE4M3, RT>;
+  constexpr int KS = D / 16, MT = D / 16, kRows = Cfg::kRows, kStages = Cfg::kStages, NSUB = Cfg::kSubs;
+  constexpr int kChunk = Cfg::kChunk, kChunkLog2 = kE4M3 ? 5 : 4;
+  constexpr int kTerms = kE4M3 ? 2 : 3;         // 16-bit terms of a weight: 11 + 11 bits of fp16, 8 + 8 + 8 of bf16
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ uint64_t full[kWarps][kStages];
   __shared__ int abort_flag;
+  __shared__ long long scratch[kWarps];
+  __shared__ int s_first;
+  __shared__ long long s_base;
 
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int quad = lane >> 2, c = lane & 3;     // fragment coordinates
-  const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len, n_splits = p.splits;
-  // block -> (split, KV head, tile of query rows, sequence), splits fastest
-  unsigned rest = blockIdx.x;
-  const int split = rest % n_splits; rest /= n_splits;
-  const int g = rest % Hkv; rest /= Hkv;
-  const int tile = rest % p.row_tiles;
-  const int b = rest / p.row_tiles;
-  const int row_base = tile * kRows;
+  const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len;
 
   if (t == 0) {
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
+    abort_flag = 0;
+    s_first = -1;
   }
   if (lane == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (t == 0) abort_flag = 0;
   __syncthreads();
   pdl_wait();
-  pdl_launch_dependents();
 
-  const int asked = p.lens[b];
-  const int len = usable_len(asked, p.c.max_pages, p.c.page_log2);
-  if (t == 0 && split == 0 && g == 0 && tile == 0 && asked != len) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
-  const int n_chunks_all = (len + kChunk - 1) / kChunk;
-  const int per = (n_chunks_all + n_splits - 1) / n_splits;
-  const int c0 = split * per, c1 = min(n_chunks_all, c0 + per);
-  const int my_chunks = c1 - c0 > warp ? (c1 - c0 - warp + kWarps - 1) / kWarps : 0;
-
-  // ---- query fragments: rows quad and (RT == 2) quad + 8 of the tile, absent rows zero ----
-  uint32_t qa[KS][2 * RT];
-  float q_scale[RT];                            // logit per accumulated unit (log2)
-  int sees[RT];                                 // entries the row sees
+  // ---- this CTA's share: units [u, u_end) of a row of (sequence, row tile x KV head, chunk) ----
+  const int HT = Hkv * p.row_tiles;
+  int b, ht, c0, c1, n_chunks;
+  long long u = 0, u_end = 0, u_begin = 0;
+  if (p.balanced) {
+    const int per = (p.c.batch + kThreads - 1) / kThreads, b0 = min(t * per, p.c.batch), b1 = min(b0 + per, p.c.batch);
+    long long mine = 0;
+    for (int x = b0; x < b1; ++x) mine += chunks_of(p, x, kChunkLog2);
+    const long long total = block_sum<kThreads>(mine, scratch) * HT;
+    // chunks of the sequences before this thread's
+    long long before = mine;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = row_base + rt * 8 + quad;
-    const bool there = r < p.rows;
-    const int i = there ? r / G : 0, h = g * G + (there ? r - i * G : 0);
-    sees[rt] = len - (T - 1 - i);
-    const uint16_t* qp = p.q + ((static_cast<size_t>(b) * T + i) * p.n_q_heads + h) * D;
-    q_scale[rt] = p.scale_log2;
-    if constexpr (kE4M3) {
-      // element order of the 8-bit K rows: k index 2c, 2c + 1, 2c + 8, 2c + 9 of a step is element 4c .. 4c + 3
-      uint2 w[KS];
-      float m = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        w[ks] = there ? *reinterpret_cast<const uint2*>(qp + ks * 16 + c * 4) : make_uint2(0u, 0u);
-        float a, d;
-        unpack16<false>(w[ks].x, a, d);
-        m = fmaxf(m, fmaxf(fabsf(a), fabsf(d)));
-        unpack16<false>(w[ks].y, a, d);
-        m = fmaxf(m, fmaxf(fabsf(a), fabsf(d)));
-      }
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      int up = m > 0.0f ? 14 - scale_log2(__float_as_uint(m)) : 0;
-      up = up > 120 ? 120 : up;                 // of a subnormal row; otherwise within [-113, 120] as it stands
-      const float f = __uint_as_float(pow2_bits(up));
-      q_scale[rt] *= __uint_as_float(pow2_bits(-up));
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        float a, d;
-        unpack16<false>(w[ks].x, a, d);
-        qa[ks][rt] = pack16<true>(a * f, d * f);
-        unpack16<false>(w[ks].y, a, d);
-        qa[ks][RT + rt] = pack16<true>(a * f, d * f);
-      }
-    } else {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qa[ks][rt] = there ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + c * 2) : 0u;
-        qa[ks][RT + rt] = there ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + c * 2 + 8) : 0u;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += y;
+    }
+    before -= mine;
+    for (int w = 0; w < warp; ++w) before += scratch[w];
+    u_begin = u = share_begin(total, blockIdx.x, gridDim.x);
+    u_end = share_begin(total, blockIdx.x + 1, gridDim.x);
+    if (u < u_end && before * HT <= u && u < (before + mine) * HT) {
+      long long base = before;
+      for (int x = b0; x < b1; ++x) {
+        const int n = chunks_of(p, x, kChunkLog2);
+        if (u < (base + n) * HT) { s_first = x; s_base = base * HT; break; }
+        base += n;
       }
     }
-  }
-  // O^T per row tile: [0] (d0, row 2c), [1] (d0, row 2c + 1), [2] (d1, row 2c), [3] (d1, row 2c + 1); (d0, d1) is
-  // (quad, quad + 8) of the 16-wide step mt for bf16 and (2 quad, 2 quad + 1) for 8-bit rows
-  float o[RT][MT][4];
-  float m_run[RT], l_part[RT], r_run[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m_run[rt] = r_run[rt] = -INFINITY;
-    l_part[rt] = 0.0f;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[rt][mt][e] = 0.0f;
+    __syncthreads();
+    b = s_first;
+    if (b < 0) return;                          // nothing for this CTA
+    n_chunks = chunks_of(p, b, kChunkLog2);
+    ht = static_cast<int>((u - s_base) / n_chunks);
+    c0 = static_cast<int>((u - s_base) - static_cast<long long>(ht) * n_chunks);
+    c1 = static_cast<int>(min(static_cast<long long>(n_chunks), c0 + (u_end - u)));
+  } else {
+    unsigned rest = blockIdx.x;                   // row tiles fastest: they read the same entries
+    const int tile = rest % p.row_tiles; rest /= p.row_tiles;
+    const int split = rest % p.splits; rest /= p.splits;
+    ht = tile * Hkv + rest % Hkv;
+    b = rest / Hkv;
+    n_chunks = chunks_of(p, b, kChunkLog2);
+    const int per = (n_chunks + p.splits - 1) / p.splits;
+    c0 = min(split * per, n_chunks);
+    c1 = min(n_chunks, c0 + per);
   }
 
   uint8_t* const ring_ptr = smem + warp * kStages * Cfg::kStageBytes;
   const uint32_t ring = smem_u32(ring_ptr);
-  const uint64_t policy = l2_policy_evict_first();
-  const int* const table = p.c.block_table + static_cast<size_t>(b) * p.c.max_pages;
-  const int page_chunks_log2 = p.c.page_log2 - 4;          // chunks of 16 entries in a page
-
-  // Page and scales of the warp's chunk i for lane i % 32, fetched for 32 chunks at a time.
-  auto page_of = [&](int i) -> int {                       // block (page * Hkv + g) of this lane's chunk i
-    if (i >= my_chunks) return 0;
-    const int pid = table[(c0 + warp + i * kWarps) >> page_chunks_log2];
-    const long long blk = pool_block(pid, p.c.n_pages, Hkv, g);
-    if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_PAGE); return g; }   // page 0 instead
-    return static_cast<int>(blk);
-  };
-  int blk_cur = page_of(lane), blk_next = page_of(32 + lane);
-  float sk_cur = 1.0f, sv_cur = 1.0f, sk_next = 1.0f, sv_next = 1.0f;
-  if constexpr (kE4M3) {
-    sk_cur = p.c.k_scales[blk_cur]; sv_cur = p.c.v_scales[blk_cur];
-    sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next];
-  }
-  auto issue = [&](int i, int blk) {                       // lane 0 only
-    const int row = ((c0 + warp + i * kWarps) & ((1 << page_chunks_log2) - 1)) * kChunk;
-    uint64_t* bar = &full[warp][i % kStages];
-    uint8_t* stage = ring_ptr + (i % kStages) * Cfg::kStageBytes;
-    mbar_arrive_expect_tx(bar, Cfg::kStageBytes);
-#pragma unroll
-    for (int x = 0; x < Cfg::kBoxes; ++x) {
-      tma_load_3d(stage + x * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk, policy);
-      tma_load_3d(stage + Cfg::kHalfBytes + x * Cfg::kBoxBytes, &tmap_v, bar, x * 64, row, blk, policy);
-    }
-  };
-  int issued = 0;
-  for (; issued < kStages - 1 && issued < my_chunks; ++issued) {
-    const int blk = __shfl_sync(0xffffffffu, blk_cur, issued);
-    if (lane == 0) issue(issued, blk);
-  }
+  const uint64_t policy = p.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+  const int page_subs_log2 = p.c.page_log2 - 4;            // steps of 16 entries in a page
   const uint32_t row7 = lane & 7;
   const uint32_t swz = Cfg::kBoxRow == 128 ? row7 : (row7 >> 1);      // 16-byte piece p of row r sits at p ^ swz
-  bool ok = true;
-  int done = 0;
-  for (int i = 0; i < my_chunks; ++i) {
-    if ((i & 31) == 0 && i > 0) {                          // the next batch of 32 chunks becomes the current one
-      blk_cur = blk_next;
-      sk_cur = sk_next; sv_cur = sv_next;
-      blk_next = page_of(i + 32 + lane);
-      if constexpr (kE4M3) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
-    }
-    if (issued < my_chunks) {                              // the stage it goes to was consumed last iteration
-      const int blk = (issued >> 5) == (i >> 5) ? __shfl_sync(0xffffffffu, blk_cur, issued & 31)
-                                                : __shfl_sync(0xffffffffu, blk_next, issued & 31);
-      if (lane == 0) issue(issued, blk);
-      ++issued;
-    }
-    ok = mbar_wait_bounded(&full[warp][i % kStages], (i / kStages) & 1, &abort_flag, p.hdr, SITE_PAGED_WAIT);
-    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-    const uint32_t ks_addr = ring + (i % kStages) * Cfg::kStageBytes;
-    const uint32_t vs_addr = ks_addr + Cfg::kHalfBytes;
-    const int key0 = (c0 + warp + i * kWarps) * kChunk;
-    const int rows = min(kChunk, len - key0);
-    if (rows < kChunk) {
-      // the sequence's last chunk: what lies behind its end in the page is not its own.  The logits are masked below, but
-      // a zero weight does not silence a NaN in V, so those V rows are cleared.
-      uint8_t* vs = ring_ptr + (i % kStages) * Cfg::kStageBytes + Cfg::kHalfBytes;
-      constexpr int kPieces = Cfg::kBoxRow / 16;
-      const int n = (kChunk - rows) * kPieces;
-      for (int j = lane; j < Cfg::kBoxes * n; j += 32) {
-        const int x = j / n, rem = j - x * n;
-        *reinterpret_cast<uint4*>(vs + x * Cfg::kBoxBytes + rows * Cfg::kBoxRow + rem * 16) = make_uint4(0u, 0u, 0u, 0u);
-      }
-      __syncwarp();
-    }
-    // ---- S = Q K^T: two tiles of 8 entries; lane holds (row quad, entries nt * 8 + 2c, + 1) in [0], [1], row quad + 8 in [2], [3] ----
-    float s[2][4];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][e] = 0.0f;
-    }
+  int stage_in = 0, stage_out = 0;                         // ring positions, carried from segment to segment
+  uint32_t phase_out = 0;
+  bool ok = true;                                          // false: a wait gave up; nothing more is copied or computed
+
+  while (true) {
+    const int g = ht % Hkv, tile = ht / Hkv, row_base = tile * kRows;
+    const int asked = p.lens[b];
+    const int len = usable_len(asked, p.c.max_pages, p.c.page_log2);
+    if (t == 0 && c0 == 0 && ht == 0 && asked != len) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
+    const int my_chunks = ok && c1 - c0 > warp ? (c1 - c0 - warp + kWarps - 1) / kWarps : 0;
+    const int* const table = p.c.block_table + static_cast<size_t>(b) * p.c.max_pages;
+    const int n_subs = (len + kSub - 1) / kSub;
+
+    // Page and scales of the warp's 16-entry step x for lane x % 32, fetched for 32 steps at a time.
+    auto block_of = [&](int x) -> int {                    // block (page * Hkv + g) of this lane's step
+      const int i = x / NSUB, sub = (c0 + warp + i * kWarps) * NSUB + x % NSUB;
+      if (i >= my_chunks || sub >= n_subs) return -1;
+      const long long blk = pool_block(table[sub >> page_subs_log2], p.c.n_pages, Hkv, g);
+      if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_PAGE); return g; }   // page 0 instead
+      return static_cast<int>(blk);
+    };
+    int blk_cur = block_of(lane), blk_next = block_of(32 + lane);
+    float sk_cur = 1.0f, sv_cur = 1.0f, sk_next = 1.0f, sv_next = 1.0f;
     if constexpr (kE4M3) {
-#pragma unroll
-      for (int k4 = 0; k4 < KS / 4; ++k4) {
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          uint32_t kb[4];                       // four 16-element steps of eight K rows
-          const uint32_t piece = k4 * 4 + (lane >> 3);
-          ldsm_x4(kb, ks_addr + (nt * 8 + row7) * Cfg::kBoxRow + ((piece ^ swz) << 4));
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int ks = k4 * 4 + y;
-            mma16<true>(s[nt], qa[ks][0], RT == 2 ? qa[ks][RT - 1] : 0u, qa[ks][RT], RT == 2 ? qa[ks][2 * RT - 1] : 0u,
-                        widen_lo(kb[y]), widen_hi(kb[y]));
-          }
-        }
-      }
-    } else {
-#pragma unroll
-      for (int k2 = 0; k2 < KS / 2; ++k2) {
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          uint32_t kb[4];
-          const uint32_t piece = (k2 & 1) * 4 + (lane >> 3);
-          ldsm_x4(kb, ks_addr + (k2 >> 1) * Cfg::kBoxBytes + (nt * 8 + row7) * 128 + ((piece ^ swz) << 4));
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int ks = k2 * 2 + y;
-            mma16<false>(s[nt], qa[ks][0], RT == 2 ? qa[ks][RT - 1] : 0u, qa[ks][RT], RT == 2 ? qa[ks][2 * RT - 1] : 0u,
-                         kb[2 * y], kb[2 * y + 1]);
-          }
-        }
-      }
+      if (blk_cur >= 0) { sk_cur = p.c.k_scales[blk_cur]; sv_cur = p.c.v_scales[blk_cur]; }
+      if (blk_next >= 0) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
     }
-    float sk = 1.0f, ev = 0.0f;
-    if constexpr (kE4M3) {
-      sk = __shfl_sync(0xffffffffu, sk_cur, i & 31);
-      ev = static_cast<float>(scale_log2(__float_as_uint(__shfl_sync(0xffffffffu, sv_cur, i & 31))));
-    }
-    uint32_t ph[RT][2], pl[RT][2];
-    float alpha[RT];
+    auto issue = [&](int i, int sub_in, int blk) {         // lane 0 only: one box of K and one of V per 128 bytes of a row
+      const int sub = (c0 + warp + i * kWarps) * NSUB + sub_in;
+      const int row = (sub & ((1 << page_subs_log2) - 1)) * kSub;
+      uint64_t* bar = &full[warp][stage_in];
+      uint8_t* stage = ring_ptr + stage_in * Cfg::kStageBytes + sub_in * kSub * Cfg::kBoxRow;
+#pragma unroll
+      for (int x = 0; x < Cfg::kBoxes; ++x) {
+        tma_load_3d(stage + x * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk, policy);
+        tma_load_3d(stage + Cfg::kHalfBytes + x * Cfg::kBoxBytes, &tmap_v, bar, x * 64, row, blk, policy);
+      }
+    };
+    // All lanes: starts the copies of the warp's chunk i (a step behind the sequence's end brings page 0: masked below).
+    auto start = [&](int i, int now) {
+      const bool next = (i * NSUB >> 5) != (now * NSUB >> 5);
+      if (lane == 0) mbar_arrive_expect_tx(&full[warp][stage_in], Cfg::kStageBytes);
+#pragma unroll
+      for (int y = 0; y < NSUB; ++y) {
+        const int from = (i * NSUB + y) & 31;
+        const int blk = next ? __shfl_sync(0xffffffffu, blk_next, from) : __shfl_sync(0xffffffffu, blk_cur, from);
+        if (lane == 0 && (y == 0 || p.box_subs == 1)) issue(i, y, max(blk, 0));
+      }
+      stage_in = stage_in + 1 == kStages ? 0 : stage_in + 1;
+    };
+    int issued = 0;
+    for (; issued < kStages - 1 && issued < my_chunks; ++issued) start(issued, 0);
+
+    // ---- query fragments: rows quad and (RT == 2) quad + 8 of the tile, absent rows zero ----
+    uint32_t qa[KS][2 * RT];
+    float q_scale[RT];                            // logit per accumulated unit (log2)
+    int sees[RT];                                 // entries the row sees
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      // ---- online softmax of row quad (+ 8 rt): its 16 logits sit in the four lanes of the quad ----
-      const float f = q_scale[rt] * sk;
-      float sv[4];
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          sv[nt * 2 + e] = key0 + nt * 8 + c * 2 + e < sees[rt] ? s[nt][rt * 2 + e] * f : -INFINITY;
-      float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float m_new = fmaxf(m_run[rt], mx);
-      const float ref = m_new == -INFINITY ? 0.0f : m_new;             // nothing seen yet: everything stays at zero
-      const float alpha_l = ex2(m_run[rt] - ref);
-      float pr[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pr[e] = ex2(sv[e] - ref);
-      l_part[rt] = l_part[rt] * alpha_l + ((pr[0] + pr[1]) + (pr[2] + pr[3]));
-      m_run[rt] = m_new;
+      const int r = row_base + rt * 8 + quad;
+      const bool there = r < p.rows;
+      const int i = there ? r / G : 0, h = g * G + (there ? r - i * G : 0);
+      sees[rt] = len - (T - 1 - i);
+      const uint16_t* qp = p.q + ((static_cast<size_t>(b) * T + i) * p.n_q_heads + h) * D;
+      q_scale[rt] = p.scale_log2;
       if constexpr (kE4M3) {
-        const float r_new = fmaxf(r_run[rt], mx + ev);
-        const float refo = r_new == -INFINITY ? 0.0f : r_new;
-        alpha[rt] = ex2(r_run[rt] - refo);
-        r_run[rt] = r_new;
-        const float shift = ev - refo + kShift;
+        // element order of the 8-bit K rows: k index 2c, 2c + 1, 2c + 8, 2c + 9 of a step is element 4c .. 4c + 3
+        uint2 w[KS];
+        float m = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pr[e] = ex2(sv[e] + shift);
+        for (int ks = 0; ks < KS; ++ks) {
+          w[ks] = there ? *reinterpret_cast<const uint2*>(qp + ks * 16 + c * 4) : make_uint2(0u, 0u);
+          float a, d;
+          unpack16<false>(w[ks].x, a, d);
+          m = fmaxf(m, fmaxf(fabsf(a), fabsf(d)));
+          unpack16<false>(w[ks].y, a, d);
+          m = fmaxf(m, fmaxf(fabsf(a), fabsf(d)));
+        }
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        int up = m > 0.0f ? 14 - scale_log2(__float_as_uint(m)) : 0;
+        up = up > 120 ? 120 : up;                 // of a subnormal row; otherwise within [-113, 120] as it stands
+        const float f = __uint_as_float(pow2_bits(up));
+        q_scale[rt] *= __uint_as_float(pow2_bits(-up));
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          float a, d;
+          unpack16<false>(w[ks].x, a, d);
+          qa[ks][rt] = pack16<true>(a * f, d * f);
+          unpack16<false>(w[ks].y, a, d);
+          qa[ks][RT + rt] = pack16<true>(a * f, d * f);
+        }
       } else {
-        alpha[rt] = alpha_l;
-      }
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        ph[rt][y] = pack16<kE4M3>(pr[2 * y], pr[2 * y + 1]);
-        float a, d;
-        unpack16<kE4M3>(ph[rt][y], a, d);
-        pl[rt][y] = pack16<kE4M3>(pr[2 * y] - a, pr[2 * y + 1] - d);
-      }
-    }
-    bool moved = false;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) moved |= alpha[rt] != 1.0f;
-    if (__any_sync(0xffffffffu, moved)) {        // the running maxima settle after a few chunks
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const float a0 = __shfl_sync(0xffffffffu, alpha[rt], 8 * c), a1 = __shfl_sync(0xffffffffu, alpha[rt], 8 * c + 4);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          o[rt][mt][0] *= a0; o[rt][mt][1] *= a1; o[rt][mt][2] *= a0; o[rt][mt][3] *= a1;
+        for (int ks = 0; ks < KS; ++ks) {
+          qa[ks][rt] = there ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + c * 2) : 0u;
+          qa[ks][RT + rt] = there ? *reinterpret_cast<const uint32_t*>(qp + ks * 16 + c * 2 + 8) : 0u;
         }
       }
     }
-    // ---- O^T += V^T P^T ----
-    if constexpr (kE4M3) {
+    // O^T per row tile: [0] (d0, row 2c), [1] (d0, row 2c + 1), [2] (d1, row 2c), [3] (d1, row 2c + 1); (d0, d1) is
+    // (quad, quad + 8) of the 16-wide step mt for bf16 and (2 quad, 2 quad + 1) for 8-bit rows
+    float o[RT][MT][4];
+    float m_run[RT], l_part[RT], r_run[RT];
 #pragma unroll
-      for (int m2 = 0; m2 < MT / 2; ++m2) {
-        uint32_t vb[4];                         // entries 0..7 and 8..15 of pieces 2 m2 and 2 m2 + 1
-        const uint32_t piece = m2 * 2 + (lane >> 4);
-        ldsm_x4_trans(vb, vs_addr + (((lane >> 3) & 1) * 8 + row7) * Cfg::kBoxRow + ((piece ^ swz) << 4));
+    for (int rt = 0; rt < RT; ++rt) {
+      m_run[rt] = r_run[rt] = -INFINITY;
+      l_part[rt] = 0.0f;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          // a word holds elements (2 quad, 2 quad + 1) of entry 2c, then of entry 2c + 1: bring equal elements together
-          const uint32_t w0 = __byte_perm(vb[2 * y], 0, 0x3120), w1 = __byte_perm(vb[2 * y + 1], 0, 0x3120);
-          const uint32_t a0 = widen_lo(w0), a1 = widen_hi(w0), a2 = widen_lo(w1), a3 = widen_hi(w1);
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            mma16<true>(o[rt][2 * m2 + y], a0, a1, a2, a3, ph[rt][0], ph[rt][1]);
-            mma16<true>(o[rt][2 * m2 + y], a0, a1, a2, a3, pl[rt][0], pl[rt][1]);
+        for (int e = 0; e < 4; ++e) o[rt][mt][e] = 0.0f;
+    }
+
+    // One pass over the chunk in stage st.  kTail: some row does not see all of it (the sequence's end, and what follows a query's
+    // own token).  Products that follow one another are independent (a dependent one waits 21 cycles, the tensor cores take one
+    // every 8), and the matrix loads are asked for a phase ahead of their use: K's together, V's before the softmax step whose
+    // latency they hide in.
+    auto pass = [&](auto tail_, int i, int st) {
+      constexpr bool kTail = decltype(tail_)::value;
+      const int key0 = (c0 + warp + i * kWarps) * kChunk;
+      const uint32_t ks_addr = ring + st * Cfg::kStageBytes, vs_addr = ks_addr + Cfg::kHalfBytes;
+      if (kTail && len - key0 < kChunk) {
+        // what lies behind the sequence's end in the page is not its own: the logits are masked, but a zero weight does not
+        // silence a NaN in V, so those V rows are cleared
+        const int rows = len - key0;
+        uint8_t* vs = ring_ptr + st * Cfg::kStageBytes + Cfg::kHalfBytes;
+        constexpr int kPieces = Cfg::kBoxRow / 16;
+        const int n = (kChunk - rows) * kPieces;
+        for (int j = lane; j < Cfg::kBoxes * n; j += 32) {
+          const int x = j / n, rem = j - x * n;
+          *reinterpret_cast<uint4*>(vs + x * Cfg::kBoxBytes + rows * Cfg::kBoxRow + rem * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+      }
+      // ---- S = Q K^T, 8 entries a tile: lane holds (row quad, entries nt * 8 + 2c, + 1) in [0], [1], row quad + 8 in [2], [3] ----
+      float s[2 * NSUB][4];
+      {
+        const uint32_t at = ks_addr + row7 * Cfg::kBoxRow + (((lane >> 3) ^ swz) << 4);
+        constexpr int kLoads = Cfg::kRowBytes / 64;             // matrix loads of eight K rows: 64 bytes of each
+        uint32_t kb[kLoads][2 * NSUB][4];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+#pragma unroll
+          for (int nt = 0; nt < 2 * NSUB; ++nt)
+            ldsm_x4(kb[l][nt], (at ^ ((l & 1) << 6)) + (l >> 1) * Cfg::kBoxBytes + nt * 8 * Cfg::kBoxRow);
+        constexpr int kEach = kE4M3 ? 4 : 2;                    // 16-element steps that a load brings
+        float d[4][4];                                          // four sums at a time: the tiles, or halves of two tiles
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+#pragma unroll
+          for (int y = 0; y < kEach; ++y)
+#pragma unroll
+            for (int nt = 0; nt < 2 * NSUB; ++nt) {
+              const int ks = l * kEach + y;
+              const uint32_t q0 = qa[ks][0], q1 = RT == 2 ? qa[ks][RT - 1] : 0u, q2 = qa[ks][RT], q3 = RT == 2 ? qa[ks][2 * RT - 1] : 0u;
+              if constexpr (kE4M3) mma16<true>(d[nt], ks == 0, q0, q1, q2, q3, widen_lo(kb[l][nt][y]), widen_hi(kb[l][nt][y]));
+              else mma16<false>(d[(y & 1) * 2 + nt], ks < 2, q0, q1, q2, q3, kb[l][nt][2 * y], kb[l][nt][2 * y + 1]);
+            }
+#pragma unroll
+        for (int nt = 0; nt < 2 * NSUB; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nt][e] = kE4M3 ? d[nt][e] : d[nt][e] + d[2 + nt][e];
+      }
+      // V's fragments, as loaded.  8-bit rows: entries 0..7 and 8..15 of step y, pieces 2l and 2l + 1; bf16: 16 elements x 16 entries
+      constexpr int kVLoads = Cfg::kRowBytes / 32;
+      uint32_t vb[kVLoads][NSUB][4];
+      {
+        const uint32_t at = kE4M3 ? vs_addr + (((lane >> 3) & 1) * 8 + row7) * Cfg::kBoxRow + (((lane >> 4) ^ swz) << 4)
+                                  : vs_addr + ((lane >> 4) * 8 + row7) * Cfg::kBoxRow + ((((lane >> 3) & 1) ^ swz) << 4);
+#pragma unroll
+        for (int l = 0; l < kVLoads; ++l)
+#pragma unroll
+          for (int y = 0; y < NSUB; ++y)
+            ldsm_x4_trans(vb[l][y], (at ^ ((l & 3) << 5)) + (l >> 2) * Cfg::kBoxBytes + y * kSub * Cfg::kBoxRow);
+      }
+      float sk[NSUB], ev[NSUB];
+#pragma unroll
+      for (int y = 0; y < NSUB; ++y) {
+        sk[y] = 1.0f;
+        ev[y] = 0.0f;
+        if constexpr (kE4M3) {
+          sk[y] = __shfl_sync(0xffffffffu, sk_cur, (i * NSUB + y) & 31);
+          ev[y] = static_cast<float>(scale_log2(__float_as_uint(__shfl_sync(0xffffffffu, sv_cur, (i * NSUB + y) & 31))));
+        }
+      }
+      uint32_t pt[RT][kTerms][NSUB][2];             // the weights as B fragments, term by term
+      float a0[RT], a1[RT];                         // what the outputs of rows 2c and 2c + 1 are scaled by
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        // ---- online softmax of row quad (+ 8 rt): its logits sit in the four lanes of the quad ----
+        if constexpr (kTail) {
+#pragma unroll
+          for (int nt = 0; nt < 2 * NSUB; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (key0 + nt * 8 + c * 2 + e >= sees[rt]) s[nt][rt * 2 + e] = -INFINITY;
+        }
+        float f[NSUB], top[NSUB];
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) {
+          f[y] = fmaxf(q_scale[rt] * sk[y], 1.17549435e-38f);            // positive, so that a masked logit stays -inf
+          top[y] = fmaxf(fmaxf(s[2 * y][2 * rt], s[2 * y][2 * rt + 1]), fmaxf(s[2 * y + 1][2 * rt], s[2 * y + 1][2 * rt + 1]));
+          top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 1));
+          top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 2)) * f[y];
+        }
+        float m_new = m_run[rt];
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) m_new = fmaxf(m_new, top[y]);
+        const float ref = m_new == -INFINITY ? 0.0f : m_new;             // nothing seen yet: everything stays at zero
+        float alpha = ex2(m_run[rt] - ref);
+        float pr[NSUB][4], sum = 0.0f;
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pr[y][e] = ex2(fmaf(s[2 * y + (e >> 1)][2 * rt + (e & 1)], f[y], -ref));
+          sum += (pr[y][0] + pr[y][1]) + (pr[y][2] + pr[y][3]);
+        }
+        l_part[rt] = fmaf(l_part[rt], alpha, sum);
+        m_run[rt] = m_new;
+        if constexpr (kE4M3) {
+          float r_new = r_run[rt];
+#pragma unroll
+          for (int y = 0; y < NSUB; ++y) r_new = fmaxf(r_new, top[y] + ev[y]);
+          const float refo = r_new == -INFINITY ? 0.0f : r_new;
+          alpha = ex2(r_run[rt] - refo);
+          r_run[rt] = r_new;
+#pragma unroll
+          for (int y = 0; y < NSUB; ++y) {
+            const float shift = ev[y] - refo + kShift;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[y][e] = ex2(fmaf(s[2 * y + (e >> 1)][2 * rt + (e & 1)], f[y], shift));
+          }
+        }
+        a0[rt] = __shfl_sync(0xffffffffu, alpha, 8 * c);
+        a1[rt] = __shfl_sync(0xffffffffu, alpha, 8 * c + 4);
+        // the weights as 16-bit terms: the leading bits cut off, then what is left (the last term rounded)
+        constexpr uint32_t kKeep = kE4M3 ? 0xffffe000u : 0xffff0000u;
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) {
+#pragma unroll
+          for (int w = 0; w < kTerms; ++w) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float lo = pr[y][2 * x], hi = pr[y][2 * x + 1];
+              if (w + 1 < kTerms) {
+                lo = __uint_as_float(__float_as_uint(lo) & kKeep);
+                hi = __uint_as_float(__float_as_uint(hi) & kKeep);
+                pr[y][2 * x] -= lo;
+                pr[y][2 * x + 1] -= hi;
+              }
+              if (!kE4M3 && w + 1 < kTerms) pt[rt][w][y][x] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+              else pt[rt][w][y][x] = pack16<kE4M3>(lo, hi);
+            }
           }
         }
       }
-    } else {
+      // ---- O^T = O^T alpha + V^T P^T.  The products of a chunk start from zero and join the running outputs with one rounding
+      // to nearest: the tensor cores cut their sums off, and over thousands of chunks that bias shows. ----
+      auto join = [&](float (&acc)[4], const float (&x)[4], float f0, float f1) {
+        acc[0] = fmaf(acc[0], f0, x[0]); acc[1] = fmaf(acc[1], f1, x[1]);
+        acc[2] = fmaf(acc[2], f0, x[2]); acc[3] = fmaf(acc[3], f1, x[3]);
+      };
+      constexpr int kTogether = 4 / RT;             // 16-element tiles of the head dimension whose sums run side by side
+#pragma unroll
+      for (int m0 = 0; m0 < MT; m0 += kTogether) {
+        float x[kTogether][RT][4];
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) {
+          uint32_t v[kTogether][4];
+#pragma unroll
+          for (int z = 0; z < kTogether; ++z) {
+            const int m = m0 + z;
+            if constexpr (kE4M3) {
+              // a word holds elements (2 quad, 2 quad + 1) of entry 2c, then of entry 2c + 1: bring equal elements together
+              const uint32_t w0 = __byte_perm(vb[m / 2][y][2 * (m & 1)], 0, 0x3120), w1 = __byte_perm(vb[m / 2][y][2 * (m & 1) + 1], 0, 0x3120);
+              v[z][0] = widen_lo(w0); v[z][1] = widen_hi(w0); v[z][2] = widen_lo(w1); v[z][3] = widen_hi(w1);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[z][e] = vb[m][0][e];
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < kTerms; ++w)
+#pragma unroll
+            for (int z = 0; z < kTogether; ++z)
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt)
+                mma16<kE4M3>(x[z][rt], y == 0 && w == 0, v[z][0], v[z][1], v[z][2], v[z][3], pt[rt][w][y][0], pt[rt][w][y][1]);
+        }
+#pragma unroll
+        for (int z = 0; z < kTogether; ++z)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) join(o[rt][m0 + z], x[z][rt], a0[rt], a1[rt]);
+      }
+    };
+    int waited = 0;                                // chunks whose copies have been waited for
+    for (int i = 0; i < my_chunks; ++i) {
+      if ((i * NSUB & 31) == 0 && i > 0) {                   // the next batch of 32 steps becomes the current one
+        blk_cur = blk_next;
+        sk_cur = sk_next; sv_cur = sv_next;
+        blk_next = block_of(i * NSUB + 32 + lane);
+        sk_next = sv_next = 1.0f;
+        if constexpr (kE4M3)
+          if (blk_next >= 0) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
+      }
+      if (issued < my_chunks) start(issued++, i);            // into the stage that was emptied last iteration
+      ok = mbar_wait_bounded(&full[warp][stage_out], phase_out, &abort_flag, p.hdr, SITE_PAGED_WAIT);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      ++waited;
+      const int st = stage_out;
+      if (++stage_out == kStages) { stage_out = 0; phase_out ^= 1; }
+      if ((c0 + warp + i * kWarps + 1) * kChunk <= len - (T - 1)) pass(std::false_type{}, i, st);
+      else pass(std::true_type{}, i, st);
+      __syncwarp();                                // every lane is done with the stage before it is refilled
+    }
+    if (lane == 0)                                 // after a wait that gave up: no copy may still be in flight
+      for (int j = waited; j < issued; ++j) {
+        const int x = stage_out + (j - waited);
+        mbar_wait_drain(&full[warp][x % kStages], phase_out ^ (x >= kStages ? 1u : 0u), p.hdr, SITE_PAGED_WAIT);
+      }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 1);
+      l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 2);
+      if constexpr (!kE4M3) r_run[rt] = m_run[rt];
+    }
+    pdl_launch_dependents();
+    // ---- the warps of the CTA merge through shared memory (the rings are idle: every copy was waited for) ----
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(smem);                                  // [warps][rows][D]
+    float4* mml = reinterpret_cast<float4*>(mo + kWarps * kRows * D);            // [warps][rows]: max, sum, reference
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        uint32_t va[4];
-        const uint32_t piece = (mt & 3) * 2 + ((lane >> 3) & 1);
-        ldsm_x4_trans(va, vs_addr + (mt >> 2) * Cfg::kBoxBytes + ((lane >> 4) * 8 + row7) * 128 + ((piece ^ swz) << 4));
+        const int d0 = mt * 16 + (kE4M3 ? 2 * quad : quad), d1 = d0 + (kE4M3 ? 1 : 8);
+        float* row0 = mo + (warp * kRows + rt * 8 + 2 * c) * D;
+        row0[d0] = o[rt][mt][0]; row0[D + d0] = o[rt][mt][1]; row0[d1] = o[rt][mt][2]; row0[D + d1] = o[rt][mt][3];
+      }
+      if (c == 0) mml[warp * kRows + rt * 8 + quad] =
+          make_float4(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f, ok ? r_run[rt] : -INFINITY, 0.0f);
+    }
+    __syncthreads();
+    const int n_rows = min(kRows, p.rows - row_base);
+    const bool whole = p.balanced ? c0 == 0 && c1 == n_chunks : p.splits == 1;
+    // where a piece's result waits for the merge: static launches by (pair, split), balanced ones by CTA (first segment or later)
+    const size_t part = (p.balanced ? 2 * static_cast<size_t>(blockIdx.x) + (u != u_begin) : static_cast<size_t>(blockIdx.x)) * kRows;
+    for (int x = t; x < n_rows * D; x += kThreads) {
+      const int r = x / D, col = x - r * D;
+      float M = -INFINITY, R = -INFINITY;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          mma16<false>(o[rt][mt], va[0], va[1], va[2], va[3], ph[rt][0], ph[rt][1]);
-          mma16<false>(o[rt][mt], va[0], va[1], va[2], va[3], pl[rt][0], pl[rt][1]);
-        }
+      for (int w = 0; w < kWarps; ++w) {
+        M = fmaxf(M, mml[w * kRows + r].x);
+        R = fmaxf(R, mml[w * kRows + r].z);
+      }
+      float L = 0.0f, acc = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float4 ml = mml[w * kRows + r];
+        if (ml.x == -INFINITY) continue;                                          // warps without entries weigh nothing
+        L = fmaf(ml.y, ex2(ml.x - M), L);
+        acc = fmaf(mo[(w * kRows + r) * D + col], ex2(ml.z - R), acc);
+      }
+      if (whole) {
+        const int row = row_base + r, i = row / G, h = g * G + row - i * G;
+        const size_t at = (static_cast<size_t>(b) * T + i) * p.n_q_heads + h;
+        p.out[at * D + col] = L > 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
+        if (p.lse != nullptr && col == 0) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+      } else {
+        if (col == 0) p.part_ml[part + r] = make_float4(M, L, R, 0.0f);
+        p.part_o[(part + r) * D + col] = acc;
       }
     }
-    __syncwarp();                                // every lane is done with the stage before it is refilled
-    done = i + 1;
-  }
-  if (lane == 0)                                 // after a wait that gave up: no copy may still be in flight
-    for (int j = done; j < issued; ++j)
-      mbar_wait_drain(&full[warp][j % kStages], (j / kStages) & 1, p.hdr, SITE_PAGED_WAIT);
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 1);
-    l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 2);
-    if constexpr (!kE4M3) r_run[rt] = m_run[rt];
-  }
-  // ---- the warps of the CTA merge through shared memory (the rings are idle: every copy was waited for) ----
-  __syncthreads();
-  float* mo = reinterpret_cast<float*>(smem);                                  // [warps][rows][D]
-  float4* mml = reinterpret_cast<float4*>(mo + kWarps * kRows * D);            // [warps][rows]: max, sum, reference
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int d0 = mt * 16 + (kE4M3 ? 2 * quad : quad), d1 = d0 + (kE4M3 ? 1 : 8);
-      float* row0 = mo + (warp * kRows + rt * 8 + 2 * c) * D;
-      row0[d0] = o[rt][mt][0]; row0[D + d0] = o[rt][mt][1]; row0[d1] = o[rt][mt][2]; row0[D + d1] = o[rt][mt][3];
+    if (!p.balanced) return;
+    // ---- the next segment of this CTA's share ----
+    u += c1 - c0;
+    if (u >= u_end) return;
+    if (++ht == HT) {
+      ht = 0;
+      do { n_chunks = chunks_of(p, ++b, kChunkLog2); } while (n_chunks == 0);       // u < u_end: there is one
     }
-    if (c == 0) mml[warp * kRows + rt * 8 + quad] =
-        make_float4(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f, ok ? r_run[rt] : -INFINITY, 0.0f);
-  }
-  __syncthreads();
-  const int n_rows = min(kRows, p.rows - row_base);
-  for (int x = t; x < n_rows * D; x += 32 * kWarps) {
-    const int r = x / D, col = x - r * D;
-    float M = -INFINITY, R = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      M = fmaxf(M, mml[w * kRows + r].x);
-      R = fmaxf(R, mml[w * kRows + r].z);
-    }
-    float L = 0.0f, acc = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float4 ml = mml[w * kRows + r];
-      if (ml.x == -INFINITY) continue;                                          // warps without entries weigh nothing
-      L = fmaf(ml.y, ex2(ml.x - M), L);
-      acc = fmaf(mo[(w * kRows + r) * D + col], ex2(ml.z - R), acc);
-    }
-    const int row = row_base + r;
-    if (n_splits == 1) {
-      const int i = row / G, h = g * G + row - i * G;
-      const size_t at = (static_cast<size_t>(b) * T + i) * p.n_q_heads + h;
-      p.out[at * D + col] = L > 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
-      if (p.lse != nullptr && col == 0) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
-    } else {
-      const size_t part = ((static_cast<size_t>(b) * Hkv + g) * n_splits + split) * p.rows + row;
-      if (col == 0) p.part_ml[part] = make_float4(M, L, R, 0.0f);
-      p.part_o[part * D + col] = acc;
-    }
+    c0 = 0;
+    c1 = static_cast<int>(min(static_cast<long long>(n_chunks), u_end - u));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                   // the merge's accesses before the next copies
+    __syncthreads();
   }
 }
 
-// Merges the splits of one query row: one block of D threads each.
+// Merges the pieces of one query row: one block of D threads each.
 template <int D, bool kE4M3>
 __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p) {
-  __shared__ float f_o[kPagedMaxSplits], f_l[kPagedMaxSplits];
+  constexpr int kChunkLog2 = kE4M3 ? 5 : 4;
+  __shared__ float f_o[kPagedMaxPieces], f_l[kPagedMaxPieces], f_m[kPagedMaxPieces];
+  __shared__ float w_max[2][D / 32];
+  __shared__ long long scratch[D / 32];
   pdl_wait();
   pdl_launch_dependents();
-  const int t = threadIdx.x, n = p.splits, G = p.group;
+  const int t = threadIdx.x, G = p.group, kRows = p.tile_rows;
   // block -> (query token of the batch, head)
   const unsigned bi = blockIdx.x / p.n_q_heads;
   const int h = blockIdx.x - bi * p.n_q_heads, b = bi / p.q_len, i = bi - b * p.q_len, g = h / G;
-  const int row = i * G + h - g * G;
-  const size_t base = (static_cast<size_t>(b) * p.c.n_kv_heads + g) * n * p.rows + row;
-  float4 ml = make_float4(-INFINITY, 0.0f, -INFINITY, 0.0f);
-  if (t < n) ml = p.part_ml[base + static_cast<size_t>(t) * p.rows];
-  if (t < n) { f_o[t] = ml.z; f_l[t] = ml.x; }
-  __syncthreads();
+  const int row = i * G + h - g * G, tile = row / kRows, r = row - tile * kRows, HT = p.c.n_kv_heads * p.row_tiles;
+  const int ht = tile * p.c.n_kv_heads + g;
+  size_t first, rest;                             // the piece that comes first, and the one behind it; then they are `step` apart
+  int n, step;
+  if (p.balanced) {
+    long long before = 0, all = 0;
+    for (int x = t; x < p.c.batch; x += D) {
+      const int k = chunks_of(p, x, kChunkLog2);
+      all += k;
+      if (x < b) before += k;
+    }
+    const long long total = block_sum<D>(all, scratch) * HT;
+    const int mine = chunks_of(p, b, kChunkLog2);
+    const long long p0 = block_sum<D>(before, scratch) * HT + static_cast<long long>(ht) * mine, p1 = p0 + mine;
+    if (mine == 0) {
+      n = 0; first = rest = 0; step = 0;
+    } else {
+      const int ca = static_cast<int>(((p0 + 1) * p.ctas - 1) / total), cb = static_cast<int>((p1 * p.ctas - 1) / total);
+      if (ca == cb) return;                       // one CTA had all of it and wrote the result
+      n = cb - ca + 1;
+      first = 2 * static_cast<size_t>(ca) + (share_begin(total, ca, p.ctas) != p0);
+      rest = 2 * static_cast<size_t>(ca + 1);
+      step = 2;
+    }
+  } else {
+    n = p.splits;
+    step = p.row_tiles;
+    first = (static_cast<size_t>(b) * p.c.n_kv_heads + g) * n * step + tile;
+    rest = first + step;
+  }
+  auto piece = [&](int s) -> size_t { return (s == 0 ? first : rest + static_cast<size_t>(s - 1) * step) * kRows + r; };
+  // the first pieces' outputs are under way before their weights are known
+  constexpr int kAhead = 24;
+  float o[kAhead];
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) o[s] = s < n ? __ldcg(p.part_o + piece(s) * D + t) : 0.0f;
   float M = -INFINITY, R = -INFINITY;
-  for (int s = 0; s < n; ++s) { M = fmaxf(M, f_l[s]); R = fmaxf(R, f_o[s]); }
+  for (int s = t; s < n; s += D) {
+    const float4 ml = __ldcg(p.part_ml + piece(s));
+    f_l[s] = ml.y;
+    f_m[s] = ml.x;
+    f_o[s] = ml.z;
+    M = fmaxf(M, ml.x);
+    R = fmaxf(R, ml.z);
+  }
+#pragma unroll
+  for (int o_ = 16; o_ >= 1; o_ >>= 1) {
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o_));
+    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, o_));
+  }
+  if ((t & 31) == 0) { w_max[0][t >> 5] = M; w_max[1][t >> 5] = R; }
   __syncthreads();
-  if (t < n) {
-    f_o[t] = ml.x == -INFINITY ? 0.0f : ex2(ml.z - R);
-    f_l[t] = ml.x == -INFINITY ? 0.0f : ml.y * ex2(ml.x - M);
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) { M = fmaxf(M, w_max[0][w]); R = fmaxf(R, w_max[1][w]); }
+  for (int s = t; s < n; s += D) {
+    const float x = f_m[s];
+    f_o[s] = x == -INFINITY ? 0.0f : ex2(f_o[s] - R);          // pieces without entries weigh nothing
+    f_l[s] = x == -INFINITY ? 0.0f : f_l[s] * ex2(x - M);
   }
   __syncthreads();
   float L = 0.0f, acc = 0.0f;
   for (int s = 0; s < n; ++s) L += f_l[s];
-  const float* o = p.part_o + base * D + t;
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s)
+    if (s < n) acc = fmaf(o[s], f_o[s], acc);
 #pragma unroll 8
-  for (int s = 0; s < n; ++s) acc = fmaf(__ldg(o + static_cast<size_t>(s) * p.rows * D), f_o[s], acc);
+  for (int s = kAhead; s < n; ++s) acc = fmaf(__ldcg(p.part_o + piece(s) * D + t), f_o[s], acc);
   const size_t at = (static_cast<size_t>(b) * p.q_len + i) * p.n_q_heads + h;
   p.out[at * D + t] = L > 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
   if (p.lse != nullptr && t == 0) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
-PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, int head_dim, bool e4m3, int max_len, long long total_len) {
-  (void)head_dim; (void)e4m3; (void)total_len;
-  constexpr int kSms = 148;
+PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len) {
+  constexpr int kCapacity = 2 * 148;              // CTAs that are resident at once
   PagedAttnPlan pl;
   pl.row_tiles_of_8 = rows <= 8 ? 1 : 2;
   pl.row_tiles = (rows + 8 * pl.row_tiles_of_8 - 1) / (8 * pl.row_tiles_of_8);
+  const int chunk = e4m3 ? 2 * kSub : kSub;
   const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
-  pl.warps = pairs > kSms ? 4 : 8;
-  const long long capacity = pairs > kSms ? 2 * kSms : kSms;
-  long long splits = capacity / pairs;
-  const long long chunks = (max_len + kChunk - 1) / kChunk;
-  const long long useful = (chunks + pl.warps - 1) / pl.warps;
+  const long long chunks = (max_len + chunk - 1) / chunk;
+  // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge kernel costs 4.5 us,
+  // a warp's pass over a chunk 0.9 us in 8 bits and 0.6 us in bf16.
+  long long splits = kCapacity / pairs;
+  const long long useful = chunks <= (e4m3 ? 24 : 32) ? 1 : (chunks + kWarps - 1) / kWarps;
   if (splits > useful) splits = useful;
-  if (splits > kPagedMaxSplits) splits = kPagedMaxSplits;
+  if (splits > kPagedMaxPieces) splits = kPagedMaxPieces;
   if (splits < 1) splits = 1;
   pl.splits = static_cast<int>(splits);
+  pl.balanced = 0;
+  pl.ctas = 0;
+  // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays about eight chunks' time for every segment it
+  // starts.  Eight sequences of 4K to 64K entries, 8 bits: 235 us static, 110 us balanced; 64 of 1638 to 2048, bf16: 77 and 89.
+  const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kCapacity - 1) / kCapacity);
+  const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kCapacity;
+  if (batch >= 2 && pairs * splits <= 4 * kCapacity && fixed > 1.2 * even + 32) {
+    pl.balanced = 1;
+    pl.ctas = kCapacity;
+    pl.splits = 1;
+  }
   return pl;
 }
 
-size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int rows, int head_dim) {
-  if (plan.splits == 1) return sizeof(WorkspaceHeader);
-  const size_t parts = static_cast<size_t>(batch) * n_kv_heads * plan.splits * rows;
-  return sizeof(WorkspaceHeader) + (parts * sizeof(float4) + 255) / 256 * 256 + parts * head_dim * sizeof(float);
+static size_t pieces_of_plan(const PagedAttnPlan& plan, int batch, int n_kv_heads) {
+  if (plan.balanced) return 2 * static_cast<size_t>(plan.ctas);
+  return plan.splits == 1 ? 0 : static_cast<size_t>(batch) * n_kv_heads * plan.row_tiles * plan.splits;
+}
+size_t paged_attn_partials_offset(const PagedAttnPlan& plan, int batch, int n_kv_heads) {
+  const size_t rows = pieces_of_plan(plan, batch, n_kv_heads) * 8 * plan.row_tiles_of_8;
+  return sizeof(WorkspaceHeader) + (rows * sizeof(float4) + 255) / 256 * 256;
+}
+size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int head_dim) {
+  const size_t rows = pieces_of_plan(plan, batch, n_kv_heads) * 8 * plan.row_tiles_of_8;
+  return paged_attn_partials_offset(plan, batch, n_kv_heads) + rows * head_dim * sizeof(float);
 }
 
-template <int D, bool kE4M3, int RT, int kWarps>
+template <int D, bool kE4M3, int RT>
 static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedAttnParams& p, cudaStream_t stream, int* launches) {
-  using Cfg = PagedCfg<D, kE4M3, RT, kWarps>;
+  using Cfg = PagedCfg<D, kE4M3, RT>;
   static PerDeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(paged_attn_kernel<D, kE4M3, RT, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    e = cudaFuncSetAttribute(paged_attn_kernel<D, kE4M3, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
     configured.set(dev);
   }
-  const long long blocks = static_cast<long long>(p.c.batch) * p.row_tiles * p.c.n_kv_heads * p.splits;
+  const long long blocks = p.balanced ? p.ctas : static_cast<long long>(p.c.batch) * p.row_tiles * p.c.n_kv_heads * p.splits;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  p.tile_rows = Cfg::kRows;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-  cfg.blockDim = dim3(32 * kWarps);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Cfg::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, kE4M3, RT, kWarps>, tk, tv, static_cast<const PagedAttnParams&>(p));
+  e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, kE4M3, RT>, tk, tv, static_cast<const PagedAttnParams&>(p));
   if (e != cudaSuccess) return e;
   *launches = 1;
-  if (p.splits == 1) return cudaSuccess;
+  if (!p.balanced && p.splits == 1) return cudaSuccess;
   cfg.gridDim = dim3(static_cast<unsigned>(p.c.batch) * p.q_len * p.n_q_heads);
   cfg.blockDim = dim3(D);
   cfg.dynamicSmemBytes = 0;
@@ -558,9 +776,7 @@ static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedA
 template <int D, bool kE4M3>
 static cudaError_t launch_f(const CUtensorMap& tk, const CUtensorMap& tv, PagedAttnParams& p, const PagedAttnPlan& plan,
                             cudaStream_t stream, int* launches) {
-  if (plan.row_tiles_of_8 == 1)
-    return plan.warps == 8 ? launch_w<D, kE4M3, 1, 8>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 1, 4>(tk, tv, p, stream, launches);
-  return plan.warps == 8 ? launch_w<D, kE4M3, 2, 8>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 2, 4>(tk, tv, p, stream, launches);
+  return plan.row_tiles_of_8 == 1 ? launch_w<D, kE4M3, 1>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 2>(tk, tv, p, stream, launches);
 }
 
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
@@ -568,6 +784,8 @@ cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap
   *launches = 0;
   p.row_tiles = plan.row_tiles;
   p.splits = plan.splits;
+  p.balanced = plan.balanced;
+  p.ctas = plan.ctas;
   if (head_dim == 128)
     return e4m3 ? launch_f<128, true>(tmap_k, tmap_v, p, plan, stream, launches) : launch_f<128, false>(tmap_k, tmap_v, p, plan, stream, launches);
   if (head_dim == 64)

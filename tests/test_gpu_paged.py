@@ -418,11 +418,9 @@ def test_pools_beyond_32_bit_offsets(fmt):
 
 
 def test_a_cache_on_another_device_is_refused():
-    class Elsewhere(Pools):
-        pass
     pools = Pools("bf16", [5], [6], 16, 1, 64, 1)
     cache = pools.cache()
-    cache._device = torch.device("cuda", torch.cuda.current_device() + 1)
+    cache._index = torch.cuda.current_device() + 1
     with pytest.raises(ValueError):
         B.fastkv_paged_attn(cache, B.make_query(n_q_heads=1, max_len=5), pools.dev_lens, pools.k, pools.k, None, workspace())
     with pytest.raises(ValueError):

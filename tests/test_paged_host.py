@@ -113,19 +113,20 @@ class Fake:
     def data_ptr(self):
         return self.ptr
 
-    def numel(self):
+    @property
+    def nbytes(self):
         return self.n
 
-    def element_size(self):
-        return 1
+
+class NullStream:
+    cuda_stream = 0
 
 
 @pytest.fixture()
 def no_device(monkeypatch):
     build.build_library()
-    monkeypatch.setattr(B, "_p", lambda t: None if t is None else (t.data_ptr() if hasattr(t, "data_ptr") else t.ctypes.data))
-    monkeypatch.setattr(B, "_stream", lambda s: None)
-    monkeypatch.setattr(B, "_on_device", lambda *a: None)
+    monkeypatch.setattr(B, "_p", lambda t: None if t is None else t.data_ptr())
+    monkeypatch.setattr(B, "_here", lambda cache: 0)
 
 
 def cache(**kw):
@@ -152,7 +153,7 @@ def status_of(fn, *a):
 
 def append(c, r, lens=Fake(), q=Fake(), k=Fake(), v=Fake(), pos=Fake(), inv=Fake(), idx=None, q_out=Fake(0x80000), new_lens=None,
            ws=Fake()):
-    B.fastkv_paged_append(c, r, lens, q, k, v, pos, inv, idx, q_out, new_lens, ws)
+    B.fastkv_paged_append(c, r, lens, q, k, v, pos, inv, idx, q_out, new_lens, ws, NullStream)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -166,7 +167,7 @@ def test_bad_caches_are_refused(no_device, kw, status):
     assert status_of(append, cache(**kw), rows()) == status
     q = B.make_query(n_q_heads=8, max_len=100)
     assert status_of(B.fastkv_paged_attn_workspace_bytes, cache(**kw), q) == status
-    assert status_of(B.fastkv_paged_attn, cache(**kw), q, Fake(), Fake(), Fake(), None, Fake()) == status
+    assert status_of(B.fastkv_paged_attn, cache(**kw), q, Fake(), Fake(), Fake(), None, Fake(), NullStream) == status
 
 
 @pytest.mark.parametrize("kw,call,status", [
@@ -202,7 +203,7 @@ def test_bad_queries_are_refused(no_device, kw, call, status):
     a = dict(lens=Fake(), q=Fake(), out=Fake(), ws=Fake(0x10000, 1 << 24))
     a.update(call)
     q = B.make_query(**args)
-    assert status_of(B.fastkv_paged_attn, cache(), q, a["lens"], a["q"], a["out"], None, a["ws"]) == status
+    assert status_of(B.fastkv_paged_attn, cache(), q, a["lens"], a["q"], a["out"], None, a["ws"], NullStream) == status
 
 
 def test_the_binding_checks_the_caches_tensors():
