@@ -364,6 +364,8 @@ int fastkv_score_static_status(void* stream, int32_t* status, int32_t* site);
  *   "prefill_skip_commit" n > 0: the prefill attention's issuer withholds the signal that S of key tile
  *                         n - 1 is ready (first query tile of every CTA); with a short wait limit the
  *                         softmax warps' bounded wait runs out without any fault (timeout test); 0: off
+ *   "paged_two_maps"      1: the paged attention copies K and V pages through a tensor map each, as it does for pools
+ *                         that lie 2^40 bytes or more apart (test); 0: through one map where it can
  *   "time_kernels"        1: record a pair of CUDA events around every kernel the library launches
  *                         (this creates events, and an event between two kernels keeps the second
  *                         from starting under the first one's tail); read with

@@ -47,6 +47,7 @@ struct DebugConfig {
   long long wait_limit_cycles = 0;  // 0 = the default of about a second
   int extra_publications = 0;       // pass 2 waits for publications that never come (timeout test)
   int score_partition = 0;          // parked kernel's partition mode: 0 = by shape, 1 = never, 2 = whenever it can run
+  int paged_two_maps = 0;           // paged attention: copies K and V apart, as pools beyond 2^40 bytes of one another need
   int prefill_skip_commit = 0;      // prefill attention: n > 0: key tile n - 1's "S ready" signal is withheld (timeout test)
 };
 DebugConfig g_debug;
@@ -359,6 +360,9 @@ int fastkv_debug_set(const char* key, int64_t value) {
     g_debug.score_partition = static_cast<int>(value);
   } else if (!std::strcmp(key, "prefill_skip_commit")) {
     g_debug.prefill_skip_commit = static_cast<int>(value < 0 ? 0 : value);
+  } else if (!std::strcmp(key, "paged_two_maps")) {
+    if (value < 0 || value > 1) return fail(FASTKV_ERR_INVALID_ARG, "debug_set: paged_two_maps is 0 or 1");
+    g_debug.paged_two_maps = static_cast<int>(value);
   } else if (!std::strcmp(key, "extra_publications")) {
     g_debug.extra_publications = static_cast<int>(value < 0 ? 0 : value);
   } else if (!std::strcmp(key, "time_kernels")) {
@@ -841,23 +845,24 @@ int check_strides(const char* name, int64_t tok, int64_t head, int head_dim, con
   if (tok % 8 || head % 8 || reinterpret_cast<uintptr_t>(base) % 16)
     return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: %s needs a 16-byte aligned base and strides that are multiples of 8 elements", name);
   if (tok < head_dim || head < head_dim) return fail(FASTKV_ERR_INVALID_ARG, "paged_append: %s strides are smaller than head_dim", name);
+  if (tok >= (1ll << 38) || head >= (1ll << 38)) return fail(FASTKV_ERR_UNSUPPORTED, "paged_append: %s strides of 2^39 bytes or more are not built", name);
   return FASTKV_OK;
 }
-// One pool as a (column, row of the page, page x head) tensor; boxes of a page's rows (at most 64 in bf16) x 128 bytes (64 for 8-bit
-// rows of 64).
-int encode_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base) {
+// One pool as a (column, row of the page, page x head) tensor; boxes of a chunk's rows x 128 bytes (64 for 8-bit rows of 64).
+// `apart` != 0: both pools, `apart` bytes from one to the other, as a fourth dimension.
+int encode_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base, uint64_t apart) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
   const cuuint64_t item = e4m3 ? 1 : 2, row = c.head_dim * item;
-  cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size),
-                        static_cast<cuuint64_t>(c.n_pages) * c.n_kv_heads};
-  cuuint64_t strides[2] = {row, row * c.page_size};
-  cuuint32_t box[3] = {static_cast<cuuint32_t>(row > 128 ? 128 / item : c.head_dim),
-                       static_cast<cuuint32_t>(paged_box_rows(e4m3, c.page_size)), 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size),
+                        static_cast<cuuint64_t>(c.n_pages) * c.n_kv_heads, 2};
+  cuuint64_t strides[3] = {row, row * c.page_size, apart};
+  cuuint32_t box[4] = {static_cast<cuuint32_t>(row > 128 ? 128 / item : c.head_dim),
+                       static_cast<cuuint32_t>(paged_box_rows(e4m3, c.page_size)), 1, 2};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, apart ? 4 : 3, const_cast<void*>(base),
+                  dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   row >= 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
@@ -934,10 +939,26 @@ int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* 
   p.q_tok = r.q_stride_tok; p.q_head = r.q_stride_head; p.k_tok = r.k_stride_tok; p.k_head = r.k_stride_head;
   p.v_tok = r.v_stride_tok; p.v_head = r.v_stride_head;
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
+  CUtensorMap maps[2];
+  memset(maps, 0, sizeof maps);
+  if (paged_append_uses_maps(p, e4m3)) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    for (int i = 0; i < 2; ++i) {
+      cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.n_kv_heads), static_cast<cuuint64_t>(r.total)};
+      cuuint64_t strides[2] = {static_cast<cuuint64_t>(i ? r.v_stride_head : r.k_stride_head) * 2, static_cast<cuuint64_t>(i ? r.v_stride_tok : r.k_stride_tok) * 2};
+      cuuint32_t box[3] = {static_cast<cuuint32_t>(c.head_dim), 1, static_cast<cuuint32_t>(c.page_size)}, estr[3] = {1, 1, 1};
+      CUresult cr = fn(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(i ? v : k), dims, strides, box, estr,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      if (cr != CUDA_SUCCESS) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(cr));
+    }
+  }
   cudaError_t e;
   {
     TimedLaunch timed(KID_PAGED_APPEND, static_cast<cudaStream_t>(stream_));
-    e = launch_paged_append(p, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_));
+    e = launch_paged_append(p, maps, c.head_dim, e4m3, static_cast<cudaStream_t>(stream_));
   }
   if (e != cudaSuccess) return cuda_fail(e, "paged_append_kernel launch");
   ++g_launches;
@@ -965,10 +986,20 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   const size_t need = round_up(paged_attn_workspace_bytes(plan, c.batch, c.n_kv_heads, c.head_dim), 256);
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
   if ((rc = check_device())) return rc;
-  CUtensorMap tmap_k, tmap_v;
-  if ((rc = encode_pool(&tmap_k, c, c.k_pages)) || (rc = encode_pool(&tmap_v, c, c.v_pages))) return rc;
   PagedAttnParams p;
   memset(&p, 0, sizeof p);
+  // a tensor map's strides are below 2^40 bytes
+  const uintptr_t ka = reinterpret_cast<uintptr_t>(c.k_pages), va = reinterpret_cast<uintptr_t>(c.v_pages);
+  const uint64_t apart = ka < va ? va - ka : ka - va;
+  p.joint = apart != 0 && apart < (1ull << 40) && !g_debug.paged_two_maps;
+  p.v_first = p.joint && va < ka;
+  CUtensorMap tmap_k, tmap_v;
+  if (p.joint) {
+    if ((rc = encode_pool(&tmap_k, c, p.v_first ? c.v_pages : c.k_pages, apart))) return rc;
+    tmap_v = tmap_k;
+  } else if ((rc = encode_pool(&tmap_k, c, c.k_pages, 0)) || (rc = encode_pool(&tmap_v, c, c.v_pages, 0))) {
+    return rc;
+  }
   p.c = paged_view(c);
   p.n_q_heads = query->n_q_heads; p.group = G; p.q_len = query->q_len; p.rows = rows;
   const float scale = query->softmax_scale > 0.0f ? query->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c.head_dim));

@@ -36,7 +36,9 @@ struct AppendParams {
   int pages_per_seq, job_slices, jobs_per_slice;           // page role (8-bit pages)
 };
 
-cudaError_t launch_paged_append(AppendParams& p, int head_dim, bool e4m3, cudaStream_t stream);
+// Whether the call reads k and v through tensor maps: (column, head, row) with boxes of a page's rows of one head, unswizzled.
+bool paged_append_uses_maps(const AppendParams& p, bool e4m3);
+cudaError_t launch_paged_append(AppendParams& p, const CUtensorMap (&maps)[2], int head_dim, bool e4m3, cudaStream_t stream);
 
 constexpr int kPagedMaxPieces = 592;   // pieces of one (sequence, KV head): the CTAs that can share it
 
@@ -47,6 +49,7 @@ struct PagedAttnParams {
   int splits;                 // static launches: CTAs that share a (sequence, KV head, row tile)
   int balanced, ctas;         // balanced launches: CTAs that share all of them
   int box_subs;               // 16-entry steps that one TMA box brings
+  int joint, v_first;         // K and V are planes of one tensor map; the V pool lies at the lower address
   float scale_log2;           // softmax scale times log2(e)
   const int* lens;
   const uint16_t* q;          // [B][q_len][Hq][d]
@@ -61,6 +64,7 @@ struct PagedAttnPlan {
   int row_tiles_of_8, row_tiles, splits, balanced, ctas;
 };
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len);
+// tmap_k: with p.joint both pools, (column, row of the page, page x head, pool); else the K pool alone and tmap_v the V pool
 size_t paged_attn_partials_offset(const PagedAttnPlan& plan, int batch, int n_kv_heads);
 size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int head_dim);
 // Entries of a page that one TMA box brings: a chunk's 32 of 8-bit pages when the page has them, else 16.

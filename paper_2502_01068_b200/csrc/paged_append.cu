@@ -22,6 +22,7 @@ namespace fastkv {
 namespace {
 
 constexpr int kPageStages = 4;         // page role: heads whose rows are on their way or in use
+constexpr int kRowStages = 8;             // row role: heads whose rows are on their way or in use
 constexpr int kSmallRows = 8;        // rows per sequence up to which the small role is used
 
 struct Row16 {                       // a lane's sixteen elements of one row: the pieces at `lo` and `hi`
@@ -205,11 +206,22 @@ __device__ __forceinline__ int owner_of_row(const AppendParams& p, int t) {
 
 }  // namespace
 
-// Row role: unit u = (slice of heads, token); heads in the order queries, keys, values.
+__device__ __forceinline__ void copy16_async(uint32_t smem_dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t at) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
+  return r;
+}
+
+// Row role: unit u = (slice of heads, token); heads in the order queries, keys, values.  Every lane copies the pieces of the
+// next heads' rows that it will need into shared-memory slots of its own: seven heads in flight a lane, no registers held,
+// nothing to synchronise.
 template <int D, bool kE4M3, bool kRot>
 __device__ void append_rows(const AppendParams& p, int block) {
   constexpr int GL = D / 16;                      // lanes of a row
-  constexpr int kBatch = 4;                        // rows loaded before the first is used
+  extern __shared__ __align__(128) uint8_t ring[];   // [kRowStages][2 pieces][threads][16 bytes]
   const int j = threadIdx.x % GL;
   const long long u = static_cast<long long>(block) * (blockDim.x / GL) + threadIdx.x / GL;
   if (u >= static_cast<long long>(p.row_slices) * p.total) return;
@@ -217,9 +229,6 @@ __device__ void append_rows(const AppendParams& p, int block) {
   const int h0 = slice * p.heads_per_unit, h1 = min(h0 + p.heads_per_unit, p.row_heads);
   const int Hq = p.n_q_heads, Hkv = p.c.n_kv_heads;
   const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
-  float cs[8], sn[8];
-  const bool turns = kRot && turned.turned && h0 < Hq + Hkv;
-  const int pos = turns ? p.pos[t] : 0;
   int b = 0, slot = -1;
   long long page = -1;                            // of bf16 pages: where row t goes; -1: nowhere
   if (!kE4M3 && h1 > Hq) {
@@ -235,51 +244,60 @@ __device__ void append_rows(const AppendParams& p, int block) {
     }
   }
   const int in_page = slot & ((1 << p.c.page_log2) - 1);
-  for (int hb = h0; hb < h1; hb += kBatch) {
-    Row16 raw[kBatch];
-    bool have[kBatch];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int h = hb + i;
-      have[i] = false;
-      if (h >= h1) continue;
+  const uint32_t slots = smem_u32(ring) + threadIdx.x * 16, piece = blockDim.x * 16;
+  auto slot_of = [&](int h) -> uint32_t { return slots + static_cast<uint32_t>(h - h0) % kRowStages * 2 * piece; };
+  auto kv_head = [&](int h) -> int { return h < Hq + Hkv ? h - Hq : h - Hq - Hkv; };
+  uint32_t here = 0;                              // by stage: whether the row exists
+  int index = 0;                                  // source row of the head that starts next
+  auto fetch = [&](int h) { if (!kE4M3 && h < h1 && h >= Hq && page >= 0) index = fetch_index<kRot>(p, t, kv_head(h)); };
+  auto start = [&](int h) {
+    const uint32_t bit = 1u << (static_cast<uint32_t>(h - h0) % kRowStages);
+    here &= ~bit;
+    if (h < h1) {
+      const uint16_t* x = nullptr;
       if (h < Hq) {
-        raw[i] = load_row(p.q + static_cast<long long>(t) * p.q_tok + h * p.q_head, turned);
-        have[i] = true;
+        x = p.q + static_cast<long long>(t) * p.q_tok + h * p.q_head;
       } else if (!kE4M3 && page >= 0) {
-        const bool is_k = h < Hq + Hkv;
-        const int g = is_k ? h - Hq : h - Hq - Hkv;
-        const long long src = source_row<kRot>(p, fetch_index<kRot>(p, t, g), b);
-        if (src < 0) continue;
-        have[i] = true;
-        if (is_k) raw[i] = load_row(p.k + src * p.k_tok + g * p.k_head, turned);
-        else raw[i] = load_row(p.v + src * p.v_tok + g * p.v_head, plain);
+        const long long src = source_row<kRot>(p, index, b);
+        const int g = kv_head(h);
+        if (src >= 0) x = h < Hq + Hkv ? p.k + src * p.k_tok + g * p.k_head : p.v + src * p.v_tok + g * p.v_head;
+      }
+      if (x != nullptr) {
+        const Pieces& at = h < Hq + Hkv ? turned : plain;
+        here |= bit;
+        copy16_async(slot_of(h), x + at.lo);
+        copy16_async(slot_of(h) + piece, x + at.hi);
       }
     }
-    if (hb == h0 && turns) angles_of(pos, p.inv_freq, j, cs, sn);       // while the first rows are on their way
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      if (!have[i]) continue;
-      const int h = hb + i;
-      const bool is_v = h >= Hq + Hkv;
-      uint16_t* dst;
-      if (h < Hq) {
-        dst = p.q_out + (static_cast<long long>(t) * Hq + h) * D;
-      } else {
-        const int g = is_v ? h - Hq - Hkv : h - Hq;
-        dst = reinterpret_cast<uint16_t*>(is_v ? p.c.v_pages : p.c.k_pages) + (((page + g) << p.c.page_log2) + in_page) * D;
-      }
-      if (kRot && !is_v && turned.turned) {
-        float x[16];
-        unpack(raw[i], x);
-        rotate16(x, cs, sn, p.adjacent);
-        raw[i].lo = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        raw[i].hi = make_uint4(pack_bf16(x[8], x[9]), pack_bf16(x[10], x[11]), pack_bf16(x[12], x[13]), pack_bf16(x[14], x[15]));
-      }
-      const Pieces& at = is_v ? plain : turned;
-      *reinterpret_cast<uint4*>(dst + at.lo) = raw[i].lo;
-      *reinterpret_cast<uint4*>(dst + at.hi) = raw[i].hi;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    fetch(h + 1);
+  };
+  fetch(h0);
+#pragma unroll 1
+  for (int h = h0; h < h0 + kRowStages - 1; ++h) start(h);
+  float cs[8], sn[8];
+  if (kRot && turned.turned && h0 < Hq + Hkv) angles_of(p.pos[t], p.inv_freq, j, cs, sn);      // while the first rows are on their way
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    start(h + kRowStages - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kRowStages - 1) : "memory");
+    if (!((here >> (static_cast<uint32_t>(h - h0) % kRowStages)) & 1u)) continue;
+    Row16 raw;
+    raw.lo = shared16(slot_of(h));
+    raw.hi = shared16(slot_of(h) + piece);
+    const bool is_v = h >= Hq + Hkv;
+    uint16_t* dst = h < Hq ? p.q_out + (static_cast<long long>(t) * Hq + h) * D
+                           : reinterpret_cast<uint16_t*>(is_v ? p.c.v_pages : p.c.k_pages) + (((page + kv_head(h)) << p.c.page_log2) + in_page) * D;
+    if (kRot && !is_v && turned.turned) {
+      float x[16];
+      unpack(raw, x);
+      rotate16(x, cs, sn, p.adjacent);
+      raw.lo = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+      raw.hi = make_uint4(pack_bf16(x[8], x[9]), pack_bf16(x[10], x[11]), pack_bf16(x[12], x[13]), pack_bf16(x[14], x[15]));
     }
+    const Pieces& at = is_v ? plain : turned;
+    *reinterpret_cast<uint4*>(dst + at.lo) = raw.lo;
+    *reinterpret_cast<uint4*>(dst + at.hi) = raw.hi;
   }
 }
 
@@ -387,12 +405,13 @@ __device__ __forceinline__ float amax_raw(const Row16& r) {
   return fmaxf(bf_lo(m), bf_hi(m));
 }
 
-// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads.  One thread per row of the page brings the
-// rows of the next heads into shared memory with bulk copies (kPageStages - 1 heads ahead; the threads that compute hold no
-// addresses of theirs); a lane group takes NS rows of a head, and the block meets once per head, over the rows' largest
-// absolute value.
+// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads.  The rows of the next heads are brought into
+// shared memory kPageStages - 1 heads ahead: a head's rows of the page by one tiled copy, or, when they are gathered, by one
+// bulk copy a row, each started by a thread of its own (a bulk copy of 256 bytes takes the copy engine ~27 cycles, which bounds
+// the gathered form).  A lane group takes NS rows of a head, and the block meets once per head, over the rows' largest absolute
+// value.
 template <int D, int NS, bool kRot>
-__device__ void append_page(const AppendParams& p, int block) {
+__device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, int block) {
   constexpr int GL = D / 16;
   extern __shared__ __align__(128) uint8_t ring[];   // [kPageStages][rows of a round][D] bf16
   __shared__ uint64_t full[kPageStages];
@@ -420,9 +439,11 @@ __device__ void append_page(const AppendParams& p, int block) {
     return;
   }
   if (threadIdx.x < 4) top[0][threadIdx.x] = 0u;
+  const bool gather = !kRot && p.idx != nullptr;
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int i = 0; i < kPageStages; ++i) mbar_init(&full[i], n_rows);
+    if (!gather) { tma_prefetch_desc(map_k); tma_prefetch_desc(map_v); }
+    for (int i = 0; i < kPageStages; ++i) mbar_init(&full[i], gather ? n_rows : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -432,8 +453,8 @@ __device__ void append_page(const AppendParams& p, int block) {
   const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
 
   // ---- the row this thread brings ----
-  const bool gather = !kRot && p.idx != nullptr;
-  const bool brings = static_cast<int>(threadIdx.x) < n_rows;
+  const bool brings = static_cast<int>(threadIdx.x) < (gather ? n_rows : 1);
+  const uint64_t policy = l2_policy_evict_first();
   const int my_side = threadIdx.x >> p.c.page_log2, my_slot = slot0 + (threadIdx.x & (P - 1));
   const bool my_fresh = brings && my_slot >= lo && my_slot < hi;
   const int my_row = r.first + (my_slot - len);
@@ -446,7 +467,18 @@ __device__ void append_page(const AppendParams& p, int block) {
   };
   auto start = [&](int k) {                       // the copies of round k; every bringing thread arrives
     if (!brings || k >= rounds) return;
-    const int job = job0 + k * side + my_side, st = k % kPageStages;
+    const int st = k % kPageStages;
+    if (!gather) {                                // one thread: a box of the page's rows for each head side by side
+      const int first = job0 + k * side, n = min(side, job1 - first);
+      mbar_arrive_expect_tx(&full[st], static_cast<uint32_t>(n) << (p.c.page_log2 + (D == 128 ? 8 : 7)));
+      for (int z = 0; z < n; ++z) {
+        const bool is_v = first + z >= Hkv;
+        tma_load_3d(ring + ((static_cast<uint32_t>(st) * n_rows + (z << p.c.page_log2)) * (D * 2)), is_v ? map_v : map_k, &full[st], 0,
+                    is_v ? first + z - Hkv : first + z, r.first + (slot0 - len), policy);
+      }
+      return;
+    }
+    const int job = job0 + k * side + my_side;
     bool take = my_fresh && job < job1;
     int src = my_row;
     if (gather && take) {
@@ -553,7 +585,8 @@ __device__ void append_page(const AppendParams& p, int block) {
 // kKind: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per lane
 // group).  The blocks from page_blocks on take the row role.
 template <int D, int kKind, bool kRot>
-__global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0) paged_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0)
+paged_append_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AppendParams p) {
   pdl_wait();
   pdl_launch_dependents();
   if (blockIdx.x == 0) {
@@ -569,38 +602,38 @@ __global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0) pa
   const int block = static_cast<int>(blockIdx.x);
   if (block >= p.page_blocks) append_rows<D, kKind != 0, kRot>(p, block - p.page_blocks);
   else if constexpr (kKind == 1) append_small<D>(p, block);
-  else if constexpr (kKind == 2) append_page<D, 1, kRot>(p, block);
-  else if constexpr (kKind == 3) append_page<D, 2, kRot>(p, block);
+  else if constexpr (kKind == 2) append_page<D, 1, kRot>(p, &map_k, &map_v, block);
+  else if constexpr (kKind == 3) append_page<D, 2, kRot>(p, &map_k, &map_v, block);
 }
 
 template <int D, int kKind, bool kRot>
-static cudaError_t launch_kind(const AppendParams& p, int blocks, int threads, cudaStream_t stream) {
+static cudaError_t launch_kind(const AppendParams& p, const CUtensorMap (&maps)[2], int blocks, int threads, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(threads);
   cfg.stream = stream;
-  if (kKind >= 2) {
-    constexpr int kRowsEach = kKind == 3 ? 2 : 1, kMost = kPageStages * kRowsEach * 32 * (kKind == 3 ? 512 : 256);
-    static PerDeviceOnce configured;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+  constexpr int kEach = kKind == 3 ? 2 * kPageStages : kKind == 2 ? kPageStages : 0;    // page role: rows of 32 bytes a thread
+  const int rows = p.row_heads == 0 ? kEach : kEach > kRowStages ? kEach : kRowStages;
+  static PerDeviceOnce configured;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!configured.done(dev)) {
+    e = cudaFuncSetAttribute(paged_append_kernel<D, kKind, kRot>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (kEach > kRowStages ? kEach : kRowStages) * 32 * (kKind == 3 ? 512 : 256));
     if (e != cudaSuccess) return e;
-    if (!configured.done(dev)) {
-      e = cudaFuncSetAttribute(paged_append_kernel<D, kKind, kRot>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-      if (e != cudaSuccess) return e;
-      configured.set(dev);
-    }
-    cfg.dynamicSmemBytes = kPageStages * kRowsEach * 32 * threads;
+    configured.set(dev);
   }
+  cfg.dynamicSmemBytes = rows * 32 * threads;
   cudaLaunchAttribute attr[1];
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind, kRot>, p);
+  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind, kRot>, maps[0], maps[1], p);
 }
 
 template <int D>
-static cudaError_t launch_d(AppendParams& p, bool e4m3, cudaStream_t stream) {
+static cudaError_t launch_d(AppendParams& p, const CUtensorMap (&maps)[2], bool e4m3, cudaStream_t stream) {
   constexpr int GL = D / 16, kSms = 148;
   const int P = 1 << p.c.page_log2, jobs = 2 * p.c.n_kv_heads;
   const bool small = p.max_new <= kSmallRows;
@@ -640,15 +673,17 @@ static cudaError_t launch_d(AppendParams& p, bool e4m3, cudaStream_t stream) {
   if (page_blocks + row_blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   p.page_blocks = static_cast<int>(page_blocks);
   const int blocks = static_cast<int>(page_blocks + row_blocks);
-  if (!e4m3) return p.rot_dim ? launch_kind<D, 0, true>(p, blocks, threads, stream) : launch_kind<D, 0, false>(p, blocks, threads, stream);
-  if (small) return launch_kind<D, 1, true>(p, blocks, threads, stream);
-  if (per_page > threads) return p.rot_dim ? launch_kind<D, 3, true>(p, blocks, threads, stream) : launch_kind<D, 3, false>(p, blocks, threads, stream);
-  return p.rot_dim ? launch_kind<D, 2, true>(p, blocks, threads, stream) : launch_kind<D, 2, false>(p, blocks, threads, stream);
+  if (!e4m3) return p.rot_dim ? launch_kind<D, 0, true>(p, maps, blocks, threads, stream) : launch_kind<D, 0, false>(p, maps, blocks, threads, stream);
+  if (small) return launch_kind<D, 1, true>(p, maps, blocks, threads, stream);
+  if (per_page > threads) return p.rot_dim ? launch_kind<D, 3, true>(p, maps, blocks, threads, stream) : launch_kind<D, 3, false>(p, maps, blocks, threads, stream);
+  return p.rot_dim ? launch_kind<D, 2, true>(p, maps, blocks, threads, stream) : launch_kind<D, 2, false>(p, maps, blocks, threads, stream);
 }
 
-cudaError_t launch_paged_append(AppendParams& p, int head_dim, bool e4m3, cudaStream_t stream) {
-  if (head_dim == 128) return launch_d<128>(p, e4m3, stream);
-  if (head_dim == 64) return launch_d<64>(p, e4m3, stream);
+bool paged_append_uses_maps(const AppendParams& p, bool e4m3) { return e4m3 && p.max_new > kSmallRows && p.idx == nullptr; }
+
+cudaError_t launch_paged_append(AppendParams& p, const CUtensorMap (&maps)[2], int head_dim, bool e4m3, cudaStream_t stream) {
+  if (head_dim == 128) return launch_d<128>(p, maps, e4m3, stream);
+  if (head_dim == 64) return launch_d<64>(p, maps, e4m3, stream);
   return cudaErrorInvalidValue;
 }
 

@@ -98,8 +98,7 @@ struct PagedCfg {
   static constexpr int kBoxes = kRowBytes > 128 ? kRowBytes / 128 : 1;     // 128-byte column blocks of a row (or one of 64)
   static constexpr int kBoxRow = kRowBytes / kBoxes;
   static constexpr int kBoxBytes = kChunk * kBoxRow;
-  static constexpr int kHalfBytes = kBoxes * kBoxBytes;                    // K (or V) rows of one stage
-  static constexpr int kStageBytes = 2 * kHalfBytes;
+  static constexpr int kStageBytes = 2 * kBoxes * kBoxBytes;               // by column block: K's rows, V's rows (see the copies)
   static constexpr int kStages = kE4M3 ? 2 : 3;   // of 8 KB each for head_dim 128
   static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
   static constexpr int kRows = 8 * RT;
@@ -154,7 +153,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 
   if (t == 0) {
     tma_prefetch_desc(&tmap_k);
-    tma_prefetch_desc(&tmap_v);
+    if (!p.joint) tma_prefetch_desc(&tmap_v);
     abort_flag = 0;
     s_first = -1;
   }
@@ -217,6 +216,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const uint32_t ring = smem_u32(ring_ptr);
   const uint64_t policy = p.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
   const int page_subs_log2 = p.c.page_log2 - 4;            // steps of 16 entries in a page
+  // inside a column block of a stage: K and V alternate by box (of a chunk's 32 rows, or of 16)
+  const uint32_t box_bytes = p.box_subs * kSub * Cfg::kBoxRow, sub_stride = NSUB == 2 && p.box_subs == 1 ? 2 * kSub * Cfg::kBoxRow : kSub * Cfg::kBoxRow;
+  const uint32_t k_off = p.v_first ? box_bytes : 0, v_off = p.v_first ? 0 : box_bytes;
   const uint32_t row7 = lane & 7;
   const uint32_t swz = Cfg::kBoxRow == 128 ? row7 : (row7 >> 1);      // 16-byte piece p of row r sits at p ^ swz
   int stage_in = 0, stage_out = 0;                         // ring positions, carried from segment to segment
@@ -246,15 +248,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (blk_cur >= 0) { sk_cur = p.c.k_scales[blk_cur]; sv_cur = p.c.v_scales[blk_cur]; }
       if (blk_next >= 0) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
     }
-    auto issue = [&](int i, int sub_in, int blk) {         // lane 0 only: one box of K and one of V per 128 bytes of a row
+    // Lane 0 only.  One copy brings a box of K and the same box of V (the pools are two planes of one tensor map), because
+    // starting a copy costs the warp ~150 cycles; where the pools lie too far apart for that, two copies fill the same places.
+    auto issue = [&](int i, int sub_in, int blk) {
       const int sub = (c0 + warp + i * kWarps) * NSUB + sub_in;
       const int row = (sub & ((1 << page_subs_log2) - 1)) * kSub;
       uint64_t* bar = &full[warp][stage_in];
-      uint8_t* stage = ring_ptr + stage_in * Cfg::kStageBytes + sub_in * kSub * Cfg::kBoxRow;
+      uint8_t* stage = ring_ptr + stage_in * Cfg::kStageBytes + sub_in * sub_stride;
 #pragma unroll
       for (int x = 0; x < Cfg::kBoxes; ++x) {
-        tma_load_3d(stage + x * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk, policy);
-        tma_load_3d(stage + Cfg::kHalfBytes + x * Cfg::kBoxBytes, &tmap_v, bar, x * 64, row, blk, policy);
+        if (p.joint) {
+          tma_load_4d(stage + x * 2 * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk, 0, policy);
+        } else {
+          tma_load_3d(stage + x * 2 * Cfg::kBoxBytes + k_off, &tmap_k, bar, x * 64, row, blk, policy);
+          tma_load_3d(stage + x * 2 * Cfg::kBoxBytes + v_off, &tmap_v, bar, x * 64, row, blk, policy);
+        }
       }
     };
     // All lanes: starts the copies of the warp's chunk i (a step behind the sequence's end brings page 0: masked below).
@@ -340,17 +348,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     auto pass = [&](auto tail_, int i, int st) {
       constexpr bool kTail = decltype(tail_)::value;
       const int key0 = (c0 + warp + i * kWarps) * kChunk;
-      const uint32_t ks_addr = ring + st * Cfg::kStageBytes, vs_addr = ks_addr + Cfg::kHalfBytes;
+      const uint32_t ks_addr = ring + st * Cfg::kStageBytes + k_off, vs_addr = ring + st * Cfg::kStageBytes + v_off;
       if (kTail && len - key0 < kChunk) {
         // what lies behind the sequence's end in the page is not its own: the logits are masked, but a zero weight does not
         // silence a NaN in V, so those V rows are cleared
         const int rows = len - key0;
-        uint8_t* vs = ring_ptr + st * Cfg::kStageBytes + Cfg::kHalfBytes;
+        uint8_t* vs = ring_ptr + st * Cfg::kStageBytes + v_off;
         constexpr int kPieces = Cfg::kBoxRow / 16;
         const int n = (kChunk - rows) * kPieces;
         for (int j = lane; j < Cfg::kBoxes * n; j += 32) {
-          const int x = j / n, rem = j - x * n;
-          *reinterpret_cast<uint4*>(vs + x * Cfg::kBoxBytes + rows * Cfg::kBoxRow + rem * 16) = make_uint4(0u, 0u, 0u, 0u);
+          const int x = j / n, rem = j - x * n, r = rows + rem / kPieces;
+          *reinterpret_cast<uint4*>(vs + x * 2 * Cfg::kBoxBytes + r / kSub * sub_stride + r % kSub * Cfg::kBoxRow + rem % kPieces * 16) =
+              make_uint4(0u, 0u, 0u, 0u);
         }
         __syncwarp();
       }
@@ -364,7 +373,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         for (int l = 0; l < kLoads; ++l)
 #pragma unroll
           for (int nt = 0; nt < 2 * NSUB; ++nt)
-            ldsm_x4(kb[l][nt], (at ^ ((l & 1) << 6)) + (l >> 1) * Cfg::kBoxBytes + nt * 8 * Cfg::kBoxRow);
+            ldsm_x4(kb[l][nt], (at ^ ((l & 1) << 6)) + (l >> 1) * 2 * Cfg::kBoxBytes + (nt >> 1) * sub_stride + (nt & 1) * 8 * Cfg::kBoxRow);
         constexpr int kEach = kE4M3 ? 4 : 2;                    // 16-element steps that a load brings
         float d[4][4];                                          // four sums at a time: the tiles, or halves of two tiles
 #pragma unroll
@@ -393,7 +402,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         for (int l = 0; l < kVLoads; ++l)
 #pragma unroll
           for (int y = 0; y < NSUB; ++y)
-            ldsm_x4_trans(vb[l][y], (at ^ ((l & 3) << 5)) + (l >> 2) * Cfg::kBoxBytes + y * kSub * Cfg::kBoxRow);
+            ldsm_x4_trans(vb[l][y], (at ^ ((l & 3) << 5)) + (l >> 2) * 2 * Cfg::kBoxBytes + y * sub_stride);
       }
       float sk[NSUB], ev[NSUB];
 #pragma unroll

@@ -356,6 +356,36 @@ def test_what_the_host_knows_of_lengths_changes_nothing(fmt):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(128, 16), (128, 64), (64, 16), (64, 128)])
+def test_attention_with_the_pools_in_either_order_or_far_apart(fmt, d, page):
+    """K and V boxes arrive by one copy where the pools allow it: K below V, V below K, and (forced) a copy each."""
+    rng = np.random.default_rng(12)
+    lens = [333, 0, 17]
+    q = bf16_rows(rng, (3, 1, 8, d))
+    query = B.make_query(n_q_heads=8, max_len=333)
+    results = []
+    for way in ("k below v", "v below k", "apart"):
+        pools = Pools(fmt, lens, lens, page, 2, d, 13)
+        both = torch.empty((2,) + tuple(pools.k.shape), dtype=pools.k.dtype, device="cuda")
+        k, v = (both[1], both[0]) if way == "v below k" else (both[0], both[1])
+        k.copy_(pools.k)
+        v.copy_(pools.v)
+        cache = B.make_paged_cache(k, v, pools.table, pools.ks, pools.vs)
+        ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
+        out, lse = torch.zeros((3, 1, 8, d), device="cuda"), torch.zeros((3, 1, 8), device="cuda")
+        B.fastkv_debug_set("paged_two_maps", int(way == "apart"))
+        try:
+            B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)
+        finally:
+            B.fastkv_debug_set("paged_two_maps", 0)
+        assert B.fastkv_device_status(ws) == (0, 0)
+        check_attention(pools, lens, q.double().numpy(), out.cpu().double().numpy(), lse.cpu().double().numpy(), d ** -0.5)
+        results.append((out.cpu(), lse.cpu()))
+    for out, lse in results[1:]:
+        assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_attention_reports_bad_pages_and_lengths(fmt):
     pools = Pools(fmt, [100, 60], [100, 60], 16, 2, 64, 1)
     q = bf16_rows(np.random.default_rng(0), (2, 1, 4, 64))
