@@ -21,7 +21,14 @@ namespace fastkv {
 
 namespace {
 
-constexpr int kPageStages = 4;         // page role: heads whose rows are on their way or in use
+constexpr int kHeads = 2;            // page role: heads of a round
+// What a call does to its rows on the way.
+enum Mode { kPlain = 0, kRotated = 1, kGathered = 2 };
+// Page role: rounds of heads on their way while one is in use.  Two for tiled copies (51 us against 58 with one, 36 864 rows of
+// 8 heads); one for gathered rows, whose copies are what bounds them, so that three blocks fit an SM (21 us against 28 with two
+// rounds and two blocks, 13107 rows of 8 heads).
+template <int kMode> constexpr int kRoundsAhead = kMode == kGathered ? 1 : 2;
+template <int kMode> constexpr int kSlotsOf = (kRoundsAhead<kMode> + 1) * kHeads;
 constexpr int kRowStages = 8;             // row role: heads whose rows are on their way or in use
 constexpr int kSmallRows = 8;        // rows per sequence up to which the small role is used
 
@@ -175,15 +182,13 @@ __device__ __forceinline__ void store_codes(uint8_t* row, const Pieces& at, cons
 }
 
 // The source row of new row `row` of head h: itself, or the kept row that idx names (-1: none such).  The index is fetched
-// apart from its use, so that a caller can have it under way before it is needed.  Rotated calls have no indices.
-template <bool kRot>
+// apart from its use, so that a caller can have it under way before it is needed.
 __device__ __forceinline__ int fetch_index(const AppendParams& p, int row, int h) {
-  if (kRot || p.idx == nullptr) return row;
+  if (p.idx == nullptr) return row;
   return p.idx[static_cast<long long>(h) * p.total + row];
 }
-template <bool kRot>
 __device__ __forceinline__ long long source_row(const AppendParams& p, int i, int b) {
-  if (kRot || p.idx == nullptr) return i;
+  if (p.idx == nullptr) return i;
   const int s0 = p.cu_src ? p.cu_src[b] : 0;
   const int L = p.cu_src ? p.cu_src[b + 1] - s0 : p.total_src;
   if (i < 0 || i >= L || s0 < 0 || static_cast<long long>(s0) + i >= p.total_src) {
@@ -218,8 +223,9 @@ __device__ __forceinline__ uint4 shared16(uint32_t at) {
 // Row role: unit u = (slice of heads, token); heads in the order queries, keys, values.  Every lane copies the pieces of the
 // next heads' rows that it will need into shared-memory slots of its own: seven heads in flight a lane, no registers held,
 // nothing to synchronise.
-template <int D, bool kE4M3, bool kRot>
+template <int D, bool kE4M3, int kMode>
 __device__ void append_rows(const AppendParams& p, int block) {
+  constexpr bool kRot = kMode == kRotated;
   constexpr int GL = D / 16;                      // lanes of a row
   extern __shared__ __align__(128) uint8_t ring[];   // [kRowStages][2 pieces][threads][16 bytes]
   const int j = threadIdx.x % GL;
@@ -249,7 +255,7 @@ __device__ void append_rows(const AppendParams& p, int block) {
   auto kv_head = [&](int h) -> int { return h < Hq + Hkv ? h - Hq : h - Hq - Hkv; };
   uint32_t here = 0;                              // by stage: whether the row exists
   int index = 0;                                  // source row of the head that starts next
-  auto fetch = [&](int h) { if (!kE4M3 && h < h1 && h >= Hq && page >= 0) index = fetch_index<kRot>(p, t, kv_head(h)); };
+  auto fetch = [&](int h) { if (!kE4M3 && h < h1 && h >= Hq && page >= 0) index = kMode == kGathered ? fetch_index(p, t, kv_head(h)) : t; };
   auto start = [&](int h) {
     const uint32_t bit = 1u << (static_cast<uint32_t>(h - h0) % kRowStages);
     here &= ~bit;
@@ -258,7 +264,7 @@ __device__ void append_rows(const AppendParams& p, int block) {
       if (h < Hq) {
         x = p.q + static_cast<long long>(t) * p.q_tok + h * p.q_head;
       } else if (!kE4M3 && page >= 0) {
-        const long long src = source_row<kRot>(p, index, b);
+        const long long src = kMode == kGathered ? source_row(p, index, b) : index;
         const int g = kv_head(h);
         if (src >= 0) x = h < Hq + Hkv ? p.k + src * p.k_tok + g * p.k_head : p.v + src * p.v_tok + g * p.v_head;
       }
@@ -346,7 +352,7 @@ __device__ void append_small(const AppendParams& p, int block) {
   float x[16];
   auto load = [&](int slot) -> bool {
     const int row = row0 + (slot - len);
-    const long long src = source_row<false>(p, fetch_index<false>(p, row, g), b);
+    const long long src = source_row(p, fetch_index(p, row, g), b);
     if (src < 0) return false;
     unpack(load_row(base + src * tok, at), x);
     if (at.turned) {
@@ -405,25 +411,26 @@ __device__ __forceinline__ float amax_raw(const Row16& r) {
   return fmaxf(bf_lo(m), bf_hi(m));
 }
 
-// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads.  The rows of the next heads are brought into
-// shared memory kPageStages - 1 heads ahead: a head's rows of the page by one tiled copy, or, when they are gathered, by one
-// bulk copy a row, each started by a thread of its own (a bulk copy of 256 bytes takes the copy engine ~27 cycles, which bounds
-// the gathered form).  A lane group takes NS rows of a head, and the block meets once per head, over the rows' largest absolute
-// value.
-template <int D, int NS, bool kRot>
+// Page role: a block takes one page of one sequence and a slice of the 2 * Hkv heads, kHeads of them a round.  A head's rows of the
+// page come into shared memory rounds ahead, by one tiled copy, or, when they are gathered, by a bulk copy a row; whoever
+// starts a copy is held up by it for some 500 cycles, so the heads of a round are started from different warps, once for
+// kHeads meetings of the block.  The block meets over the largest absolute value of each head's rows; the rows are read from
+// shared memory once for it and once more to be encoded, which leaves the registers to more blocks per SM.
+template <int D, int NS, int kMode>
 __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, int block) {
-  constexpr int GL = D / 16;
-  extern __shared__ __align__(128) uint8_t ring[];   // [kPageStages][rows of a round][D] bf16
-  __shared__ uint64_t full[kPageStages];
-  __shared__ uint32_t top[3][4];                  // by round: the bits of the largest absolute value, per head side by side
-  __shared__ uint8_t absent[kPageStages][128];    // gathered rows whose index names no row
+  constexpr int GL = D / 16, kPageSlots = kSlotsOf<kMode>;
+  constexpr bool kRot = kMode == kRotated, gather = kMode == kGathered;
+  extern __shared__ __align__(128) uint8_t ring[];   // [kPageSlots][rows of a slot][D] bf16
+  __shared__ uint64_t full[kPageSlots];
+  __shared__ uint32_t top[3][kHeads][4];          // by round: the bits of the largest absolute value, per head (and side by side)
+  __shared__ uint8_t absent[kPageSlots][128];     // gathered rows whose index names no row
   __shared__ int abort_flag;
   const int P = 1 << p.c.page_log2, Hkv = p.c.n_kv_heads, jobs = 2 * Hkv;
   const int threads = blockDim.x, groups = threads / GL, j = threadIdx.x % GL, grp = threadIdx.x / GL;
   const int lane = threadIdx.x & 31;
-  const int side = groups > P ? groups / P : 1;   // heads that a small page lets the block take side by side (4 at most)
+  const int side = groups > P ? groups / P : 1;   // heads that a small page lets a slot hold side by side (4 at most)
   const int mine = grp >> p.c.page_log2;          // which of them (0 when side == 1)
-  const int n_rows = groups * NS;                 // rows of a round
+  const int n_rows = groups * NS;                 // rows of a slot
   const int item = block / p.job_slices, slice = block - item * p.job_slices;
   const int b = item / p.pages_per_seq, which = item - b * p.pages_per_seq;
   const int len = p.lens[b];
@@ -438,38 +445,42 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
     if (threadIdx.x == 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_PAGE);
     return;
   }
-  if (threadIdx.x < 4) top[0][threadIdx.x] = 0u;
-  const bool gather = !kRot && p.idx != nullptr;
+  if (threadIdx.x < kHeads * 4) (&top[0][0][0])[threadIdx.x] = 0u;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     if (!gather) { tma_prefetch_desc(map_k); tma_prefetch_desc(map_v); }
-    for (int i = 0; i < kPageStages; ++i) mbar_init(&full[i], gather ? n_rows : 1);
+    for (int i = 0; i < kPageSlots; ++i) mbar_init(&full[i], gather ? n_rows : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   const int n_old = max(0, min(len - slot0, P));
   const int job0 = slice * p.jobs_per_slice, job1 = min(job0 + p.jobs_per_slice, jobs);
-  const int rounds = (job1 - job0 + side - 1) / side;
+  const int fills = (job1 - job0 + side - 1) / side;            // slots to be filled in all
+  const int rounds = (fills + kHeads - 1) / kHeads;
   const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
 
-  // ---- the row this thread brings ----
-  const bool brings = static_cast<int>(threadIdx.x) < (gather ? n_rows : 1);
+  // ---- what this thread brings: fill m of every kHeads is started by thread 32 * (m % kHeads), or, gathered, by the n_rows threads
+  // from n_rows * (m % kHeads) on, one row each ----
   const uint64_t policy = l2_policy_evict_first();
-  const int my_side = threadIdx.x >> p.c.page_log2, my_slot = slot0 + (threadIdx.x & (P - 1));
-  const bool my_fresh = brings && my_slot >= lo && my_slot < hi;
+  const int my_fill = gather ? static_cast<int>(threadIdx.x) / n_rows : static_cast<int>(threadIdx.x) / 32;
+  const bool brings = my_fill < kHeads && (gather || lane == 0);
+  const int my_row_of_slot = static_cast<int>(threadIdx.x) - my_fill * n_rows;
+  const int my_side = my_row_of_slot >> p.c.page_log2, my_slot = slot0 + (my_row_of_slot & (P - 1));
+  const bool my_fresh = gather && brings && my_slot >= lo && my_slot < hi;
   const int my_row = r.first + (my_slot - len);
   const int src0 = gather && p.cu_src ? p.cu_src[b] : 0;          // where the sequence's source rows start, and how many
   const int src_n = gather ? min(p.cu_src ? p.cu_src[b + 1] - src0 : p.total_src, src0 >= 0 ? p.total_src - src0 : 0) : 0;
-  int index = 0;                                  // source row of the round that starts next
+  int index = 0;                                  // source row of the fill that this thread starts next
   auto fetch = [&](int k) {
-    const int job = job0 + k * side + my_side, g = job >= Hkv ? job - Hkv : job;
-    if (gather && my_fresh && job < job1) index = p.idx[static_cast<long long>(g) * p.total + my_row];
+    const int job = job0 + (k * kHeads + my_fill) * side + my_side, g = job >= Hkv ? job - Hkv : job;
+    if (my_fresh && job < job1) index = p.idx[static_cast<long long>(g) * p.total + my_row];
   };
-  auto start = [&](int k) {                       // the copies of round k; every bringing thread arrives
-    if (!brings || k >= rounds) return;
-    const int st = k % kPageStages;
-    if (!gather) {                                // one thread: a box of the page's rows for each head side by side
-      const int first = job0 + k * side, n = min(side, job1 - first);
+  auto start = [&](int k) {                       // this thread's part of round k's copies; every bringing thread arrives
+    const int m = k * kHeads + my_fill;
+    if (!brings || m >= fills) return;
+    const int st = m % kPageSlots;
+    if (!gather) {                                // a box of the page's rows for each head side by side
+      const int first = job0 + m * side, n = min(side, job1 - first);
       mbar_arrive_expect_tx(&full[st], static_cast<uint32_t>(n) << (p.c.page_log2 + (D == 128 ? 8 : 7)));
       for (int z = 0; z < n; ++z) {
         const bool is_v = first + z >= Hkv;
@@ -478,22 +489,20 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
       }
       return;
     }
-    const int job = job0 + k * side + my_side;
+    const int job = job0 + m * side + my_side;
     bool take = my_fresh && job < job1;
-    int src = my_row;
-    if (gather && take) {
+    if (take) {
       const bool good = index >= 0 && index < src_n;
       if (!good) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_APPEND_INDEX);
-      absent[st][threadIdx.x] = !good;
+      absent[st][my_row_of_slot] = !good;
       take = good;
-      src = src0 + index;
     }
     if (take) {
       const bool is_v = job >= Hkv;
-      const int g = is_v ? job - Hkv : job;
+      const int g = is_v ? job - Hkv : job, src = src0 + index;
       const uint16_t* x = is_v ? p.v + g * p.v_head + src * p.v_tok : p.k + g * p.k_head + src * p.k_tok;
       mbar_arrive_expect_tx(&full[st], D * 2);
-      bulk_row(ring + (static_cast<size_t>(st) * n_rows + threadIdx.x) * (D * 2), x, D * 2, &full[st]);
+      bulk_row(ring + (static_cast<size_t>(st) * n_rows + my_row_of_slot) * (D * 2), x, D * 2, &full[st]);
     } else {
       mbar_arrive(&full[st]);
     }
@@ -501,15 +510,14 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
   };
   fetch(0);
   __syncthreads();                                // barriers and top[0] are set
-#pragma unroll
-  for (int k = 0; k < kPageStages - 1; ++k) start(k);
+  for (int k = 0; k < kRoundsAhead<kMode>; ++k) start(k);
 
   // ---- the rows this lane group computes ----
   bool fresh[NS];
   float cs[NS][8], sn[NS][8];
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
-    const int slot = slot0 + ((grp + n * groups) & (P - 1));
+    const int slot = slot0 + ((grp + n * groups) & (P - 1));    // side == 1 whenever NS > 1
     fresh[n] = slot >= lo && slot < hi;
     if constexpr (kRot)
       if (fresh[n] && turned.turned && job0 < Hkv) angles_of(p.pos[r.first + (slot - len)], p.inv_freq, j, cs[n], sn[n]);
@@ -517,74 +525,82 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
   bool ok = true;
   int now = 0;                                    // k % 3
   for (int k = 0; k < rounds; ++k) {
-    const int st = k % kPageStages;
-    start(k + kPageStages - 1);                   // into the stage that was read before the last meeting
-    const int job = job0 + k * side + mine;
-    const bool on = job < job1;
-    const bool is_v = job >= Hkv;
-    const int g = is_v ? job - Hkv : job;
-    const Pieces& at = is_v ? plain : turned;
-    const long long block_row = static_cast<long long>(pid) * Hkv + g;
-    float* const scales = is_v ? p.c.v_scales : p.c.k_scales;
-    const float old_scale = on && n_old > 0 ? scales[block_row] : 0.0f;
-    ok = ok && mbar_wait_bounded(&full[st], (k / kPageStages) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT);
-    Row16 raw[NS];
-    float x[NS][16];
-    bool here[NS];
-    float m = 0.0f;
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      const int at_row = grp + n * groups;
-      here[n] = ok && on && fresh[n] && !(gather && absent[st][at_row]);
-      if (!here[n]) continue;
-      raw[n] = load_row(reinterpret_cast<const uint16_t*>(ring + (static_cast<uint32_t>(st) * n_rows + at_row) * (D * 2)), at);
-      if (kRot && !is_v) {
-        unpack(raw[n], x[n]);
-        if (at.turned) rotate16(x[n], cs[n], sn[n], p.adjacent);
-        m = fmaxf(m, amax16(x[n]));
-      } else {
-        m = fmaxf(m, amax_raw(raw[n]));
-      }
-    }
-    // magnitudes order like their bits
-    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+    float old_scale[kHeads];
+    uint32_t here = 0;                            // bit z * NS + n: this lane group has row n of head z
     const int next = now == 2 ? 0 : now + 1;
-    if (lane == 0 && most != 0u) atomicMax(&top[now][mine], most);
-    if (threadIdx.x < 4) top[next][threadIdx.x] = 0u;          // last read two rounds ago
-    __syncthreads();                              // also: every thread has read the old scale
-    int e = scale_exponent(top[now][mine]);
-    now = next;
-    if (!on || !ok) continue;
-    const int e_old = scale_log2(__float_as_uint(old_scale));
-    if (n_old > 0 && e_old > e) e = e_old;
-    const float inv = __uint_as_float(pow2_bits(-e));
-    uint8_t* const rows = (is_v ? p.c.v_pages : p.c.k_pages) + (block_row << p.c.page_log2) * D;
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      const int in_page = (grp + n * groups) & (P - 1);
-      if (here[n]) {
-        if (!(kRot && !is_v)) unpack(raw[n], x[n]);
-        store_codes(rows + in_page * D, at, x[n], inv);
+    for (int z = 0; z < kHeads; ++z) {
+      const int m = k * kHeads + z, st = m % kPageSlots, job = job0 + m * side + mine;
+      const bool on = job < job1, is_v = job >= Hkv;
+      old_scale[z] = on && n_old > 0 ? (is_v ? p.c.v_scales : p.c.k_scales)[static_cast<long long>(pid) * Hkv + (is_v ? job - Hkv : job)] : 0.0f;
+      if (m < fills) ok = ok && mbar_wait_bounded(&full[st], (m / kPageSlots) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT);
+      const Pieces& at = is_v ? plain : turned;
+      float big = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const int at_row = grp + n * groups;
+        if (!(ok && on && fresh[n]) || (gather && absent[st][at_row])) continue;
+        here |= 1u << (z * NS + n);
+        const Row16 raw = load_row(reinterpret_cast<const uint16_t*>(ring + (static_cast<uint32_t>(st) * n_rows + at_row) * (D * 2)), at);
+        if (kRot && !is_v) {
+          float x[16];
+          unpack(raw, x);
+          if (at.turned) rotate16(x, cs[n], sn[n], p.adjacent);
+          big = fmaxf(big, amax16(x));
+        } else {
+          big = fmaxf(big, amax_raw(raw));
+        }
       }
-      if (n_old > 0 && e > e_old && in_page < n_old) {
-        const float ratio = __uint_as_float(pow2_bits(max(e_old - e, -126)));
-        uint4* w = reinterpret_cast<uint4*>(rows + in_page * D + 16 * j);
-        uint4 c = *w;
-        c.x = rescale_e4m3(c.x, ratio); c.y = rescale_e4m3(c.y, ratio);
-        c.z = rescale_e4m3(c.z, ratio); c.w = rescale_e4m3(c.w, ratio);
-        *w = c;
-      }
+      // magnitudes order like their bits
+      const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(big));
+      if (lane == 0 && most != 0u) atomicMax(&top[now][z][mine], most);
     }
-    if ((grp & (P - 1)) == 0 && j == 0) scales[block_row] = __uint_as_float(pow2_bits(e));
+    if (threadIdx.x < kHeads * 4) (&top[next][0][0])[threadIdx.x] = 0u;             // last read two rounds ago
+    __syncthreads();                              // also: every thread has read the old scales, and is done with the round before
+    start(k + kRoundsAhead<kMode>);               // into the slots of the round before
+#pragma unroll
+    for (int z = 0; z < kHeads; ++z) {
+      const int m = k * kHeads + z, st = m % kPageSlots, job = job0 + m * side + mine;
+      if (job >= job1 || !ok) continue;
+      const bool is_v = job >= Hkv;
+      const int g = is_v ? job - Hkv : job;
+      const Pieces& at = is_v ? plain : turned;
+      const long long block_row = static_cast<long long>(pid) * Hkv + g;
+      int e = scale_exponent(top[now][z][mine]);
+      const int e_old = scale_log2(__float_as_uint(old_scale[z]));
+      if (n_old > 0 && e_old > e) e = e_old;
+      const float inv = __uint_as_float(pow2_bits(-e));
+      uint8_t* const rows = (is_v ? p.c.v_pages : p.c.k_pages) + (block_row << p.c.page_log2) * D;
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const int at_row = grp + n * groups, in_page = at_row & (P - 1);
+        if ((here >> (z * NS + n)) & 1u) {
+          float x[16];
+          unpack(load_row(reinterpret_cast<const uint16_t*>(ring + (static_cast<uint32_t>(st) * n_rows + at_row) * (D * 2)), at), x);
+          if (kRot && !is_v && at.turned) rotate16(x, cs[n], sn[n], p.adjacent);
+          store_codes(rows + in_page * D, at, x, inv);
+        }
+        if (n_old > 0 && e > e_old && in_page < n_old) {
+          const float ratio = __uint_as_float(pow2_bits(max(e_old - e, -126)));
+          uint4* w = reinterpret_cast<uint4*>(rows + in_page * D + 16 * j);
+          uint4 c = *w;
+          c.x = rescale_e4m3(c.x, ratio); c.y = rescale_e4m3(c.y, ratio);
+          c.z = rescale_e4m3(c.z, ratio); c.w = rescale_e4m3(c.w, ratio);
+          *w = c;
+        }
+      }
+      if ((grp & (P - 1)) == 0 && j == 0) ((is_v ? p.c.v_scales : p.c.k_scales))[block_row] = __uint_as_float(pow2_bits(e));
+    }
+    now = next;
   }
   if (!ok)                                        // a wait gave up: no copy may still be in flight when the block leaves
-    for (int k = max(0, rounds - kPageStages); k < rounds; ++k)
-      mbar_wait_drain(&full[k % kPageStages], (k / kPageStages) & 1, p.hdr, SITE_APPEND_WAIT);
+    for (int m = max(0, fills - kPageSlots); m < fills; ++m)
+      mbar_wait_drain(&full[m % kPageSlots], (m / kPageSlots) & 1, p.hdr, SITE_APPEND_WAIT);
 }
 
 // kKind: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per lane
 // group).  The blocks from page_blocks on take the row role.
-template <int D, int kKind, bool kRot>
+template <int D, int kKind, int kMode>
 __global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0)
 paged_append_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AppendParams p) {
   pdl_wait();
@@ -600,26 +616,26 @@ paged_append_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   }
   // the long blocks of the page role come first, so that the short ones of the row role fill the gaps they leave
   const int block = static_cast<int>(blockIdx.x);
-  if (block >= p.page_blocks) append_rows<D, kKind != 0, kRot>(p, block - p.page_blocks);
+  if (block >= p.page_blocks) append_rows<D, kKind != 0, kMode>(p, block - p.page_blocks);
   else if constexpr (kKind == 1) append_small<D>(p, block);
-  else if constexpr (kKind == 2) append_page<D, 1, kRot>(p, &map_k, &map_v, block);
-  else if constexpr (kKind == 3) append_page<D, 2, kRot>(p, &map_k, &map_v, block);
+  else if constexpr (kKind == 2) append_page<D, 1, kMode>(p, &map_k, &map_v, block);
+  else if constexpr (kKind == 3) append_page<D, 2, kMode>(p, &map_k, &map_v, block);
 }
 
-template <int D, int kKind, bool kRot>
+template <int D, int kKind, int kMode>
 static cudaError_t launch_kind(const AppendParams& p, const CUtensorMap (&maps)[2], int blocks, int threads, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(threads);
   cfg.stream = stream;
-  constexpr int kEach = kKind == 3 ? 2 * kPageStages : kKind == 2 ? kPageStages : 0;    // page role: rows of 32 bytes a thread
+  constexpr int kEach = kKind == 3 ? 2 * kSlotsOf<kMode> : kKind == 2 ? kSlotsOf<kMode> : 0;    // page role: rows of 32 bytes a thread
   const int rows = p.row_heads == 0 ? kEach : kEach > kRowStages ? kEach : kRowStages;
   static PerDeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(paged_append_kernel<D, kKind, kRot>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    e = cudaFuncSetAttribute(paged_append_kernel<D, kKind, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (kEach > kRowStages ? kEach : kRowStages) * 32 * (kKind == 3 ? 512 : 256));
     if (e != cudaSuccess) return e;
     configured.set(dev);
@@ -629,7 +645,14 @@ static cudaError_t launch_kind(const AppendParams& p, const CUtensorMap (&maps)[
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind, kRot>, maps[0], maps[1], p);
+  return cudaLaunchKernelEx(&cfg, paged_append_kernel<D, kKind, kMode>, maps[0], maps[1], p);
+}
+
+template <int D, int kMode>
+static cudaError_t launch_mode(const AppendParams& p, const CUtensorMap (&maps)[2], bool e4m3, bool two_rows, int blocks, int threads,
+                               cudaStream_t stream) {
+  if (!e4m3) return launch_kind<D, 0, kMode>(p, maps, blocks, threads, stream);
+  return two_rows ? launch_kind<D, 3, kMode>(p, maps, blocks, threads, stream) : launch_kind<D, 2, kMode>(p, maps, blocks, threads, stream);
 }
 
 template <int D>
@@ -658,9 +681,9 @@ static cudaError_t launch_d(AppendParams& p, const CUtensorMap (&maps)[2], bool 
     if (small) {
       page_blocks = (items * jobs + threads / GL - 1) / (threads / GL);
     } else {
-      // Page role: a block walks all heads of its page; with fewer pages than the SMs hold blocks, the heads are split over as
-      // many blocks as still run at once.
-      long long slices = 1LL * kSms * (threads == 512 ? 1 : p.rot_dim ? 2 : 3) / items;
+      // Page role: a block walks all heads of its page; with fewer pages than the SMs hold blocks (as far as the slots' shared
+      // memory goes), the heads are split over as many blocks as still run at once.
+      long long slices = static_cast<long long>(kSms) * (threads == 512 ? 1 : per_page > threads ? (p.idx ? 3 : 2) : 4) / items;
       const int side = per_page < threads ? threads / per_page : 1;
       if (slices > jobs / side) slices = jobs / side;
       if (slices < 1) slices = 1;
@@ -673,10 +696,11 @@ static cudaError_t launch_d(AppendParams& p, const CUtensorMap (&maps)[2], bool 
   if (page_blocks + row_blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
   p.page_blocks = static_cast<int>(page_blocks);
   const int blocks = static_cast<int>(page_blocks + row_blocks);
-  if (!e4m3) return p.rot_dim ? launch_kind<D, 0, true>(p, maps, blocks, threads, stream) : launch_kind<D, 0, false>(p, maps, blocks, threads, stream);
-  if (small) return launch_kind<D, 1, true>(p, maps, blocks, threads, stream);
-  if (per_page > threads) return p.rot_dim ? launch_kind<D, 3, true>(p, maps, blocks, threads, stream) : launch_kind<D, 3, false>(p, maps, blocks, threads, stream);
-  return p.rot_dim ? launch_kind<D, 2, true>(p, maps, blocks, threads, stream) : launch_kind<D, 2, false>(p, maps, blocks, threads, stream);
+  if (e4m3 && small) return launch_kind<D, 1, kRotated>(p, maps, blocks, threads, stream);       // the small role looks for itself
+  const bool two_rows = e4m3 && per_page > threads;
+  if (p.rot_dim) return launch_mode<D, kRotated>(p, maps, e4m3, two_rows, blocks, threads, stream);
+  if (p.idx) return launch_mode<D, kGathered>(p, maps, e4m3, two_rows, blocks, threads, stream);
+  return launch_mode<D, kPlain>(p, maps, e4m3, two_rows, blocks, threads, stream);
 }
 
 bool paged_append_uses_maps(const AppendParams& p, bool e4m3) { return e4m3 && p.max_new > kSmallRows && p.idx == nullptr; }

@@ -214,6 +214,25 @@ def test_append_kept_rows_equals_compact_then_append(fmt, Hkv, d, page):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("kept", [5, 100])
+def test_append_kept_rows_of_a_head_major_source(fmt, kept):
+    """Keys and values that are stored head by head, [n_kv_heads, rows, head_dim]: the rows that idx names, exactly."""
+    rng = np.random.default_rng(kept)
+    Hkv, d, L = 4, 128, 777
+    k, v = bf16_rows(rng, (Hkv, L, d)), bf16_rows(rng, (Hkv, L, d))
+    idx = np.stack([np.sort(rng.permutation(L)[:kept]) for _ in range(Hkv)]).astype(np.int32)
+    pools = Pools(fmt, [0], [kept], 32, Hkv, d, 3)
+    before = [None if t is None else t.cpu().clone() for t in (pools.k, pools.v, pools.ks, pools.vs)]
+    rows = B.make_new_rows(batch=1, total=kept, n_kv_heads=Hkv, head_dim=d, total_src=L, k_stride_tok=d, k_stride_head=L * d,
+                           v_stride_tok=d, v_stride_head=L * d)
+    ws = workspace()
+    B.fastkv_paged_append(pools.cache(), rows, pools.dev_lens, None, k.cuda(), v.cuda(), None, None, torch.from_numpy(idx).cuda(), None, None, ws)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    pick = lambda x: x.double().numpy()[np.arange(Hkv)[:, None], idx].transpose(1, 0, 2)  # noqa: E731
+    check_append(pools, before, [0], [kept], [pick(k)], [pick(v)], False)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 40])
 def test_append_reports_what_it_cannot_write(fmt, n):
     """A page id outside the pool, rows beyond the block table's room, an index outside its sequence: reported, and nothing but
