@@ -356,7 +356,7 @@ int fastkv_score_static_status(void* stream, int32_t* status, int32_t* site);
  *                         1 never; 2 whenever the shape allows it
  *   "fused_heads"         path 2: KV heads scored side by side in one phase (0: by size)
  *   "fused_lead"          path 2: phases the first read may lead the second (0: by size)
- *   "wait_limit_cycles"   clock cycles a device-side wait of the scoring kernels polls before it
+ *   "wait_limit_cycles"   clock cycles a device-side wait of the scoring, prefill and paged kernels polls before it
  *                         gives up and raises FASTKV_ERR_DEVICE_TIMEOUT (0: about a second)
  *   "extra_publications"  the scoring kernels' second pass waits for this many publications of
  *                         softmax statistics beyond those that will arrive; with a short wait limit
@@ -364,6 +364,10 @@ int fastkv_score_static_status(void* stream, int32_t* status, int32_t* site);
  *   "prefill_skip_commit" n > 0: the prefill attention's issuer withholds the signal that S of key tile
  *                         n - 1 is ready (first query tile of every CTA); with a short wait limit the
  *                         softmax warps' bounded wait runs out without any fault (timeout test); 0: off
+ *   "paged_skip_copy"     n > 0: the paged attention withholds the copies of the first pair of warps' n-th chunk of every
+ *                         segment, the paged append (8-bit pages, more than 8 rows per sequence) those of every block's
+ *                         n-th head; with a short wait limit the wait for them runs out without any fault (timeout
+ *                         test); 0: off
  *   "paged_two_maps"      1: the paged attention copies K and V pages through a tensor map each, as it does for pools
  *                         that lie 2^40 bytes or more apart (test); 0: through one map where it can
  *   "time_kernels"        1: record a pair of CUDA events around every kernel the library launches

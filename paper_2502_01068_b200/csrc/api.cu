@@ -48,6 +48,7 @@ struct DebugConfig {
   int extra_publications = 0;       // pass 2 waits for publications that never come (timeout test)
   int score_partition = 0;          // parked kernel's partition mode: 0 = by shape, 1 = never, 2 = whenever it can run
   int paged_two_maps = 0;           // paged attention: copies K and V apart, as pools beyond 2^40 bytes of one another need
+  int paged_skip_copy = 0;          // paged kernels: n > 0: the copies of chunk (or fill) n - 1 are withheld (timeout test)
   int prefill_skip_commit = 0;      // prefill attention: n > 0: key tile n - 1's "S ready" signal is withheld (timeout test)
 };
 DebugConfig g_debug;
@@ -363,6 +364,8 @@ int fastkv_debug_set(const char* key, int64_t value) {
   } else if (!std::strcmp(key, "paged_two_maps")) {
     if (value < 0 || value > 1) return fail(FASTKV_ERR_INVALID_ARG, "debug_set: paged_two_maps is 0 or 1");
     g_debug.paged_two_maps = static_cast<int>(value);
+  } else if (!std::strcmp(key, "paged_skip_copy")) {
+    g_debug.paged_skip_copy = static_cast<int>(value < 0 ? 0 : value);
   } else if (!std::strcmp(key, "extra_publications")) {
     g_debug.extra_publications = static_cast<int>(value < 0 ? 0 : value);
   } else if (!std::strcmp(key, "time_kernels")) {
@@ -939,6 +942,8 @@ int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* 
   p.q_tok = r.q_stride_tok; p.q_head = r.q_stride_head; p.k_tok = r.k_stride_tok; p.k_head = r.k_stride_head;
   p.v_tok = r.v_stride_tok; p.v_head = r.v_stride_head;
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;
+  p.skip_copy = g_debug.paged_skip_copy - 1;
   const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
   CUtensorMap maps[2];
   memset(maps, 0, sizeof maps);
@@ -1010,6 +1015,8 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   p.part_ml = reinterpret_cast<float4*>(ws + sizeof(WorkspaceHeader));
   p.part_o = reinterpret_cast<float*>(ws + paged_attn_partials_offset(plan, c.batch, c.n_kv_heads));
   p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+  p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;
+  p.skip_copy = g_debug.paged_skip_copy - 1;
   cudaError_t e;
   int launched = 0;
   {

@@ -62,6 +62,7 @@ enum Site : int {
   SITE_PAGED_PAGE = 40,
   SITE_PAGED_LEN = 41,
   SITE_APPEND_WAIT = 42,
+  SITE_PAGED_EMPTY = 43,
 };
 
 // Records `text` as the calling thread's last error (see fastkv_last_error) and returns `status`.

@@ -31,6 +31,8 @@ struct AppendParams {
   uint16_t* q_out;
   long long q_tok, q_head, k_tok, k_head, v_tok, v_head;   // strides, elements
   WorkspaceHeader* hdr;
+  long long wait_limit;       // cycles a wait polls before it gives up
+  int skip_copy;              // test hook: this fill of the page role's slots is not started (-1: none)
   // work split, filled in by the launcher
   int page_blocks, heads_per_unit, row_heads, row_slices;  // row role, behind the page role's blocks
   int pages_per_seq, job_slices, jobs_per_slice;           // page role (8-bit pages)
@@ -49,6 +51,8 @@ struct PagedAttnParams {
   int splits;                 // static launches: CTAs that share a (sequence, KV head, row tile)
   int balanced, ctas;         // balanced launches: CTAs that share all of them
   int box_subs;               // 16-entry steps that one TMA box brings
+  long long wait_limit;       // cycles a wait polls before it gives up
+  int skip_copy;              // test hook: the first pair of warps gets no copies for this chunk of a segment (-1: none)
   int joint, v_first;         // K and V are planes of one tensor map; the V pool lies at the lower address
   float scale_log2;           // softmax scale times log2(e)
   const int* lens;

@@ -477,7 +477,7 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
   };
   auto start = [&](int k) {                       // this thread's part of round k's copies; every bringing thread arrives
     const int m = k * kHeads + my_fill;
-    if (!brings || m >= fills) return;
+    if (!brings || m >= fills || m == p.skip_copy) return;
     const int st = m % kPageSlots;
     if (!gather) {                                // a box of the page's rows for each head side by side
       const int first = job0 + m * side, n = min(side, job1 - first);
@@ -533,7 +533,7 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
       const int m = k * kHeads + z, st = m % kPageSlots, job = job0 + m * side + mine;
       const bool on = job < job1, is_v = job >= Hkv;
       old_scale[z] = on && n_old > 0 ? (is_v ? p.c.v_scales : p.c.k_scales)[static_cast<long long>(pid) * Hkv + (is_v ? job - Hkv : job)] : 0.0f;
-      if (m < fills) ok = ok && mbar_wait_bounded(&full[st], (m / kPageSlots) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT);
+      if (m < fills) ok = ok && mbar_wait_bounded(&full[st], (m / kPageSlots) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT, p.wait_limit);
       const Pieces& at = is_v ? plain : turned;
       float big = 0.0f;
 #pragma unroll
@@ -595,7 +595,10 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
   }
   if (!ok)                                        // a wait gave up: no copy may still be in flight when the block leaves
     for (int m = max(0, fills - kPageSlots); m < fills; ++m)
-      mbar_wait_drain(&full[m % kPageSlots], (m / kPageSlots) & 1, p.hdr, SITE_APPEND_WAIT);
+      if (p.skip_copy < 0 || m % kPageSlots != p.skip_copy % kPageSlots)
+        mbar_wait_drain(&full[m % kPageSlots], (m / kPageSlots) & 1, p.hdr, SITE_APPEND_WAIT);
+      else                                        // the withheld fill's barrier stays a phase behind the copies behind it
+        mbar_wait_drain(&full[m % kPageSlots], ((m - kPageSlots) / kPageSlots) & 1, nullptr, SITE_APPEND_WAIT, p.wait_limit);
 }
 
 // kKind: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per lane

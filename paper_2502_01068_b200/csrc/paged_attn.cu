@@ -82,10 +82,16 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
   return r;
 }
 
-// Four warps per CTA, two CTAs per SM: eight warps that may hold 255 registers each.  The chain from one chunk's logits to its
-// outputs is long and every warp walks it alone, so what counts is how much independent work the compiler can weave into it,
-// and that takes registers.
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+// A CTA is four warps that compute and four that bring the data, one for each of them; two CTAs per SM.  The chain from a chunk's
+// logits to its outputs is long and every warp walks it alone, so what counts is how much independent work the compiler can
+// weave into it, and that takes registers: the launch's 128 a thread are split 216 to 40.  Starting a chunk's copies (page, box,
+// barrier) held a computing warp up for ~600 cycles, a third of its pass; a warp of its own does it in the meantime and runs
+// ahead into the CTA's next segment.
+constexpr int kWarps = 4, kComputing = 32 * kWarps, kThreads = 2 * kComputing;
+constexpr int kLaunchRegs = 128, kComputeRegs = 216, kBringRegs = 40;
+static_assert(kComputeRegs + kBringRegs == 2 * kLaunchRegs, "the warpgroups' shares add up to what the CTA was launched with");
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <int D, bool kE4M3, int RT>
 struct PagedCfg {
@@ -99,11 +105,15 @@ struct PagedCfg {
   static constexpr int kBoxRow = kRowBytes / kBoxes;
   static constexpr int kBoxBytes = kChunk * kBoxRow;
   static constexpr int kStageBytes = 2 * kBoxes * kBoxBytes;               // by column block: K's rows, V's rows (see the copies)
-  static constexpr int kStages = kE4M3 ? 2 : 3;   // of 8 KB each for head_dim 128
+  // Per computing warp, of 8 KB each for head_dim 128.  A third stage of 8-bit rows makes long caches slower (131072 entries: 52
+  // against 49.5 us): what is in flight is enough, and fewer streams leave memory pages open longer.
+  static constexpr int kStages = kE4M3 ? 2 : 3;
   static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
   static constexpr int kRows = 8 * RT;
-  static constexpr int kMergeBytes = kWarps * kRows * (D * 4 + 16);        // the warps' outputs and (max, sum, reference)
-  static constexpr int kSmem = (kRingBytes > kMergeBytes ? kRingBytes : kMergeBytes) + 1024;
+  static constexpr int kMergeCols = RT == 1 ? 64 : 32;                     // the warps' outputs meet so many columns at a time
+  static constexpr int kMergeLd = kMergeCols + 4;
+  static constexpr int kMergeBytes = kWarps * kRows * (kMergeLd * 4 + 16);
+  static constexpr int kSmem = kRingBytes + kMergeBytes + 1024;
 };
 
 // Sum over the block of one value per thread; every thread gets it.  `scratch`: one word per warp.
@@ -141,14 +151,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   constexpr int kTerms = kE4M3 ? 2 : 3;         // 16-bit terms of a weight: 11 + 11 bits of fp16, 8 + 8 + 8 of bf16
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  __shared__ uint64_t full[kWarps][kStages];
+  __shared__ uint64_t full[kWarps][kStages], empty[kWarps][kStages];
+  __shared__ float2 scale_of[kWarps][kStages][NSUB];       // 8-bit pages, by 16 entries of a stage: K's scale, log2 of V's
+  __shared__ float weight_of[kWarps][kRows];               // what a warp's outputs count for in the merge
+  __shared__ long long at_of[kRows];                       // where a row's result goes, in units of D floats
   __shared__ int abort_flag;
-  __shared__ long long scratch[kWarps];
+  __shared__ long long scratch[kThreads / 32];
   __shared__ int s_first;
   __shared__ long long s_base;
 
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int quad = lane >> 2, c = lane & 3;     // fragment coordinates
   const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len;
 
   if (t == 0) {
@@ -157,8 +169,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     abort_flag = 0;
     s_first = -1;
   }
-  if (lane == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
+  if (lane == 0 && warp < kWarps) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[warp][i], 1); mbar_init(&empty[warp][i], 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -212,73 +224,130 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     c1 = min(n_chunks, c0 + per);
   }
 
-  uint8_t* const ring_ptr = smem + warp * kStages * Cfg::kStageBytes;
-  const uint32_t ring = smem_u32(ring_ptr);
-  const uint64_t policy = p.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-  const int page_subs_log2 = p.c.page_log2 - 4;            // steps of 16 entries in a page
+  // Moves on to the next segment of the share; false when there is none.
+  auto advance = [&]() -> bool {
+    if (!p.balanced) return false;
+    u += c1 - c0;
+    if (u >= u_end) return false;
+    if (++ht == HT) {
+      ht = 0;
+      do { n_chunks = chunks_of(p, ++b, kChunkLog2); } while (n_chunks == 0);       // u < u_end: there is one
+    }
+    c0 = 0;
+    c1 = static_cast<int>(min(static_cast<long long>(n_chunks), u_end - u));
+    return true;
+  };
+  const int pair = warp & (kWarps - 1);                    // the computing warp, and the one that brings its data
+  uint8_t* const ring_ptr = smem + pair * kStages * Cfg::kStageBytes;
   // inside a column block of a stage: K and V alternate by box (of a chunk's 32 rows, or of 16)
   const uint32_t box_bytes = p.box_subs * kSub * Cfg::kBoxRow, sub_stride = NSUB == 2 && p.box_subs == 1 ? 2 * kSub * Cfg::kBoxRow : kSub * Cfg::kBoxRow;
   const uint32_t k_off = p.v_first ? box_bytes : 0, v_off = p.v_first ? 0 : box_bytes;
-  const uint32_t row7 = lane & 7;
-  const uint32_t swz = Cfg::kBoxRow == 128 ? row7 : (row7 >> 1);      // 16-byte piece p of row r sits at p ^ swz
-  int stage_in = 0, stage_out = 0;                         // ring positions, carried from segment to segment
-  uint32_t phase_out = 0;
+  int stage = 0;                                           // position in the ring, carried from segment to segment
+  uint32_t phase = 0;
+  auto step = [&]() { if (++stage == kStages) { stage = 0; phase ^= 1; } };
   bool ok = true;                                          // false: a wait gave up; nothing more is copied or computed
 
-  while (true) {
+  if (warp >= kWarps) {
+    // ================= a warp that brings data =================
+    give_registers<kBringRegs>();
+    const uint64_t policy = p.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+    const int page_subs_log2 = p.c.page_log2 - 4;          // steps of 16 entries in a page
+    int issued = 0;                                        // chunks whose copies were started, up to kStages
+    do {
+      const int g = ht % Hkv;
+      const int len = usable_len(p.lens[b], p.c.max_pages, p.c.page_log2);
+      const int my_chunks = c1 - c0 > pair ? (c1 - c0 - pair + kWarps - 1) / kWarps : 0;
+      const int* const table = p.c.block_table + static_cast<size_t>(b) * p.c.max_pages;
+      const int n_subs = (len + kSub - 1) / kSub;
+      // Page and scales of the 16-entry step x for lane x % 32, fetched for 32 steps at a time, a batch ahead: table -> scale is
+      // a chain of two trips to memory.
+      auto block_of = [&](int x) -> int {                  // block (page * Hkv + g) of this lane's step, -1 behind the end
+        const int i = x / NSUB, sub = (c0 + pair + i * kWarps) * NSUB + x % NSUB;
+        if (i >= my_chunks || sub >= n_subs) return -1;
+        const long long blk = pool_block(table[sub >> page_subs_log2], p.c.n_pages, Hkv, g);
+        if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_PAGE); return g; }   // page 0 instead
+        return static_cast<int>(blk);
+      };
+      auto scales_at = [&](int blk) -> float2 {
+        if (!kE4M3 || blk < 0) return make_float2(1.0f, 0.0f);
+        return make_float2(p.c.k_scales[blk], static_cast<float>(scale_log2(__float_as_uint(p.c.v_scales[blk]))));
+      };
+      int blk_cur = block_of(lane), blk_next = block_of(32 + lane);
+      float2 sc_cur = scales_at(blk_cur), sc_next = scales_at(blk_next);
+      for (int i = 0; i < my_chunks; ++i) {
+        if ((i * NSUB & 31) == 0 && i > 0) {               // the next batch of 32 steps becomes the current one
+          blk_cur = blk_next;
+          sc_cur = sc_next;
+          blk_next = block_of(i * NSUB + 32 + lane);
+          sc_next = scales_at(blk_next);
+        }
+        if (issued == kStages) {                           // the stage has to be empty again
+          ok = mbar_wait_nap(&empty[pair][stage], phase ^ 1, &abort_flag, p.hdr, SITE_PAGED_EMPTY, p.wait_limit);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        } else {
+          ++issued;
+        }
+        const int here = lane - (i * NSUB & 31);           // this lane's step of the chunk, if it has one
+        if (kE4M3 && here >= 0 && here < NSUB) scale_of[pair][stage][here] = sc_cur;
+        int blk[NSUB];
+#pragma unroll
+        for (int y = 0; y < NSUB; ++y) blk[y] = max(__shfl_sync(0xffffffffu, blk_cur, (i * NSUB + y) & 31), 0);
+        __syncwarp();                                      // the scales are there before the barrier says so
+        const bool withheld = pair == 0 && i == p.skip_copy;     // test hook
+        if (lane == 0 && !withheld) {
+          // One copy brings a box of K and the same box of V (the pools are two planes of one tensor map); where the pools lie
+          // too far apart for that, two copies fill the same places.  A step behind the sequence's end brings page 0.
+          uint64_t* bar = &full[pair][stage];
+          mbar_arrive_expect_tx(bar, Cfg::kStageBytes);
+#pragma unroll
+          for (int y = 0; y < NSUB; ++y) {
+            if (y > 0 && p.box_subs != 1) break;
+            const int sub = (c0 + pair + i * kWarps) * NSUB + y;
+            const int row = (sub & ((1 << page_subs_log2) - 1)) * kSub;
+            uint8_t* dst = ring_ptr + stage * Cfg::kStageBytes + y * sub_stride;
+#pragma unroll
+            for (int x = 0; x < Cfg::kBoxes; ++x) {
+              if (p.joint) {
+                tma_load_4d(dst + x * 2 * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk[y], 0, policy);
+              } else {
+                tma_load_3d(dst + x * 2 * Cfg::kBoxBytes + k_off, &tmap_k, bar, x * 64, row, blk[y], policy);
+                tma_load_3d(dst + x * 2 * Cfg::kBoxBytes + v_off, &tmap_v, bar, x * 64, row, blk[y], policy);
+              }
+            }
+          }
+        }
+        __syncwarp();
+        step();
+      }
+    } while (ok && advance());
+    if (lane == 0) {                                       // no copy is in flight when the warp leaves, whatever the others do
+      for (int j = 0; j < issued; ++j) {
+        if (stage == 0) { stage = kStages; phase ^= 1; }
+        --stage;
+        if (pair != 0 || p.skip_copy < 0) mbar_wait_drain(&full[pair][stage], phase, p.hdr, SITE_PAGED_WAIT);
+        else mbar_wait_drain(&full[pair][stage], phase, nullptr, SITE_PAGED_WAIT, p.wait_limit);   // the withheld one never arrives
+      }
+    }
+    return;
+  }
+
+  // ================= the warps that compute =================
+  take_registers<kComputeRegs>();
+  const int quad = lane >> 2, c = lane & 3;                // fragment coordinates
+  const uint32_t ring = smem_u32(ring_ptr);
+  const uint32_t row7 = lane & 7;
+  const uint32_t swz = Cfg::kBoxRow == 128 ? row7 : (row7 >> 1);      // 16-byte piece p of row r sits at p ^ swz
+  float* const mo = reinterpret_cast<float*>(smem + Cfg::kRingBytes);                          // [warps][rows][columns]
+  float4* const mml = reinterpret_cast<float4*>(mo + kWarps * kRows * Cfg::kMergeLd);        // [warps][rows]: max, sum, reference
+  auto meet = []() { asm volatile("bar.sync 1, %0;" ::"n"(kComputing) : "memory"); };
+
+  do {
     const int g = ht % Hkv, tile = ht / Hkv, row_base = tile * kRows;
     const int asked = p.lens[b];
     const int len = usable_len(asked, p.c.max_pages, p.c.page_log2);
     if (t == 0 && c0 == 0 && ht == 0 && asked != len) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
     const int my_chunks = ok && c1 - c0 > warp ? (c1 - c0 - warp + kWarps - 1) / kWarps : 0;
-    const int* const table = p.c.block_table + static_cast<size_t>(b) * p.c.max_pages;
-    const int n_subs = (len + kSub - 1) / kSub;
-
-    // Page and scales of the warp's 16-entry step x for lane x % 32, fetched for 32 steps at a time.
-    auto block_of = [&](int x) -> int {                    // block (page * Hkv + g) of this lane's step
-      const int i = x / NSUB, sub = (c0 + warp + i * kWarps) * NSUB + x % NSUB;
-      if (i >= my_chunks || sub >= n_subs) return -1;
-      const long long blk = pool_block(table[sub >> page_subs_log2], p.c.n_pages, Hkv, g);
-      if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_PAGE); return g; }   // page 0 instead
-      return static_cast<int>(blk);
-    };
-    int blk_cur = block_of(lane), blk_next = block_of(32 + lane);
-    float sk_cur = 1.0f, sv_cur = 1.0f, sk_next = 1.0f, sv_next = 1.0f;
-    if constexpr (kE4M3) {
-      if (blk_cur >= 0) { sk_cur = p.c.k_scales[blk_cur]; sv_cur = p.c.v_scales[blk_cur]; }
-      if (blk_next >= 0) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
-    }
-    // Lane 0 only.  One copy brings a box of K and the same box of V (the pools are two planes of one tensor map), because
-    // starting a copy costs the warp ~150 cycles; where the pools lie too far apart for that, two copies fill the same places.
-    auto issue = [&](int i, int sub_in, int blk) {
-      const int sub = (c0 + warp + i * kWarps) * NSUB + sub_in;
-      const int row = (sub & ((1 << page_subs_log2) - 1)) * kSub;
-      uint64_t* bar = &full[warp][stage_in];
-      uint8_t* stage = ring_ptr + stage_in * Cfg::kStageBytes + sub_in * sub_stride;
-#pragma unroll
-      for (int x = 0; x < Cfg::kBoxes; ++x) {
-        if (p.joint) {
-          tma_load_4d(stage + x * 2 * Cfg::kBoxBytes, &tmap_k, bar, x * 64, row, blk, 0, policy);
-        } else {
-          tma_load_3d(stage + x * 2 * Cfg::kBoxBytes + k_off, &tmap_k, bar, x * 64, row, blk, policy);
-          tma_load_3d(stage + x * 2 * Cfg::kBoxBytes + v_off, &tmap_v, bar, x * 64, row, blk, policy);
-        }
-      }
-    };
-    // All lanes: starts the copies of the warp's chunk i (a step behind the sequence's end brings page 0: masked below).
-    auto start = [&](int i, int now) {
-      const bool next = (i * NSUB >> 5) != (now * NSUB >> 5);
-      if (lane == 0) mbar_arrive_expect_tx(&full[warp][stage_in], Cfg::kStageBytes);
-#pragma unroll
-      for (int y = 0; y < NSUB; ++y) {
-        const int from = (i * NSUB + y) & 31;
-        const int blk = next ? __shfl_sync(0xffffffffu, blk_next, from) : __shfl_sync(0xffffffffu, blk_cur, from);
-        if (lane == 0 && (y == 0 || p.box_subs == 1)) issue(i, y, max(blk, 0));
-      }
-      stage_in = stage_in + 1 == kStages ? 0 : stage_in + 1;
-    };
-    int issued = 0;
-    for (; issued < kStages - 1 && issued < my_chunks; ++issued) start(issued, 0);
 
     // ---- query fragments: rows quad and (RT == 2) quad + 8 of the tile, absent rows zero ----
     uint32_t qa[KS][2 * RT];
@@ -361,6 +430,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           *reinterpret_cast<uint4*>(vs + x * 2 * Cfg::kBoxBytes + r / kSub * sub_stride + r % kSub * Cfg::kBoxRow + rem % kPieces * 16) =
               make_uint4(0u, 0u, 0u, 0u);
         }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before the stage's next copies
         __syncwarp();
       }
       // ---- S = Q K^T, 8 entries a tile: lane holds (row quad, entries nt * 8 + 2c, + 1) in [0], [1], row quad + 8 in [2], [3] ----
@@ -410,8 +480,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         sk[y] = 1.0f;
         ev[y] = 0.0f;
         if constexpr (kE4M3) {
-          sk[y] = __shfl_sync(0xffffffffu, sk_cur, (i * NSUB + y) & 31);
-          ev[y] = static_cast<float>(scale_log2(__float_as_uint(__shfl_sync(0xffffffffu, sv_cur, (i * NSUB + y) & 31))));
+          const float2 sc = scale_of[warp][st][y];
+          sk[y] = sc.x;
+          ev[y] = sc.y;
         }
       }
       uint32_t pt[RT][kTerms][NSUB][2];             // the weights as B fragments, term by term
@@ -524,32 +595,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           for (int rt = 0; rt < RT; ++rt) join(o[rt][m0 + z], x[z][rt], a0[rt], a1[rt]);
       }
     };
-    int waited = 0;                                // chunks whose copies have been waited for
     for (int i = 0; i < my_chunks; ++i) {
-      if ((i * NSUB & 31) == 0 && i > 0) {                   // the next batch of 32 steps becomes the current one
-        blk_cur = blk_next;
-        sk_cur = sk_next; sv_cur = sv_next;
-        blk_next = block_of(i * NSUB + 32 + lane);
-        sk_next = sv_next = 1.0f;
-        if constexpr (kE4M3)
-          if (blk_next >= 0) { sk_next = p.c.k_scales[blk_next]; sv_next = p.c.v_scales[blk_next]; }
-      }
-      if (issued < my_chunks) start(issued++, i);            // into the stage that was emptied last iteration
-      ok = mbar_wait_bounded(&full[warp][stage_out], phase_out, &abort_flag, p.hdr, SITE_PAGED_WAIT);
+      ok = mbar_wait_bounded(&full[warp][stage], phase, &abort_flag, p.hdr, SITE_PAGED_WAIT, p.wait_limit);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      ++waited;
-      const int st = stage_out;
-      if (++stage_out == kStages) { stage_out = 0; phase_out ^= 1; }
-      if ((c0 + warp + i * kWarps + 1) * kChunk <= len - (T - 1)) pass(std::false_type{}, i, st);
-      else pass(std::true_type{}, i, st);
-      __syncwarp();                                // every lane is done with the stage before it is refilled
+      if ((c0 + warp + i * kWarps + 1) * kChunk <= len - (T - 1)) pass(std::false_type{}, i, stage);
+      else pass(std::true_type{}, i, stage);
+      __syncwarp();                                // every lane is done with the stage
+      if (lane == 0) mbar_arrive(&empty[warp][stage]);
+      step();
     }
-    if (lane == 0)                                 // after a wait that gave up: no copy may still be in flight
-      for (int j = waited; j < issued; ++j) {
-        const int x = stage_out + (j - waited);
-        mbar_wait_drain(&full[warp][x % kStages], phase_out ^ (x >= kStages ? 1u : 0u), p.hdr, SITE_PAGED_WAIT);
-      }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 1);
@@ -557,65 +612,81 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if constexpr (!kE4M3) r_run[rt] = m_run[rt];
     }
     pdl_launch_dependents();
-    // ---- the warps of the CTA merge through shared memory (the rings are idle: every copy was waited for) ----
-    __syncthreads();
-    float* mo = reinterpret_cast<float*>(smem);                                  // [warps][rows][D]
-    float4* mml = reinterpret_cast<float4*>(mo + kWarps * kRows * D);            // [warps][rows]: max, sum, reference
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const int d0 = mt * 16 + (kE4M3 ? 2 * quad : quad), d1 = d0 + (kE4M3 ? 1 : 8);
-        float* row0 = mo + (warp * kRows + rt * 8 + 2 * c) * D;
-        row0[d0] = o[rt][mt][0]; row0[D + d0] = o[rt][mt][1]; row0[d1] = o[rt][mt][2]; row0[D + d1] = o[rt][mt][3];
-      }
-      if (c == 0) mml[warp * kRows + rt * 8 + quad] =
-          make_float4(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f, ok ? r_run[rt] : -INFINITY, 0.0f);
-    }
-    __syncthreads();
+    // ---- the warps merge through shared memory: a thread per row weighs the warps, then the outputs join, columns by columns ----
     const int n_rows = min(kRows, p.rows - row_base);
     const bool whole = p.balanced ? c0 == 0 && c1 == n_chunks : p.splits == 1;
-    // where a piece's result waits for the merge: static launches by (pair, split), balanced ones by CTA (first segment or later)
-    const size_t part = (p.balanced ? 2 * static_cast<size_t>(blockIdx.x) + (u != u_begin) : static_cast<size_t>(blockIdx.x)) * kRows;
-    for (int x = t; x < n_rows * D; x += kThreads) {
-      const int r = x / D, col = x - r * D;
-      float M = -INFINITY, R = -INFINITY;
+    meet();                                        // the last segment's merge has been read
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        M = fmaxf(M, mml[w * kRows + r].x);
-        R = fmaxf(R, mml[w * kRows + r].z);
-      }
-      float L = 0.0f, acc = 0.0f;
+    for (int rt = 0; rt < RT; ++rt)
+      if (c == 0) mml[warp * kRows + rt * 8 + quad] =
+          make_float4(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f, ok ? r_run[rt] : -INFINITY, 0.0f);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float4 ml = mml[w * kRows + r];
-        if (ml.x == -INFINITY) continue;                                          // warps without entries weigh nothing
-        L = fmaf(ml.y, ex2(ml.x - M), L);
-        acc = fmaf(mo[(w * kRows + r) * D + col], ex2(ml.z - R), acc);
+    for (int cut = 0; cut < D / Cfg::kMergeCols; ++cut) {
+      if (cut > 0) meet();                         // the columns before have been read
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int m = 0; m < Cfg::kMergeCols / 16; ++m) {
+          const float (&x)[4] = o[rt][cut * (Cfg::kMergeCols / 16) + m];
+          float* row0 = mo + (warp * kRows + rt * 8 + 2 * c) * Cfg::kMergeLd + m * 16;
+          if constexpr (kE4M3) {
+            *reinterpret_cast<float2*>(row0 + 2 * quad) = make_float2(x[0], x[2]);
+            *reinterpret_cast<float2*>(row0 + Cfg::kMergeLd + 2 * quad) = make_float2(x[1], x[3]);
+          } else {
+            row0[quad] = x[0]; row0[Cfg::kMergeLd + quad] = x[1];
+            row0[quad + 8] = x[2]; row0[Cfg::kMergeLd + quad + 8] = x[3];
+          }
+        }
       }
-      if (whole) {
-        const int row = row_base + r, i = row / G, h = g * G + row - i * G;
-        const size_t at = (static_cast<size_t>(b) * T + i) * p.n_q_heads + h;
-        p.out[at * D + col] = L > 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
-        if (p.lse != nullptr && col == 0) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
-      } else {
-        if (col == 0) p.part_ml[part + r] = make_float4(M, L, R, 0.0f);
-        p.part_o[(part + r) * D + col] = acc;
+      meet();
+      if (cut == 0) {
+        if (t < n_rows) {
+          float M = -INFINITY, R = -INFINITY, L = 0.0f;
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            M = fmaxf(M, mml[w * kRows + t].x);
+            R = fmaxf(R, mml[w * kRows + t].z);
+          }
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            const float4 ml = mml[w * kRows + t];
+            if (ml.x != -INFINITY) L = fmaf(ml.y, ex2(ml.x - M), L);              // warps without entries weigh nothing
+          }
+          const float last = !whole ? 1.0f : L > 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            const float4 ml = mml[w * kRows + t];
+            weight_of[w][t] = ml.x != -INFINITY ? ex2(ml.z - R) * last : 0.0f;
+          }
+          if (whole) {
+            const int r = row_base + t, i = r / G, h = g * G + r - i * G;
+            const long long at = (static_cast<long long>(b) * T + i) * p.n_q_heads + h;
+            at_of[t] = at;
+            if (p.lse != nullptr) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+          } else {
+            // where a piece waits for the merge: static launches by (pair, split), balanced ones by CTA (first segment or later)
+            const long long at = (p.balanced ? 2 * static_cast<long long>(blockIdx.x) + (u != u_begin) : static_cast<long long>(blockIdx.x)) * kRows + t;
+            at_of[t] = at;
+            p.part_ml[at] = make_float4(M, L, R, 0.0f);
+          }
+        }
+        meet();
+      }
+      constexpr int kQuads = Cfg::kMergeCols / 4;
+      float* const dst = whole ? p.out : p.part_o;
+      for (int x = t; x < n_rows * kQuads; x += kComputing) {
+        const int r = x / kQuads, col = (x - r * kQuads) * 4;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = weight_of[w][r];
+          const float4 y = *reinterpret_cast<const float4*>(mo + (w * kRows + r) * Cfg::kMergeLd + col);
+          sum.x = fmaf(y.x, f, sum.x); sum.y = fmaf(y.y, f, sum.y); sum.z = fmaf(y.z, f, sum.z); sum.w = fmaf(y.w, f, sum.w);
+        }
+        *reinterpret_cast<float4*>(dst + at_of[r] * D + cut * Cfg::kMergeCols + col) = sum;
       }
     }
-    if (!p.balanced) return;
-    // ---- the next segment of this CTA's share ----
-    u += c1 - c0;
-    if (u >= u_end) return;
-    if (++ht == HT) {
-      ht = 0;
-      do { n_chunks = chunks_of(p, ++b, kChunkLog2); } while (n_chunks == 0);       // u < u_end: there is one
-    }
-    c0 = 0;
-    c1 = static_cast<int>(min(static_cast<long long>(n_chunks), u_end - u));
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                   // the merge's accesses before the next copies
-    __syncthreads();
-  }
+  } while (advance());
 }
 
 // Merges the pieces of one query row: one block of D threads each.
@@ -711,10 +782,11 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   const int chunk = e4m3 ? 2 * kSub : kSub;
   const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
   const long long chunks = (max_len + chunk - 1) / chunk;
-  // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge kernel costs 4.5 us,
-  // a warp's pass over a chunk 0.9 us in 8 bits and 0.6 us in bf16.
+  // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge kernel costs 4 to 5 us,
+  // a warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (700 entries in 8 bits: 8.3 us whole, 7.1 in nine splits;
+  // 257: 5.3 whole, 6.3 in three).
   long long splits = kCapacity / pairs;
-  const long long useful = chunks <= (e4m3 ? 24 : 32) ? 1 : (chunks + kWarps - 1) / kWarps;
+  const long long useful = chunks <= (e4m3 ? 16 : 24) ? 1 : (chunks + kWarps - 1) / kWarps;
   if (splits > useful) splits = useful;
   if (splits > kPagedMaxPieces) splits = kPagedMaxPieces;
   if (splits < 1) splits = 1;
@@ -722,7 +794,8 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   pl.balanced = 0;
   pl.ctas = 0;
   // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays about eight chunks' time for every segment it
-  // starts.  Eight sequences of 4K to 64K entries, 8 bits: 235 us static, 110 us balanced; 64 of 1638 to 2048, bf16: 77 and 89.
+  // starts.  Eight sequences of 4K to 64K entries, 8 bits: 235 us static, 109 us balanced; 32 of 819 to 1638, four query
+  // tokens: 26 and 47; 64 of 1638 to 2048, bf16: 75 and 87.
   const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kCapacity - 1) / kCapacity);
   const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kCapacity;
   if (batch >= 2 && pairs * splits <= 4 * kCapacity && fixed > 1.2 * even + 32) {
@@ -756,6 +829,10 @@ static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedA
   if (!configured.done(dev)) {
     e = cudaFuncSetAttribute(paged_attn_kernel<D, kE4M3, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
+    // the split of the registers holds for this launch size only: a build that differs must not run
+    cudaFuncAttributes fa;
+    if ((e = cudaFuncGetAttributes(&fa, paged_attn_kernel<D, kE4M3, RT>)) != cudaSuccess) return e;
+    if (fa.numRegs != kLaunchRegs) return cudaErrorLaunchOutOfResources;
     configured.set(dev);
   }
   const long long blocks = p.balanced ? p.ctas : static_cast<long long>(p.c.batch) * p.row_tiles * p.c.n_kv_heads * p.splits;

@@ -477,6 +477,64 @@ def test_a_cache_on_another_device_is_refused():
                               None, None, None, None, None, workspace())
 
 
+# ---- waits that run out -----------------------------------------------------------------------------------------------------
+@pytest.fixture
+def short_waits():
+    """A poll limit of about 2 ms, and copies withheld as the test asks; the defaults afterwards."""
+    def withhold(n):
+        B.fastkv_debug_set("wait_limit_cycles", 4_000_000)
+        B.fastkv_debug_set("paged_skip_copy", n)
+
+    yield withhold
+    B.fastkv_debug_set("wait_limit_cycles", 0)
+    B.fastkv_debug_set("paged_skip_copy", 0)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,n", [([3000], 1), ([3000], 2), ([90], 1), ([20000, 40, 3000], 3), ([20000, 40, 3000], 1)])
+def test_an_attention_whose_data_never_comes_gives_up(fmt, lens, n, short_waits):
+    pools = Pools(fmt, lens, lens, 32, 2, 128, 5)
+    q = bf16_rows(np.random.default_rng(5), (len(lens), 1, 8, 128))
+    cache, query = pools.cache(), B.make_query(n_q_heads=8, max_len=max(lens), total_len=sum(lens))
+    ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
+    out, lse = torch.zeros((len(lens), 1, 8, 128), device="cuda"), torch.zeros((len(lens), 1, 8), device="cuda")
+    short_waits(n)
+    B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)
+    status, site = B.fastkv_device_status(ws)
+    if n == 1 or max(lens) > 10000:                        # a short sequence's split may have no n-th chunk to withhold
+        assert status == B.ERR_DEVICE_TIMEOUT
+    assert (site in (39, 43)) if status == B.ERR_DEVICE_TIMEOUT else (status, site) == (0, 0)
+    B.fastkv_debug_set("paged_skip_copy", 0)
+    ws.zero_()
+    B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)          # and the next call is right
+    assert B.fastkv_device_status(ws) == (0, 0)
+    check_attention(pools, lens, q.double().numpy(), out.cpu().double().numpy(), lse.cpu().double().numpy(), 128 ** -0.5)
+
+
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("n", [1, 2, 7])
+def test_an_append_whose_rows_never_come_gives_up(gather, n, short_waits):
+    rng = np.random.default_rng(6)
+    Hkv, d, new = 4, 128, 100
+    k = bf16_rows(rng, (new, Hkv, d)).cuda()
+    idx = torch.arange(new, dtype=torch.int32, device="cuda").expand(Hkv, new).contiguous() if gather else None
+    rows = B.make_new_rows(batch=1, total=new, n_kv_heads=Hkv, head_dim=d, total_src=new if gather else 0)
+    for withheld in (n, 0):
+        pools = Pools("e4m3", [0], [new], 64, Hkv, d, 7)
+        before = [t.cpu().clone() for t in (pools.k, pools.v, pools.ks, pools.vs)]
+        ws = workspace()
+        short_waits(withheld)
+        B.fastkv_paged_append(pools.cache(), rows, pools.dev_lens, None, k, k, None, None, idx, None, None, ws)
+        if withheld:
+            status, site = B.fastkv_device_status(ws)
+            # the heads are split over blocks, so that a block may have no n-th one
+            assert (status, site) in ((B.ERR_DEVICE_TIMEOUT, 42), (0, 0)) if n > 1 else (status, site) == (B.ERR_DEVICE_TIMEOUT, 42)
+        else:
+            assert B.fastkv_device_status(ws) == (0, 0)
+            x = k.cpu().double().numpy()
+            check_append(pools, before, [0], [new], [x], [x], False)
+
+
 # ---- together -----------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_decoding_behind_a_selection(fmt):
