@@ -274,6 +274,8 @@ int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* 
  *   out[b, i, h, :] = sum_t softmax_t(scale * <q[b, i, h], K[t, h / G]>) * V[t, h / G, :]
  * q: bf16, dense [batch, q_len, n_q_heads, head_dim], 16-byte aligned; out: fp32, the same shape; lse (optional): fp32
  * [batch, q_len, n_q_heads], natural log.  A query that sees no entry gives out 0 and lse -infinity.
+ * What a query token does not see never reaches it, NaN and infinities included; a NaN that it sees makes the outputs that
+ * depend on it NaN, an infinity makes them NaN or infinite.
  * max_len and total_len are what the HOST knows of lens (their maximum and sum, or bounds); they size the launch, and
  * results do not depend on them beyond rounding.  A length beyond the block table's room is cut to it, a page id outside the
  * pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.

@@ -59,8 +59,8 @@ struct PagedAttnParams {
   const uint16_t* q;          // [B][q_len][Hq][d]
   float* out;                 // [B][q_len][Hq][d]
   float* lse;                 // [B][q_len][Hq], may be null
-  float4* part_ml;            // [pieces][8]: (max, sum, reference of the outputs, -)
-  float* part_o;              // [pieces][8][d]
+  float4* part_ml;            // [pieces][tile_rows]: (max, sum, reference of the outputs, -)
+  float* part_o;              // [pieces][tile_rows][d]
   WorkspaceHeader* hdr;
 };
 
@@ -68,11 +68,11 @@ struct PagedAttnPlan {
   int row_tiles_of_8, row_tiles, splits, balanced, ctas;
 };
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len);
-// tmap_k: with p.joint both pools, (column, row of the page, page x head, pool); else the K pool alone and tmap_v the V pool
 size_t paged_attn_partials_offset(const PagedAttnPlan& plan, int batch, int n_kv_heads);
 size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int head_dim);
 // Entries of a page that one TMA box brings: a chunk's 32 of 8-bit pages when the page has them, else 16.
 inline int paged_box_rows(bool e4m3, int page_size) { return e4m3 && page_size >= 32 ? 32 : 16; }
+// tmap_k: with p.joint both pools, (column, row of the page, page x head, pool); else the K pool alone and tmap_v the V pool
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
                               int head_dim, bool e4m3, cudaStream_t stream, int* launches);
 

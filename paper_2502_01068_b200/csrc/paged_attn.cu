@@ -7,19 +7,26 @@
 // query rows that share it.  The products run as warp-level m16n8k16 tensor-core products, whose only job is to keep the
 // instruction count per entry low; a tcgen05 tile has 128 rows and these have 8 or 16.
 //
-// Split-KV: one CTA per (split of the entries, KV head, sequence, tile of query rows); inside it every warp owns a ring of
-// shared-memory stages (16 entries of K and of V each, filled by one lane with tiled TMA copies) and its own online softmax.
+// Split-KV: a CTA takes a split of the entries of one (sequence, KV head, tile of query rows), or an even share of all of them;
+// inside it four warps compute, each with a ring of shared-memory stages that a warp of its own fills with tiled TMA copies (32
+// entries of K and V a stage in 8 bits, 16 in bf16) and its own online softmax.
 //   S [rows x 16 entries] = Q K^T: A = the query rows, B = K rows as stored;
 //   O^T [d x rows] += V^T P^T:     A = V through the transposing matrix load, B = P in the layout S comes out in.
-// Pages hold 16 rows or more, so that a chunk of 16 entries never straddles two pages; each lane keeps the page and the scales
-// of one of the next 32 chunks, fetched a batch ahead, because the table -> scale chain would cost two trips to memory.
+// Pages hold 16 rows or more, so that a step of 16 entries never straddles two pages.
 //
-// 8-bit pages: a code is exact in fp16, so K and V are widened in registers and the products are fp16 x fp16 -> fp32.  The
-// queries (bf16) go into fp16 exactly after a power-of-two shift per row that brings the row's largest element to [2^14, 2^15).
-// K's scale multiplies the logits.  V's scale 2^v is an addend of the exponent: the outputs accumulate 2^(l + v - R) * code
-// against their own running reference R = max(l + v), the sum of exponentials 2^(l - M) against M = max(l) as usual, and
-// out = O / L * 2^(R - M): the weights of the second product stay in (0, 1] whatever the pages' scales are.
-// P goes in as two 16-bit terms (value and rounding remainder), so the result carries fp32-level error.
+// 8-bit pages: a code is exact in fp16, so K and V are widened in registers and the products are fp16 x fp16 -> fp32 (warp-level
+// products of 8-bit operands are no native instruction here: a step of theirs took 30 cycles against 8).  The queries (bf16) go
+// into fp16 after a power-of-two shift per row that brings the row's largest element to [2^14, 2^15): exact down to 2^-28 of it,
+// and what is smaller is off by at most 2^-39 of the largest.  K's scale multiplies the logits.  V's scale 2^v is an addend of
+// the exponent: the outputs accumulate 2^(l + v - R) * code against their own running reference R = max(l + v), the sum of
+// exponentials 2^(l - M) against M = max(l) as usual, and out = O / L * 2^(R - M): the weights of the second product stay in
+// (0, 1] whatever the pages' scales are.
+// P goes in as 16-bit terms (value and rounding remainders; two in fp16, three in bf16), so the result carries fp32-level error.
+//
+// Measured, in us (and the share of a plain copy's bandwidth over the bytes the entries take): one sequence of 131072 entries,
+// 8 bits, 49.4 (83 %); eight of 4K to 64K, 109 (89 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
+// tokens, 8 bits, 26.5 (49 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.4:
+// launch, table -> page -> copy, one pass, merge.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -80,6 +87,12 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
   uint32_t r;
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, b;\n\t}" : "=r"(r) : "r"(w));
   return r;
+}
+
+// All ones in the elements of a word that are NaN or infinite.
+template <bool kE4M3>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return kE4M3 ? __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) : __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u);
 }
 
 // A CTA is four warps that compute and four that bring the data, one for each of them; two CTAs per SM.  The chain from a chunk's
@@ -410,6 +423,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         for (int e = 0; e < 4; ++e) o[rt][mt][e] = 0.0f;
     }
 
+    bool spoilt = false;                          // elements of V were cleared because not every row sees them
+
     // One pass over the chunk in stage st.  kTail: some row does not see all of it (the sequence's end, and what follows a query's
     // own token).  Products that follow one another are independent (a dependent one waits 21 cycles, the tensor cores take one
     // every 8), and the matrix loads are asked for a phase ahead of their use: K's together, V's before the softmax step whose
@@ -418,9 +433,34 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       constexpr bool kTail = decltype(tail_)::value;
       const int key0 = (c0 + warp + i * kWarps) * kChunk;
       const uint32_t ks_addr = ring + st * Cfg::kStageBytes + k_off, vs_addr = ring + st * Cfg::kStageBytes + v_off;
+      // What a row does not see must not reach it: its logit is masked, but a zero weight does not silence a NaN or an infinity in
+      // V.  Between the query tokens' own entries, which only some rows see, such elements are cleared, and handed to the rows
+      // that do see them when the segment is through.
+      if (kTail && T > 1) {
+        const int own0 = max(0, len - (T - 1) - key0), own1 = min(kChunk, len - key0);
+        uint8_t* vs = ring_ptr + st * Cfg::kStageBytes + v_off;
+        constexpr int kPieces = Cfg::kBoxRow / 16;
+        const int n = max(own1 - own0, 0) * kPieces;
+        bool found = false;
+        for (int j = lane; j < Cfg::kBoxes * n; j += 32) {
+          const int x = j / n, rem = j - x * n, r = own0 + rem / kPieces;
+          uint4* const at = reinterpret_cast<uint4*>(vs + x * 2 * Cfg::kBoxBytes + r / kSub * sub_stride + r % kSub * Cfg::kBoxRow + rem % kPieces * 16);
+          uint4 w = *at;
+          const uint32_t bad = not_finite<kE4M3>(w.x) | not_finite<kE4M3>(w.y) | not_finite<kE4M3>(w.z) | not_finite<kE4M3>(w.w);
+          if (bad != 0) {
+            w.x &= ~not_finite<kE4M3>(w.x); w.y &= ~not_finite<kE4M3>(w.y); w.z &= ~not_finite<kE4M3>(w.z); w.w &= ~not_finite<kE4M3>(w.w);
+            *at = w;
+            found = true;
+          }
+        }
+        if (__any_sync(0xffffffffu, found)) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                 // before the stage's next copies
+          spoilt = true;
+        }
+        __syncwarp();
+      }
       if (kTail && len - key0 < kChunk) {
-        // what lies behind the sequence's end in the page is not its own: the logits are masked, but a zero weight does not
-        // silence a NaN in V, so those V rows are cleared
+        // what lies behind the sequence's end in the page is not its own
         const int rows = len - key0;
         uint8_t* vs = ring_ptr + st * Cfg::kStageBytes + v_off;
         constexpr int kPieces = Cfg::kBoxRow / 16;
@@ -612,6 +652,30 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if constexpr (!kE4M3) r_run[rt] = m_run[rt];
     }
     pdl_launch_dependents();
+    if (spoilt) {                                  // rare: the elements that were cleared, from the pool
+#pragma unroll 1
+      for (int key = max(len - (T - 1), 0); key < len; ++key) {
+        const int x = key / kChunk - c0 - warp;
+        if (x < 0 || x % kWarps != 0 || x / kWarps >= my_chunks) continue;     // another warp's chunk
+        long long blk = pool_block(p.c.block_table[static_cast<size_t>(b) * p.c.max_pages + (key >> p.c.page_log2)], p.c.n_pages, Hkv, g);
+        if (blk < 0) blk = g;                      // as the copies take it
+        const uint8_t* const row = p.c.v_pages + ((blk << p.c.page_log2) + (key & ((1 << p.c.page_log2) - 1))) * Cfg::kRowBytes;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            float v;
+            if constexpr (kE4M3) v = (row[m * 16 + 2 * quad + z] & 0x7f) == 0x7f ? NAN : 0.0f;
+            else v = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[m * 16 + quad + 8 * z]) << 16);
+            if (isfinite(v)) continue;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (key < len - (T - 1 - (row_base + rt * 8 + 2 * c + e) / G)) o[rt][m][2 * z + e] += v;
+          }
+      }
+    }
     // ---- the warps merge through shared memory: a thread per row weighs the warps, then the outputs join, columns by columns ----
     const int n_rows = min(kRows, p.rows - row_base);
     const bool whole = p.balanced ? c0 == 0 && c1 == n_chunks : p.splits == 1;
@@ -650,19 +714,19 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) {
             const float4 ml = mml[w * kRows + t];
-            if (ml.x != -INFINITY) L = fmaf(ml.y, ex2(ml.x - M), L);              // warps without entries weigh nothing
+            if (ml.y != 0.0f) L = fmaf(ml.y, ex2(ml.x - M), L);                   // warps without entries weigh nothing; NaN stays
           }
-          const float last = !whole ? 1.0f : L > 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
+          const float last = !whole ? 1.0f : L != 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) {
             const float4 ml = mml[w * kRows + t];
-            weight_of[w][t] = ml.x != -INFINITY ? ex2(ml.z - R) * last : 0.0f;
+            weight_of[w][t] = ml.y != 0.0f ? ex2(ml.z - R) * last : 0.0f;
           }
           if (whole) {
             const int r = row_base + t, i = r / G, h = g * G + r - i * G;
             const long long at = (static_cast<long long>(b) * T + i) * p.n_q_heads + h;
             at_of[t] = at;
-            if (p.lse != nullptr) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+            if (p.lse != nullptr) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
           } else {
             // where a piece waits for the merge: static launches by (pair, split), balanced ones by CTA (first segment or later)
             const long long at = (p.balanced ? 2 * static_cast<long long>(blockIdx.x) + (u != u_begin) : static_cast<long long>(blockIdx.x)) * kRows + t;
@@ -717,6 +781,8 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
     const int mine = chunks_of(p, b, kChunkLog2);
     const long long p0 = block_sum<D>(before, scratch) * HT + static_cast<long long>(ht) * mine, p1 = p0 + mine;
     if (mine == 0) {
+      // no CTA of the main kernel came by to report a length below zero
+      if (t == 0 && h == 0 && i == 0 && p.lens[b] < 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
       n = 0; first = rest = 0; step = 0;
     } else {
       const int ca = static_cast<int>(((p0 + 1) * p.ctas - 1) / total), cb = static_cast<int>((p1 * p.ctas - 1) / total);
@@ -757,9 +823,9 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
 #pragma unroll
   for (int w = 0; w < D / 32; ++w) { M = fmaxf(M, w_max[0][w]); R = fmaxf(R, w_max[1][w]); }
   for (int s = t; s < n; s += D) {
-    const float x = f_m[s];
-    f_o[s] = x == -INFINITY ? 0.0f : ex2(f_o[s] - R);          // pieces without entries weigh nothing
-    f_l[s] = x == -INFINITY ? 0.0f : f_l[s] * ex2(x - M);
+    const float l = f_l[s];                                    // 0: a piece without entries weighs nothing; NaN stays
+    f_o[s] = l == 0.0f ? 0.0f : ex2(f_o[s] - R);
+    f_l[s] = l == 0.0f ? 0.0f : l * ex2(f_m[s] - M);
   }
   __syncthreads();
   float L = 0.0f, acc = 0.0f;
@@ -770,8 +836,8 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
 #pragma unroll 8
   for (int s = kAhead; s < n; ++s) acc = fmaf(__ldcg(p.part_o + piece(s) * D + t), f_o[s], acc);
   const size_t at = (static_cast<size_t>(b) * p.q_len + i) * p.n_q_heads + h;
-  p.out[at * D + t] = L > 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
-  if (p.lse != nullptr && t == 0) p.lse[at] = L > 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  p.out[at * D + t] = L != 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
+  if (p.lse != nullptr && t == 0) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len) {

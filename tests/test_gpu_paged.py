@@ -341,6 +341,70 @@ def test_attention_of_several_query_tokens(fmt, T, Hq, Hkv, d):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_attention_masks_what_is_not_finite(fmt):
+    """A query token does not see the entries of the tokens behind it, whatever they hold: its outputs are those of a cache
+    without them.  Where it does see a NaN in V, that element is NaN; an infinity leaves it NaN or infinite; a NaN in K makes
+    the whole row NaN, and none of it spreads to the other sequences, heads or rows."""
+    T, Hq, Hkv, d, lens = 4, 8, 2, 128, [700, 66, 5]
+    pools = Pools(fmt, lens, lens, 32, Hkv, d, 3)
+    pools.k64, pools.v64 = [x.copy() for x in pools.k64], [x.copy() for x in pools.v64]
+    bad_code = {"nan": 0x7F, "inf": 0xFF}
+
+    def spoil(name, b, t, h, col, what):
+        pid, row = int(pools.table_np[b, t // 32]), t % 32
+        if fmt == "bf16":
+            getattr(pools, name)[pid, h, row, col] = float(what)
+        else:
+            getattr(pools, name)[pid, h, row, col] = bad_code[what]
+
+    spoil("v", 0, 699, 1, 77, "nan")             # the last token's own entry: seen by token 3 alone
+    spoil("v", 0, 697, 0, 5, "inf")              # by tokens 1, 2 and 3
+    spoil("v", 1, 65, 1, 0, "inf")
+    spoil("v", 1, 64, 1, 127, "nan")             # by tokens 2 and 3; 63 and 64 lie in different pages
+    spoil("k", 1, 65, 0, 9, "nan")
+    spoil("v", 2, 3, 0, 64, "nan")
+    spoil("k", 2, 2, 1, 3, "nan")                # by tokens 1, 2 and 3
+    q = bf16_rows(np.random.default_rng(8), (len(lens), T, Hq, d))
+    cache = pools.cache()
+    for longest, total in ((66, 0), (700, 0), (20000, 771)):           # whole, split, dealt out
+        query = B.make_query(n_q_heads=Hq, q_len=T, max_len=longest, total_len=total)
+        ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
+        out, lse = (torch.full(s, 7.0, device="cuda") for s in ((len(lens), T, Hq, d), (len(lens), T, Hq)))
+        B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)
+        assert B.fastkv_device_status(ws) == (0, 0)
+        out, lse = out.cpu().double().numpy(), lse.cpu().double().numpy()
+        wild = np.zeros(out.shape, dtype=bool)
+        lost = np.zeros(lse.shape, dtype=bool)
+        wild[0, 3, 4:, 77] = wild[0, 1:, :4, 5] = wild[1, 3, 4:, 0] = wild[1, 2:, 4:, 127] = wild[2, 2:, :4, 64] = True
+        lost[1, 3, :4] = lost[2, 1:, 4:] = True
+        assert np.array_equal(np.isnan(lse), lost)
+        assert np.array_equal(~np.isfinite(out), wild | lost[..., None])
+        for b, n in enumerate(lens):
+            for i in range(T):
+                want, want_lse, mass, size = attention(q[b, i].double().numpy(), pools.k64[b], pools.v64[b], n - (T - 1 - i), d ** -0.5)
+                good = ~(wild[b, i] | lost[b, i][:, None])
+                delta = (d / 16 + 8) * 2.0 ** -23 * size[:, None] + 2.0 ** -23 * np.abs(want_lse)[:, None]
+                tol = (2 * delta + 2.0 ** -20 + (n / 16 + 16) * 2.0 ** -23) * mass + 1e-30
+                assert np.all((np.abs(out[b, i] - want) <= tol)[good])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_a_length_below_zero_is_reported_however_the_batch_is_dealt(fmt):
+    lens = [20000, 40, 3000, 90]
+    pools = Pools(fmt, lens, lens, 32, 2, 64, 5)
+    q = bf16_rows(np.random.default_rng(5), (4, 1, 8, 64))
+    cache = pools.cache()
+    for total in (sum(lens), 4 * 20000):
+        query = B.make_query(n_q_heads=8, max_len=20000, total_len=total)
+        ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
+        out, lse = torch.full((4, 1, 8, 64), 7.0, device="cuda"), torch.full((4, 1, 8), 7.0, device="cuda")
+        pools.dev_lens[1] = -3
+        B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)
+        assert B.fastkv_device_status(ws) == (B.ERR_DEVICE_INDEX, 41)
+        check_attention(pools, [20000, 0, 3000, 90], q.double().numpy(), out.cpu().double().numpy(), lse.cpu().double().numpy(), 64 ** -0.5)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_attention_of_batches_larger_than_the_machine(fmt):
     rng = np.random.default_rng(2)
     lens = [int(x) for x in rng.integers(0, 300, 70)]
