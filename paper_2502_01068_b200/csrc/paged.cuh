@@ -42,7 +42,7 @@ struct AppendParams {
 bool paged_append_uses_maps(const AppendParams& p, bool e4m3);
 cudaError_t launch_paged_append(AppendParams& p, const CUtensorMap (&maps)[2], int head_dim, bool e4m3, cudaStream_t stream);
 
-constexpr int kPagedMaxPieces = 592;   // pieces of one (sequence, KV head): the CTAs that can share it
+constexpr int kPagedCtas = 2 * 148;      // attention CTAs that are resident at once: the most pieces of one (sequence, KV head)
 
 struct PagedAttnParams {
   PagedView c;

@@ -9,10 +9,14 @@
 // Eight lanes (four for head_dim 64) handle one row of one head: sixteen elements each, as two 16-byte pieces chosen so
 // that both halves of every rotated pair are the lane's own.
 //   Row role   (bf16 pages; queries of either format): a lane group takes one token and a run of heads, so that the
-//              angles are formed once per run.
-//   Page role  (8-bit pages, calls of more than 8 rows per sequence): a block takes one page and walks a run of heads; the
-//              page's rows of one head sit in registers while their largest absolute value is found.
-//   Small role (8-bit pages, up to 8 rows per sequence): a lane group takes one (page, head) and its few new rows.
+//              angles are formed once per run.  A prompt of 8192 tokens, 32 query and 8 KV heads of 128, bf16: 34.6 us, 89 % of a
+//              plain copy's rate over what it reads and writes.
+//   Page role  (8-bit pages, calls of more than 8 rows per sequence): a block takes one page and walks a run of heads, whose rows
+//              of the page wait in shared memory while their largest absolute value is found and are encoded from there.
+//              36 864 rows in eight ragged prompts, rotated, with their queries: 146 us, 87 %; 13107 kept rows of 8 heads,
+//              gathered row by row: 20.7 us, 60 % (a copy started for every 256 bytes).
+//   Small role (8-bit pages, up to 8 rows per sequence): a lane group takes one (page, head) and its few new rows; 64 sequences,
+//              one row each: 3.7 us, as good as launching and three dependent trips to memory.
 // Rows that were in a page before keep their codes unless the new rows need a larger scale; then the codes are re-encoded
 // by the ratio, a power of two, which is exact but for codes that become subnormal.
 #include "paged.cuh"
@@ -29,7 +33,7 @@ enum Mode { kPlain = 0, kRotated = 1, kGathered = 2 };
 // rounds and two blocks, 13107 rows of 8 heads).
 template <int kMode> constexpr int kRoundsAhead = kMode == kGathered ? 1 : 2;
 template <int kMode> constexpr int kSlotsOf = (kRoundsAhead<kMode> + 1) * kHeads;
-constexpr int kRowStages = 8;             // row role: heads whose rows are on their way or in use
+constexpr int kRowStages = 8;        // row role: heads whose rows are on their way or in use
 constexpr int kSmallRows = 8;        // rows per sequence up to which the small role is used
 
 struct Row16 {                       // a lane's sixteen elements of one row: the pieces at `lo` and `hi`
@@ -665,8 +669,8 @@ static cudaError_t launch_d(AppendParams& p, const CUtensorMap (&maps)[2], bool 
   const bool small = p.max_new <= kSmallRows;
   const int per_page = P * GL;                    // lanes that hold a page's rows of one head, one row per lane group
   const int threads = e4m3 && !small && per_page > 512 ? 512 : 256;
-  // Row role: a token's heads are split over as many lane groups as it takes to put two blocks on every SM (what their registers allow); a
-  // long call keeps them together, so that a token's angles are formed once.
+  // Row role: a token's heads are split over as many lane groups as it takes to put two blocks on every SM (what their registers
+  // allow); a long call keeps them together, so that a token's angles are formed once.
   p.row_heads = p.n_q_heads + (e4m3 ? 0 : jobs);
   const long long groups = static_cast<long long>(kSms) * 2 * (256 / GL);
   long long hpu = p.row_heads > 0 ? (static_cast<long long>(p.total) * p.row_heads + groups - 1) / groups : 1;

@@ -757,7 +757,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 template <int D, bool kE4M3>
 __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p) {
   constexpr int kChunkLog2 = kE4M3 ? 5 : 4;
-  __shared__ float f_o[kPagedMaxPieces], f_l[kPagedMaxPieces], f_m[kPagedMaxPieces];
+  __shared__ float f_o[kPagedCtas], f_l[kPagedCtas], f_m[kPagedCtas];
   __shared__ float w_max[2][D / 32];
   __shared__ long long scratch[D / 32];
   pdl_wait();
@@ -841,7 +841,6 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
 }
 
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len) {
-  constexpr int kCapacity = 2 * 148;              // CTAs that are resident at once
   PagedAttnPlan pl;
   pl.row_tiles_of_8 = rows <= 8 ? 1 : 2;
   pl.row_tiles = (rows + 8 * pl.row_tiles_of_8 - 1) / (8 * pl.row_tiles_of_8);
@@ -851,10 +850,10 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge kernel costs 4 to 5 us,
   // a warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (700 entries in 8 bits: 8.3 us whole, 7.1 in nine splits;
   // 257: 5.3 whole, 6.3 in three).
-  long long splits = kCapacity / pairs;
+  long long splits = kPagedCtas / pairs;
   const long long useful = chunks <= (e4m3 ? 16 : 24) ? 1 : (chunks + kWarps - 1) / kWarps;
   if (splits > useful) splits = useful;
-  if (splits > kPagedMaxPieces) splits = kPagedMaxPieces;
+  if (splits > kPagedCtas) splits = kPagedCtas;
   if (splits < 1) splits = 1;
   pl.splits = static_cast<int>(splits);
   pl.balanced = 0;
@@ -862,11 +861,11 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays about eight chunks' time for every segment it
   // starts.  Eight sequences of 4K to 64K entries, 8 bits: 235 us static, 109 us balanced; 32 of 819 to 1638, four query
   // tokens: 26 and 47; 64 of 1638 to 2048, bf16: 75 and 87.
-  const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kCapacity - 1) / kCapacity);
-  const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kCapacity;
-  if (batch >= 2 && pairs * splits <= 4 * kCapacity && fixed > 1.2 * even + 32) {
+  const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kPagedCtas - 1) / kPagedCtas);
+  const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kPagedCtas;
+  if (batch >= 2 && pairs * splits <= 4 * kPagedCtas && fixed > 1.2 * even + 32) {
     pl.balanced = 1;
-    pl.ctas = kCapacity;
+    pl.ctas = kPagedCtas;
     pl.splits = 1;
   }
   return pl;

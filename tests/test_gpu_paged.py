@@ -666,6 +666,72 @@ def test_decoding_behind_a_selection(fmt):
         pos.add_(1)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_sequences_may_share_pages_for_reading(fmt):
+    """Three sequences whose first pages are the same ones, each with pages of its own behind them."""
+    P, Hkv, d, lens = 32, 2, 128, [200, 170, 96]
+    pools = Pools(fmt, lens, lens, P, Hkv, d, 3)
+    for b in (1, 2):
+        pools.table_np[b, :3] = pools.table_np[0, :3]
+        for x in (pools.k64, pools.v64):
+            x[b][:96] = x[0][:96]
+    pools.table = torch.from_numpy(pools.table_np).cuda()
+    q = bf16_rows(np.random.default_rng(8), (3, 2, 8, d))
+    cache, query = pools.cache(), B.make_query(n_q_heads=8, q_len=2, max_len=200)
+    ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
+    out, lse = torch.zeros((3, 2, 8, d), device="cuda"), torch.zeros((3, 2, 8), device="cuda")
+    B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    check_attention(pools, lens, q.double().numpy(), out.cpu().double().numpy(), lse.cpu().double().numpy(), d ** -0.5)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [5, 70])
+def test_a_kept_row_may_be_named_twice(fmt, n):
+    rng = np.random.default_rng(n)
+    Hkv, d, src = 2, 64, 40
+    k, v = (bf16_rows(rng, (src, Hkv, d)).cuda() for _ in range(2))
+    idx = torch.from_numpy(rng.integers(0, src, (Hkv, n)).astype(np.int32)).cuda()
+    idx[:, 1] = idx[:, 0]
+    pools = Pools(fmt, [3], [3 + n], 16, Hkv, d, 2)
+    before = [None if t is None else t.cpu().clone() for t in (pools.k, pools.v, pools.ks, pools.vs)]
+    ws = workspace()
+    B.fastkv_paged_append(pools.cache(), B.make_new_rows(batch=1, total=n, n_kv_heads=Hkv, head_dim=d, total_src=src), pools.dev_lens,
+                          None, k, v, None, None, idx, None, None, ws)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    at = idx.cpu().numpy().T
+    take = lambda x: x.cpu().double().numpy()[at, np.arange(Hkv)[None]]  # noqa: E731
+    check_append(pools, before, [3], [n], [take(k)], [take(v)], False)
+
+
+def test_two_graphs_may_share_a_workspace():
+    """Graphs of two attention calls of different shapes over one workspace, replayed by turns: each gives what it gave alone."""
+    made, need = [], 0
+    for lens, Hq, seed in (([5000], 8, 1), ([20000, 40, 3000, 90], 16, 2)):
+        pools = Pools("e4m3", lens, lens, 32, 2, 128, seed)
+        q = bf16_rows(np.random.default_rng(seed), (len(lens), 1, Hq, 128)).cuda()
+        cache, query = pools.cache(), B.make_query(n_q_heads=Hq, max_len=max(lens), total_len=sum(lens))
+        need = max(need, B.fastkv_paged_attn_workspace_bytes(cache, query))
+        made.append((pools, q, cache, query, torch.zeros((len(lens), 1, Hq, 128), device="cuda")))
+    ws = workspace(need)
+    alone, graphs = [], []
+    for pools, q, cache, query, out in made:
+        B.fastkv_paged_attn(cache, query, pools.dev_lens, q, out, None, ws)
+        alone.append(out.cpu())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.fastkv_paged_attn(cache, query, pools.dev_lens, q, out, None, ws)
+        graphs.append(graph)
+    for _ in range(10):
+        for (_, _, _, _, out), graph in zip(made, graphs):
+            out.zero_()
+            graph.replay()
+    torch.cuda.synchronize()
+    assert B.fastkv_device_status(ws) == (0, 0)
+    for (_, _, _, _, out), ref in zip(made, alone):
+        assert torch.equal(out.cpu(), ref)
+
+
 def test_calls_on_two_streams_do_not_meet():
     """Two caches with their own workspaces, their calls interleaved on two streams: the same results as one after the other."""
     made = []
