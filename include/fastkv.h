@@ -367,9 +367,9 @@ int fastkv_score_static_status(void* stream, int32_t* status, int32_t* site);
  *                         n - 1 is ready (first query tile of every CTA); with a short wait limit the
  *                         softmax warps' bounded wait runs out without any fault (timeout test); 0: off
  *   "paged_skip_copy"     n > 0: the paged attention withholds the copies of the first pair of warps' n-th chunk of every
- *                         segment, the paged append (8-bit pages, more than 8 rows per sequence) those of every block's
- *                         n-th head; with a short wait limit the wait for them runs out without any fault (timeout
- *                         test); 0: off
+ *                         segment, the paged append (new tokens into 8-bit pages, more than 8 rows per sequence) those of
+ *                         every block's n-th head; with a short wait limit the wait for them runs out without any fault
+ *                         (timeout test); 0: off
  *   "paged_two_maps"      1: the paged attention copies K and V pages through a tensor map each, as it does for pools
  *                         that lie 2^40 bytes or more apart (test); 0: through one map where it can
  *   "time_kernels"        1: record a pair of CUDA events around every kernel the library launches
