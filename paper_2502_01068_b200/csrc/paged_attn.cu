@@ -147,6 +147,10 @@ __device__ __forceinline__ int chunks_of(const PagedAttnParams& p, int b, int ch
   return (usable_len(p.lens[b], p.c.max_pages, p.c.page_log2) + (1 << chunk_log2) - 1) >> chunk_log2;
 }
 
+// CTAs that get a share: no more than there are units, so that every CTA between a pair's first and last holds a piece of it.
+__device__ __forceinline__ int sharing_ctas(const PagedAttnParams& p, long long total) {
+  return static_cast<int>(min(static_cast<long long>(p.ctas), total));
+}
 // First unit of CTA c when `total` units are dealt evenly to n CTAs.
 __device__ __forceinline__ long long share_begin(long long total, int c, int n) { return total * c / n; }
 
@@ -208,8 +212,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     }
     before -= mine;
     for (int w = 0; w < warp; ++w) before += scratch[w];
-    u_begin = u = share_begin(total, blockIdx.x, gridDim.x);
-    u_end = share_begin(total, blockIdx.x + 1, gridDim.x);
+    const int ctas = sharing_ctas(p, total);
+    if (static_cast<int>(blockIdx.x) < ctas) {
+      u_begin = u = share_begin(total, blockIdx.x, ctas);
+      u_end = share_begin(total, blockIdx.x + 1, ctas);
+    }
     if (u < u_end && before * HT <= u && u < (before + mine) * HT) {
       long long base = before;
       for (int x = b0; x < b1; ++x) {
@@ -768,7 +775,7 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
   const int h = blockIdx.x - bi * p.n_q_heads, b = bi / p.q_len, i = bi - b * p.q_len, g = h / G;
   const int row = i * G + h - g * G, tile = row / kRows, r = row - tile * kRows, HT = p.c.n_kv_heads * p.row_tiles;
   const int ht = tile * p.c.n_kv_heads + g;
-  size_t first, rest;                             // the piece that comes first, and the one behind it; then they are `step` apart
+  long long first, rest;                          // piece 0 is at `first`, piece s > 0 at rest + s * step
   int n, step;
   if (p.balanced) {
     long long before = 0, all = 0;
@@ -778,35 +785,38 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
       if (x < b) before += k;
     }
     const long long total = block_sum<D>(all, scratch) * HT;
-    const int mine = chunks_of(p, b, kChunkLog2);
+    const int mine = chunks_of(p, b, kChunkLog2), ctas = sharing_ctas(p, total);
     const long long p0 = block_sum<D>(before, scratch) * HT + static_cast<long long>(ht) * mine, p1 = p0 + mine;
+    first = rest = 0;
+    n = step = 0;
     if (mine == 0) {
       // no CTA of the main kernel came by to report a length below zero
       if (t == 0 && h == 0 && i == 0 && p.lens[b] < 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
-      n = 0; first = rest = 0; step = 0;
     } else {
-      const int ca = static_cast<int>(((p0 + 1) * p.ctas - 1) / total), cb = static_cast<int>((p1 * p.ctas - 1) / total);
+      const int ca = static_cast<int>(((p0 + 1) * ctas - 1) / total), cb = static_cast<int>((p1 * ctas - 1) / total);
       if (ca == cb) return;                       // one CTA had all of it and wrote the result
       n = cb - ca + 1;
-      first = 2 * static_cast<size_t>(ca) + (share_begin(total, ca, p.ctas) != p0);
-      rest = 2 * static_cast<size_t>(ca + 1);
       step = 2;
+      rest = 2 * static_cast<long long>(ca);
+      first = rest + (share_begin(total, ca, ctas) != p0);
     }
   } else {
     n = p.splits;
     step = p.row_tiles;
-    first = (static_cast<size_t>(b) * p.c.n_kv_heads + g) * n * step + tile;
-    rest = first + step;
+    first = rest = (static_cast<long long>(b) * p.c.n_kv_heads + g) * n * step + tile;
   }
-  auto piece = [&](int s) -> size_t { return (s == 0 ? first : rest + static_cast<size_t>(s - 1) * step) * kRows + r; };
+  const float* const outputs = p.part_o + (rest * kRows + r) * D + t;
+  const float4* const sums = p.part_ml + rest * kRows + r;
+  const size_t apart = static_cast<size_t>(step) * kRows;
+  const long long extra = (first - rest) * kRows;
   // the first pieces' outputs are under way before their weights are known
-  constexpr int kAhead = 24;
+  constexpr int kAhead = 12;
   float o[kAhead];
 #pragma unroll
-  for (int s = 0; s < kAhead; ++s) o[s] = s < n ? __ldcg(p.part_o + piece(s) * D + t) : 0.0f;
+  for (int s = 0; s < kAhead; ++s) o[s] = s < n ? __ldcg(outputs + (s == 0 ? extra : s * apart) * D) : 0.0f;
   float M = -INFINITY, R = -INFINITY;
   for (int s = t; s < n; s += D) {
-    const float4 ml = __ldcg(p.part_ml + piece(s));
+    const float4 ml = __ldcg(sums + (s == 0 ? extra : s * apart));
     f_l[s] = ml.y;
     f_m[s] = ml.x;
     f_o[s] = ml.z;
@@ -834,7 +844,7 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
   for (int s = 0; s < kAhead; ++s)
     if (s < n) acc = fmaf(o[s], f_o[s], acc);
 #pragma unroll 8
-  for (int s = kAhead; s < n; ++s) acc = fmaf(__ldcg(p.part_o + piece(s) * D + t), f_o[s], acc);
+  for (int s = kAhead; s < n; ++s) acc = fmaf(__ldcg(outputs + s * apart * D), f_o[s], acc);
   const size_t at = (static_cast<size_t>(b) * p.q_len + i) * p.n_q_heads + h;
   p.out[at * D + t] = L != 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
   if (p.lse != nullptr && t == 0) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;

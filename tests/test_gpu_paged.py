@@ -28,7 +28,10 @@ def bf16_rows(rng, shape, gain=1.0):
 
 
 def workspace(nbytes=256):
-    return torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+    """A header of zeros, and behind it what no call may read before it has written it: NaN in every word."""
+    ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+    ws[:256] = 0
+    return ws
 
 
 def inv_freq(rot, base=500000.0):
@@ -439,6 +442,14 @@ def test_what_the_host_knows_of_lengths_changes_nothing(fmt):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[0, 0, 0], [40, 0, 1], [70, 333, 64, 1], [130] * 20])
+@pytest.mark.parametrize("T", [1, 5])
+def test_batches_far_shorter_than_the_host_thinks(fmt, lens, T):
+    """Dealt out evenly, there are fewer chunks than CTAs: some of them get none, and whoever joins the pieces must know it."""
+    run_attention(fmt, lens, 16, 8, 2, 64, T=T, seed=9, max_len=40000, total_len=50000)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("d,page", [(128, 16), (128, 64), (64, 16), (64, 128)])
 def test_attention_with_the_pools_in_either_order_or_far_apart(fmt, d, page):
     """K and V boxes arrive by one copy where the pools allow it: K below V, V below K, and (forced) a copy each."""
@@ -569,7 +580,7 @@ def test_an_attention_whose_data_never_comes_gives_up(fmt, lens, n, short_waits)
         assert status == B.ERR_DEVICE_TIMEOUT
     assert (site in (39, 43)) if status == B.ERR_DEVICE_TIMEOUT else (status, site) == (0, 0)
     B.fastkv_debug_set("paged_skip_copy", 0)
-    ws.zero_()
+    ws[:256] = 0
     B.fastkv_paged_attn(cache, query, pools.dev_lens, q.cuda(), out, lse, ws)          # and the next call is right
     assert B.fastkv_device_status(ws) == (0, 0)
     check_attention(pools, lens, q.double().numpy(), out.cpu().double().numpy(), lse.cpu().double().numpy(), 128 ** -0.5)
