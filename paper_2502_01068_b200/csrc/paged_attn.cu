@@ -24,8 +24,8 @@
 // P goes in as 16-bit terms (value and rounding remainders; two in fp16, three in bf16), so the result carries fp32-level error.
 //
 // Measured, in us (and the share of a plain copy's bandwidth over the bytes the entries take): one sequence of 131072 entries,
-// 8 bits, 49.4 (83 %); eight of 4K to 64K, 109 (89 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
-// tokens, 8 bits, 26.5 (49 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.4:
+// 8 bits, 47 (87 %); eight of 4K to 64K, 105 (92 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
+// tokens, 8 bits, 27 (48 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.4:
 // launch, table -> page -> copy, one pass, merge.
 #include <type_traits>
 
@@ -760,16 +760,17 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   } while (advance());
 }
 
-// Merges the pieces of one query row: one block of D threads each.
+// Merges the pieces of one query row, a block each: the warps share the pieces out, every one of them weighs all pieces for itself,
+// and their sums meet once.  All of it is latency (an empty kernel here costs 1 us, this one 2.3 for 37 pieces a row): the outputs are
+// asked for before their weights are known, what can be is worked out before the wait for the main kernel, and there is little
+// code, because instructions that run once come from memory, too (loops unrolled for 24 loads in flight: 4 us).
+constexpr int kMergeWarps = 8;
 template <int D, bool kE4M3>
-__global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p) {
-  constexpr int kChunkLog2 = kE4M3 ? 5 : 4;
-  __shared__ float f_o[kPagedCtas], f_l[kPagedCtas], f_m[kPagedCtas];
-  __shared__ float w_max[2][D / 32];
-  __shared__ long long scratch[D / 32];
-  pdl_wait();
+__global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const PagedAttnParams p) {
+  constexpr int kChunkLog2 = kE4M3 ? 5 : 4, V = D / 32, kAhead = 8;
+  __shared__ float acc[kMergeWarps][D];
   pdl_launch_dependents();
-  const int t = threadIdx.x, G = p.group, kRows = p.tile_rows;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, warps = blockDim.x >> 5, G = p.group, kRows = p.tile_rows;
   // block -> (query token of the batch, head)
   const unsigned bi = blockIdx.x / p.n_q_heads;
   const int h = blockIdx.x - bi * p.n_q_heads, b = bi / p.q_len, i = bi - b * p.q_len, g = h / G;
@@ -778,15 +779,20 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
   long long first, rest;                          // piece 0 is at `first`, piece s > 0 at rest + s * step
   int n, step;
   if (p.balanced) {
-    long long before = 0, all = 0;
-    for (int x = t; x < p.c.batch; x += D) {
+    long long before = 0, total = 0;              // every warp for itself
+    for (int x = lane; x < p.c.batch; x += 32) {
       const int k = chunks_of(p, x, kChunkLog2);
-      all += k;
+      total += k;
       if (x < b) before += k;
     }
-    const long long total = block_sum<D>(all, scratch) * HT;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+      total += __shfl_xor_sync(0xffffffffu, total, o);
+      before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    total *= HT;
     const int mine = chunks_of(p, b, kChunkLog2), ctas = sharing_ctas(p, total);
-    const long long p0 = block_sum<D>(before, scratch) * HT + static_cast<long long>(ht) * mine, p1 = p0 + mine;
+    const long long p0 = before * HT + static_cast<long long>(ht) * mine, p1 = p0 + mine;
     first = rest = 0;
     n = step = 0;
     if (mine == 0) {
@@ -805,48 +811,80 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p)
     step = p.row_tiles;
     first = rest = (static_cast<long long>(b) * p.c.n_kv_heads + g) * n * step + tile;
   }
-  const float* const outputs = p.part_o + (rest * kRows + r) * D + t;
+  const float* const outputs = p.part_o + (rest * kRows + r) * D + lane * V;
   const float4* const sums = p.part_ml + rest * kRows + r;
   const size_t apart = static_cast<size_t>(step) * kRows;
   const long long extra = (first - rest) * kRows;
-  // the first pieces' outputs are under way before their weights are known
-  constexpr int kAhead = 12;
-  float o[kAhead];
+  struct Part { float x[V]; };
+  auto load = [&](int s) -> Part {
+    const float* const at = outputs + (s == 0 ? extra : s * apart) * D;
+    Part y;
+    if constexpr (V == 4) {
+      const float4 w = __ldcg(reinterpret_cast<const float4*>(at));
+      y.x[0] = w.x; y.x[1] = w.y; y.x[2] = w.z; y.x[3] = w.w;
+    } else {
+      const float2 w = __ldcg(reinterpret_cast<const float2*>(at));
+      y.x[0] = w.x; y.x[1] = w.y;
+    }
+    return y;
+  };
+  auto sums_of = [&](int s) -> float4 { return __ldcg(sums + (s == 0 ? extra : s * apart)); };
+  const float4 none = make_float4(-INFINITY, 0.0f, -INFINITY, 0.0f);
+  pdl_wait();                                     // the lengths were there before any block of the main kernel let this one start
+  const float4 ml0 = lane < n ? sums_of(lane) : none, ml1 = 32 + lane < n ? sums_of(32 + lane) : none;
+  Part ahead[kAhead];
 #pragma unroll
-  for (int s = 0; s < kAhead; ++s) o[s] = s < n ? __ldcg(outputs + (s == 0 ? extra : s * apart) * D) : 0.0f;
-  float M = -INFINITY, R = -INFINITY;
-  for (int s = t; s < n; s += D) {
-    const float4 ml = __ldcg(sums + (s == 0 ? extra : s * apart));
-    f_l[s] = ml.y;
-    f_m[s] = ml.x;
-    f_o[s] = ml.z;
+  for (int k = 0; k < kAhead; ++k)
+    if (warp + k * warps < n) ahead[k] = load(warp + k * warps);
+  float M = fmaxf(ml0.x, ml1.x), R = fmaxf(ml0.z, ml1.z), L = 0.0f;
+  for (int s = 64 + lane; s < n; s += 32) {
+    const float4 ml = sums_of(s);
     M = fmaxf(M, ml.x);
     R = fmaxf(R, ml.z);
   }
 #pragma unroll
-  for (int o_ = 16; o_ >= 1; o_ >>= 1) {
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o_));
-    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, o_));
+  for (int o = 16; o >= 1; o >>= 1) {
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, o));
   }
-  if ((t & 31) == 0) { w_max[0][t >> 5] = M; w_max[1][t >> 5] = R; }
-  __syncthreads();
+  // pieces without entries weigh nothing; NaN stays
+  auto exp_sum = [&](const float4& ml) -> float { return ml.y == 0.0f ? 0.0f : ml.y * ex2(ml.x - M); };
+  auto weight = [&](const float4& ml) -> float { return ml.y == 0.0f ? 0.0f : ex2(ml.z - R); };
+  L = exp_sum(ml0) + exp_sum(ml1);
+  for (int s = 64 + lane; s < n; s += 32) L += exp_sum(sums_of(s));
 #pragma unroll
-  for (int w = 0; w < D / 32; ++w) { M = fmaxf(M, w_max[0][w]); R = fmaxf(R, w_max[1][w]); }
-  for (int s = t; s < n; s += D) {
-    const float l = f_l[s];                                    // 0: a piece without entries weighs nothing; NaN stays
-    f_o[s] = l == 0.0f ? 0.0f : ex2(f_o[s] - R);
-    f_l[s] = l == 0.0f ? 0.0f : l * ex2(f_m[s] - M);
+  for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  const float w0 = weight(ml0), w1 = weight(ml1);
+  float sum[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int s = warp + k * warps;
+    if (s < n) {                                  // at most 64 pieces this way, kAhead * kMergeWarps
+      const float f = __shfl_sync(0xffffffffu, s < 32 ? w0 : w1, s & 31);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[e] = fmaf(ahead[k].x[e], f, sum[e]);
+    }
   }
-  __syncthreads();
-  float L = 0.0f, acc = 0.0f;
-  for (int s = 0; s < n; ++s) L += f_l[s];
+#pragma unroll 2
+  for (int s = warp + kAhead * warps; s < n; s += warps) {
+    const Part y = load(s);
+    const float f = weight(sums_of(s));
 #pragma unroll
-  for (int s = 0; s < kAhead; ++s)
-    if (s < n) acc = fmaf(o[s], f_o[s], acc);
-#pragma unroll 8
-  for (int s = kAhead; s < n; ++s) acc = fmaf(__ldcg(outputs + s * apart * D), f_o[s], acc);
+    for (int e = 0; e < V; ++e) sum[e] = fmaf(y.x[e], f, sum[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) acc[warp][lane * V + e] = sum[e];
+  __syncthreads();
   const size_t at = (static_cast<size_t>(b) * p.q_len + i) * p.n_q_heads + h;
-  p.out[at * D + t] = L != 0.0f ? acc / L * ex2(R - M - (kE4M3 ? kShift : 0.0f)) : 0.0f;
+  const float scale = L != 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
+  for (int x = t; x < D; x += blockDim.x) {
+    float o = 0.0f;
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) o += acc[w][x];
+    p.out[at * D + x] = o * scale;
+  }
   if (p.lse != nullptr && t == 0) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
@@ -857,23 +895,24 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   const int chunk = e4m3 ? 2 * kSub : kSub;
   const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
   const long long chunks = (max_len + chunk - 1) / chunk;
-  // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge kernel costs 4 to 5 us,
-  // a warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (700 entries in 8 bits: 8.3 us whole, 7.1 in nine splits;
-  // 257: 5.3 whole, 6.3 in three).
+  // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge costs 2 to 3 us, a
+  // warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (one sequence, 8 bits: 400 entries 7.2 us whole and 6.7 in
+  // four splits, 320 entries 5.8 and 6.2; bf16: 400 entries 6.8 and 5.7, four sequences of 257 6.8 and 7.1).
   long long splits = kPagedCtas / pairs;
-  const long long useful = chunks <= (e4m3 ? 16 : 24) ? 1 : (chunks + kWarps - 1) / kWarps;
+  const long long useful = chunks <= (e4m3 ? 12 : 18) ? 1 : (chunks + kWarps - 1) / kWarps;
   if (splits > useful) splits = useful;
   if (splits > kPagedCtas) splits = kPagedCtas;
   if (splits < 1) splits = 1;
   pl.splits = static_cast<int>(splits);
   pl.balanced = 0;
   pl.ctas = 0;
-  // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays about eight chunks' time for every segment it
-  // starts.  Eight sequences of 4K to 64K entries, 8 bits: 235 us static, 109 us balanced; 32 of 819 to 1638, four query
-  // tokens: 26 and 47; 64 of 1638 to 2048, bf16: 75 and 87.
+  // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays six to eight chunks' time for every segment it
+  // starts, and its merge has every row to look at.  Static and balanced, in us: eight sequences of 4K to 64K entries, 8 bits, 235
+  // and 105; four of 500 to 20000 29.5 and 27.8; 16 of 200 to 4000 26.2 and 27.0; 64 of 2K to 8K 128 and 110; 32 of 819 to 1638,
+  // four query tokens, 27 and 44; 64 of 1638 to 2048, bf16, 75 and 83; 24 of 100 to 4000 47 and 42.
   const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kPagedCtas - 1) / kPagedCtas);
   const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kPagedCtas;
-  if (batch >= 2 && pairs * splits <= 4 * kPagedCtas && fixed > 1.2 * even + 32) {
+  if (batch >= 2 && pairs * splits <= 4 * kPagedCtas && fixed > 1.2 * even + 24) {
     pl.balanced = 1;
     pl.ctas = kPagedCtas;
     pl.splits = 1;
@@ -927,7 +966,10 @@ static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedA
   *launches = 1;
   if (!p.balanced && p.splits == 1) return cudaSuccess;
   cfg.gridDim = dim3(static_cast<unsigned>(p.c.batch) * p.q_len * p.n_q_heads);
-  cfg.blockDim = dim3(D);
+  // warps of a row's block: no more than it has pieces, of balanced launches twice what it has on the average
+  const long long pairs = static_cast<long long>(p.c.batch) * p.c.n_kv_heads * p.row_tiles;
+  const long long pieces = p.balanced ? 1 + 2 * static_cast<long long>(p.ctas) / pairs : p.splits;
+  cfg.blockDim = dim3(32 * static_cast<unsigned>(pieces < kMergeWarps ? pieces : kMergeWarps));
   cfg.dynamicSmemBytes = 0;
   e = cudaLaunchKernelEx(&cfg, paged_merge_kernel<D, kE4M3>, static_cast<const PagedAttnParams&>(p));
   if (e == cudaSuccess) *launches = 2;
