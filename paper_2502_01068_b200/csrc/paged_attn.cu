@@ -187,17 +187,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     s_first = -1;
   }
   if (lane == 0 && warp < kWarps) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&full[warp][i], 1); mbar_init(&empty[warp][i], 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&full[warp][i], kE4M3 ? 2 : 1); mbar_init(&empty[warp][i], 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  __syncthreads();
-  pdl_wait();
-
   // ---- this CTA's share: units [u, u_end) of a row of (sequence, row tile x KV head, chunk) ----
   const int HT = Hkv * p.row_tiles;
-  int b, ht, c0, c1, n_chunks;
+  int b = 0, ht = 0, split = 0, c0, c1, n_chunks;
   long long u = 0, u_end = 0, u_begin = 0;
+  if (!p.balanced) {
+    unsigned rest = blockIdx.x;                   // row tiles fastest: they read the same entries
+    const int tile = rest % p.row_tiles; rest /= p.row_tiles;
+    split = rest % p.splits; rest /= p.splits;
+    ht = tile * Hkv + rest % Hkv;
+    b = rest / Hkv;
+  }
+  __syncthreads();
+  pdl_wait();
   if (p.balanced) {
     const int per = (p.c.batch + kThreads - 1) / kThreads, b0 = min(t * per, p.c.batch), b1 = min(b0 + per, p.c.batch);
     long long mine = 0;
@@ -233,11 +239,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     c0 = static_cast<int>((u - s_base) - static_cast<long long>(ht) * n_chunks);
     c1 = static_cast<int>(min(static_cast<long long>(n_chunks), c0 + (u_end - u)));
   } else {
-    unsigned rest = blockIdx.x;                   // row tiles fastest: they read the same entries
-    const int tile = rest % p.row_tiles; rest /= p.row_tiles;
-    const int split = rest % p.splits; rest /= p.splits;
-    ht = tile * Hkv + rest % Hkv;
-    b = rest / Hkv;
     n_chunks = chunks_of(p, b, kChunkLog2);
     const int per = (n_chunks + p.splits - 1) / p.splits;
     c0 = min(split * per, n_chunks);
@@ -308,12 +309,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         } else {
           ++issued;
         }
-        const int here = lane - (i * NSUB & 31);           // this lane's step of the chunk, if it has one
-        if (kE4M3 && here >= 0 && here < NSUB) scale_of[pair][stage][here] = sc_cur;
         int blk[NSUB];
 #pragma unroll
         for (int y = 0; y < NSUB; ++y) blk[y] = max(__shfl_sync(0xffffffffu, blk_cur, (i * NSUB + y) & 31), 0);
-        __syncwarp();                                      // the scales are there before the barrier says so
         const bool withheld = pair == 0 && i == p.skip_copy;     // test hook
         if (lane == 0 && !withheld) {
           // One copy brings a box of K and the same box of V (the pools are two planes of one tensor map); where the pools lie
@@ -336,6 +334,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
               }
             }
           }
+        }
+        if constexpr (kE4M3) {
+          // The scales follow: the first ones are a trip to memory behind the table, which the copies need not wait for.
+          const int here = lane - (i * NSUB & 31);         // this lane's step of the chunk, if it has one
+          if (here >= 0 && here < NSUB) scale_of[pair][stage][here] = sc_cur;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[pair][stage]);
         }
         __syncwarp();
         step();
