@@ -239,6 +239,7 @@ __device__ void append_rows(const AppendParams& p, int block) {
   const int h0 = slice * p.heads_per_unit, h1 = min(h0 + p.heads_per_unit, p.row_heads);
   const int Hq = p.n_q_heads, Hkv = p.c.n_kv_heads;
   const Pieces turned = pieces_of(j, D, kRot ? p.rot_dim : 0, p.adjacent), plain = pieces_of(j, D, 0, 0);
+  pdl_wait();
   int b = 0, slot = -1;
   long long page = -1;                            // of bf16 pages: where row t goes; -1: nowhere
   if (!kE4M3 && h1 > Hq) {
@@ -327,6 +328,7 @@ __device__ void append_small(const AppendParams& p, int block) {
   const int g = is_v ? job - Hkv : job;
   const Pieces at = is_v ? pieces_of(j, D, 0, 0) : pieces_of(j, D, p.rot_dim, p.adjacent);
   const int P = 1 << p.c.page_log2;
+  pdl_wait();
   int len = 0, lo = 0, hi = 0, row0 = 0;           // slots [lo, hi) of the sequence are this unit's new rows
   long long block_row = -1;
   int pg = 0;
@@ -432,6 +434,7 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
   const int n_rows = groups * NS;                 // rows of a slot
   const int item = block / p.job_slices, slice = block - item * p.job_slices;
   const int b = item / p.pages_per_seq, which = item - b * p.pages_per_seq;
+  pdl_wait();
   const int len = p.lens[b];
   RowRange r;
   new_rows_of(p.cu_new, p.uniform, p.total, p.max_new, b, len, p.c.max_pages, p.c.page_log2, &r);
@@ -640,9 +643,9 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
 template <int D, int kKind, int kMode>
 __global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0)
 paged_append_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AppendParams p) {
-  pdl_wait();
-  pdl_launch_dependents();
+  pdl_launch_dependents();                        // every role waits for earlier kernels once it knows what it is to do
   if (blockIdx.x == 0) {
+    pdl_wait();
     for (int b = threadIdx.x; b < p.c.batch; b += blockDim.x) {
       RowRange r;
       const int len = p.lens[b];
