@@ -68,6 +68,7 @@ class PagedCache(ctypes.Structure):
                 ("format", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
                 ("v_scales", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
+    _device = _index = None             # where its tensors are (make_paged_cache)
 
 
 class NewRows(ctypes.Structure):

@@ -344,6 +344,13 @@ def test_attention_of_several_query_tokens(fmt, T, Hq, Hkv, d):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("max_len,total", [(130, 0), (40000, 0), (40000, 1000)])
+def test_attention_of_a_whole_stretch_of_query_tokens(fmt, max_len, total):
+    """As many query tokens as entries, more than entries, and fewer; every tile of rows has its own masks."""
+    run_attention(fmt, [130, 330, 64, 0], 32, 6, 2, 64, T=130, seed=4, max_len=max_len, total_len=total)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_attention_masks_what_is_not_finite(fmt):
     """A query token does not see the entries of the tokens behind it, whatever they hold: its outputs are those of a cache
     without them.  Where it does see a NaN in V, that element is NaN; an infinity leaves it NaN or infinite; a NaN in K makes
