@@ -895,11 +895,16 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
 
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len) {
   PagedAttnPlan pl;
-  pl.row_tiles_of_8 = rows <= 8 ? 1 : 2;
-  pl.row_tiles = (rows + 8 * pl.row_tiles_of_8 - 1) / (8 * pl.row_tiles_of_8);
   const int chunk = e4m3 ? 2 * kSub : kSub;
-  const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
   const long long chunks = (max_len + chunk - 1) / chunk;
+  // More than 8 query rows: 16 of them share an entry's loads, unless the call is so small that CTAs of 8 rows all run at once and
+  // have some 512 entries or fewer each to go through (four query tokens, 16 and 8 rows a CTA, in us: one sequence of 250 entries,
+  // 8 bits, 6.7 and 5.8, of 2000 8.9 and 8.1, of 13107 13.9 and 14.6; 16 of 380, bf16, 13.9 and 10.0; 32 of 819 to 1638, 8 bits,
+  // 26.8 and 39).
+  const long long pairs_of_8 = static_cast<long long>(batch) * n_kv_heads * ((rows + 7) / 8);
+  pl.row_tiles_of_8 = rows <= 8 || (pairs_of_8 <= kPagedCtas && pairs_of_8 * max_len <= 512LL * kPagedCtas) ? 1 : 2;
+  pl.row_tiles = (rows + 8 * pl.row_tiles_of_8 - 1) / (8 * pl.row_tiles_of_8);
+  const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
   // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge costs 2 to 3 us, a
   // warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (one sequence, 8 bits: 400 entries 7.2 us whole and 6.7 in
   // four splits, 320 entries 5.8 and 6.2; bf16: 400 entries 6.8 and 5.7, four sequences of 257 6.8 and 7.1).
