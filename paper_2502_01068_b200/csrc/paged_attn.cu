@@ -916,13 +916,16 @@ PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, in
   pl.splits = static_cast<int>(splits);
   pl.balanced = 0;
   pl.ctas = 0;
-  // Chunks of the busiest CTA, static against an even deal; a balanced CTA pays six to eight chunks' time for every segment it
-  // starts, and its merge has every row to look at.  Static and balanced, in us: eight sequences of 4K to 64K entries, 8 bits, 235
-  // and 105; four of 500 to 20000 29.5 and 27.8; 16 of 200 to 4000 26.2 and 27.0; 64 of 2K to 8K 128 and 110; 32 of 819 to 1638,
-  // four query tokens, 27 and 44; 64 of 1638 to 2048, bf16, 75 and 83; 24 of 100 to 4000 47 and 42.
-  const double fixed = static_cast<double>((chunks + splits - 1) / splits) * ((pairs * splits + kPagedCtas - 1) / kPagedCtas);
-  const double even = static_cast<double>(total_len) / chunk * n_kv_heads * pl.row_tiles / kPagedCtas;
-  if (batch >= 2 && pairs * splits <= 4 * kPagedCtas && fixed > 1.2 * even + 24) {
+  // Static or dealt out evenly: entries that the busiest CTA goes through against the mean.  Static launches of several waves even
+  // themselves out but for about half a sequence.  Against that stands what a balanced launch pays: CTAs start and join two
+  // segments or more, and the merge looks at every row; measured, some 512 entries' time and 5 more for every pair, 7.5 where 16 rows
+  // share a CTA.  Static and balanced, in us: eight sequences of 4K to 64K entries, 8 bits, 235 and 105; four of 500 to 20000 29.5 and
+  // 27.8; 16 of 400 to 8000 44 and 37; 16 of 200 to 4000 26 and 27; 24 of 100 to 1638 19.5 and 26; 64 of 100 to 1000 24.5 and 38, of
+  // 2K to 8K 128 and 110; four query tokens, 32 of 819 to 1638, 27 and 44, 16 of 400 to 8000 61 and 55.
+  const double per = static_cast<double>((chunks + splits - 1) / splits) * chunk;
+  const double even = static_cast<double>(total_len) * n_kv_heads * pl.row_tiles / kPagedCtas;
+  const double busiest = pairs * splits <= kPagedCtas ? per : even + 0.5 * per;
+  if (batch >= 2 && busiest - even > 512.0 + (pl.row_tiles_of_8 == 1 ? 5.0 : 7.5) * pairs) {
     pl.balanced = 1;
     pl.ctas = kPagedCtas;
     pl.splits = 1;

@@ -344,7 +344,7 @@ def test_attention_of_several_query_tokens(fmt, T, Hq, Hkv, d):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-@pytest.mark.parametrize("max_len,total", [(130, 0), (40000, 0), (40000, 1000)])
+@pytest.mark.parametrize("max_len,total", [(130, 0), (40000, 0), (40000, 1000), (900000, 1000)])
 def test_attention_of_a_whole_stretch_of_query_tokens(fmt, max_len, total):
     """As many query tokens as entries, more than entries, and fewer; every tile of rows has its own masks."""
     run_attention(fmt, [130, 330, 64, 0], 32, 6, 2, 64, T=130, seed=4, max_len=max_len, total_len=total)
@@ -376,7 +376,7 @@ def test_attention_masks_what_is_not_finite(fmt):
     spoil("k", 2, 2, 1, 3, "nan")                # by tokens 1, 2 and 3
     q = bf16_rows(np.random.default_rng(8), (len(lens), T, Hq, d))
     cache = pools.cache()
-    for longest, total in ((66, 0), (700, 0), (20000, 771)):           # whole, split, dealt out
+    for longest, total in ((66, 0), (700, 0), (20000, 771), (200000, 771)):       # whole, split in two ways, dealt out
         query = B.make_query(n_q_heads=Hq, q_len=T, max_len=longest, total_len=total)
         ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
         out, lse = (torch.full(s, 7.0, device="cuda") for s in ((len(lens), T, Hq, d), (len(lens), T, Hq)))
@@ -404,8 +404,8 @@ def test_a_length_below_zero_is_reported_however_the_batch_is_dealt(fmt):
     pools = Pools(fmt, lens, lens, 32, 2, 64, 5)
     q = bf16_rows(np.random.default_rng(5), (4, 1, 8, 64))
     cache = pools.cache()
-    for total in (sum(lens), 4 * 20000):
-        query = B.make_query(n_q_heads=8, max_len=20000, total_len=total)
+    for longest, total in ((20000, sum(lens)), (20000, 4 * 20000), (200000, sum(lens))):
+        query = B.make_query(n_q_heads=8, max_len=longest, total_len=total)
         ws = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query))
         out, lse = torch.full((4, 1, 8, 64), 7.0, device="cuda"), torch.full((4, 1, 8), 7.0, device="cuda")
         pools.dev_lens[1] = -3
@@ -451,9 +451,10 @@ def test_what_the_host_knows_of_lengths_changes_nothing(fmt):
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("lens", [[0, 0, 0], [40, 0, 1], [70, 333, 64, 1], [130] * 20])
 @pytest.mark.parametrize("T", [1, 5])
-def test_batches_far_shorter_than_the_host_thinks(fmt, lens, T):
+@pytest.mark.parametrize("longest", [40000, 400000])
+def test_batches_far_shorter_than_the_host_thinks(fmt, lens, T, longest):
     """Dealt out evenly, there are fewer chunks than CTAs: some of them get none, and whoever joins the pieces must know it."""
-    run_attention(fmt, lens, 16, 8, 2, 64, T=T, seed=9, max_len=40000, total_len=50000)
+    run_attention(fmt, lens, 16, 8, 2, 64, T=T, seed=9, max_len=longest, total_len=50000)
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
@@ -573,7 +574,8 @@ def short_waits():
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-@pytest.mark.parametrize("lens,n", [([3000], 1), ([3000], 2), ([90], 1), ([20000, 40, 3000], 3), ([20000, 40, 3000], 1)])
+@pytest.mark.parametrize("lens,n", [([3000], 1), ([3000], 2), ([90], 1), ([20000, 40, 3000], 3), ([20000, 40, 3000], 1),
+                                    ([60000, 40, 3000], 2)])
 def test_an_attention_whose_data_never_comes_gives_up(fmt, lens, n, short_waits):
     pools = Pools(fmt, lens, lens, 32, 2, 128, 5)
     q = bf16_rows(np.random.default_rng(5), (len(lens), 1, 8, 128))
@@ -723,10 +725,10 @@ def test_a_kept_row_may_be_named_twice(fmt, n):
     check_append(pools, before, [3], [n], [take(k)], [take(v)], False)
 
 
-def test_two_graphs_may_share_a_workspace():
-    """Graphs of two attention calls of different shapes over one workspace, replayed by turns: each gives what it gave alone."""
+def test_graphs_may_share_a_workspace():
+    """Graphs of attention calls of different shapes over one workspace, replayed by turns: each gives what it gave alone."""
     made, need = [], 0
-    for lens, Hq, seed in (([5000], 8, 1), ([20000, 40, 3000, 90], 16, 2)):
+    for lens, Hq, seed in (([5000], 8, 1), ([20000, 40, 3000, 90], 16, 2), ([60000, 40, 3000], 8, 3)):
         pools = Pools("e4m3", lens, lens, 32, 2, 128, seed)
         q = bf16_rows(np.random.default_rng(seed), (len(lens), 1, Hq, 128)).cuda()
         cache, query = pools.cache(), B.make_query(n_q_heads=Hq, max_len=max(lens), total_len=sum(lens))
