@@ -36,6 +36,7 @@ struct AppendParams {
   // work split, filled in by the launcher
   int page_blocks, heads_per_unit, row_heads, row_slices;  // row role, behind the page role's blocks
   int pages_per_seq, job_slices, jobs_per_slice;           // page role (8-bit pages)
+  int small_log2;             // small role: lane groups of a (page, head)
 };
 
 // Whether the call reads k and v through tensor maps: (column, head, row) with boxes of a page's rows of one head, unswizzled.

@@ -15,8 +15,8 @@
 //              of the page wait in shared memory while their largest absolute value is found and are encoded from there.
 //              36 864 rows in eight ragged prompts, rotated, with their queries: 146 us, 87 %; 13107 kept rows of 8 heads,
 //              gathered: 18 us, 69 % (launch and the chain length -> table -> index -> row take 4 of them).
-//   Small role (8-bit pages, up to 8 rows per sequence): a lane group takes one (page, head) and its few new rows; 64 sequences,
-//              one row each: 3.7 us, as good as launching and three dependent trips to memory.
+//   Small role (8-bit pages, up to 8 rows per sequence): a lane group for each new row of a (page, head); 64 sequences, one row
+//              each: 3.6 us, as good as launching and three dependent trips to memory.
 // Rows that were in a page before keep their codes unless the new rows need a larger scale; then the codes are re-encoded
 // by the ratio, a power of two, which is exact but for codes that become subnormal.
 #include "paged.cuh"
@@ -312,13 +312,18 @@ __device__ void append_rows(const AppendParams& p, int block) {
   }
 }
 
-// Small role: unit u = (sequence, which of its touched pages, head of K or V); one lane group each.  Every lane of the
-// warp takes part in the shuffles, so idle units walk through with nothing to do.
+// Small role: unit u = (sequence, which of its touched pages, head of K or V), a lane group for each new row it may have (a power
+// of two, 2^small_log2).  Every row is read and its angles formed once, all of them side by side: what costs here is the chain
+// from the length to the codes (five rows took 8.6 us when one lane group went through them, now 3.6, one row 3.1).  The
+// groups of a unit share out the old rows that have to be encoded again.  Idle units walk through with nothing to do, because
+// every thread takes part in the shuffles and the meeting.
 template <int D>
 __device__ void append_small(const AppendParams& p, int block) {
   constexpr int GL = D / 16;
-  const int j = threadIdx.x % GL, Hkv = p.c.n_kv_heads, jobs = 2 * Hkv;
-  const long long u = static_cast<long long>(block) * (blockDim.x / GL) + threadIdx.x / GL;
+  __shared__ float warp_top[8];
+  const int grp = threadIdx.x / GL, j = threadIdx.x % GL, Hkv = p.c.n_kv_heads, jobs = 2 * Hkv;
+  const int mates = 1 << p.small_log2, mine = grp & (mates - 1);
+  const long long u = static_cast<long long>(block) * ((blockDim.x / GL) >> p.small_log2) + (grp >> p.small_log2);
   const long long units = static_cast<long long>(p.c.batch) * p.pages_per_seq * jobs;
   const bool live = u < units;
   const long long item = live ? u / jobs : 0;
@@ -353,50 +358,54 @@ __device__ void append_small(const AppendParams& p, int block) {
   float* const scales = is_v ? p.c.v_scales : p.c.k_scales;
   const int n_old = block_row >= 0 ? max(0, min(len - (pg << p.c.page_log2), P)) : 0;
   const float old_scale = n_old > 0 ? scales[block_row] : 0.0f;
-  const uint16_t* const base = is_v ? p.v + g * p.v_head : p.k + g * p.k_head;
-  const long long tok = is_v ? p.v_tok : p.k_tok;
-  float x[16];
-  auto load = [&](int slot) -> bool {
-    const int row = row0 + (slot - len);
-    const long long src = source_row(p, fetch_index(p, row, g), b);
-    if (src < 0) return false;
-    unpack(load_row(base + src * tok, at), x);
-    if (at.turned) {
-      float cs[8], sn[8];
-      angles_of(p.pos[row], p.inv_freq, j, cs, sn);
-      rotate16(x, cs, sn, p.adjacent);
-    }
-    return true;
-  };
-  float m = 0.0f;
+  float x[16], m = 0.0f;
   bool got = false;
-  for (int s = lo; s < hi; ++s) {
-    got = load(s);
-    if (got) m = fmaxf(m, amax16(x));
+  if (lo + mine < hi) {
+    const int row = row0 + (lo + mine - len);
+    const long long src = source_row(p, fetch_index(p, row, g), b);
+    if (src >= 0) {
+      got = true;
+      unpack(load_row((is_v ? p.v + g * p.v_head : p.k + g * p.k_head) + src * (is_v ? p.v_tok : p.k_tok), at), x);
+      if (at.turned) {
+        float cs[8], sn[8];
+        angles_of(p.pos[row], p.inv_freq, j, cs, sn);
+        rotate16(x, cs, sn, p.adjacent);
+      }
+      m = amax16(x);
+    }
   }
-#pragma unroll
-  for (int o = 1; o < GL; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const int lanes = GL << p.small_log2;            // of a unit: 4 to 64, in a row
+  for (int o = 1; o < min(lanes, 32); o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lanes > 32) {                                // a unit of two warps; the same for the whole call
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) warp_top[warp] = m;
+    __syncthreads();                               // also: both have read the old scale
+    m = fmaxf(m, warp_top[warp ^ 1]);
+  }
   if (hi <= lo) return;
   int e = scale_exponent(__float_as_uint(m));
   const int e_old = scale_log2(__float_as_uint(old_scale));
   if (n_old > 0 && e_old > e) e = e_old;
-  const float inv = __uint_as_float(pow2_bits(-e));
   uint8_t* const rows = (is_v ? p.c.v_pages : p.c.k_pages) + (block_row << p.c.page_log2) * D;
+  if (got) store_codes(rows + ((lo + mine) & (P - 1)) * D, at, x, __uint_as_float(pow2_bits(-e)));
   if (n_old > 0 && e > e_old) {                    // the rows that were there take the larger scale
     const float ratio = __uint_as_float(pow2_bits(max(e_old - e, -126)));
-    for (int r = 0; r < n_old; ++r) {
-      uint4* w = reinterpret_cast<uint4*>(rows + r * D + 16 * j);
-      uint4 c = *w;
-      c.x = rescale_e4m3(c.x, ratio); c.y = rescale_e4m3(c.y, ratio);
-      c.z = rescale_e4m3(c.z, ratio); c.w = rescale_e4m3(c.w, ratio);
-      *w = c;
+    uint4* const w = reinterpret_cast<uint4*>(rows + 16 * j);
+    for (int r0 = mine; r0 < n_old; r0 += 8 * mates) {             // eight rows' loads under way together
+      uint4 c[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i * mates < n_old) c[i] = w[(r0 + i * mates) * GL];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (r0 + i * mates >= n_old) continue;
+        c[i].x = rescale_e4m3(c[i].x, ratio); c[i].y = rescale_e4m3(c[i].y, ratio);
+        c[i].z = rescale_e4m3(c[i].z, ratio); c[i].w = rescale_e4m3(c[i].w, ratio);
+        w[(r0 + i * mates) * GL] = c[i];
+      }
     }
   }
-  if (j == 0) scales[block_row] = __uint_as_float(pow2_bits(e));
-  for (int s = lo; s < hi; ++s) {
-    if (hi - lo > 1) got = load(s);
-    if (got) store_codes(rows + (s & (P - 1)) * D, at, x, inv);
-  }
+  if (mine == 0 && j == 0) scales[block_row] = __uint_as_float(pow2_bits(e));
 }
 
 // The larger of two pairs of bf16 magnitudes (a NaN gives way, as with fmaxf).
@@ -719,7 +728,9 @@ static cudaError_t launch_d(AppendParams& p, const CUtensorMap (&maps)[2], bool 
     p.pages_per_seq = p.max_new == 1 ? 1 : (p.max_new + P - 2) / P + 1;
     const long long items = static_cast<long long>(p.c.batch) * p.pages_per_seq;
     if (small) {
-      page_blocks = (items * jobs + threads / GL - 1) / (threads / GL);
+      p.small_log2 = p.max_new == 1 ? 0 : p.max_new == 2 ? 1 : p.max_new <= 4 ? 2 : 3;
+      const int units = (threads / GL) >> p.small_log2;            // of a block
+      page_blocks = (items * jobs + units - 1) / units;
     } else {
       // Page role: a block walks all heads of its page; with fewer pages than the SMs hold blocks (as far as the slots' shared
       // memory goes), the heads are split over as many blocks as still run at once (13107 gathered rows, pages of 64: 18 us in 410
