@@ -9,11 +9,11 @@
 // Eight lanes (four for head_dim 64) handle one row of one head: sixteen elements each, as two 16-byte pieces chosen so
 // that both halves of every rotated pair are the lane's own.
 //   Row role   (bf16 pages; queries of either format): a lane group takes one token and a run of heads, so that the
-//              angles are formed once per run.  A prompt of 8192 tokens, 32 query and 8 KV heads of 128, bf16: 34.6 us, 89 % of a
+//              angles are formed once per run.  A prompt of 8192 tokens, 32 query and 8 KV heads of 128, bf16: 34.4 us, 89 % of a
 //              plain copy's rate over what it reads and writes.
 //   Page role  (8-bit pages, calls of more than 8 rows per sequence): a block takes one page and walks a run of heads, whose rows
 //              of the page wait in shared memory while their largest absolute value is found and are encoded from there.
-//              36 864 rows in eight ragged prompts, rotated, with their queries: 146 us, 87 %; 13107 kept rows of 8 heads,
+//              some 36 900 rows in eight ragged prompts, rotated, with their queries: 147 us, 87 %; 13107 kept rows of 8 heads,
 //              gathered: 18 us, 69 % (launch and the chain length -> table -> index -> row take 4 of them).
 //   Small role (8-bit pages, up to 8 rows per sequence): a lane group for each new row of a (page, head); 64 sequences, one row
 //              each: 3.6 us, as good as launching and three dependent trips to memory.
@@ -28,7 +28,7 @@ namespace {
 constexpr int kHeads = 2;            // page role: heads of a round
 // What a call does to its rows on the way.
 enum Mode { kPlain = 0, kRotated = 1, kGathered = 2 };
-// Page role: rounds of heads on their way while one is in use.  Two for tiled copies (51 us against 58 with one, 36 864 rows of
+// Page role: rounds of heads on their way while one is in use.  Two for tiled copies (51 us against 58 with one, some 36 900 rows of
 // 8 heads); one for gathered rows, so that three blocks fit an SM (18 us against 25.5 with two rounds and two blocks, 13107 rows
 // of 8 heads).
 template <int kMode> constexpr int kRoundsAhead = kMode == kGathered ? 1 : 2;

@@ -24,7 +24,7 @@
 // P goes in as 16-bit terms (value and rounding remainders; two in fp16, three in bf16), so the result carries fp32-level error.
 //
 // Measured, in us (and the share of a plain copy's bandwidth over the bytes the entries take): one sequence of 131072 entries,
-// 8 bits, 47 (87 %); eight of 4K to 64K, 105 (92 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
+// 8 bits, 47 (87 %); eight of 4K to 64K, 106 (91 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
 // tokens, 8 bits, 27 (48 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.4:
 // launch, table -> page -> copy, one pass, merge.
 #include <type_traits>
