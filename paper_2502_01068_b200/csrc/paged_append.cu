@@ -654,7 +654,7 @@ __global__ void __launch_bounds__(kKind == 3 ? 512 : 256, kKind <= 1 ? 2 : 0)
 paged_append_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AppendParams p) {
   pdl_launch_dependents();                        // every role waits for earlier kernels once it knows what it is to do
   if (blockIdx.x == 0) {
-    pdl_wait();
+    pdl_wait();                                   // and with this block's, who waits for this kernel waits for them, too
     for (int b = threadIdx.x; b < p.c.batch; b += blockDim.x) {
       RowRange r;
       const int len = p.lens[b];

@@ -805,7 +805,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
       if (t == 0 && h == 0 && i == 0 && p.lens[b] < 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PAGED_LEN);
     } else {
       const int ca = static_cast<int>(((p0 + 1) * ctas - 1) / total), cb = static_cast<int>((p1 * ctas - 1) / total);
-      if (ca == cb) return;                       // one CTA had all of it and wrote the result
+      if (ca == cb) {                             // one CTA had all of it and wrote the result
+        pdl_wait();                               // who waits for this kernel waits for the main one
+        return;
+      }
       n = cb - ca + 1;
       step = 2;
       rest = 2 * static_cast<long long>(ca);

@@ -725,6 +725,33 @@ def test_a_kept_row_may_be_named_twice(fmt, n):
     check_append(pools, before, [3], [n], [take(k)], [take(v)], False)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("longest,total", [(96, 0), (200000, 1000)])
+def test_an_append_behind_an_attention_waits_for_it(fmt, longest, total):
+    """The entries that an attention call reads are written over by the append behind it, call after call: each attention sees
+    the entries that were there when it was called.  Dealt out evenly, 37 sequences of 8 heads are one pair for every CTA, and
+    the kernel behind the main one has nothing to merge."""
+    n, Hkv, d, P = 37, 8, 64, 32
+    pools = Pools(fmt, [96] * n, [96] * n, P, Hkv, d, 8)
+    rng = np.random.default_rng(8)
+    q = bf16_rows(rng, (n, 1, 2 * Hkv, d))
+    cache, query = pools.cache(), B.make_query(n_q_heads=2 * Hkv, max_len=longest, total_len=total)
+    ws, wa = workspace(B.fastkv_paged_attn_workspace_bytes(cache, query)), workspace()
+    first = [bf16_rows(rng, (n * 32, Hkv, d)).cuda() for _ in range(2)]
+    rows = B.make_new_rows(batch=n, total=n * 32, max_new=32, n_kv_heads=Hkv, head_dim=d)
+    at64 = torch.full((n,), 64, dtype=torch.int32, device="cuda")
+    outs = [torch.zeros((n, 1, 2 * Hkv, d), device="cuda") for _ in range(8)]
+    qd = q.cuda()
+    for k, out in enumerate(outs):                                      # the last page of every sequence holds one set, the other, ...
+        src = first[0] if k % 2 == 0 else first[1]
+        B.fastkv_paged_append(cache, rows, at64, None, src, src, None, None, None, None, None, wa)
+        B.fastkv_paged_attn(cache, query, pools.dev_lens, qd, out, None, ws)
+    assert B.fastkv_device_status(ws) == (0, 0) and B.fastkv_device_status(wa) == (0, 0)
+    for k in (2, 4, 6):
+        assert torch.equal(outs[k], outs[0]) and torch.equal(outs[k + 1], outs[1])
+    assert not torch.equal(outs[0], outs[1])
+
+
 def test_graphs_may_share_a_workspace():
     """Graphs of attention calls of different shapes over one workspace, replayed by turns: each gives what it gave alone."""
     made, need = [], 0
