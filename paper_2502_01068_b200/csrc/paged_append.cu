@@ -562,9 +562,10 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
       return load_row(reinterpret_cast<const uint16_t*>(ring + (static_cast<uint32_t>(st) * n_rows + grp + n * groups) * (D * 2)), at);
     }
   };
-  bool ok = true;
+  int ok = 1;                                     // of the whole block, once it has met
   int now = 0;                                    // k % 3
-  for (int k = 0; k < rounds; ++k) {
+  int k = 0;
+  for (; k < rounds; ++k) {
     float old_scale[kHeads];
     uint32_t here = 0;                            // bit z * NS + n: this lane group has row n of head z
     const int next = now == 2 ? 0 : now + 1;
@@ -580,7 +581,7 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
       const int m = k * kHeads + z, st = m % kPageSlots, job = job0 + m * side + mine;
       const bool on = job < job1, is_v = job >= Hkv;
       old_scale[z] = on && n_old > 0 ? (is_v ? p.c.v_scales : p.c.k_scales)[static_cast<long long>(pid) * Hkv + (is_v ? job - Hkv : job)] : 0.0f;
-      if (!gather && m < fills) ok = ok && mbar_wait_bounded(&full[st], (m / kPageSlots) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT, p.wait_limit);
+      if (!gather && m < fills && ok) ok = mbar_wait_bounded(&full[st], (m / kPageSlots) & 1, &abort_flag, p.hdr, SITE_APPEND_WAIT, p.wait_limit);
       const Pieces& at = is_v ? plain : turned;
       float big = 0.0f;
 #pragma unroll
@@ -602,12 +603,20 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
       if (lane == 0 && most != 0u) atomicMax(&top[now][z][mine], most);
     }
     if (threadIdx.x < kHeads * 4) (&top[next][0][0])[threadIdx.x] = 0u;             // last read two rounds ago
-    __syncthreads();                              // also: every thread has read the old scales, and is done with the round before
-    if constexpr (!gather) start_boxes(k + kRoundsAhead<kMode>);                       // into the slots of the round before
+    // Every thread has read the old scales, and is done with the round before.  Tiled: the block agrees on whether the round's rows
+    // are there, so that a head is written by all of it or by none; after a wait that gave up nothing more is started, because
+    // nobody would wait for the copies before it in the same slots.
+    if constexpr (gather) {
+      __syncthreads();
+    } else {
+      ok = __syncthreads_and(ok);
+      if (!ok) break;
+      start_boxes(k + kRoundsAhead<kMode>);       // into the slots of the round before
+    }
 #pragma unroll
     for (int z = 0; z < kHeads; ++z) {
       const int m = k * kHeads + z, st = m % kPageSlots, job = job0 + m * side + mine;
-      if (job >= job1 || !ok) continue;
+      if (job >= job1) continue;
       const bool is_v = job >= Hkv;
       const int g = is_v ? job - Hkv : job;
       const Pieces& at = is_v ? plain : turned;
@@ -639,12 +648,9 @@ __device__ void append_page(const AppendParams& p, const CUtensorMap* map_k, con
     }
     now = next;
   }
-  if (!ok)                                        // a wait gave up: no copy may still be in flight when the block leaves
-    for (int m = max(0, fills - kPageSlots); m < fills; ++m)
-      if (p.skip_copy < 0 || m % kPageSlots != p.skip_copy % kPageSlots)
-        mbar_wait_drain(&full[m % kPageSlots], (m / kPageSlots) & 1, p.hdr, SITE_APPEND_WAIT);
-      else                                        // the withheld fill's barrier stays a phase behind the copies behind it
-        mbar_wait_drain(&full[m % kPageSlots], ((m - kPageSlots) / kPageSlots) & 1, nullptr, SITE_APPEND_WAIT, p.wait_limit);
+  if (!ok)                                        // round k's copies and those ahead of it may be in flight: none when the block leaves
+    for (int m = k * kHeads; m < min(fills, (k + kRoundsAhead<kMode>) * kHeads); ++m)
+      if (m != p.skip_copy) mbar_wait_drain(&full[m % kPageSlots], (m / kPageSlots) & 1, p.hdr, SITE_APPEND_WAIT);
 }
 
 // kKind: 0 bf16 pages (row role only), 1 8-bit pages with the small role, 2 and 3 with the page role (one, two rows per lane
