@@ -1011,8 +1011,7 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   p.scale_log2 = scale * 1.4426950408889634f;
   p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  p.box_subs = paged_box_rows(c.format == FASTKV_CACHE_E4M3, c.page_size) / 16;
-  p.part_ml = reinterpret_cast<float4*>(ws + sizeof(WorkspaceHeader));
+  p.part_ml = reinterpret_cast<float2*>(ws + sizeof(WorkspaceHeader));
   p.part_o = reinterpret_cast<float*>(ws + paged_attn_partials_offset(plan, c.batch, c.n_kv_heads));
   p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
   p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;

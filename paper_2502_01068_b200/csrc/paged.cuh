@@ -51,7 +51,6 @@ struct PagedAttnParams {
   int row_tiles, tile_rows;   // tiles the rows are cut into, and rows of a tile (8 or 16)
   int splits;                 // static launches: CTAs that share a (sequence, KV head, row tile)
   int balanced, ctas;         // balanced launches: CTAs that share all of them
-  int box_subs;               // 16-entry steps that one TMA box brings
   long long wait_limit;       // cycles a wait polls before it gives up
   int skip_copy;              // test hook: the first pair of warps gets no copies for this chunk of a segment (-1: none)
   int joint, v_first;         // K and V are planes of one tensor map; the V pool lies at the lower address
@@ -60,7 +59,7 @@ struct PagedAttnParams {
   const uint16_t* q;          // [B][q_len][Hq][d]
   float* out;                 // [B][q_len][Hq][d]
   float* lse;                 // [B][q_len][Hq], may be null
-  float4* part_ml;            // [pieces][tile_rows]: (max, sum, reference of the outputs, -)
+  float2* part_ml;            // [pieces][tile_rows]: (max, sum)
   float* part_o;              // [pieces][tile_rows][d]
   WorkspaceHeader* hdr;
 };

@@ -17,11 +17,14 @@
 // 8-bit pages: a code is exact in fp16, so K and V are widened in registers and the products are fp16 x fp16 -> fp32 (warp-level
 // products of 8-bit operands are no native instruction here: a step of theirs took 30 cycles against 8).  The queries (bf16) go
 // into fp16 after a power-of-two shift per row that brings the row's largest element to [2^14, 2^15): exact down to 2^-28 of it,
-// and what is smaller is off by at most 2^-39 of the largest.  K's scale multiplies the logits.  V's scale 2^v is an addend of
-// the exponent: the outputs accumulate 2^(l + v - R) * code against their own running reference R = max(l + v), the sum of
-// exponentials 2^(l - M) against M = max(l) as usual, and out = O / L * 2^(R - M): the weights of the second product stay in
-// (0, 1] whatever the pages' scales are.
-// P goes in as 16-bit terms (value and rounding remainders; two in fp16, three in bf16), so the result carries fp32-level error.
+// and what is smaller is off by at most 2^-39 of the largest.  K's scale multiplies the logits.  V's scale stays out of the weights,
+// whose range in fp16 is short: the codes of a step (16 or 32 entries of one page) are summed with weights 2^(l - m) that count from the
+// step's own largest logit m, and the sum joins the running outputs in fp32, times V's scale and 2^(m - M).  So neither the
+// scales of other pages nor the weights of other steps cost a step's entries any of their bits.  Pages of 16 join twice as often (32
+// sequences of up to 1638 entries, four query tokens: 28.9 us, with pages of 128 26.9).
+// P goes in as 16-bit terms (value and rounding remainders).  Three in bf16: 24 bits, whatever the weight.  Two in fp16: 22 bits, or
+// (both terms rounded to a multiple of 2^-24, the weights 2^15 times too large) off by at most 2^-39 of the step's largest weight: all
+// in all 2^-22 of sum p |v| and, step by step, 2^-39 of the largest weight times the sum of the |v|.
 //
 // Measured, in us (and the share of a plain copy's bandwidth over the bytes the entries take): one sequence of 131072 entries,
 // 8 bits, 47 (87 %); eight of 4K to 64K, 106 (91 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
@@ -36,8 +39,10 @@ namespace fastkv {
 namespace {
 
 constexpr int kSub = 16;            // entries of one step of the second product; a page holds a whole number of them
-constexpr float kShift = 14.0f;     // 8-bit pages: the weights of the second product are 2^14 times too large, so that the
-                                    // remainder term of the largest of them is far from fp16's subnormals
+// 8-bit pages: the weights of the second product are 2^15 times too large, so that the remainder term of the largest of them is far
+// from fp16's subnormals, and the running outputs 2^32 times too small: 2^31 entries of the largest value, 448 * 2^120, stay finite.
+constexpr float kWeightGain = 32768.0f, kOutGain = 4294967296.0f;
+constexpr float kScaleGain = 1.0f / (kWeightGain * kOutGain);   // what V's scale, 2^-64 or more, is multiplied by at the join
 
 __device__ __forceinline__ void ldsm_x4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -106,13 +111,16 @@ static_assert(kComputeRegs + kBringRegs == 2 * kLaunchRegs, "the warpgroups' sha
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-template <int D, bool kE4M3, int RT>
+// kOwnPage: 8-bit pages of 16 entries, where the two halves of a chunk lie in different pages.
+template <int D, bool kE4M3, int RT, bool kOwnPage>
 struct PagedCfg {
   static constexpr int kItem = kE4M3 ? 1 : 2;
   // 8-bit rows go through in chunks of 32 entries: two independent halves, and the work that does not depend on the chunk's size
   // (waits, shuffles, rescaling) is paid half as often.
   static constexpr int kSubs = kE4M3 ? 2 : 1;
   static constexpr int kChunk = kSub * kSubs;                              // entries per stage
+  static constexpr int kBoxSubs = kOwnPage ? 1 : kSubs;                    // 16-entry steps that one TMA box brings
+  static constexpr int kParts = kOwnPage ? kSubs : 1;                      // parts of a chunk whose sums join apart
   static constexpr int kRowBytes = D * kItem;
   static constexpr int kBoxes = kRowBytes > 128 ? kRowBytes / 128 : 1;     // 128-byte column blocks of a row (or one of 64)
   static constexpr int kBoxRow = kRowBytes / kBoxes;
@@ -125,7 +133,7 @@ struct PagedCfg {
   static constexpr int kRows = 8 * RT;
   static constexpr int kMergeCols = RT == 1 ? 64 : 32;                     // the warps' outputs meet so many columns at a time
   static constexpr int kMergeLd = kMergeCols + 4;
-  static constexpr int kMergeBytes = kWarps * kRows * (kMergeLd * 4 + 16);
+  static constexpr int kMergeBytes = kWarps * kRows * (kMergeLd * 4 + 8);
   static constexpr int kSmem = kRingBytes + kMergeBytes + 1024;
 };
 
@@ -159,17 +167,17 @@ __device__ __forceinline__ long long share_begin(long long total, int c, int n) 
 // p.balanced == 0: one segment per CTA, (split of the entries, KV head, row tile, sequence).  p.balanced == 1: the chunks of all
 // (sequence, row tile, KV head) triples in a row are dealt evenly to the grid's CTAs, so that sequences of very different
 // lengths load every SM alike; a CTA walks the segments its share touches.
-template <int D, bool kE4M3, int RT>
+template <int D, bool kE4M3, int RT, bool kOwnPage>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedAttnParams p) {
-  using Cfg = PagedCfg<D, kE4M3, RT>;
-  constexpr int KS = D / 16, MT = D / 16, kRows = Cfg::kRows, kStages = Cfg::kStages, NSUB = Cfg::kSubs;
+  using Cfg = PagedCfg<D, kE4M3, RT, kOwnPage>;
+  constexpr int KS = D / 16, MT = D / 16, kRows = Cfg::kRows, kStages = Cfg::kStages, NSUB = Cfg::kSubs, kParts = Cfg::kParts;
   constexpr int kChunk = Cfg::kChunk, kChunkLog2 = kE4M3 ? 5 : 4;
   constexpr int kTerms = kE4M3 ? 2 : 3;         // 16-bit terms of a weight: 11 + 11 bits of fp16, 8 + 8 + 8 of bf16
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   __shared__ uint64_t full[kWarps][kStages], empty[kWarps][kStages];
-  __shared__ float2 scale_of[kWarps][kStages][NSUB];       // 8-bit pages, by 16 entries of a stage: K's scale, log2 of V's
+  __shared__ float2 scale_of[kWarps][kStages][NSUB];       // 8-bit pages, by 16 entries of a stage: K's scale, V's times kScaleGain
   __shared__ float weight_of[kWarps][kRows];               // what a warp's outputs count for in the merge
   __shared__ long long at_of[kRows];                       // where a row's result goes, in units of D floats
   __shared__ int abort_flag;
@@ -261,7 +269,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const int pair = warp & (kWarps - 1);                    // the computing warp, and the one that brings its data
   uint8_t* const ring_ptr = smem + pair * kStages * Cfg::kStageBytes;
   // inside a column block of a stage: K and V alternate by box (of a chunk's 32 rows, or of 16)
-  const uint32_t box_bytes = p.box_subs * kSub * Cfg::kBoxRow, sub_stride = NSUB == 2 && p.box_subs == 1 ? 2 * kSub * Cfg::kBoxRow : kSub * Cfg::kBoxRow;
+  constexpr uint32_t box_bytes = Cfg::kBoxSubs * kSub * Cfg::kBoxRow, sub_stride = (kOwnPage ? 2 : 1) * kSub * Cfg::kBoxRow;
   const uint32_t k_off = p.v_first ? box_bytes : 0, v_off = p.v_first ? 0 : box_bytes;
   int stage = 0;                                           // position in the ring, carried from segment to segment
   uint32_t phase = 0;
@@ -291,7 +299,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       };
       auto scales_at = [&](int blk) -> float2 {
         if (!kE4M3 || blk < 0) return make_float2(1.0f, 0.0f);
-        return make_float2(p.c.k_scales[blk], static_cast<float>(scale_log2(__float_as_uint(p.c.v_scales[blk]))));
+        return make_float2(p.c.k_scales[blk], p.c.v_scales[blk] * kScaleGain);
       };
       int blk_cur = block_of(lane), blk_next = block_of(32 + lane);
       float2 sc_cur = scales_at(blk_cur), sc_next = scales_at(blk_next);
@@ -320,7 +328,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           mbar_arrive_expect_tx(bar, Cfg::kStageBytes);
 #pragma unroll
           for (int y = 0; y < NSUB; ++y) {
-            if (y > 0 && p.box_subs != 1) break;
+            if (y >= kParts) break;
             const int sub = (c0 + pair + i * kWarps) * NSUB + y;
             const int row = (sub & ((1 << page_subs_log2) - 1)) * kSub;
             uint8_t* dst = ring_ptr + stage * Cfg::kStageBytes + y * sub_stride;
@@ -364,7 +372,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const uint32_t row7 = lane & 7;
   const uint32_t swz = Cfg::kBoxRow == 128 ? row7 : (row7 >> 1);      // 16-byte piece p of row r sits at p ^ swz
   float* const mo = reinterpret_cast<float*>(smem + Cfg::kRingBytes);                          // [warps][rows][columns]
-  float4* const mml = reinterpret_cast<float4*>(mo + kWarps * kRows * Cfg::kMergeLd);        // [warps][rows]: max, sum, reference
+  float2* const mml = reinterpret_cast<float2*>(mo + kWarps * kRows * Cfg::kMergeLd);        // [warps][rows]: max, sum
   auto meet = []() { asm volatile("bar.sync 1, %0;" ::"n"(kComputing) : "memory"); };
 
   do {
@@ -424,10 +432,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     // O^T per row tile: [0] (d0, row 2c), [1] (d0, row 2c + 1), [2] (d1, row 2c), [3] (d1, row 2c + 1); (d0, d1) is
     // (quad, quad + 8) of the 16-wide step mt for bf16 and (2 quad, 2 quad + 1) for 8-bit rows
     float o[RT][MT][4];
-    float m_run[RT], l_part[RT], r_run[RT];
+    float m_run[RT], l_part[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      m_run[rt] = r_run[rt] = -INFINITY;
+      m_run[rt] = -INFINITY;
       l_part[rt] = 0.0f;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -526,19 +534,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           for (int y = 0; y < NSUB; ++y)
             ldsm_x4_trans(vb[l][y], (at ^ ((l & 3) << 5)) + (l >> 2) * 2 * Cfg::kBoxBytes + y * sub_stride);
       }
-      float sk[NSUB], ev[NSUB];
+      float2 sc[NSUB];                              // the pages' scales
 #pragma unroll
-      for (int y = 0; y < NSUB; ++y) {
-        sk[y] = 1.0f;
-        ev[y] = 0.0f;
-        if constexpr (kE4M3) {
-          const float2 sc = scale_of[warp][st][y];
-          sk[y] = sc.x;
-          ev[y] = sc.y;
-        }
-      }
+      for (int y = 0; y < NSUB; ++y) sc[y] = kE4M3 ? scale_of[warp][st][y] : make_float2(1.0f, 1.0f);
       uint32_t pt[RT][kTerms][NSUB][2];             // the weights as B fragments, term by term
       float a0[RT], a1[RT];                         // what the outputs of rows 2c and 2c + 1 are scaled by
+      float g0[RT][kParts], g1[RT][kParts];         // 8-bit pages: and what their new sums are
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         // ---- online softmax of row quad (+ 8 rt): its logits sit in the four lanes of the quad ----
@@ -549,42 +550,57 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             for (int e = 0; e < 2; ++e)
               if (key0 + nt * 8 + c * 2 + e >= sees[rt]) s[nt][rt * 2 + e] = -INFINITY;
         }
-        float f[NSUB], top[NSUB];
+        float f[NSUB], most[NSUB], top[NSUB];       // most: the largest unit; top: what it is as a logit (log2)
 #pragma unroll
         for (int y = 0; y < NSUB; ++y) {
-          f[y] = fmaxf(q_scale[rt] * sk[y], 1.17549435e-38f);            // positive, so that a masked logit stays -inf
-          top[y] = fmaxf(fmaxf(s[2 * y][2 * rt], s[2 * y][2 * rt + 1]), fmaxf(s[2 * y + 1][2 * rt], s[2 * y + 1][2 * rt + 1]));
-          top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 1));
-          top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 2)) * f[y];
+          f[y] = fmaxf(q_scale[rt] * sc[y].x, 1.17549435e-38f);          // positive, so that a masked logit stays -inf
+          most[y] = fmaxf(fmaxf(s[2 * y][2 * rt], s[2 * y][2 * rt + 1]), fmaxf(s[2 * y + 1][2 * rt], s[2 * y + 1][2 * rt + 1]));
+          most[y] = fmaxf(most[y], __shfl_xor_sync(0xffffffffu, most[y], 1));
+          most[y] = fmaxf(most[y], __shfl_xor_sync(0xffffffffu, most[y], 2));
+          top[y] = most[y] * f[y];
         }
         float m_new = m_run[rt];
 #pragma unroll
         for (int y = 0; y < NSUB; ++y) m_new = fmaxf(m_new, top[y]);
         const float ref = m_new == -INFINITY ? 0.0f : m_new;             // nothing seen yet: everything stays at zero
-        float alpha = ex2(m_run[rt] - ref);
-        float pr[NSUB][4], sum = 0.0f;
-#pragma unroll
-        for (int y = 0; y < NSUB; ++y) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pr[y][e] = ex2(fmaf(s[2 * y + (e >> 1)][2 * rt + (e & 1)], f[y], -ref));
-          sum += (pr[y][0] + pr[y][1]) + (pr[y][2] + pr[y][3]);
-        }
-        l_part[rt] = fmaf(l_part[rt], alpha, sum);
-        m_run[rt] = m_new;
+        const float alpha = ex2(m_run[rt] - ref);
+        float pr[NSUB][4];
         if constexpr (kE4M3) {
-          float r_new = r_run[rt];
+          float from[kParts], gain[kParts], sum[kParts];                 // from: the unit that a part's weights count from
 #pragma unroll
-          for (int y = 0; y < NSUB; ++y) r_new = fmaxf(r_new, top[y] + ev[y]);
-          const float refo = r_new == -INFINITY ? 0.0f : r_new;
-          alpha = ex2(r_run[rt] - refo);
-          r_run[rt] = r_new;
+          for (int z = 0; z < kParts; ++z) {
+            from[z] = kOwnPage ? most[z] : fmaxf(most[0], most[NSUB - 1]);
+            gain[z] = ex2((kOwnPage ? top[z] : fmaxf(top[0], top[NSUB - 1])) - ref);
+            if (from[z] == -INFINITY) from[z] = 0.0f;
+            sum[z] = 0.0f;
+          }
 #pragma unroll
           for (int y = 0; y < NSUB; ++y) {
-            const float shift = ev[y] - refo + kShift;
+            const int z = kOwnPage ? y : 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pr[y][e] = ex2(fmaf(s[2 * y + (e >> 1)][2 * rt + (e & 1)], f[y], shift));
+            for (int e = 0; e < 4; ++e) pr[y][e] = ex2((s[2 * y + (e >> 1)][2 * rt + (e & 1)] - from[z]) * f[y]);      // at most 1
+            sum[z] += (pr[y][0] + pr[y][1]) + (pr[y][2] + pr[y][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[y][e] *= kWeightGain;
           }
+#pragma unroll
+          for (int z = 0; z < kParts; ++z) {
+            l_part[rt] = fmaf(sum[z], gain[z], z == 0 ? l_part[rt] * alpha : l_part[rt]);
+            gain[z] *= sc[z].y;
+            g0[rt][z] = __shfl_sync(0xffffffffu, gain[z], 8 * c);
+            g1[rt][z] = __shfl_sync(0xffffffffu, gain[z], 8 * c + 4);
+          }
+        } else {
+          float sum = 0.0f;
+#pragma unroll
+          for (int y = 0; y < NSUB; ++y) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[y][e] = ex2(fmaf(s[2 * y + (e >> 1)][2 * rt + (e & 1)], f[y], -ref));
+            sum += (pr[y][0] + pr[y][1]) + (pr[y][2] + pr[y][3]);
+          }
+          l_part[rt] = fmaf(l_part[rt], alpha, sum);
         }
+        m_run[rt] = m_new;
         a0[rt] = __shfl_sync(0xffffffffu, alpha, 8 * c);
         a1[rt] = __shfl_sync(0xffffffffu, alpha, 8 * c + 4);
         // the weights as 16-bit terms: the leading bits cut off, then what is left (the last term rounded)
@@ -608,43 +624,52 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           }
         }
       }
-      // ---- O^T = O^T alpha + V^T P^T.  The products of a chunk start from zero and join the running outputs with one rounding
-      // to nearest: the tensor cores cut their sums off, and over thousands of chunks that bias shows. ----
-      auto join = [&](float (&acc)[4], const float (&x)[4], float f0, float f1) {
-        acc[0] = fmaf(acc[0], f0, x[0]); acc[1] = fmaf(acc[1], f1, x[1]);
-        acc[2] = fmaf(acc[2], f0, x[2]); acc[3] = fmaf(acc[3], f1, x[3]);
+      // ---- O^T = O^T alpha + V^T P^T.  The products of a chunk (of each page's part) start from zero and join the running outputs with
+      // one rounding to nearest: the tensor cores cut their sums off, and over thousands of chunks that bias shows. ----
+      auto join = [&](float (&acc)[4], const float (&x)[4], int rt, int z) {
+        if constexpr (kE4M3) {
+          const float b0 = z == 0 ? a0[rt] : 1.0f, b1 = z == 0 ? a1[rt] : 1.0f;
+          acc[0] = fmaf(x[0], g0[rt][z], acc[0] * b0); acc[1] = fmaf(x[1], g1[rt][z], acc[1] * b1);
+          acc[2] = fmaf(x[2], g0[rt][z], acc[2] * b0); acc[3] = fmaf(x[3], g1[rt][z], acc[3] * b1);
+        } else {
+          acc[0] = fmaf(acc[0], a0[rt], x[0]); acc[1] = fmaf(acc[1], a1[rt], x[1]);
+          acc[2] = fmaf(acc[2], a0[rt], x[2]); acc[3] = fmaf(acc[3], a1[rt], x[3]);
+        }
       };
-      constexpr int kTogether = 4 / RT;             // 16-element tiles of the head dimension whose sums run side by side
+      constexpr int kTogether = 4 / RT / kParts;    // 16-element tiles of the head dimension whose sums run side by side
 #pragma unroll
       for (int m0 = 0; m0 < MT; m0 += kTogether) {
-        float x[kTogether][RT][4];
+        float x[kParts][kTogether][RT][4];
+        uint32_t v[NSUB][kTogether][4];
 #pragma unroll
-        for (int y = 0; y < NSUB; ++y) {
-          uint32_t v[kTogether][4];
+        for (int y = 0; y < NSUB; ++y)
 #pragma unroll
           for (int z = 0; z < kTogether; ++z) {
             const int m = m0 + z;
             if constexpr (kE4M3) {
               // a word holds elements (2 quad, 2 quad + 1) of entry 2c, then of entry 2c + 1: bring equal elements together
               const uint32_t w0 = __byte_perm(vb[m / 2][y][2 * (m & 1)], 0, 0x3120), w1 = __byte_perm(vb[m / 2][y][2 * (m & 1) + 1], 0, 0x3120);
-              v[z][0] = widen_lo(w0); v[z][1] = widen_hi(w0); v[z][2] = widen_lo(w1); v[z][3] = widen_hi(w1);
+              v[y][z][0] = widen_lo(w0); v[y][z][1] = widen_hi(w0); v[y][z][2] = widen_lo(w1); v[y][z][3] = widen_hi(w1);
             } else {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[z][e] = vb[m][0][e];
+              for (int e = 0; e < 4; ++e) v[y][z][e] = vb[m][0][e];
             }
           }
 #pragma unroll
-          for (int w = 0; w < kTerms; ++w)
+        for (int n = 0; n < NSUB * kTerms; ++n) {     // by half, then by term; halves that join apart take turns
+          const int y = kOwnPage ? n % NSUB : n / kTerms, w = kOwnPage ? n / NSUB : n % kTerms, part = kOwnPage ? y : 0;
 #pragma unroll
-            for (int z = 0; z < kTogether; ++z)
+          for (int z = 0; z < kTogether; ++z)
 #pragma unroll
-              for (int rt = 0; rt < RT; ++rt)
-                mma16<kE4M3>(x[z][rt], y == 0 && w == 0, v[z][0], v[z][1], v[z][2], v[z][3], pt[rt][w][y][0], pt[rt][w][y][1]);
+            for (int rt = 0; rt < RT; ++rt)
+              mma16<kE4M3>(x[part][z][rt], n < kParts, v[y][z][0], v[y][z][1], v[y][z][2], v[y][z][3], pt[rt][w][y][0], pt[rt][w][y][1]);
         }
 #pragma unroll
-        for (int z = 0; z < kTogether; ++z)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) join(o[rt][m0 + z], x[z][rt], a0[rt], a1[rt]);
+          for (int z = 0; z < kTogether; ++z)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) join(o[rt][m0 + z], x[part][z][rt], rt, part);
       }
     };
     for (int i = 0; i < my_chunks; ++i) {
@@ -661,7 +686,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     for (int rt = 0; rt < RT; ++rt) {
       l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 1);
       l_part[rt] += __shfl_xor_sync(0xffffffffu, l_part[rt], 2);
-      if constexpr (!kE4M3) r_run[rt] = m_run[rt];
     }
     pdl_launch_dependents();
     if (spoilt) {                                  // rare: the elements that were cleared, from the pool
@@ -694,8 +718,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     meet();                                        // the last segment's merge has been read
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
-      if (c == 0) mml[warp * kRows + rt * 8 + quad] =
-          make_float4(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f, ok ? r_run[rt] : -INFINITY, 0.0f);
+      if (c == 0) mml[warp * kRows + rt * 8 + quad] = make_float2(ok ? m_run[rt] : -INFINITY, ok ? l_part[rt] : 0.0f);
 #pragma unroll
     for (int cut = 0; cut < D / Cfg::kMergeCols; ++cut) {
       if (cut > 0) meet();                         // the columns before have been read
@@ -717,22 +740,19 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       meet();
       if (cut == 0) {
         if (t < n_rows) {
-          float M = -INFINITY, R = -INFINITY, L = 0.0f;
+          float M = -INFINITY, L = 0.0f;
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) M = fmaxf(M, mml[w * kRows + t].x);
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) {
-            M = fmaxf(M, mml[w * kRows + t].x);
-            R = fmaxf(R, mml[w * kRows + t].z);
-          }
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            const float4 ml = mml[w * kRows + t];
+            const float2 ml = mml[w * kRows + t];
             if (ml.y != 0.0f) L = fmaf(ml.y, ex2(ml.x - M), L);                   // warps without entries weigh nothing; NaN stays
           }
-          const float last = !whole ? 1.0f : L != 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
+          const float last = !whole ? 1.0f : L != 0.0f ? (kE4M3 ? kOutGain : 1.0f) / L : 0.0f;
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) {
-            const float4 ml = mml[w * kRows + t];
-            weight_of[w][t] = ml.y != 0.0f ? ex2(ml.z - R) * last : 0.0f;
+            const float2 ml = mml[w * kRows + t];
+            weight_of[w][t] = ml.y != 0.0f ? ex2(ml.x - M) * last : 0.0f;
           }
           if (whole) {
             const int r = row_base + t, i = r / G, h = g * G + r - i * G;
@@ -743,7 +763,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             // where a piece waits for the merge: static launches by (pair, split), balanced ones by CTA (first segment or later)
             const long long at = (p.balanced ? 2 * static_cast<long long>(blockIdx.x) + (u != u_begin) : static_cast<long long>(blockIdx.x)) * kRows + t;
             at_of[t] = at;
-            p.part_ml[at] = make_float4(M, L, R, 0.0f);
+            p.part_ml[at] = make_float2(M, L);
           }
         }
         meet();
@@ -820,7 +840,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
     first = rest = (static_cast<long long>(b) * p.c.n_kv_heads + g) * n * step + tile;
   }
   const float* const outputs = p.part_o + (rest * kRows + r) * D + lane * V;
-  const float4* const sums = p.part_ml + rest * kRows + r;
+  const float2* const sums = p.part_ml + rest * kRows + r;
   const size_t apart = static_cast<size_t>(step) * kRows;
   const long long extra = (first - rest) * kRows;
   struct Part { float x[V]; };
@@ -836,33 +856,28 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
     }
     return y;
   };
-  auto sums_of = [&](int s) -> float4 { return __ldcg(sums + (s == 0 ? extra : s * apart)); };
-  const float4 none = make_float4(-INFINITY, 0.0f, -INFINITY, 0.0f);
+  auto sums_of = [&](int s) -> float2 { return __ldcg(sums + (s == 0 ? extra : s * apart)); };
+  const float2 none = make_float2(-INFINITY, 0.0f);
   pdl_wait();                                     // the lengths were there before any block of the main kernel let this one start
-  const float4 ml0 = lane < n ? sums_of(lane) : none, ml1 = 32 + lane < n ? sums_of(32 + lane) : none;
+  const float2 ml0 = lane < n ? sums_of(lane) : none, ml1 = 32 + lane < n ? sums_of(32 + lane) : none;
   Part ahead[kAhead];
 #pragma unroll
   for (int k = 0; k < kAhead; ++k)
     if (warp + k * warps < n) ahead[k] = load(warp + k * warps);
-  float M = fmaxf(ml0.x, ml1.x), R = fmaxf(ml0.z, ml1.z), L = 0.0f;
-  for (int s = 64 + lane; s < n; s += 32) {
-    const float4 ml = sums_of(s);
-    M = fmaxf(M, ml.x);
-    R = fmaxf(R, ml.z);
-  }
+  float M = fmaxf(ml0.x, ml1.x), L = 0.0f;
+  for (int s = 64 + lane; s < n; s += 32) M = fmaxf(M, sums_of(s).x);
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) {
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, o));
-  }
+  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   // pieces without entries weigh nothing; NaN stays
-  auto exp_sum = [&](const float4& ml) -> float { return ml.y == 0.0f ? 0.0f : ml.y * ex2(ml.x - M); };
-  auto weight = [&](const float4& ml) -> float { return ml.y == 0.0f ? 0.0f : ex2(ml.z - R); };
-  L = exp_sum(ml0) + exp_sum(ml1);
-  for (int s = 64 + lane; s < n; s += 32) L += exp_sum(sums_of(s));
+  auto weight = [&](const float2& ml) -> float { return ml.y == 0.0f ? 0.0f : ex2(ml.x - M); };
+  const float w0 = weight(ml0), w1 = weight(ml1);
+  L = ml0.y * w0 + ml1.y * w1;
+  for (int s = 64 + lane; s < n; s += 32) {
+    const float2 ml = sums_of(s);
+    L += ml.y * weight(ml);
+  }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-  const float w0 = weight(ml0), w1 = weight(ml1);
   float sum[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) sum[e] = 0.0f;
@@ -886,7 +901,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
   for (int e = 0; e < V; ++e) acc[warp][lane * V + e] = sum[e];
   __syncthreads();
   const size_t at = (static_cast<size_t>(b) * p.q_len + i) * p.n_q_heads + h;
-  const float scale = L != 0.0f ? ex2(R - M - (kE4M3 ? kShift : 0.0f)) / L : 0.0f;
+  const float scale = L != 0.0f ? (kE4M3 ? kOutGain : 1.0f) / L : 0.0f;
   for (int x = t; x < D; x += blockDim.x) {
     float o = 0.0f;
 #pragma unroll 4
@@ -942,26 +957,26 @@ static size_t pieces_of_plan(const PagedAttnPlan& plan, int batch, int n_kv_head
 }
 size_t paged_attn_partials_offset(const PagedAttnPlan& plan, int batch, int n_kv_heads) {
   const size_t rows = pieces_of_plan(plan, batch, n_kv_heads) * 8 * plan.row_tiles_of_8;
-  return sizeof(WorkspaceHeader) + (rows * sizeof(float4) + 255) / 256 * 256;
+  return sizeof(WorkspaceHeader) + (rows * sizeof(float2) + 255) / 256 * 256;
 }
 size_t paged_attn_workspace_bytes(const PagedAttnPlan& plan, int batch, int n_kv_heads, int head_dim) {
   const size_t rows = pieces_of_plan(plan, batch, n_kv_heads) * 8 * plan.row_tiles_of_8;
   return paged_attn_partials_offset(plan, batch, n_kv_heads) + rows * head_dim * sizeof(float);
 }
 
-template <int D, bool kE4M3, int RT>
+template <int D, bool kE4M3, int RT, bool kOwnPage>
 static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedAttnParams& p, cudaStream_t stream, int* launches) {
-  using Cfg = PagedCfg<D, kE4M3, RT>;
+  using Cfg = PagedCfg<D, kE4M3, RT, kOwnPage>;
   static PerDeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(paged_attn_kernel<D, kE4M3, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    e = cudaFuncSetAttribute(paged_attn_kernel<D, kE4M3, RT, kOwnPage>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
     // the split of the registers holds for this launch size only: a build that differs must not run
     cudaFuncAttributes fa;
-    if ((e = cudaFuncGetAttributes(&fa, paged_attn_kernel<D, kE4M3, RT>)) != cudaSuccess) return e;
+    if ((e = cudaFuncGetAttributes(&fa, paged_attn_kernel<D, kE4M3, RT, kOwnPage>)) != cudaSuccess) return e;
     if (fa.numRegs != kLaunchRegs) return cudaErrorLaunchOutOfResources;
     configured.set(dev);
   }
@@ -977,7 +992,7 @@ static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedA
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, kE4M3, RT>, tk, tv, static_cast<const PagedAttnParams&>(p));
+  e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, kE4M3, RT, kOwnPage>, tk, tv, static_cast<const PagedAttnParams&>(p));
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (!p.balanced && p.splits == 1) return cudaSuccess;
@@ -995,7 +1010,11 @@ static cudaError_t launch_w(const CUtensorMap& tk, const CUtensorMap& tv, PagedA
 template <int D, bool kE4M3>
 static cudaError_t launch_f(const CUtensorMap& tk, const CUtensorMap& tv, PagedAttnParams& p, const PagedAttnPlan& plan,
                             cudaStream_t stream, int* launches) {
-  return plan.row_tiles_of_8 == 1 ? launch_w<D, kE4M3, 1>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 2>(tk, tv, p, stream, launches);
+  if constexpr (kE4M3) {
+    if (p.c.page_log2 == 4)
+      return plan.row_tiles_of_8 == 1 ? launch_w<D, kE4M3, 1, true>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 2, true>(tk, tv, p, stream, launches);
+  }
+  return plan.row_tiles_of_8 == 1 ? launch_w<D, kE4M3, 1, false>(tk, tv, p, stream, launches) : launch_w<D, kE4M3, 2, false>(tk, tv, p, stream, launches);
 }
 
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
