@@ -85,9 +85,9 @@ __device__ __forceinline__ Pieces pieces_of(int j, int dim, int rot_dim, int adj
 }
 
 // cos and sin of the eight pairs 8j .. 8j + 7 at position `pos`.  The angle is formed in fp64 in quarter turns, pos * f * 2 / pi,
-// with the rounding error of the product added back after the whole quarters are gone; what is left, at most an eighth of
-// a turn, goes through the Taylor series of sin and cos (to x^13 and x^14: off by 2e-14 and 1e-15, so that the one rounding to
-// fp32 is the right one but for one value in millions).  24 fp64 instructions a pair.
+// with the rounding errors of both products (pos * f alone needs 55 bits) added back after the whole quarters are gone; what is
+// left, at most an eighth of a turn, goes through the Taylor series of sin and cos (to x^13 and x^14: off by 2e-14 and 1e-15, so
+// that the one rounding to fp32 is the right one but for one value in millions).  26 fp64 instructions a pair.
 __device__ __forceinline__ void angles_of(int pos, const float* inv_freq, int j, float (&cs)[8], float (&sn)[8]) {
   const double kQuarters = 0.6366197723675814, kQuartersLow = -3.935735335036497e-17;      // 2 / pi, high and low part
   const double kHalfPi = 1.5707963267948966;
@@ -97,9 +97,9 @@ __device__ __forceinline__ void angles_of(int pos, const float* inv_freq, int j,
   const double dpos = static_cast<double>(pos);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const double a = dpos * static_cast<double>(f[e]);
+    const double freq = static_cast<double>(f[e]), a = dpos * freq, a_low = fma(dpos, freq, -a);
     const double t = a * kQuarters, whole = t + kRound;
-    const double rest = (t - (whole - kRound)) + fma(a, kQuartersLow, fma(a, kQuarters, -t));
+    const double rest = (t - (whole - kRound)) + fma(a_low, kQuarters, fma(a, kQuartersLow, fma(a, kQuarters, -t)));
     const double x = rest * kHalfPi, z = x * x;
     double s = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);
     s = fma(z, s, 1.0 / 362880.0); s = fma(z, s, -1.0 / 5040.0); s = fma(z, s, 1.0 / 120.0); s = fma(z, s, -1.0 / 6.0);
