@@ -152,7 +152,7 @@ __device__ __forceinline__ long long block_sum(long long x, long long* scratch) 
 }
 
 __device__ __forceinline__ int chunks_of(const PagedAttnParams& p, int b, int chunk_log2) {
-  return (usable_len(p.lens[b], p.c.max_pages, p.c.page_log2) + (1 << chunk_log2) - 1) >> chunk_log2;
+  return chunk_count(usable_len(p.lens[b], p.c.max_pages, p.c.page_log2), chunk_log2);
 }
 
 // CTAs that get a share: no more than there are units, so that every CTA between a pair's first and last holds a piece of it.
@@ -672,11 +672,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             for (int rt = 0; rt < RT; ++rt) join(o[rt][m0 + z], x[part][z][rt], rt, part);
       }
     };
+    const int all_see = chunks_all_see(len, T, kChunkLog2);
     for (int i = 0; i < my_chunks; ++i) {
       ok = mbar_wait_bounded(&full[warp][stage], phase, &abort_flag, p.hdr, SITE_PAGED_WAIT, p.wait_limit);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if ((c0 + warp + i * kWarps + 1) * kChunk <= len - (T - 1)) pass(std::false_type{}, i, stage);
+      if (c0 + warp + i * kWarps < all_see) pass(std::false_type{}, i, stage);
       else pass(std::true_type{}, i, stage);
       __syncwarp();                                // every lane is done with the stage
       if (lane == 0) mbar_arrive(&empty[warp][stage]);
@@ -914,14 +915,14 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 2) paged_merge_kernel(const 
 PagedAttnPlan plan_paged_attn(int batch, int n_kv_heads, int rows, bool e4m3, int max_len, long long total_len) {
   PagedAttnPlan pl;
   const int chunk = e4m3 ? 2 * kSub : kSub;
-  const long long chunks = (max_len + chunk - 1) / chunk;
+  const long long chunks = chunk_count(max_len, e4m3 ? 5 : 4);
   // More than 8 query rows: 16 of them share an entry's loads, unless the call is so small that CTAs of 8 rows all run at once and
   // have some 512 entries or fewer each to go through (four query tokens, 16 and 8 rows a CTA, in us: one sequence of 250 entries,
   // 8 bits, 6.7 and 5.8, of 2000 8.9 and 8.1, of 13107 13.9 and 14.6; 16 of 380, bf16, 13.9 and 10.0; 32 of 819 to 1638, 8 bits,
   // 26.8 and 39).
-  const long long pairs_of_8 = static_cast<long long>(batch) * n_kv_heads * ((rows + 7) / 8);
+  const long long pairs_of_8 = static_cast<long long>(batch) * n_kv_heads * ((rows + 7LL) / 8);
   pl.row_tiles_of_8 = rows <= 8 || (pairs_of_8 <= kPagedCtas && pairs_of_8 * max_len <= 512LL * kPagedCtas) ? 1 : 2;
-  pl.row_tiles = (rows + 8 * pl.row_tiles_of_8 - 1) / (8 * pl.row_tiles_of_8);
+  pl.row_tiles = chunk_count(rows, pl.row_tiles_of_8 == 1 ? 3 : 4);
   const long long pairs = static_cast<long long>(batch) * n_kv_heads * pl.row_tiles;
   // Splits: as many as run at once, each with a chunk for every warp.  Short sequences stay whole: the merge costs 2 to 3 us, a
   // warp's pass over a chunk 0.75 us in 8 bits and 0.55 us in bf16 (one sequence, 8 bits: 400 entries 7.2 us whole and 6.7 in

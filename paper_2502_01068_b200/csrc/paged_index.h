@@ -38,6 +38,14 @@ FASTKV_HD int usable_len(int len, int max_pages, int page_log2) {
   return len > room ? static_cast<int>(room) : len;
 }
 
+// Chunks of 2^chunk_log2 entries that hold `len` >= 0 entries, without a sum that could pass 2^31 - 1.
+FASTKV_HD int chunk_count(int len, int chunk_log2) { return len <= 0 ? 0 : ((len - 1) >> chunk_log2) + 1; }
+// The first chunks of them that every one of q_len query tokens sees all of.
+FASTKV_HD int chunks_all_see(int len, int q_len, int chunk_log2) {
+  const int all = len - (q_len - 1);
+  return all <= 0 ? 0 : all >> chunk_log2;
+}
+
 // New rows of sequence b: [first, first + count) of the call's rows, cut to the rows that exist and to the room behind
 // `len` entries.  Returns whether nothing had to be cut.
 struct RowRange {
