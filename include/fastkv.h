@@ -224,7 +224,8 @@ typedef struct fastkv_paged_cache {
 /*
  * The rows one fastkv_paged_append call brings.  Sequence b owns rows cu_new[b] .. cu_new[b+1]-1 of the call's
  * [total] rows (cu_new == NULL: max_new rows each, total == batch * max_new); they become its entries lens[b],
- * lens[b] + 1, ...
+ * lens[b] + 1, ...  Rows that no sequence owns (a padded batch, cu_new[batch] < total) go into no page; their queries are rotated
+ * like the others.
  *   Source, new tokens (total_src == 0): k, v [total, n_kv_heads, head_dim] and, with n_q_heads > 0, q
  *     [total, n_q_heads, head_dim], bf16, strides in elements.
  *   Source, kept rows (total_src > 0): row r of KV head g is row cu_src[b] + idx[g, r] of k and v
@@ -251,7 +252,7 @@ typedef struct fastkv_new_rows {
 
 /*
  * Appends `rows` behind the lens[b] entries of every sequence, in one launch.  lens: DEVICE int32 [batch], read only;
- * new_lens (may be NULL, must not overlap lens): DEVICE int32 [batch], receives lens[b] plus the rows written.
+ * new_lens (may be NULL, must not overlap lens): DEVICE int32 [batch], receives lens[b] plus the rows that there is room for.
  * q_out: bf16, dense [total, n_q_heads, head_dim], the rotated queries; may be q itself when q is dense.
  * Bf16 pages and q_out: rotated in fp32, rounded once.  8-bit pages: a page that had entries keeps its scale unless a new
  * row needs a larger one (the smallest 2^e with 448 * 2^e >= the largest absolute value), in which case the entries that
@@ -259,9 +260,11 @@ typedef struct fastkv_new_rows {
  * need.  Codes are rounded once, from fp32, to nearest even.  Entries behind the new length and pages that no row falls in
  * are left as they were.
  * Reported in the status word (FASTKV_ERR_DEVICE_INDEX), never dereferenced: a page id outside the pool, an index outside
- * its sequence, rows beyond max_new, total or the block table's room; those rows are not written.  The status word is not
- * cleared by this call.  workspace: 256 bytes (the header), 256-byte aligned.  Calls that write the same sequences must be
- * ordered.
+ * its sequence, rows beyond max_new, total or the block table's room; those rows are not written.  A row that is refused for its
+ * page id or index keeps its slot, and new_lens counts it: read entries by new_lens only behind a status of 0.  After a wait that
+ * ran out (FASTKV_ERR_DEVICE_TIMEOUT) a KV head of a page, K or V, is either as it was or has all of the call's rows.
+ * workspace: 256 bytes (the header), 256-byte aligned.  The status word in it is not cleared by this call: zero a new workspace's
+ * first 256 bytes once (or use one that fastkv_score has seen).  Calls that write the same sequences must be ordered.
  */
 int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* rows, const int32_t* lens, const void* q,
                         const void* k, const void* v, const int32_t* pos, const float* inv_freq, const int32_t* idx,
@@ -275,12 +278,16 @@ int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* 
  * q: bf16, dense [batch, q_len, n_q_heads, head_dim], 16-byte aligned; out: fp32, the same shape; lse (optional): fp32
  * [batch, q_len, n_q_heads], natural log.  A query that sees no entry gives out 0 and lse -infinity.
  * What a query token does not see never reaches it, NaN and infinities included; a NaN that it sees makes the outputs that
- * depend on it NaN, an infinity makes them NaN or infinite.
+ * depend on it NaN, an infinity in V makes them NaN or infinite.  An entry whose logit is -infinity weighs nothing, a logit
+ * of +infinity makes its row NaN, and a query whose logits are all -infinity counts as one that sees no entry.
+ * Accuracy: products, maxima and sums in fp32.  8-bit pages: a query's elements below 2^-28 of its largest are rounded to
+ * multiples of 2^-38 of that; the weights of 32 neighbouring entries (16 for pages of 16) carry 22 bits, or 2^-39 of their largest.
  * max_len and total_len are what the HOST knows of lens (their maximum and sum, or bounds); they size the launch, and
  * results do not depend on them beyond rounding.  A length beyond the block table's room is cut to it, a page id outside the
- * pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
+ * pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear
+ * (zero a new workspace's first 256 bytes once).
  * workspace: >= fastkv_paged_attn_workspace_bytes for this cache and query, 256-byte aligned; not shared by calls that
- * may overlap.
+ * may overlap.  The size may rise and fall with max_len and total_len; 5 MiB are enough for all of them.
  */
 typedef struct fastkv_query {
   int32_t n_q_heads;         /* a multiple of the cache's n_kv_heads                                 */
