@@ -10,13 +10,14 @@
 // that both halves of every rotated pair are the lane's own.
 //   Row role   (bf16 pages; queries of either format): a lane group takes one token and a run of heads, so that the
 //              angles are formed once per run.  A prompt of 8192 tokens, 32 query and 8 KV heads of 128, bf16: 34.4 us, 89 % of a
-//              plain copy's rate over what it reads and writes.
+//              plain copy's rate over what it reads and writes; 13107 kept rows, 23.6 us, 70 %.
 //   Page role  (8-bit pages, calls of more than 8 rows per sequence): a block takes one page and walks a run of heads, whose rows
 //              of the page wait in shared memory while their largest absolute value is found and are encoded from there.
-//              some 36 900 rows in eight ragged prompts, rotated, with their queries: 147 us, 87 %; 13107 kept rows of 8 heads,
+//              some 36 900 rows in eight ragged prompts, rotated, with their queries: 148 us, 86 %; 13107 kept rows of 8 heads,
 //              gathered: 18 us, 69 % (launch and the chain length -> table -> index -> row take 4 of them).
 //   Small role (8-bit pages, up to 8 rows per sequence): a lane group for each new row of a (page, head); 64 sequences, one row
-//              each: 3.6 us, as good as launching and three dependent trips to memory.
+//              each: 3.6 us, as good as launching and three dependent trips to memory; 10 us where every page of 64 takes a larger
+//              scale, so that its old rows are encoded again.
 // Rows that were in a page before keep their codes unless the new rows need a larger scale; then the codes are re-encoded
 // by the ratio, a power of two, which is exact but for codes that become subnormal.
 #include "paged.cuh"

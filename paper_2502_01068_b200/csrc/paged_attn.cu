@@ -27,8 +27,8 @@
 // in all 2^-22 of sum p |v| and, step by step, 2^-39 of the largest weight times the sum of the |v|.
 //
 // Measured, in us (and the share of a plain copy's bandwidth over the bytes the entries take): one sequence of 131072 entries,
-// 8 bits, 47 (87 %); eight of 4K to 64K, 106 (91 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
-// tokens, 8 bits, 27 (48 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.4:
+// 8 bits, 46.6 (88 %); eight of 4K to 64K, 107 (91 %); 64 of 1638 to 2048, bf16, 75 (98 %); 32 of 819 to 1638 with four query
+// tokens, 8 bits, 27 (48 %: two row tiles double the products and the softmax, so that the instructions bound it); 257 entries 5.1:
 // launch, table -> page -> copy, one pass, merge.
 #include <type_traits>
 
