@@ -40,8 +40,9 @@ namespace {
 
 constexpr int kSub = 16;            // entries of one step of the second product; a page holds a whole number of them
 // 8-bit pages: the weights of the second product are 2^15 times too large, so that the remainder term of the largest of them is far
-// from fp16's subnormals, and the running outputs 2^32 times too small: 2^31 entries of the largest value, 448 * 2^120, stay finite.
-constexpr float kWeightGain = 32768.0f, kOutGain = 4294967296.0f;
+// from fp16's subnormals, and the running outputs 2^16 times too small, between fp32's two ends: 2^15 entries of the largest value,
+// 448 * 2^120, and all weights together stay finite, and a weight times V's scale keeps its bits down to 2^-95.
+constexpr float kWeightGain = 32768.0f, kOutGain = 65536.0f;
 constexpr float kScaleGain = 1.0f / (kWeightGain * kOutGain);   // what V's scale, 2^-64 or more, is multiplied by at the join
 
 __device__ __forceinline__ void ldsm_x4(uint32_t (&r)[4], uint32_t addr) {

@@ -64,7 +64,7 @@ def check_turned(pools, before, lens, news, k64, v64, rotated):
     old_scales = before[2].double().numpy()
     mine = torch.zeros(raw.shape[0], P, dtype=torch.bool)               # entries that the call may write
     for b, (n0, n) in enumerate(zip(lens, news)):
-        for pg in range(n0 // P, (n0 + n - 1) // P + 1):
+        for pg in range(n0 // P, (n0 + n - 1) // P + 1) if n else ():
             pid, first, lo, hi = int(pools.table_np[b, pg]), pg * P, max(n0, pg * P), min(n0 + n, pg * P + P)
             new = k64[b][lo - n0:hi - n0].transpose(1, 0, 2)             # [Hkv, m, d]
             slack = 2.0 ** -20 * np.abs(new).max(axis=-1, keepdims=True)

@@ -74,6 +74,24 @@ def test_a_large_page_of_little_weight(where, page, d, T):
     attend(pools, LENS, q, scale=1.0)
 
 
+@pytest.mark.parametrize("page,d,T", [(16, 128, 1), (64, 128, 3), (32, 64, 1)])
+def test_small_entries_of_little_weight(page, d, T):
+    """One page has all the weight, but zeros in every other column: there the others count alone, with 2^-63 of the weight and 2^-30 of
+    the usual scale, which fp32 holds."""
+    pools = Pools("e4m3", LENS, LENS, page, 2, d, 26, v_exp=(-30, -28))
+    pools.ks[:] = 2.0 ** -3
+    pools.k[:] = 0
+    pools.k[:, :, :, 0] = torch.tensor(-352.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+    for b, n in enumerate(LENS):
+        for pid in pages_of(pools, b, n, "middle"):
+            pools.k[pid, :, :, 0] = 0
+            pools.v[pid, :, :, ::2] &= 0x80
+    mirror(pools, LENS)
+    q = bf16_rows(np.random.default_rng(6), (len(LENS), T, 8, d), 0.1)
+    q[..., 0] = 1.0
+    attend(pools, LENS, q, scale=1.0)
+
+
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("n,at", [(1, 0), (70, 3), (70, 69)])
 def test_an_appended_infinity_costs_its_own_page_alone(page, n, at):
