@@ -301,6 +301,55 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
                       float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The attention weight that every cached entry draws, accumulated over steps (the fused attention of decoding never forms the
+ * attention matrix; an eviction needs its column sums).  For the query tokens that fastkv_paged_attn (or fastkv_prefix_attn) was
+ * called for, with the lse it wrote:
+ *   weights[b, g, t] = decay * weights[b, g, t] + sum over i and over heads h of group g, where i sees t, of
+ *                      exp(scale * <q[b, i, h], K[t, g]> - lse[b, i, h])
+ * for entries t of sequence b; what query token i sees is as in fastkv_paged_attn.  The last q_len entries are the query tokens' own:
+ * their weight starts here, what was in the array is not read.  weights: fp32 [batch, n_kv_heads, weights_stride]; what lies behind
+ * a sequence's length is neither read nor written.  q as in fastkv_paged_attn; lse: fp32 [batch, q_len, n_q_heads], natural log; a
+ * row whose lse is -infinity (a query that saw nothing) draws nothing.  decay: finite, >= 0.  What a query does not see never reaches
+ * a weight, NaN and infinities included.  Products, exponentials and sums in fp32, in a fixed order.
+ * max_len and total_len size the launch, as in fastkv_paged_attn.  A length beyond the block table's room or weights_stride is cut
+ * to it, a page id outside the pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which
+ * this call does not clear.  workspace: 256 bytes (the header), 256-byte aligned.
+ */
+int fastkv_paged_weights(const fastkv_paged_cache* cache, const fastkv_query* query, const int32_t* lens, const void* q,
+                         const float* lse, float decay, float* weights, int64_t weights_stride, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated weight, in place: KVCompress (App. B.1: per KV head the entries of largest score, the window always) for a
+ * cache that has grown while decoding.  A sequence with lens[b] > limit keeps, for each KV head, its last `window` entries and the
+ * m = keep - window others of largest weight (ties to the lower slot; -0 counts as 0, NaN as the lowest); the others are untouched.
+ * Entries move within the sequence's pages:
+ *   a kept entry in a slot below m, the window's aside, stays; the r-th free slot below m (ascending) takes the r-th other kept one
+ *   (ascending); window entry lens[b] - window + i goes to slot m + i.
+ * Slots behind the new length are left as they were; pages that lie there altogether may be given to other sequences.  8-bit pages: a
+ * page that receives entries takes the largest scale of the pages that its entries come from, its own among them if an entry stays;
+ * codes are encoded again, code * old / new, rounded to nearest even.
+ *   weights, ids: fp32 and int32 [batch, n_kv_heads, stride] (ids may be NULL; what the caller knows the entries by, positions say);
+ *   new_weights, new_ids: the same shape, receive those of the entries by their new slots (copies, for sequences that are not cut);
+ *   may not overlap weights and ids; new_ids goes with ids.  new_lens (may be NULL, must not overlap lens): int32 [batch].
+ * All pages a sequence of the call holds belong to it alone if it is cut.  A length below 0 or beyond max_len, stride or the block
+ * table's room leaves the sequence as it is, new_lens[b] = lens[b] and nothing written to new_weights and new_ids; a page id
+ * outside the pool is never dereferenced, rows that would be read from or written to it are not moved.  Both are reported in the
+ * status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
+ * workspace: >= fastkv_paged_evict_workspace_bytes, 256-byte aligned; not shared by calls that may overlap.
+ */
+typedef struct fastkv_eviction {
+  int32_t keep;              /* entries that a sequence is cut to, >= 1                              */
+  int32_t limit;             /* sequences with more entries are cut; >= keep                         */
+  int32_t window;            /* last entries that are always kept, 0 .. keep                         */
+  int32_t max_len;           /* HOST: longest length                                                 */
+} fastkv_eviction;
+int fastkv_paged_evict_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_eviction* eviction, size_t* bytes);
+int fastkv_paged_evict(const fastkv_paged_cache* cache, const fastkv_eviction* eviction, const int32_t* lens, const float* weights,
+                       const int32_t* ids, int64_t stride, float* new_weights, int32_t* new_ids, int32_t* new_lens,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Synchronises `stream`, then copies the device status word of `workspace` to the HOST
  * integers *status (a fastkv_status) and *site (which wait or check raised it; 0 if none).
  */
@@ -389,7 +438,7 @@ int fastkv_debug_set(const char* key, int64_t value);
 /*
  * Sum of the device durations (HOST double, milliseconds) and number of launches recorded for one
  * kernel class since the last query (0 scoring kernel, 1 pooling kernel, 2 selection, 3 compaction,
- * 4 decode attention, 5 prefill attention, 6 window scores, 7 paged append, 8 paged attention); waits for the recorded launches and forgets them.  *name receives a static
+ * 4 decode attention, 5 prefill attention, 6 window scores, 7 paged append, 8 paged attention, 9 accumulated weights, 10 eviction); waits for the recorded launches and forgets them.  *name receives a static
  * string.  Any of the three outputs may be NULL.  No counterpart in the paper (measurement aid).
  */
 int fastkv_debug_kernel_time(int32_t kernel, double* total_ms, int64_t* launches, const char** name);

@@ -25,6 +25,7 @@ ROT_HALVES, ROT_ADJACENT = 0, 1
 EXPORTS = ["fastkv_workspace_bytes", "fastkv_score", "fastkv_select_kv", "fastkv_select_tsp", "fastkv_select",
            "fastkv_compact", "fastkv_decode_attn_workspace_bytes", "fastkv_decode_attn", "fastkv_prefill_workspace_bytes",
            "fastkv_prefill_attention", "fastkv_paged_append", "fastkv_paged_attn_workspace_bytes", "fastkv_paged_attn",
+           "fastkv_paged_weights", "fastkv_paged_evict_workspace_bytes", "fastkv_paged_evict",
            "fastkv_device_status", "fastkv_layer_host_arena_bytes",
            "fastkv_layer_host", "fastkv_score_static", "fastkv_score_static_status", "fastkv_debug_set",
            "fastkv_debug_kernel_time",
@@ -87,6 +88,11 @@ class Query(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float), ("total_len", ctypes.c_int64)]
 
 
+class Eviction(ctypes.Structure):
+    """fastkv_eviction"""
+    _fields_ = [("keep", ctypes.c_int32), ("limit", ctypes.c_int32), ("window", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -122,6 +128,10 @@ def _load():
         lib.fastkv_paged_append.argtypes = [pc, pn] + [vp] * 10 + [sz, vp]
         lib.fastkv_paged_attn_workspace_bytes.argtypes = [pc, pq, ctypes.POINTER(sz)]
         lib.fastkv_paged_attn.argtypes = [pc, pq, vp, vp, vp, vp, vp, sz, vp]
+        pv = ctypes.POINTER(Eviction)
+        lib.fastkv_paged_weights.argtypes = [pc, pq, vp, vp, vp, ctypes.c_float, vp, ctypes.c_int64, vp, sz, vp]
+        lib.fastkv_paged_evict_workspace_bytes.argtypes = [pc, pv, ctypes.POINTER(sz)]
+        lib.fastkv_paged_evict.argtypes = [pc, pv, vp, vp, vp, ctypes.c_int64, vp, vp, vp, vp, sz, vp]
         lib.fastkv_score_static_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
         lib.fastkv_debug_set.argtypes = [ctypes.c_char_p, ctypes.c_int64]
         lib.fastkv_debug_kernel_time.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_double),
@@ -360,6 +370,59 @@ def fastkv_paged_attn(cache: PagedCache, query: Query, lens, q, out, lse, worksp
         torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
     if rc != FASTKV_OK:
         raise FastKVError(rc, "fastkv_paged_attn")
+
+
+def _entry_rows(cache: PagedCache, x, dtype, name: str):
+    """Weights or ids: dense [batch, n_kv_heads, stride], on the cache's device."""
+    if x.dim() != 3 or x.shape[0] != cache.batch or x.shape[1] != cache.n_kv_heads or x.dtype != dtype:
+        raise ValueError("%s: %s [batch, n_kv_heads, stride]" % (name, dtype))
+    if not x.is_contiguous() or x.device != cache._device:
+        raise ValueError("%s must be dense and on the cache's device" % name)
+
+
+def fastkv_paged_weights(cache: PagedCache, query: Query, lens, q, lse, decay: float, weights, workspace, stream=None) -> None:
+    """Add the attention weight that query.q_len new tokens per sequence give each entry to decay * weights; see the header."""
+    dev = _here(cache)
+    _entry_rows(cache, weights, torch.float32, "weights")
+    rc = (_lib or _load()).fastkv_paged_weights(
+        cache, query, None if lens is None else lens.data_ptr(), None if q is None else q.data_ptr(),
+        None if lse is None else lse.data_ptr(), decay, weights.data_ptr(), weights.shape[2], workspace.data_ptr(), workspace.nbytes,
+        torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if rc != FASTKV_OK:
+        raise FastKVError(rc, "fastkv_paged_weights")
+
+
+def make_eviction(*, keep: int, max_len: int, limit: Optional[int] = None, window: int = 8) -> Eviction:
+    """Fill a fastkv_eviction; limit defaults to keep."""
+    v = Eviction()
+    v.keep, v.limit, v.window, v.max_len = keep, keep if limit is None else limit, window, max_len
+    return v
+
+
+def fastkv_paged_evict_workspace_bytes(cache: PagedCache, eviction: Eviction) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_load().fastkv_paged_evict_workspace_bytes(ctypes.byref(cache), ctypes.byref(eviction), ctypes.byref(n)),
+           "fastkv_paged_evict_workspace_bytes")
+    return int(n.value)
+
+
+def fastkv_paged_evict(cache: PagedCache, eviction: Eviction, lens, weights, ids, new_weights, new_ids, new_lens, workspace,
+                       stream=None) -> None:
+    """Cut sequences of more than eviction.limit entries to eviction.keep, by weight, in place; see the header."""
+    dev = _here(cache)
+    _entry_rows(cache, weights, torch.float32, "weights")
+    for x, dtype, name in ((new_weights, torch.float32, "new_weights"), (ids, torch.int32, "ids"), (new_ids, torch.int32, "new_ids")):
+        if x is not None:
+            _entry_rows(cache, x, dtype, name)
+            if x.shape != weights.shape:
+                raise ValueError("%s is shaped like weights" % name)
+    rc = (_lib or _load()).fastkv_paged_evict(
+        cache, eviction, None if lens is None else lens.data_ptr(), weights.data_ptr(), None if ids is None else ids.data_ptr(),
+        weights.shape[2], None if new_weights is None else new_weights.data_ptr(), None if new_ids is None else new_ids.data_ptr(),
+        None if new_lens is None else new_lens.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+        torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if rc != FASTKV_OK:
+        raise FastKVError(rc, "fastkv_paged_evict")
 
 
 def fastkv_device_status(workspace, stream=None):

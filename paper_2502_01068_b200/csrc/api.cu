@@ -55,9 +55,10 @@ DebugConfig g_debug;
 
 // ---- optional per-kernel timing ("time_kernels" hook): a pair of events around every launch ----------
 enum KernelId { KID_SCORE = 0, KID_POOL = 1, KID_SELECT = 2, KID_COMPACT = 3, KID_DECODE = 4, KID_PREFILL = 5,
-                KID_WINDOW_SCORES = 6, KID_PAGED_APPEND = 7, KID_PAGED_ATTN = 8, KID_COUNT = 9 };
+                KID_WINDOW_SCORES = 6, KID_PAGED_APPEND = 7, KID_PAGED_ATTN = 8,
+                KID_PAGED_WEIGHTS = 9, KID_PAGED_EVICT = 10, KID_COUNT = 11 };
 const char* const kKernelNames[KID_COUNT] = {"score", "pool", "select", "compact", "decode_attn", "prefill_attn",
-                                             "window_scores", "paged_append", "paged_attn"};
+                                             "window_scores", "paged_append", "paged_attn", "paged_weights", "paged_evict"};
 struct KernelTimes {
   bool on = false;
   std::mutex mu;
@@ -882,6 +883,9 @@ int check_query(const fastkv_paged_cache* c, const fastkv_query* q) {
   if (rows > 0x7fffffffLL) return fail(FASTKV_ERR_UNSUPPORTED, "paged_attn: more than 2^31 - 1 query rows");
   return FASTKV_OK;
 }
+float softmax_scale_of(const fastkv_paged_cache& c, const fastkv_query& q) {
+  return q.softmax_scale > 0.0f ? q.softmax_scale : 1.0f / std::sqrt(static_cast<float>(c.head_dim));
+}
 PagedAttnPlan plan_of(const fastkv_paged_cache& c, const fastkv_query& q) {
   const long long total = q.total_len > 0 ? q.total_len : static_cast<long long>(c.batch) * q.max_len;
   return plan_paged_attn(c.batch, c.n_kv_heads, q.n_q_heads / c.n_kv_heads * q.q_len, c.format == FASTKV_CACHE_E4M3, q.max_len,
@@ -1007,8 +1011,7 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   }
   p.c = paged_view(c);
   p.n_q_heads = query->n_q_heads; p.group = G; p.q_len = query->q_len; p.rows = rows;
-  const float scale = query->softmax_scale > 0.0f ? query->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c.head_dim));
-  p.scale_log2 = scale * 1.4426950408889634f;
+  p.scale_log2 = softmax_scale_of(c, *query) * 1.4426950408889634f;
   p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.part_ml = reinterpret_cast<float2*>(ws + sizeof(WorkspaceHeader));
@@ -1024,6 +1027,119 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
   }
   g_launches += launched;
   if (e != cudaSuccess) return cuda_fail(e, "paged_attn_kernel launch");
+  return FASTKV_OK;
+}
+
+namespace {
+bool overlap(const void* a, const void* b, unsigned long long bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < bytes : x - y < bytes;
+}
+// fp32 or int32 rows for every (sequence, KV head)
+int check_entry_rows(const char* call, const fastkv_paged_cache& c, int64_t stride) {
+  if (stride < 1) return fail(FASTKV_ERR_INVALID_ARG, "%s: the stride of the weights must be >= 1", call);
+  if (stride > (1ll << 31)) return fail(FASTKV_ERR_UNSUPPORTED, "%s: weights of more than 2^31 entries a row", call);
+  if (static_cast<long long>(c.batch) * c.n_kv_heads > 65535)
+    return fail(FASTKV_ERR_UNSUPPORTED, "%s: more than 65535 (sequence, KV head) pairs", call);
+  return FASTKV_OK;
+}
+}  // namespace
+
+int fastkv_paged_weights(const fastkv_paged_cache* cache, const fastkv_query* query, const int32_t* lens, const void* q,
+                         const float* lse, float decay, float* weights, int64_t weights_stride, void* workspace,
+                         size_t workspace_bytes, void* stream_) {
+  int rc = check_query(cache, query);
+  if (rc) return rc;
+  if (!lens || !q || !lse || !weights) return fail(FASTKV_ERR_INVALID_ARG, "paged_weights: lens, q, lse and weights are required");
+  if (!(decay >= 0.0f) || std::isinf(decay)) return fail(FASTKV_ERR_INVALID_ARG, "paged_weights: decay must be finite and >= 0");
+  if (reinterpret_cast<uintptr_t>(q) % 16) return fail(FASTKV_ERR_UNSUPPORTED, "paged_weights: q must be 16-byte aligned");
+  const fastkv_paged_cache& c = *cache;
+  if ((rc = check_entry_rows("paged_weights", c, weights_stride))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader)))) return rc;
+  if ((rc = check_device())) return rc;
+  PagedWeightsParams p;
+  memset(&p, 0, sizeof p);
+  p.c = paged_view(c);
+  p.n_q_heads = query->n_q_heads; p.group = query->n_q_heads / c.n_kv_heads; p.q_len = query->q_len; p.rows = p.group * p.q_len;
+  p.scale = softmax_scale_of(c, *query); p.decay = decay;
+  p.total_len = query->total_len > 0 ? query->total_len : static_cast<long long>(c.batch) * query->max_len;
+  p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.lse = lse; p.weights = weights; p.stride = weights_stride;
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  cudaError_t e;
+  {
+    TimedLaunch timed(KID_PAGED_WEIGHTS, static_cast<cudaStream_t>(stream_));
+    e = launch_paged_weights(p, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_));
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "paged_weights_kernel launch");
+  ++g_launches;
+  return FASTKV_OK;
+}
+
+namespace {
+int check_eviction(const fastkv_paged_cache* c, const fastkv_eviction* v) {
+  int rc = check_paged_cache(c);
+  if (rc) return rc;
+  if (v == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: eviction is NULL");
+  if (v->keep < 1 || v->limit < v->keep) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: need 1 <= keep <= limit");
+  if (v->window < 0 || v->window > v->keep) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: window must be in 0 .. keep");
+  if (v->max_len < 1) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: max_len must be >= 1");
+  return FASTKV_OK;
+}
+size_t evict_bytes(const fastkv_paged_cache& c, const fastkv_eviction& v) {
+  // a call that can cut nothing plans nothing
+  const size_t pairs = v.max_len > v.limit ? static_cast<size_t>(c.batch) * c.n_kv_heads : 0;
+  return round_up(sizeof(WorkspaceHeader) + pairs * evict_plan_words(v.keep, v.window) * sizeof(int), 256);
+}
+}  // namespace
+
+int fastkv_paged_evict_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_eviction* eviction, size_t* bytes) {
+  int rc = check_eviction(cache, eviction);
+  if (rc) return rc;
+  if (bytes == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = evict_bytes(*cache, *eviction);
+  return FASTKV_OK;
+}
+
+int fastkv_paged_evict(const fastkv_paged_cache* cache, const fastkv_eviction* eviction, const int32_t* lens, const float* weights,
+                       const int32_t* ids, int64_t stride, float* new_weights, int32_t* new_ids, int32_t* new_lens,
+                       void* workspace, size_t workspace_bytes, void* stream_) {
+  int rc = check_eviction(cache, eviction);
+  if (rc) return rc;
+  if (!lens || !weights || !new_weights) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: lens, weights and new_weights are required");
+  if ((ids != nullptr) != (new_ids != nullptr)) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: ids and new_ids go together");
+  const fastkv_paged_cache& c = *cache;
+  if ((rc = check_entry_rows("paged_evict", c, stride))) return rc;
+  const unsigned long long bytes = static_cast<unsigned long long>(c.batch) * c.n_kv_heads * stride * 4;
+  const void* in[2] = {weights, ids};
+  const void* out[2] = {new_weights, new_ids};
+  for (const void* x : in)
+    for (const void* y : out)
+      if (x != nullptr && y != nullptr && overlap(x, y, bytes))
+        return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: new_weights and new_ids must not overlap weights and ids");
+  if (new_ids != nullptr && overlap(new_weights, new_ids, bytes)) return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: new_weights and new_ids must not overlap");
+  if (new_lens != nullptr && overlap(lens, new_lens, static_cast<unsigned long long>(c.batch) * 4))
+    return fail(FASTKV_ERR_INVALID_ARG, "paged_evict: new_lens must not overlap lens");
+  if ((rc = check_workspace(workspace, workspace_bytes, evict_bytes(c, *eviction)))) return rc;
+  if ((rc = check_device())) return rc;
+  EvictParams p;
+  memset(&p, 0, sizeof p);
+  p.c = paged_view(c);
+  p.keep = eviction->keep; p.limit = eviction->limit; p.window = eviction->window; p.max_len = eviction->max_len;
+  p.row_bytes = c.head_dim * (c.format == FASTKV_CACHE_E4M3 ? 1 : 2);
+  p.lens = lens; p.new_lens = new_lens; p.weights = weights; p.ids = ids; p.new_weights = new_weights; p.new_ids = new_ids; p.stride = stride;
+  p.plan = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  cudaError_t e;
+  {
+    TimedLaunch timed(KID_PAGED_EVICT, static_cast<cudaStream_t>(stream_));
+    e = launch_evict_plan(p, static_cast<cudaStream_t>(stream_));
+    if (e == cudaSuccess) {
+      ++g_launches;
+      e = launch_evict_move(p, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_));
+    }
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "paged_evict kernels launch");
+  ++g_launches;
   return FASTKV_OK;
 }
 

@@ -63,6 +63,10 @@ enum Site : int {
   SITE_PAGED_LEN = 41,
   SITE_APPEND_WAIT = 42,
   SITE_PAGED_EMPTY = 43,
+  SITE_WEIGHTS_PAGE = 44,
+  SITE_WEIGHTS_LEN = 45,
+  SITE_EVICT_PAGE = 46,
+  SITE_EVICT_LEN = 47,
 };
 
 // Records `text` as the calling thread's last error (see fastkv_last_error) and returns `status`.

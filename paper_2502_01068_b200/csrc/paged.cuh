@@ -76,4 +76,38 @@ inline int paged_box_rows(bool e4m3, int page_size) { return e4m3 && page_size >
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
                               int head_dim, bool e4m3, cudaStream_t stream, int* launches);
 
+struct PagedWeightsParams {
+  PagedView c;
+  int n_q_heads, group, q_len, rows;     // rows = group * q_len query rows per (sequence, KV head)
+  int ctas;                   // CTAs that share all entries, filled in by the launcher
+  float scale, decay;
+  long long total_len;        // HOST: entries of all sequences (grid sizing)
+  const int* lens;
+  const uint16_t* q;          // [B][q_len][Hq][d]
+  const float* lse;           // [B][q_len][Hq], natural log
+  float* weights;             // [B][Hkv][stride]
+  long long stride;
+  WorkspaceHeader* hdr;
+};
+cudaError_t launch_paged_weights(PagedWeightsParams& p, int head_dim, bool e4m3, cudaStream_t stream);
+
+struct EvictParams {
+  PagedView c;
+  int keep, limit, window, max_len, row_bytes;
+  const int* lens;
+  int* new_lens;
+  const float* weights;       // [B][Hkv][stride], as ids, new_weights and new_ids
+  const int* ids;             // may be null
+  float* new_weights;
+  int* new_ids;               // null with ids
+  long long stride;
+  int* plan;                  // [B][Hkv][evict_plan_words]
+  WorkspaceHeader* hdr;
+};
+// A (sequence, KV head)'s plan: how many of the first keep - window slots keep their entry; for each of those slots -1 or the
+// number of the entry that moves in; the slots of the kept candidates by rank (written from the first that moves on).
+inline long long evict_plan_words(int keep, int window) { return (2ll * (keep - window) + 1 + 3) / 4 * 4; }
+cudaError_t launch_evict_plan(const EvictParams& p, cudaStream_t stream);
+cudaError_t launch_evict_move(const EvictParams& p, bool e4m3, cudaStream_t stream);
+
 }  // namespace fastkv

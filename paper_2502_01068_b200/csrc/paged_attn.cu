@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "paged.cuh"
+#include "paged_mma.cuh"
 
 namespace fastkv {
 
@@ -44,56 +45,6 @@ constexpr int kSub = 16;            // entries of one step of the second product
 // 448 * 2^120, and all weights together stay finite, and a weight times V's scale keeps its bits down to 2^-95.
 constexpr float kWeightGain = 32768.0f, kOutGain = 65536.0f;
 constexpr float kScaleGain = 1.0f / (kWeightGain * kOutGain);   // what V's scale, 2^-64 or more, is multiplied by at the join
-
-__device__ __forceinline__ void ldsm_x4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ldsm_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-// D[16x8] += A[16x16] B[16x8], fp32 accumulators; `first`: D = A B.
-template <bool kHalf>
-__device__ __forceinline__ void mma16(float (&c)[4], bool first, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  const float z0 = first ? 0.0f : c[0], z1 = first ? 0.0f : c[1], z2 = first ? 0.0f : c[2], z3 = first ? 0.0f : c[3];
-  if constexpr (kHalf)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
-}
-// Two floats to a pair of 16-bit values (`lo` in the low half), and what the rounding left over.
-template <bool kHalf>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
-  uint32_t r;
-  if constexpr (kHalf) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-template <bool kHalf>
-__device__ __forceinline__ void unpack16(uint32_t w, float& lo, float& hi) {
-  if constexpr (kHalf) {
-    asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(w));
-  } else {
-    lo = __uint_as_float(w << 16);
-    hi = __uint_as_float(w & 0xffff0000u);
-  }
-}
-// The two low, or the two high, codes of a word as fp16 values.
-__device__ __forceinline__ uint32_t widen_lo(uint32_t w) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\t}" : "=r"(r) : "r"(w));
-  return r;
-}
-__device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, b;\n\t}" : "=r"(r) : "r"(w));
-  return r;
-}
 
 // All ones in the elements of a word that are NaN or infinite.
 template <bool kE4M3>

@@ -1,0 +1,165 @@
+"""Accumulated attention weights of paged entries against the 64-bit formula."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_01068_b200 import binding as B
+from tests.paged_reference import Pools
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(pools, q, lse, lens, old, decay, scale):
+    """(weights, bound on the error): q [B, T, Hq, d] float64, lse [B, T, Hq] as given, old [B, Hkv, stride].
+
+    A logit is off by at most d 2^-23 of sum scale |q k| (d products summed in fp32, cut off or rounded), its difference to lse and
+    the exponent's scaling by 2^-23 of their size, the exponential by 2^-21; the sums and the decay by one rounding each."""
+    want, slack = old.copy(), np.zeros_like(old)
+    Bn, T, Hq, d = q.shape
+    G = Hq // pools.Hkv
+    for b in range(Bn):
+        n = lens[b]
+        k = pools.k64[b][:n]
+        for g in range(pools.Hkv):
+            w, e = np.zeros(n), np.zeros(n)
+            for i in range(T):
+                sees = max(0, n - (T - 1 - i))
+                for h in range(g * G, (g + 1) * G):
+                    if lse[b, i, h] == -np.inf:
+                        continue
+                    x = scale * (k[:sees, g] @ q[b, i, h])
+                    size = scale * (np.abs(k[:sees, g]) @ np.abs(q[b, i, h]))
+                    p = np.exp(x - lse[b, i, h])
+                    w[:sees] += p
+                    e[:sees] += p * (d * 2.0 ** -23 * size + 2.0 ** -22 * (np.abs(x) + abs(lse[b, i, h])) + 2.0 ** -21)
+            first = max(0, n - T)
+            w[:first] += decay * old[b, g, :first]
+            want[b, g, :n] = w
+            slack[b, g, :n] = e + (T * G + 4) * 2.0 ** -24 * w + 2.0 ** -120
+    return want, slack
+
+
+def lse_of(pools, q, lens, scale):
+    Bn, T, Hq, d = q.shape
+    G = Hq // pools.Hkv
+    out = np.full((Bn, T, Hq), -np.inf)
+    for b in range(Bn):
+        for i in range(T):
+            sees = lens[b] - (T - 1 - i)
+            for h in range(Hq):
+                if sees > 0:
+                    x = scale * (pools.k64[b][:sees, h // G] @ q[b, i, h])
+                    out[b, i, h] = x.max() + math.log(np.exp(x - x.max()).sum())
+    return out.astype(np.float32)
+
+
+def workspace():
+    return torch.zeros(256, dtype=torch.uint8, device="cuda")
+
+
+def run(fmt, lens, page, Hq, Hkv, d, T=1, decay=1.0, seed=0, stride=None, scale=0.0, gain=1.0, total_len=None):
+    rng = np.random.default_rng(seed)
+    pools = Pools(fmt, lens, lens, page, Hkv, d, seed + 1)
+    q = torch.from_numpy(rng.standard_normal((len(lens), T, Hq, d)) * gain).to(torch.bfloat16)
+    q64 = q.double().numpy()
+    by = scale or 1.0 / math.sqrt(d)
+    lse = lse_of(pools, q64, lens, by)
+    stride = stride or max(max(lens), 1) + 5
+    old = np.exp(rng.standard_normal((len(lens), Hkv, stride))).astype(np.float32)
+    for b, n in enumerate(lens):                          # what may not be read: NaN
+        old[b, :, max(0, n - T):] = np.nan
+    w = torch.from_numpy(old).cuda()
+    ws = workspace()
+    query = B.make_query(n_q_heads=Hq, q_len=T, max_len=max(max(lens), 1), total_len=sum(lens) if total_len is None else total_len,
+                         softmax_scale=scale)
+    B.fastkv_paged_weights(pools.cache(), query, pools.dev_lens, q.cuda(), torch.from_numpy(lse).cuda(), decay, w, ws)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    want, slack = reference(pools, q64, lse.astype(np.float64), lens, old.astype(np.float64), float(np.float32(decay)), by)
+    got = w.cpu().double().numpy()
+    for b, n in enumerate(lens):
+        assert np.array_equal(got[b, :, n:], old[b, :, n:].astype(np.float64), equal_nan=True), "rows behind the end"
+        bad = ~(np.abs(got[b, :, :n] - want[b, :, :n]) <= slack[b, :, :n])
+        assert not bad.any(), (b, np.argwhere(bad)[:5], got[b, :, :n][bad][:5], want[b, :, :n][bad][:5])
+    return got
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hq,Hkv,T", [(4, 1, 1), (6, 2, 1), (8, 8, 3), (32, 4, 2), (14, 2, 5)])
+def test_against_the_formula(fmt, d, page, Hq, Hkv, T):
+    run(fmt, [1, 257, 16, 700, 33], page, Hq, Hkv, d, T, decay=0.75, seed=page + T)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [0, 1, 15, 127, 128, 129, 255, 511, 512, 513, 1500])
+def test_lengths(fmt, n):
+    run(fmt, [n], 16, 4, 1, 128, seed=n)
+    run(fmt, [3, n, 0, 40], 32, 4, 2, 64, T=2, seed=n)
+
+
+def test_many_sequences_and_a_bound_that_is_off():
+    lens = [int(x) for x in np.random.default_rng(5).integers(0, 90, 300)]
+    run("bf16", lens, 16, 2, 2, 64, seed=9)
+    run("e4m3", lens, 16, 2, 1, 128, seed=9, total_len=1)
+
+
+def test_query_tokens_ahead_of_the_cache():
+    """More query tokens than entries: the first ones see nothing, their lse is -infinity and they draw nothing."""
+    run("bf16", [2, 1, 0, 5], 16, 4, 2, 64, T=4, seed=3)
+
+
+def test_scale_and_sharp_rows():
+    run("bf16", [300], 16, 8, 2, 128, scale=0.5, gain=4.0, seed=4)
+    run("e4m3", [300], 16, 8, 2, 128, scale=0.25, gain=4.0, seed=4)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_what_a_query_does_not_see_never_reaches_a_weight(fmt):
+    """The last token's key is NaN: the first query token's row has no part of it."""
+    pools = Pools(fmt, [40], [40], 16, 1, 64, 1)
+    pid = int(pools.table_np[0, 39 // 16])
+    (pools.k if fmt == "bf16" else pools.k.view(torch.float8_e4m3fn))[pid, :, 39 % 16] = float("nan")
+    q = torch.randn(1, 2, 2, 64, device="cuda").to(torch.bfloat16)
+    lse = torch.tensor([[[0.0, 0.0], [0.0, -math.inf]]], device="cuda")
+    w, ws = torch.zeros(1, 1, 40, device="cuda"), workspace()
+    B.fastkv_paged_weights(pools.cache(), B.make_query(n_q_heads=2, q_len=2, max_len=40), pools.dev_lens, q, lse, 1.0, w, ws)
+    x = w[0, 0].cpu()
+    assert torch.isfinite(x[:39]).all() and torch.isnan(x[39])
+
+
+def test_reports_and_keeps_to_its_rows():
+    pools = Pools("bf16", [100, 50], [100, 50], 16, 1, 64, 1)
+    pools.table[0, 1] = 10 ** 6
+    lens = torch.tensor([1000, 50], dtype=torch.int32, device="cuda")           # beyond the table's room of 112
+    q = torch.randn(2, 1, 2, 64, device="cuda").to(torch.bfloat16)
+    w, ws = torch.full((2, 1, 60), 7.0, device="cuda"), workspace()
+    B.fastkv_paged_weights(pools.cache(), B.make_query(n_q_heads=2, max_len=112), lens, q, torch.zeros(2, 1, 2, device="cuda"), 1.0, w, ws)
+    assert B.fastkv_device_status(ws)[0] == B.ERR_DEVICE_INDEX
+    assert (w[1, 0, 50:] == 7.0).all() and not (w[1, 0, :50] == 7.0).any()
+
+
+def test_same_bits_twice_on_a_stream_and_from_a_graph():
+    pools = Pools("e4m3", [900, 40, 333], [900, 40, 333], 32, 2, 128, 1)
+    q = torch.randn(3, 2, 8, 128, device="cuda").to(torch.bfloat16)
+    lse = torch.full((3, 2, 8), 4.0, device="cuda")
+    query = B.make_query(n_q_heads=8, q_len=2, max_len=900, total_len=1273)
+    first = torch.rand(3, 2, 900, device="cuda")
+    cache, ws = pools.cache(), workspace()
+    a = first.clone()
+    B.fastkv_paged_weights(cache, query, pools.dev_lens, q, lse, 0.5, a, ws)
+    b, side = first.clone(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.fastkv_paged_weights(cache, query, pools.dev_lens, q, lse, 0.5, b, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    c = first.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.fastkv_paged_weights(cache, query, pools.dev_lens, q, lse, 0.5, c, ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and torch.equal(a, c)
