@@ -301,6 +301,39 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
                       float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The same attention for sequences that share a long prefix (one document or system prompt behind a batch of requests; several answers
+ * to one prompt): the prefix's entries are in pages of their own, in the cache's pools, and are attended once for all sequences that
+ * share them.  `cache` and `lens` describe the sequences' own entries, behind the prefix: query token i of sequence b sees all entries
+ * of b's prefix and its own entries 0 .. lens[b] - (q_len - 1 - i) - 1, and the softmax runs over both together.
+ * Sequences cu_seqs[p] .. cu_seqs[p + 1] - 1 share prefix p; cu_seqs ascends (equal values: a prefix that nobody uses); sequences before
+ * the first and behind the last have no prefix.  cu_seqs == NULL: one prefix that all share.  prefix->lens may be 0.
+ * q: bf16, dense [batch, q_len, n_q_heads, head_dim], 16-byte aligned; out: bf16, the same shape, 16-byte aligned; lse (optional): fp32
+ * [batch, q_len, n_q_heads], natural log, over prefix and own entries (what fastkv_paged_weights wants for the own entries).
+ * A query that sees no entry gives out 0 and lse -infinity.  NaN and infinities as in fastkv_paged_attn; what lies behind a prefix's
+ * last entry in its page never reaches an output.
+ * Accuracy: products with the prefix in bf16 x bf16 -> fp32 (8-bit entries widen exactly), the softmax's weights of prefix entries
+ * rounded to bf16, all sums and the merge in fp32, one rounding to bf16 at the end; own entries as in fastkv_paged_attn.
+ * max_len of `prefix` and of `query` and total_len size the launch only.  A length beyond the table's room is cut to it, a page id
+ * outside the pool reads page 0 instead, a cu_seqs that descends or leaves 0 .. batch leaves the outputs of prefixed sequences
+ * unspecified; all are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
+ * At most 1024 prefixes and 128 query heads per KV head.
+ * workspace: >= fastkv_prefix_attn_workspace_bytes, 256-byte aligned; not shared by calls that may overlap.
+ */
+typedef struct fastkv_prefix {
+  int32_t n_prefixes;        /* >= 1: rows of table                                                  */
+  int32_t max_pages;         /* pages a row of table has room for                                    */
+  int32_t max_len;           /* HOST: longest prefix, >= 1                                           */
+  int32_t reserved;          /* 0                                                                    */
+  const int32_t* table;      /* DEVICE int32 [n_prefixes, max_pages]: pages of the cache's pools     */
+  const int32_t* lens;       /* DEVICE int32 [n_prefixes]                                            */
+  const int32_t* cu_seqs;    /* DEVICE int32 [n_prefixes + 1], or NULL with one prefix               */
+} fastkv_prefix;
+int fastkv_prefix_attn_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_prefix* prefix, const fastkv_query* query,
+                                       size_t* bytes);
+int fastkv_prefix_attn(const fastkv_paged_cache* cache, const fastkv_prefix* prefix, const fastkv_query* query, const int32_t* lens,
+                       const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The attention weight that every cached entry draws, accumulated over steps (the fused attention of decoding never forms the
  * attention matrix; an eviction needs its column sums).  For the query tokens that fastkv_paged_attn (or fastkv_prefix_attn) was
  * called for, with the lse it wrote:
@@ -426,6 +459,8 @@ int fastkv_score_static_status(void* stream, int32_t* status, int32_t* site);
  *                         segment, the paged append (new tokens into 8-bit pages, more than 8 rows per sequence) those of
  *                         every block's n-th head; with a short wait limit the wait for them runs out without any fault
  *                         (timeout test); 0: off
+ *   "prefix_skip_commit"  n > 0: the prefix attention withholds the signal that S of the n-th chunk of every CTA's share is ready
+ *                         (first row tile); with a short wait limit the waits for it run out without any fault (timeout test); 0: off
  *   "paged_two_maps"      1: the paged attention copies K and V pages through a tensor map each, as it does for pools
  *                         that lie 2^40 bytes or more apart (test); 0: through one map where it can
  *   "time_kernels"        1: record a pair of CUDA events around every kernel the library launches
@@ -438,7 +473,8 @@ int fastkv_debug_set(const char* key, int64_t value);
 /*
  * Sum of the device durations (HOST double, milliseconds) and number of launches recorded for one
  * kernel class since the last query (0 scoring kernel, 1 pooling kernel, 2 selection, 3 compaction,
- * 4 decode attention, 5 prefill attention, 6 window scores, 7 paged append, 8 paged attention, 9 accumulated weights, 10 eviction); waits for the recorded launches and forgets them.  *name receives a static
+ * 4 decode attention, 5 prefill attention, 6 window scores, 7 paged append, 8 paged attention, 9 accumulated weights, 10 eviction,
+ * 11 prefix attention and its merge); waits for the recorded launches and forgets them.  *name receives a static
  * string.  Any of the three outputs may be NULL.  No counterpart in the paper (measurement aid).
  */
 int fastkv_debug_kernel_time(int32_t kernel, double* total_ms, int64_t* launches, const char** name);

@@ -25,6 +25,7 @@ ROT_HALVES, ROT_ADJACENT = 0, 1
 EXPORTS = ["fastkv_workspace_bytes", "fastkv_score", "fastkv_select_kv", "fastkv_select_tsp", "fastkv_select",
            "fastkv_compact", "fastkv_decode_attn_workspace_bytes", "fastkv_decode_attn", "fastkv_prefill_workspace_bytes",
            "fastkv_prefill_attention", "fastkv_paged_append", "fastkv_paged_attn_workspace_bytes", "fastkv_paged_attn",
+           "fastkv_prefix_attn_workspace_bytes", "fastkv_prefix_attn",
            "fastkv_paged_weights", "fastkv_paged_evict_workspace_bytes", "fastkv_paged_evict",
            "fastkv_device_status", "fastkv_layer_host_arena_bytes",
            "fastkv_layer_host", "fastkv_score_static", "fastkv_score_static_status", "fastkv_debug_set",
@@ -88,6 +89,13 @@ class Query(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float), ("total_len", ctypes.c_int64)]
 
 
+class Prefix(ctypes.Structure):
+    """fastkv_prefix"""
+    _fields_ = [("n_prefixes", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("cu_seqs", ctypes.c_void_p)]
+    _device = None                      # where its tensors are (make_prefix)
+
+
 class Eviction(ctypes.Structure):
     """fastkv_eviction"""
     _fields_ = [("keep", ctypes.c_int32), ("limit", ctypes.c_int32), ("window", ctypes.c_int32), ("max_len", ctypes.c_int32)]
@@ -128,6 +136,9 @@ def _load():
         lib.fastkv_paged_append.argtypes = [pc, pn] + [vp] * 10 + [sz, vp]
         lib.fastkv_paged_attn_workspace_bytes.argtypes = [pc, pq, ctypes.POINTER(sz)]
         lib.fastkv_paged_attn.argtypes = [pc, pq, vp, vp, vp, vp, vp, sz, vp]
+        px = ctypes.POINTER(Prefix)
+        lib.fastkv_prefix_attn_workspace_bytes.argtypes = [pc, px, pq, ctypes.POINTER(sz)]
+        lib.fastkv_prefix_attn.argtypes = [pc, px, pq, vp, vp, vp, vp, vp, sz, vp]
         pv = ctypes.POINTER(Eviction)
         lib.fastkv_paged_weights.argtypes = [pc, pq, vp, vp, vp, ctypes.c_float, vp, ctypes.c_int64, vp, sz, vp]
         lib.fastkv_paged_evict_workspace_bytes.argtypes = [pc, pv, ctypes.POINTER(sz)]
@@ -370,6 +381,46 @@ def fastkv_paged_attn(cache: PagedCache, query: Query, lens, q, out, lse, worksp
         torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
     if rc != FASTKV_OK:
         raise FastKVError(rc, "fastkv_paged_attn")
+
+
+def make_prefix(table, lens, *, max_len: int, cu_seqs=None) -> Prefix:
+    """Fill a fastkv_prefix: table int32 [n_prefixes, max_pages], lens int32 [n_prefixes], cu_seqs int32 [n_prefixes + 1] (not needed
+    with one prefix that all sequences share).  All dense, on the cache's device."""
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("table is int32 [n_prefixes, max_pages]")
+    n = table.shape[0]
+    for x, size, name in ((lens, n, "lens"), (cu_seqs, n + 1, "cu_seqs")):
+        if x is not None and (x.dtype != torch.int32 or x.dim() != 1 or x.shape[0] != size):
+            raise ValueError("%s is int32 [%d]" % (name, size))
+    parts = [x for x in (table, lens, cu_seqs) if x is not None]
+    if any(not x.is_contiguous() or x.device != table.device for x in parts):
+        raise ValueError("the prefix's tensors must be dense and on one device")
+    p = Prefix()
+    p.n_prefixes, p.max_pages = table.shape
+    p.max_len, p.table, p.lens, p.cu_seqs = max_len, _p(table), _p(lens), _p(cu_seqs)
+    p._keep_alive = parts               # the struct only holds addresses: the tensors must outlive it
+    p._device = table.device
+    return p
+
+
+def fastkv_prefix_attn_workspace_bytes(cache: PagedCache, prefix: Prefix, query: Query) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_load().fastkv_prefix_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(prefix), ctypes.byref(query), ctypes.byref(n)),
+           "fastkv_prefix_attn_workspace_bytes")
+    return int(n.value)
+
+
+def fastkv_prefix_attn(cache: PagedCache, prefix: Prefix, query: Query, lens, q, out, lse, workspace, stream=None) -> None:
+    """Attention of query.q_len new tokens per sequence over shared prefixes and the sequences' own entries; see the header."""
+    dev = _here(cache)
+    if prefix._device != cache._device:
+        raise ValueError("the prefix is on %s, the cache on %s" % (prefix._device, cache._device))
+    rc = (_lib or _load()).fastkv_prefix_attn(
+        cache, prefix, query, None if lens is None else lens.data_ptr(), None if q is None else q.data_ptr(),
+        None if out is None else out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+        torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if rc != FASTKV_OK:
+        raise FastKVError(rc, "fastkv_prefix_attn")
 
 
 def _entry_rows(cache: PagedCache, x, dtype, name: str):

@@ -1,5 +1,6 @@
 // C ABI of the FastKV selection path: argument validation, workspace carving, TMA descriptor
 // encoding and kernel launches.  Declarations and contracts live in include/fastkv.h.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -49,6 +50,7 @@ struct DebugConfig {
   int score_partition = 0;          // parked kernel's partition mode: 0 = by shape, 1 = never, 2 = whenever it can run
   int paged_two_maps = 0;           // paged attention: copies K and V apart, as pools beyond 2^40 bytes of one another need
   int paged_skip_copy = 0;          // paged kernels: n > 0: the copies of chunk (or fill) n - 1 are withheld (timeout test)
+  int prefix_skip_commit = 0;       // prefix attention: n > 0: the "S ready" signal of a CTA's n-th chunk is withheld (timeout test)
   int prefill_skip_commit = 0;      // prefill attention: n > 0: key tile n - 1's "S ready" signal is withheld (timeout test)
 };
 DebugConfig g_debug;
@@ -56,9 +58,9 @@ DebugConfig g_debug;
 // ---- optional per-kernel timing ("time_kernels" hook): a pair of events around every launch ----------
 enum KernelId { KID_SCORE = 0, KID_POOL = 1, KID_SELECT = 2, KID_COMPACT = 3, KID_DECODE = 4, KID_PREFILL = 5,
                 KID_WINDOW_SCORES = 6, KID_PAGED_APPEND = 7, KID_PAGED_ATTN = 8,
-                KID_PAGED_WEIGHTS = 9, KID_PAGED_EVICT = 10, KID_COUNT = 11 };
+                KID_PAGED_WEIGHTS = 9, KID_PAGED_EVICT = 10, KID_PREFIX_ATTN = 11, KID_COUNT = 12 };
 const char* const kKernelNames[KID_COUNT] = {"score", "pool", "select", "compact", "decode_attn", "prefill_attn",
-                                             "window_scores", "paged_append", "paged_attn", "paged_weights", "paged_evict"};
+                                             "window_scores", "paged_append", "paged_attn", "paged_weights", "paged_evict", "prefix_attn"};
 struct KernelTimes {
   bool on = false;
   std::mutex mu;
@@ -362,6 +364,8 @@ int fastkv_debug_set(const char* key, int64_t value) {
     g_debug.score_partition = static_cast<int>(value);
   } else if (!std::strcmp(key, "prefill_skip_commit")) {
     g_debug.prefill_skip_commit = static_cast<int>(value < 0 ? 0 : value);
+  } else if (!std::strcmp(key, "prefix_skip_commit")) {
+    g_debug.prefix_skip_commit = static_cast<int>(value < 0 ? 0 : value);
   } else if (!std::strcmp(key, "paged_two_maps")) {
     if (value < 0 || value > 1) return fail(FASTKV_ERR_INVALID_ARG, "debug_set: paged_two_maps is 0 or 1");
     g_debug.paged_two_maps = static_cast<int>(value);
@@ -891,6 +895,45 @@ PagedAttnPlan plan_of(const fastkv_paged_cache& c, const fastkv_query& q) {
   return plan_paged_attn(c.batch, c.n_kv_heads, q.n_q_heads / c.n_kv_heads * q.q_len, c.format == FASTKV_CACHE_E4M3, q.max_len,
                          total);
 }
+// The launches of a paged attention whose arguments have been checked; partials lie behind the workspace's header.
+int enqueue_paged_attn(const fastkv_paged_cache& c, const fastkv_query& query, const PagedAttnPlan& plan, const int32_t* lens, const void* q,
+                       float* out, float* lse, void* workspace, void* stream_) {
+  int rc;
+  const int G = query.n_q_heads / c.n_kv_heads, rows = G * query.q_len;
+  PagedAttnParams p;
+  memset(&p, 0, sizeof p);
+  // a tensor map's strides are below 2^40 bytes
+  const uintptr_t ka = reinterpret_cast<uintptr_t>(c.k_pages), va = reinterpret_cast<uintptr_t>(c.v_pages);
+  const uint64_t apart = ka < va ? va - ka : ka - va;
+  p.joint = apart != 0 && apart < (1ull << 40) && !g_debug.paged_two_maps;
+  p.v_first = p.joint && va < ka;
+  CUtensorMap tmap_k, tmap_v;
+  if (p.joint) {
+    if ((rc = encode_pool(&tmap_k, c, p.v_first ? c.v_pages : c.k_pages, apart))) return rc;
+    tmap_v = tmap_k;
+  } else if ((rc = encode_pool(&tmap_k, c, c.k_pages, 0)) || (rc = encode_pool(&tmap_v, c, c.v_pages, 0))) {
+    return rc;
+  }
+  p.c = paged_view(c);
+  p.n_q_heads = query.n_q_heads; p.group = G; p.q_len = query.q_len; p.rows = rows;
+  p.scale_log2 = softmax_scale_of(c, query) * 1.4426950408889634f;
+  p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.part_ml = reinterpret_cast<float2*>(ws + sizeof(WorkspaceHeader));
+  p.part_o = reinterpret_cast<float*>(ws + paged_attn_partials_offset(plan, c.batch, c.n_kv_heads));
+  p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+  p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;
+  p.skip_copy = g_debug.paged_skip_copy - 1;
+  cudaError_t e;
+  int launched = 0;
+  {
+    TimedLaunch timed(KID_PAGED_ATTN, static_cast<cudaStream_t>(stream_));
+    e = launch_paged_attn(tmap_k, tmap_v, p, plan, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_), &launched);
+  }
+  g_launches += launched;
+  if (e != cudaSuccess) return cuda_fail(e, "paged_attn_kernel launch");
+  return FASTKV_OK;
+}
 }  // namespace
 
 int fastkv_paged_append(const fastkv_paged_cache* cache, const fastkv_new_rows* rows, const int32_t* lens, const void* q,
@@ -991,42 +1034,121 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
     return fail(FASTKV_ERR_UNSUPPORTED, "paged_attn: q and out must be 16-byte aligned");
   const fastkv_paged_cache& c = *cache;
   const PagedAttnPlan plan = plan_of(c, *query);
-  const int G = query->n_q_heads / c.n_kv_heads, rows = G * query->q_len;
   const size_t need = round_up(paged_attn_workspace_bytes(plan, c.batch, c.n_kv_heads, c.head_dim), 256);
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
   if ((rc = check_device())) return rc;
-  PagedAttnParams p;
-  memset(&p, 0, sizeof p);
-  // a tensor map's strides are below 2^40 bytes
-  const uintptr_t ka = reinterpret_cast<uintptr_t>(c.k_pages), va = reinterpret_cast<uintptr_t>(c.v_pages);
-  const uint64_t apart = ka < va ? va - ka : ka - va;
-  p.joint = apart != 0 && apart < (1ull << 40) && !g_debug.paged_two_maps;
-  p.v_first = p.joint && va < ka;
-  CUtensorMap tmap_k, tmap_v;
-  if (p.joint) {
-    if ((rc = encode_pool(&tmap_k, c, p.v_first ? c.v_pages : c.k_pages, apart))) return rc;
-    tmap_v = tmap_k;
-  } else if ((rc = encode_pool(&tmap_k, c, c.k_pages, 0)) || (rc = encode_pool(&tmap_v, c, c.v_pages, 0))) {
-    return rc;
-  }
-  p.c = paged_view(c);
-  p.n_q_heads = query->n_q_heads; p.group = G; p.q_len = query->q_len; p.rows = rows;
-  p.scale_log2 = softmax_scale_of(c, *query) * 1.4426950408889634f;
-  p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.out = out; p.lse = lse;
+  return enqueue_paged_attn(c, *query, plan, lens, q, out, lse, workspace, stream_);
+}
+
+namespace {
+struct PrefixLayout {
+  PagedAttnPlan own;
+  int tile_tokens, tile_rows, max_units, ctas;
+  size_t off_own_out, off_own_lse, off_ml, off_o, bytes;
+};
+int check_prefix(const fastkv_paged_cache* c, const fastkv_prefix* x, const fastkv_query* q, PrefixLayout* lay) {
+  int rc = check_query(c, q);
+  if (rc) return rc;
+  if (x == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: prefix is NULL");
+  if (x->n_prefixes < 1 || x->max_pages < 1 || x->max_len < 1) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: n_prefixes, max_pages and max_len must be >= 1");
+  if (x->reserved != 0) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: reserved must be 0");
+  if (!x->table || !x->lens) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: the prefix's table and lens are required");
+  if (x->n_prefixes > 1 && x->cu_seqs == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: cu_seqs is required with more than one prefix");
+  if (x->n_prefixes > kMaxPrefixes) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than %d prefixes", kMaxPrefixes);
+  if (static_cast<long long>(x->max_pages) * c->page_size > 0x7fffffffLL)
+    return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: a row of the prefixes' table holds more than 2^31 - 1 entries");
+  const int G = q->n_q_heads / c->n_kv_heads;
+  if (G > 128) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than 128 query heads per KV head");
+  if (c->n_kv_heads > 65535) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than 65535 KV heads");
+  const long long tokens = static_cast<long long>(c->batch) * q->q_len;
+  lay->own = plan_of(*c, *q);
+  lay->tile_tokens = 128 / G;
+  lay->tile_rows = static_cast<int>(round_up(static_cast<size_t>(std::min(tokens * G, static_cast<long long>(lay->tile_tokens) * G)), 32));
+  // each prefix may end inside a pair of tiles, but all together they have no more query tokens than the batch
+  const long long units = (std::min(static_cast<long long>(x->n_prefixes), tokens) + tokens / (2 * lay->tile_tokens)) * c->n_kv_heads;
+  if (units > 0x3fffffffLL) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: too many query rows");
+  lay->max_units = static_cast<int>(units);
+  lay->ctas = static_cast<int>(std::min(static_cast<long long>(kPrefixCtas), units * chunk_count(x->max_len, 7)));
+  const size_t pieces = static_cast<size_t>(units + lay->ctas);
+  size_t off = round_up(paged_attn_workspace_bytes(lay->own, c->batch, c->n_kv_heads, c->head_dim), 256);
+  auto take = [&](size_t n) { const size_t o = off; off += round_up(n, 256); return o; };
+  lay->off_own_out = take(static_cast<size_t>(tokens) * q->n_q_heads * c->head_dim * 4);
+  lay->off_own_lse = take(static_cast<size_t>(tokens) * q->n_q_heads * 4);
+  lay->off_ml = take(pieces * 2 * lay->tile_rows * sizeof(float2));
+  lay->off_o = take(pieces * 2 * lay->tile_rows * c->head_dim * 4);
+  lay->bytes = off;
+  return FASTKV_OK;
+}
+// A pool for tiles of 128 entries, a page's rows at a time: bf16 in swizzled boxes of 64 columns, codes as they are.
+int encode_prefix_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
+  const cuuint64_t row = static_cast<cuuint64_t>(c.head_dim) * (e4m3 ? 1 : 2);
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size), static_cast<cuuint64_t>(c.n_pages) * c.n_kv_heads};
+  cuuint64_t strides[2] = {row, row * c.page_size};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(e4m3 ? c.head_dim : 64), static_cast<cuuint32_t>(c.page_size), 1}, estr[3] = {1, 1, 1};
+  CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+  return FASTKV_OK;
+}
+}  // namespace
+
+int fastkv_prefix_attn_workspace_bytes(const fastkv_paged_cache* cache, const fastkv_prefix* prefix, const fastkv_query* query,
+                                       size_t* bytes) {
+  PrefixLayout lay;
+  int rc = check_prefix(cache, prefix, query, &lay);
+  if (rc) return rc;
+  if (bytes == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = lay.bytes;
+  return FASTKV_OK;
+}
+
+int fastkv_prefix_attn(const fastkv_paged_cache* cache, const fastkv_prefix* prefix, const fastkv_query* query, const int32_t* lens,
+                       const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream_) {
+  PrefixLayout lay;
+  int rc = check_prefix(cache, prefix, query, &lay);
+  if (rc) return rc;
+  if (!lens || !q || !out) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: lens, q and out are required");
+  if (reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(out) % 16)
+    return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: q and out must be 16-byte aligned");
+  const fastkv_paged_cache& c = *cache;
+  if ((rc = check_workspace(workspace, workspace_bytes, lay.bytes))) return rc;
+  if ((rc = check_device())) return rc;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  p.part_ml = reinterpret_cast<float2*>(ws + sizeof(WorkspaceHeader));
-  p.part_o = reinterpret_cast<float*>(ws + paged_attn_partials_offset(plan, c.batch, c.n_kv_heads));
-  p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+  PrefixParams p;
+  memset(&p, 0, sizeof p);
+  p.c = paged_view(c);
+  p.n_prefixes = prefix->n_prefixes; p.max_pages = prefix->max_pages; p.table = prefix->table; p.lens = prefix->lens; p.cu_seqs = prefix->cu_seqs;
+  p.n_q_heads = query->n_q_heads; p.group = query->n_q_heads / c.n_kv_heads; p.q_len = query->q_len;
+  p.tile_tokens = lay.tile_tokens; p.tile_rows = lay.tile_rows; p.max_units = lay.max_units; p.ctas = lay.ctas;
   p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;
-  p.skip_copy = g_debug.paged_skip_copy - 1;
+  p.skip_commit = g_debug.prefix_skip_commit - 1;
+  p.scale_log2 = softmax_scale_of(c, *query) * 1.4426950408889634f;
+  p.part_ml = reinterpret_cast<float2*>(ws + lay.off_ml);
+  p.part_o = reinterpret_cast<float*>(ws + lay.off_o);
+  float* own_out = reinterpret_cast<float*>(ws + lay.off_own_out);
+  float* own_lse = reinterpret_cast<float*>(ws + lay.off_own_lse);
+  p.own_out = own_out; p.own_lse = own_lse;
+  p.out = static_cast<uint16_t*>(out); p.lse = lse;
+  p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+  CUtensorMap tmap_q, tmap_k, tmap_v;
+  const long long tokens = static_cast<long long>(c.batch) * query->q_len;
+  if ((rc = encode_bf16_3d(&tmap_q, q, c.head_dim, query->n_q_heads, tokens, c.head_dim, static_cast<long long>(query->n_q_heads) * c.head_dim,
+                           p.group, lay.tile_tokens)) ||
+      (rc = encode_prefix_pool(&tmap_k, c, c.k_pages)) || (rc = encode_prefix_pool(&tmap_v, c, c.v_pages)))
+    return rc;
+  if ((rc = enqueue_paged_attn(c, *query, lay.own, lens, q, own_out, own_lse, workspace, stream_))) return rc;
   cudaError_t e;
   int launched = 0;
   {
-    TimedLaunch timed(KID_PAGED_ATTN, static_cast<cudaStream_t>(stream_));
-    e = launch_paged_attn(tmap_k, tmap_v, p, plan, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_), &launched);
+    TimedLaunch timed(KID_PREFIX_ATTN, static_cast<cudaStream_t>(stream_));
+    e = launch_prefix_attn(tmap_q, tmap_k, tmap_v, p, c.head_dim, c.format == FASTKV_CACHE_E4M3, static_cast<cudaStream_t>(stream_), &launched);
   }
   g_launches += launched;
-  if (e != cudaSuccess) return cuda_fail(e, "paged_attn_kernel launch");
+  if (e != cudaSuccess) return cuda_fail(e, "prefix_attn_kernel launch");
   return FASTKV_OK;
 }
 

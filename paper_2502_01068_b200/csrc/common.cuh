@@ -67,6 +67,19 @@ enum Site : int {
   SITE_WEIGHTS_LEN = 45,
   SITE_EVICT_PAGE = 46,
   SITE_EVICT_LEN = 47,
+  SITE_PREFIX_RING = 48,
+  SITE_PREFIX_DRAIN = 49,
+  SITE_PREFIX_Q = 50,
+  SITE_PREFIX_K = 51,
+  SITE_PREFIX_V = 52,
+  SITE_PREFIX_P = 53,
+  SITE_PREFIX_S = 54,
+  SITE_PREFIX_O = 55,
+  SITE_PREFIX_TURN = 56,
+  SITE_PREFIX_RAW = 57,
+  SITE_PREFIX_PAGE = 58,
+  SITE_PREFIX_LEN = 59,
+  SITE_PREFIX_GROUP = 60,
 };
 
 // Records `text` as the calling thread's last error (see fastkv_last_error) and returns `status`.
@@ -309,6 +322,36 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32(int m, int n) {
          | (1u << 7)                     // A format bf16
          | (1u << 10)                    // B format bf16
          | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// MN-major operand tile as TMA writes it (rows of 128 bytes = 64 elements of the MN dimension, one row per
+// K index, 128-byte swizzle): 64-element MN chunks are `chunk_bytes` apart (leading byte offset), groups of
+// eight K rows 1024 bytes apart (stride byte offset).
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t chunk_bytes) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>((chunk_bytes >> 4) & 0x3FFFu) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]: A is read from tensor memory (lane = row, two bf16 per 32-bit column)
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// True in exactly one lane of the (converged) warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t pred;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+  return pred != 0;
 }
 // 32 lanes x 32 consecutive fp32 columns of tensor memory -> 32 registers per thread
 // (thread = lane of its warp's quarter, register i = column i).

@@ -76,6 +76,33 @@ inline int paged_box_rows(bool e4m3, int page_size) { return e4m3 && page_size >
 cudaError_t launch_paged_attn(const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, PagedAttnParams& p, const PagedAttnPlan& plan,
                               int head_dim, bool e4m3, cudaStream_t stream, int* launches);
 
+constexpr int kPrefixCtas = 148;         // CTAs of the prefix attention that are resident at once, one per SM
+constexpr int kMaxPrefixes = 1024;
+
+struct PrefixParams {
+  PagedView c;                // batch, pools (its block table is the sequences' own and not used)
+  int n_prefixes, max_pages;  // rows of the prefixes' table, and pages a row has room for
+  int n_q_heads, group, q_len;
+  int tile_tokens;            // query tokens of a tile: 128 / group
+  int tile_rows;              // rows of a tile that a piece has room for
+  int max_units, ctas;
+  long long wait_limit;
+  int skip_commit;            // test hook: the S of this chunk (of every CTA's first tile) is never signalled (-1: none)
+  float scale_log2;
+  const int* table;           // [n_prefixes][max_pages]
+  const int* lens;            // [n_prefixes]
+  const int* cu_seqs;         // [n_prefixes + 1] or null
+  float2* part_ml;            // [pieces][2 tiles][tile_rows]: (reference, sum)
+  float* part_o;              // [pieces][2 tiles][d][tile_rows]
+  const float* own_out;       // [B][q_len][Hq][d], the attention over the sequences' own entries
+  const float* own_lse;       // [B][q_len][Hq]
+  uint16_t* out;              // [B][q_len][Hq][d] bf16
+  float* lse;                 // may be null
+  WorkspaceHeader* hdr;
+};
+cudaError_t launch_prefix_attn(const CUtensorMap& tmap_q, const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, const PrefixParams& p,
+                               int head_dim, bool e4m3, cudaStream_t stream, int* launches);
+
 struct PagedWeightsParams {
   PagedView c;
   int n_q_heads, group, q_len, rows;     // rows = group * q_len query rows per (sequence, KV head)

@@ -1,0 +1,267 @@
+"""Attention over shared prefixes and the sequences' own entries against the 64-bit formula."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_01068_b200 import binding as B
+from tests.paged_reference import Pools, attention
+
+pytestmark = pytest.mark.gpu
+
+
+class Shared:
+    """Prefixes and sequences in one pool: rows 0 .. n - 1 of the pools' table are the prefixes'."""
+
+    def __init__(self, fmt, plens, lens, page, Hkv, d, seed, cu=None):
+        self.pools = Pools(fmt, list(plens) + list(lens), list(plens) + list(lens), page, Hkv, d, seed)
+        n = len(plens)
+        self.n, self.plens, self.lens, self.cu = n, list(plens), list(lens), cu
+        self.ptable, self.table = self.pools.table[:n].contiguous(), self.pools.table[n:].contiguous()
+        self.dev_plens, self.dev_lens = self.pools.dev_lens[:n].contiguous(), self.pools.dev_lens[n:].contiguous()
+        self.dev_cu = None if cu is None else torch.tensor(cu, dtype=torch.int32, device="cuda")
+
+    def cache(self):
+        p = self.pools
+        return B.make_paged_cache(p.k, p.v, self.table, p.ks, p.vs)
+
+    def prefix(self, max_len=None):
+        return B.make_prefix(self.ptable, self.dev_plens, max_len=max_len or max(1, max(self.plens)), cu_seqs=self.dev_cu)
+
+    def prefix_of(self, b):
+        if self.cu is None:
+            return 0
+        return next((i for i in range(self.n) if self.cu[i] <= b < self.cu[i + 1]), None)
+
+    def entries(self, b):
+        i, p = self.prefix_of(b), self.pools
+        k, v = p.k64[self.n + b], p.v64[self.n + b]
+        if i is None:
+            return 0, k, v
+        return self.plens[i], np.concatenate([p.k64[i], k]), np.concatenate([p.v64[i], v])
+
+
+def call(sh, q, scale=0.0, lse=True, max_len=None, own_max=None, total_len=None, stream=None, ws=None):
+    Bn, T, Hq, d = q.shape
+    cache, prefix = sh.cache(), sh.prefix(max_len)
+    query = B.make_query(n_q_heads=Hq, q_len=T, max_len=own_max or max(1, max(sh.lens)), total_len=sum(sh.lens) if total_len is None else total_len,
+                         softmax_scale=scale)
+    if ws is None:
+        # what a workspace holds is anything but its header
+        ws = torch.full((B.fastkv_prefix_attn_workspace_bytes(cache, prefix, query),), 0xFF, dtype=torch.uint8, device="cuda")
+        ws[:256] = 0
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    l = torch.full((Bn, T, Hq), float("nan"), device="cuda") if lse else None
+    B.fastkv_prefix_attn(cache, prefix, query, sh.dev_lens, q, out, l, ws, stream)
+    return out, l, ws
+
+
+def check(sh, q, out, lse, scale=0.0, rows=None):
+    """A weight is rounded to bf16 (2^-8 of it) and so is the output; a logit is off by at most d 2^-23 of sum scale |q k|, which moves
+    weights and their sum; exponentials, sums and the merge add 2^-20."""
+    Bn, T, Hq, d = q.shape
+    by = scale or 1.0 / math.sqrt(d)
+    q64, o64 = q.double().cpu().numpy(), out.double().cpu().numpy()
+    l64 = None if lse is None else lse.double().cpu().numpy()
+    for b, i in rows or [(b, i) for b in range(Bn) for i in range(T)]:
+        n, k, v = sh.entries(b)
+        sees = n + max(0, sh.lens[b] - (T - 1 - i))
+        want, want_lse, mass, size = attention(q64[b, i], k, v, sees, by)
+        rel = d * 2.0 ** -23 * size + 2.0 ** -20
+        slack = 2.0 ** -8 * (mass + np.abs(want)) * 1.01 + 2 * rel[:, None] * mass
+        bad = ~(np.abs(o64[b, i] - want) <= slack)
+        assert not bad.any(), (b, i, np.argwhere(bad)[:4], o64[b, i][bad][:4], want[bad][:4])
+        if l64 is not None:
+            for h in range(Hq):
+                if sees == 0:
+                    assert l64[b, i, h] == -np.inf
+                else:
+                    assert abs(l64[b, i, h] - want_lse[h]) <= rel[h] + 2.0 ** -21 * (abs(want_lse[h]) + 1), (b, i, h, l64[b, i, h], want_lse[h])
+
+
+def run(fmt, plens, lens, page, Hq, Hkv, d, T=1, cu=None, seed=0, scale=0.0, gain=1.0, rows=None, **kw):
+    sh = Shared(fmt, plens, lens, page, Hkv, d, seed, cu)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    q = (torch.randn(len(lens), T, Hq, d, device="cuda", generator=gen) * gain).to(torch.bfloat16)
+    out, lse, ws = call(sh, q, scale, **kw)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    check(sh, q, out, lse, scale, rows)
+    return sh, q, out, lse
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 127, 128, 129, 300, 1000, 0])
+def test_lengths_of_the_prefix(fmt, d, n):
+    run(fmt, [n], [5, 1, 40], 16, 4, 1, d, seed=n)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hq,Hkv,T", [(8, 8, 1), (6, 2, 2), (14, 2, 1), (8, 1, 5), (12, 4, 3)])
+def test_against_the_formula(fmt, page, Hq, Hkv, T):
+    run(fmt, [777], [3, 90, 17, 1], page, Hq, Hkv, 128, T, seed=page + T)
+    run(fmt, [500], [30, 9], page, Hq, Hkv, 64, T, seed=page + T)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch,Hq,Hkv,T", [(32, 4, 1, 1), (33, 4, 1, 1), (64, 4, 1, 1), (65, 4, 1, 1), (40, 8, 2, 2), (70, 3, 1, 3), (300, 1, 1, 1), (3, 64, 1, 2),
+                                            (2, 128, 1, 1), (2, 100, 1, 2)])
+def test_row_tiles(fmt, batch, Hq, Hkv, T):
+    """One tile, two, pairs of them with a ragged last one; heads that do not divide a tile."""
+    run(fmt, [1500], [1 + (7 * b) % 23 for b in range(batch)], 32, Hq, Hkv, 128, T, seed=batch, rows=[(b, b % T) for b in range(0, batch, max(1, batch // 12))] + [(batch - 1, T - 1)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_several_prefixes(fmt, d):
+    """Prefixes of all lengths, one that nobody uses, one of length 0, sequences before the first and behind the last."""
+    run(fmt, [400, 77, 1300, 0, 128], [4, 30, 1, 9, 60, 2, 7, 8, 33, 5, 12], 16, 8, 2, d, T=2, cu=[1, 4, 4, 7, 8, 10], seed=3)
+    run(fmt, [90, 4000], [4] * 80, 64, 4, 1, d, cu=[0, 70, 80], seed=4, rows=[(0, 0), (31, 0), (32, 0), (69, 0), (70, 0), (79, 0)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_many_prefixes(fmt):
+    rng = np.random.default_rng(2)
+    cu = np.concatenate([[0], np.cumsum(rng.integers(0, 4, 200))]).tolist()
+    run(fmt, [int(x) for x in rng.integers(0, 300, 200)], [int(x) for x in rng.integers(0, 20, cu[-1])], 16, 2, 1, 64, cu=cu, seed=5,
+        rows=[(b, 0) for b in range(0, cu[-1], 9)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_long_prefix_on_every_sm(fmt):
+    run(fmt, [40000], [100, 3, 800, 64], 64, 16, 4, 128, seed=6)
+    run(fmt, [20000], [9] * 70, 128, 4, 1, 128, seed=7, rows=[(0, 0), (63, 0), (64, 0), (69, 0)])
+
+
+def test_nothing_to_see():
+    """No prefix and no entries of one's own, query tokens ahead of the cache, a prefix alone."""
+    sh, q, out, lse = run("bf16", [0], [0, 3, 1], 16, 4, 2, 64, T=3, seed=1)
+    assert (out[0] == 0).all() and (lse[0] == -math.inf).all()
+    run("e4m3", [200], [0, 0], 16, 4, 2, 64, T=2, seed=1, total_len=1)
+
+
+def test_scale_and_sharp_rows():
+    """Logits of a hundred: the reference moves, earlier sums and outputs are rescaled."""
+    for fmt in ("bf16", "e4m3"):
+        run(fmt, [3000], [50] * 3, 32, 8, 2, 128, scale=0.5, gain=3.0, seed=8)
+        run(fmt, [3000], [50] * 40, 32, 8, 2, 128, scale=0.5, gain=3.0, seed=9, rows=[(0, 0), (20, 0), (39, 0)])
+
+
+def test_bounds_that_are_off():
+    run("bf16", [900], [70, 3], 16, 4, 2, 64, max_len=10, own_max=1, total_len=1, seed=2)
+    run("e4m3", [900], [70, 3], 16, 4, 2, 64, max_len=10 ** 6, own_max=10 ** 6, total_len=0, seed=2, lse=False)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,batch", [(64, 2), (128, 2), (128, 40)])
+def test_nan_and_infinities_where_they_are_seen(fmt, d, batch):
+    """The pools' other entries, those behind the prefix in its last page among them, are NaN in every test; here one entry of the
+    prefix, too: its sequences' rows get it, and no other's."""
+    sh = Shared(fmt, [200, 333], [9] * batch, 32, 2, d, 3, cu=[0, batch // 2, batch])
+    pid = int(sh.pools.table_np[0, 70 // 32])
+    for pool in (sh.pools.k, sh.pools.v):
+        x = pool if fmt == "bf16" else pool.view(torch.float8_e4m3fn)
+        x[pid, 0, 70 % 32, 5] = float("nan")
+    q = torch.randn(batch, 1, 8, d, device="cuda").to(torch.bfloat16)
+    out, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    half = batch // 2
+    assert torch.isnan(out[:half, :, :4]).all() and torch.isnan(lse[:half, :, :4]).all()
+    check(sh, q, out, lse, rows=[(half, 0), (batch - 1, 0)])
+    assert not torch.isnan(out[:half, :, 4:]).any() and not torch.isnan(lse[:half, :, 4:]).any()
+
+
+def test_entries_that_weigh_nothing():
+    """Logits of -infinity in the whole prefix: only the own entries count; in all entries: like a query that sees none."""
+    sh = Shared("bf16", [300], [20, 20], 16, 1, 64, 3)
+    q = torch.ones(2, 1, 2, 64, device="cuda").to(torch.bfloat16)
+    for row in range(19):
+        sh.pools.k[int(sh.pools.table_np[0, row])][0, :] = -math.inf
+    out, lse, ws = call(sh, q)
+    n, k, v = sh.entries(0)
+    want, want_lse, _, _ = attention(q[0, 0].double().cpu().numpy(), k[n:], v[n:], 20, 0.125)
+    assert np.allclose(lse[0, 0].double().cpu().numpy(), want_lse, rtol=1e-5) and np.allclose(out[0, 0].double().cpu().numpy(), want, rtol=2.0 ** -8, atol=1e-5)
+    sh.pools.k[sh.table[0].long()] = -math.inf
+    out, lse, ws = call(sh, q)
+    assert (out[0] == 0).all() and (lse[0] == -math.inf).all()
+
+
+def test_reports():
+    sh = Shared("bf16", [300, 90], [20, 20], 16, 1, 64, 3, cu=[0, 1, 2])
+    q = torch.randn(2, 1, 2, 64, device="cuda").to(torch.bfloat16)
+    good = sh.ptable.clone()
+    for bad in (-1, 10 ** 6):
+        sh.ptable = good.clone()
+        sh.ptable[0, 3] = bad
+        assert B.fastkv_device_status(call(sh, q)[2]) == (B.ERR_DEVICE_INDEX, 58)
+    sh.ptable = good
+    for n in (-1, 16 * good.shape[1] + 1):
+        sh.dev_plens[0] = n
+        assert B.fastkv_device_status(call(sh, q)[2]) == (B.ERR_DEVICE_INDEX, 59)
+    sh.dev_plens[0] = 300
+    for cu in ([0, 2, 1], [-1, 1, 2], [0, 1, 3], [5, 1, 0]):
+        sh.dev_cu = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        assert B.fastkv_device_status(call(sh, q)[2]) == (B.ERR_DEVICE_INDEX, 60)
+    sh.dev_cu = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    out, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    check(sh, q, out, lse)
+
+
+def test_groups_that_overlap_have_no_room():
+    """A cu_seqs that goes back and forth would name every sequence many times over."""
+    n = 64
+    sh = Shared("bf16", [150] * n, [3] * 8, 16, 1, 64, 3, cu=[0, 8] * (n // 2) + [8])
+    q = torch.randn(8, 1, 128, 64, device="cuda").to(torch.bfloat16)
+    out, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (B.ERR_DEVICE_INDEX, 60)
+
+
+def test_same_bits_twice_on_a_stream_and_from_a_graph():
+    for fmt in ("bf16", "e4m3"):
+        sh = Shared(fmt, [5000, 333], [40, 9, 300, 5], 32, 2, 128, 1, cu=[0, 3, 4])
+        q = torch.randn(4, 2, 8, 128, device="cuda").to(torch.bfloat16)
+        a, la, ws = call(sh, q)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            b, lb, _ = call(sh, q, stream=side, ws=ws)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c, lc, _ = call(sh, q, ws=ws)
+            e, le, _ = call(sh, q, ws=ws)                  # two calls share a workspace in one graph
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in ((a, b), (a, c), (a, e)):
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+        assert torch.equal(la, lb) and torch.equal(la, lc) and torch.equal(la, le)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [2, 140])
+def test_a_wait_that_runs_out(fmt, batch):
+    """A completion that is never signalled: the waits for it run out, the kernel ends, and the next call is whole.  (Of few rows the second
+    chunk is the other tile's.)"""
+    sh = Shared(fmt, [30000, 600], [9] * batch, 32, 2, 128, 3, cu=[0, batch // 2, batch])
+    q = torch.randn(batch, 1, 8, 128, device="cuda").to(torch.bfloat16)
+    for n in (1, 2, 3):
+        B.fastkv_debug_set("wait_limit_cycles", 2_000_000)
+        B.fastkv_debug_set("prefix_skip_commit", n)
+        try:
+            _, _, ws = call(sh, q)
+            status, site = B.fastkv_device_status(ws)
+        finally:
+            B.fastkv_debug_set("wait_limit_cycles", 0)
+            B.fastkv_debug_set("prefix_skip_commit", 0)
+        if n == 2 and batch == 2:
+            assert (status, site) == (0, 0)
+        else:
+            assert status == B.ERR_DEVICE_TIMEOUT and 48 <= site <= 57
+        out, lse, ws = call(sh, q)
+        assert B.fastkv_device_status(ws) == (0, 0)
+        check(sh, q, out, lse, rows=[(0, 0), (batch - 1, 0)])
