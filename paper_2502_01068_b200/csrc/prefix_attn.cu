@@ -11,12 +11,13 @@
 // A CTA's roles:
 //   loaders    one warp: K and V tiles page by page (TMA, a box per page and 64 columns) into their rings, ahead into the next
 //              segment; one warp: a segment's Q, as soon as the one before is through with it;
-//   widening   (8-bit pages) four warps: codes from the raw ring to bf16 tiles in the layout that TMA would write, times the
-//              page's scale: a power of two, so exact;
+//   widening   (8-bit pages) eight warps: codes from the raw ring to 16-bit tiles in the layout that TMA would write.  K to fp16, one
+//              instruction for two codes, K's scale going onto the logits; V to bf16, times the page's scale, so that the scales of
+//              pages far apart cost a weight none of its bits.  Both exact;
 //   issuers    one warp per row tile: per chunk O += P V of the chunk before, then S = Q K^T (tcgen05.mma 128 x 128 x d, fp32 in
 //              tensor memory), in that order from one thread, so that S may overwrite the P that the contraction before has read;
-//   softmax    eight warps per row tile, two threads per row: online softmax in log2 units with a lazily raised reference; P goes
-//              back, in bf16, into the first half of the thread's own S columns.
+//   softmax    four warps per row tile, a thread per row, which holds most of the chunk's 128 logits in registers: online softmax in log2
+//              units with a lazily raised reference; P goes back, in bf16, into the first half of the row's S columns.
 // With more than 128 rows the two tiles hold different rows and take every chunk, their contractions alternating.  With 128 or fewer
 // both work on the same rows and take every other chunk: one's softmax runs under the other's contractions.
 // Tensor memory (512 columns): S (and P inside it) of tile A at 0, of tile B at 128; O of A at 256, of B at 256 + d.
@@ -34,43 +35,64 @@ namespace fastkv {
 namespace {
 
 constexpr int kTile = 128;                     // rows of a tile, entries of a chunk
-constexpr int kCtrlWarps = 4;                  // K and V, issuer of tile A, issuer of tile B, Q
-constexpr int kSoftmaxWarps = 8;               // per tile
-constexpr int kWideWarps = 4;
-constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 bf16: one swizzled column block of a tile
+constexpr int kStep = 64;                      // entries of a softmax step: half a chunk, so that a tile's S has two buffers
+constexpr int kCtrlWarps = 4;                  // loader of K and V, issuer of tile A, issuer of tile B, loader of Q
+constexpr int kSoftmaxWarps = 4;               // per tile
+constexpr int kWideKWarps = 4, kWideVWarps = 8, kWideWarps = kWideKWarps + kWideVWarps;
+constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
 constexpr float kSlackLog2 = 8.0f;
 
-template <int D, bool kE4M3>
+// kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
+template <int D, bool kE4M3, bool kOne>
 struct PrefixCfg {
   static constexpr int KH = D / 64;
   static constexpr int kTileBytes = KH * kHalfBytes;
-  static constexpr int kStages = kE4M3 && D == 128 ? 1 : 2;               // bf16 tiles of K, and of V
+  // Tiles of Q, K and V, and in 8 bits the raw chunks of K and of V.  V waits for the softmax: two tiles of V in bf16 leave a load less time
+  // than memory takes.
+  static constexpr int kQTiles = kOne ? 1 : 2, kKTiles = kE4M3 ? (D == 128 && !kOne ? 1 : 2) : (kOne ? 3 : 2), kVTiles = kE4M3 ? 2 : 3;
   static constexpr int kRawBytes = kTile * D;                              // codes of a chunk's K or V
-  static constexpr int kRaw = kE4M3 ? (D == 128 ? 5 : 8) : 1;              // (one unused in bf16)
+  static constexpr int kRaw = kE4M3 ? (D == 128 ? 2 : 4) : 1;              // raw chunks of each (none in bf16)
   static constexpr int kWarps = kCtrlWarps + 2 * kSoftmaxWarps + (kE4M3 ? kWideWarps : 0);
   static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kXchBytes = 2 * 2 * 2 * kTile * 4;                  // what the two halves of a row exchange
-  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + (kE4M3 ? kRaw * kRawBytes : 0) + kXchBytes + 1024;
+  // behind the tiles: the scan of the prefixes, rows' shifts, pages' scales, barriers
+  static constexpr int kScanBytes = 512, kExtra = kScanBytes + 2 * kTile + 128 + 896;
+  static constexpr int kSmem = (kQTiles + kKTiles + kVTiles) * kTileBytes + (kE4M3 ? 2 * kRaw * kRawBytes : 0) + kExtra;
+  static_assert(kWarps <= 32 && kSmem <= 232448, "shared memory of a CTA");
+  // 8-bit pages: the launch's 80 registers a thread go 40 to the control warps, 112 to the softmax warps and 72 to the widening ones.
+  static constexpr int kLaunchRegs = 80, kCtrlRegs = 40, kSoftmaxRegs = 112, kWideRegs = 72;
+  static_assert(kCtrlRegs + 2 * kSoftmaxRegs + 3 * kWideRegs <= 6 * kLaunchRegs, "the warpgroups' shares are within what the CTA was launched with");
 };
 
-// Chunks are numbered along a CTA's share.  Chunk n's K and V are in tile n % kStages, and their barriers are those of n's parity, also
-// where there is one tile: then a row tile that takes every other chunk waits on barriers of its own, in order (one that waited for a
-// phase two ahead would be answered by the phase before), and the two issuers start every segment together.
+// Chunks are numbered along a CTA's share.  Chunk n's K and V are in tiles n % kKTiles and n % kVTiles, their barriers are number n % 4: no
+// fewer than chunks in flight, and a barrier serves chunks of one parity, so that a row tile that takes every other chunk has
+// barriers of its own and waits on each in order (one that waited for a phase two ahead would be answered by the phase before).  The
+// two issuers start every segment together, when all earlier chunks have been used.
+constexpr int kBars = 4;
+
+// What the roles have to know of a segment; the loader of Q leaves it with Q.
+struct Brief {
+  int unit, n0, chunks;                        // number of its first chunk along the share, and how many
+  int seen, tokens, dual;                      // entries from its first chunk to the prefix's end; query tokens; two tiles of different rows
+  int group, g, c0, len;                       // prefix, KV head, first chunk of the prefix, entries of the prefix
+  // chunks that tile x takes, and the number of its j-th along the share: all, or those of its parity
+  __device__ __forceinline__ int skip(int x) const { return dual ? 0 : (n0 ^ x) & 1; }
+  __device__ __forceinline__ int chunks_of(int x) const { return dual ? chunks : (chunks + 1 - skip(x)) >> 1; }
+  __device__ __forceinline__ int chunk(int x, int j) const { return n0 + (dual ? j : skip(x) + 2 * j); }
+};
+
 template <int NR>
 struct PrefixBarriers {
-  uint64_t q_full, q_empty, v_tail;
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t raw_full[NR], raw_empty[NR];
-  uint64_t s_full[2], p_full[2];               // per tile: S is there; every softmax warp has stored its part of P
-  uint64_t o_done[2], o_free[2];               // per tile: a segment's O is complete; its softmax warps have read it
-  uint64_t turn[2];                            // turn[x]: the other tile's issuer has issued the block that goes before x's next one
+  uint64_t q_full, q_empty, q_wide, v_tail;
+  uint64_t k_full[kBars], k_empty[kBars], v_full[kBars], v_empty[kBars];
+  uint64_t raw_full[2][NR], raw_empty[2][NR];  // K, V
+  uint64_t s_full[2][2], p_full[2][2];         // per tile and buffer: S is there; every softmax warp has stored its part of P
+  uint64_t o_step[2];                          // per tile: O has the next step's product
+  uint64_t o_done[2], o_free[2];               // per tile: a segment's O is complete; the softmax warps have read it
   uint64_t drained[2];
+  Brief brief[2];                              // of even and odd segments
   uint32_t tmem_base;
-  int abort_flag;
-  int first_group;
+  int abort_flag, first_group, first_unit;
   long long first_chunk;
-  int first_unit;
-  long long scratch[32], scratch_u[32];
 };
 
 // ---- which rows and entries belong together ----
@@ -108,42 +130,66 @@ struct Segment {
     tokens = min(of.tokens - first, 2 * p.tile_tokens);
     dual = tokens > p.tile_tokens;
   }
-  // chunks that tile x takes, and the number of its j-th: all, or those of its parity
-  __device__ __forceinline__ int skip(int x) const { return dual ? 0 : (n0 ^ x) & 1; }
-  __device__ __forceinline__ int chunks_of(int x) const { return dual ? c1 - c0 : (c1 - c0 + 1 - skip(x)) >> 1; }
-  __device__ __forceinline__ int chunk(int x, int j) const { return n0 + (dual ? j : skip(x) + 2 * j); }
-  __device__ __forceinline__ int rows_of(const PrefixParams& p, int x) const {
-    return (dual ? (x == 0 ? p.tile_tokens : tokens - p.tile_tokens) : tokens) * p.group;
-  }
 };
 
-__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b, float s) {     // eight codes to bf16, times s
-  uint4 r;
+// Eight codes as fp16: one conversion for two of them, of which an SM does 16 a cycle.
+__device__ __forceinline__ uint4 widen8_half(uint32_t a, uint32_t b) { return make_uint4(widen_lo(a), widen_hi(a), widen_lo(b), widen_hi(b)); }
+
+// Codes as bf16 times a power of two, without conversions (two of them for a pair, with the rounding back to bf16, took twice as long):
+// a code's bits moved to bf16's places are the code times 2^-120, subnormals included, and a bf16 product brings it back, exactly.
+// Only NaN (all ones, what 480 would be) needs to be told apart: its excess over 464 stays behind in `odd`.
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen2_bf16(uint32_t em, uint32_t sign, uint32_t up, uint32_t times, uint32_t& odd) {
+  uint32_t over;
+  asm("fma.rn.relu.bf16x2 %0, %1, %2, %3;" : "=r"(over) : "r"(em), "r"(0x7b807b80u), "r"(0xc3e8c3e8u));       // em * 2^120 - 464
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(odd), "r"(over));
+  const uint32_t r = bf16x2_mul((sign & 0x80008000u) | em, up);
+  return times == 0x3f803f80u ? r : bf16x2_mul(r, times);
+}
+// Four codes come out in the order 0, 2, 1, 3: even ones and odd ones are two masks of the word.
+__device__ __forceinline__ uint4 widen8_bf16(uint32_t a, uint32_t b, uint32_t up, uint32_t times, uint32_t& odd) {
+  constexpr uint32_t kMask = 0x07f007f0u;
+  return make_uint4(widen2_bf16((a << 4) & kMask, a << 8, up, times, odd), widen2_bf16((a >> 4) & kMask, a, up, times, odd),
+                    widen2_bf16((b << 4) & kMask, b << 8, up, times, odd), widen2_bf16((b >> 4) & kMask, b, up, times, odd));
+}
+// The same, in the same order, by conversions, which know NaN.
+__device__ __forceinline__ uint4 widen8_any(uint32_t a, uint32_t b, float s) {
+  uint4 r = widen8_half(__byte_perm(a, 0, 0x3120), __byte_perm(b, 0, 0x3120));
   float lo, hi;
-  unpack16<true>(widen_lo(a), lo, hi); r.x = pack16<false>(lo * s, hi * s);
-  unpack16<true>(widen_hi(a), lo, hi); r.y = pack16<false>(lo * s, hi * s);
-  unpack16<true>(widen_lo(b), lo, hi); r.z = pack16<false>(lo * s, hi * s);
-  unpack16<true>(widen_hi(b), lo, hi); r.w = pack16<false>(lo * s, hi * s);
+  unpack16<true>(r.x, lo, hi); r.x = pack16<false>(lo * s, hi * s);
+  unpack16<true>(r.y, lo, hi); r.y = pack16<false>(lo * s, hi * s);
+  unpack16<true>(r.z, lo, hi); r.z = pack16<false>(lo * s, hi * s);
+  unpack16<true>(r.w, lo, hi); r.w = pack16<false>(lo * s, hi * s);
   return r;
 }
 
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 }  // namespace
 
-template <int D, bool kE4M3>
-__global__ void __launch_bounds__(PrefixCfg<D, kE4M3>::kThreads, 1)
+template <int D, bool kE4M3, bool kOne>
+__global__ void __launch_bounds__(PrefixCfg<D, kE4M3, kOne>::kThreads, 1)
 prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v, const PrefixParams p) {
-  using Cfg = PrefixCfg<D, kE4M3>;
-  constexpr int NS = Cfg::kStages, NR = Cfg::kRaw, KH = Cfg::KH, kThreads = Cfg::kThreads, kWarps = Cfg::kWarps;
+  using Cfg = PrefixCfg<D, kE4M3, kOne>;
+  constexpr int NK = Cfg::kKTiles, NV = Cfg::kVTiles, NR = Cfg::kRaw, KH = Cfg::KH, kThreads = Cfg::kThreads, kWarps = Cfg::kWarps;
   extern __shared__ __align__(1024) uint8_t smem[];       // the tiles need 1024-byte alignment (128-byte swizzle atoms)
-  uint8_t* const sQ = smem;                               // two row tiles
-  uint8_t* const sK = sQ + 2 * Cfg::kTileBytes;
-  uint8_t* const sV = sK + NS * Cfg::kTileBytes;
-  uint8_t* const sRaw = sV + NS * Cfg::kTileBytes;
-  float* const xch_all = reinterpret_cast<float*>(sRaw + (kE4M3 ? NR * Cfg::kRawBytes : 0));
+  uint8_t* const sQ = smem;                               // one or two row tiles
+  uint8_t* const sK = sQ + Cfg::kQTiles * Cfg::kTileBytes;
+  uint8_t* const sV = sK + NK * Cfg::kTileBytes;
+  uint8_t* const sRaw = sV + NV * Cfg::kTileBytes;
+  // 8-bit pages: the power of two that a row of Q was shifted by, and K's scales of a chunk's pages
+  long long* const scan = reinterpret_cast<long long*>(sRaw + (kE4M3 ? 2 * NR * Cfg::kRawBytes : 0));
+  int8_t* const row_shift = reinterpret_cast<int8_t*>(scan) + Cfg::kScanBytes;                    // [tile][row]
+  float* const page_scale = reinterpret_cast<float*>(row_shift + 2 * kTile);                      // [kBars][8]
   using Barriers = PrefixBarriers<NR>;
-  static_assert(sizeof(Barriers) <= 1024, "the barriers have a kilobyte");
-  Barriers* const bars = reinterpret_cast<Barriers*>(reinterpret_cast<uint8_t*>(xch_all) + Cfg::kXchBytes);
+  static_assert(sizeof(Barriers) <= 896, "what is set aside for the barriers");
+  Barriers* const bars = reinterpret_cast<Barriers*>(page_scale + kBars * 8);
 
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const int Hkv = p.c.n_kv_heads, G = p.group;
@@ -181,16 +227,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       const long long y = __shfl_up_sync(0xffffffffu, before, o), z = __shfl_up_sync(0xffffffffu, before_u, o);
       if (lane >= o) { before += y; before_u += z; }
     }
-    if (lane == 31) { bars->scratch[warp] = before; bars->scratch_u[warp] = before_u; }
+    if (lane == 31) { scan[warp] = before; scan[32 + warp] = before_u; }
     if (t == 0) bars->first_group = -1;
     __syncthreads();
     before -= mine;
     before_u -= units;
     long long total = 0, total_u = 0;
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) { before += bars->scratch[w]; before_u += bars->scratch_u[w]; }
-      total += bars->scratch[w];
-      total_u += bars->scratch_u[w];
+      if (w < warp) { before += scan[w]; before_u += scan[32 + w]; }
+      total += scan[w];
+      total_u += scan[32 + w];
     }
     if (total_u > p.max_units) {                          // groups that overlap: there is no room for their pieces
       if (blockIdx.x == 0 && t == 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_GROUP);
@@ -250,20 +296,22 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   if (t == 0) {
     mbar_init(&bars->q_full, 1);
     mbar_init(&bars->q_empty, 2);
+    mbar_init(&bars->q_wide, 8);
     mbar_init(&bars->v_tail, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->k_full[i], kE4M3 ? kWideWarps : 1); mbar_init(&bars->k_empty[i], 2);
-      mbar_init(&bars->v_full[i], kE4M3 ? kWideWarps : 1); mbar_init(&bars->v_empty[i], 2);
+    for (int i = 0; i < kBars; ++i) {
+      mbar_init(&bars->k_full[i], kE4M3 ? kWideKWarps : 1); mbar_init(&bars->k_empty[i], 2);
+      mbar_init(&bars->v_full[i], kE4M3 ? kWideVWarps : 1); mbar_init(&bars->v_empty[i], 2);
     }
-    for (int i = 0; i < NR; ++i) { mbar_init(&bars->raw_full[i], 1); mbar_init(&bars->raw_empty[i], kWideWarps); }
+    for (int kv = 0; kv < 2; ++kv)
+      for (int i = 0; i < NR; ++i) { mbar_init(&bars->raw_full[kv][i], 1); mbar_init(&bars->raw_empty[kv][i], kv ? kWideVWarps : kWideKWarps); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->s_full[i], 1);
-      mbar_init(&bars->p_full[i], kSoftmaxWarps);
+      for (int h = 0; h < 2; ++h) { mbar_init(&bars->s_full[i][h], 1); mbar_init(&bars->p_full[i][h], kSoftmaxWarps); }
+      mbar_init(&bars->o_step[i], 1);
       mbar_init(&bars->o_done[i], 1);
       mbar_init(&bars->o_free[i], kSoftmaxWarps);
-      mbar_init(&bars->turn[i], 1);
-      mbar_init(&bars->drained[i], 1);
     }
+    mbar_init(&bars->drained[0], 1);
+    mbar_init(&bars->drained[1], 1);
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -295,6 +343,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 
   if (warp == 0) {
     // ---------------- loader of K and V ----------------
+    if constexpr (kE4M3) give_registers<Cfg::kCtrlRegs>();
     const uint64_t pol_kv = l2_policy_evict_normal();
     constexpr int kCols = kE4M3 ? 1 : KH;                 // boxes of a page's rows
     const uint32_t box_bytes = static_cast<uint32_t>(P) * (kE4M3 ? D : 128);
@@ -321,25 +370,24 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (c + 1 < s.c1) next = block_of(s, c + 1, lane / kCols);
         if constexpr (kE4M3) {
           for (int kv = 0; kv < 2; ++kv) {
-            const int r = 2 * n + kv, slot = r % NR;
-            if (r >= NR) ok = wait(&bars->raw_empty[slot], (r / NR - 1) & 1);
+            const int slot = n % NR;
+            if (n >= NR) ok = wait(&bars->raw_empty[kv][slot], (n / NR - 1) & 1);
             if (!ok) break;
-            bring(kv ? &tmap_v : &tmap_k, sRaw + slot * Cfg::kRawBytes, &bars->raw_full[slot], blk);
-            k_out = r + 1;
+            bring(kv ? &tmap_v : &tmap_k, sRaw + (kv * NR + slot) * Cfg::kRawBytes, &bars->raw_full[kv][slot], blk);
+            (kv ? v_out : k_out) = n + 1;
           }
         } else {
-          const int par = n & 1;
-          const uint32_t freed = ((n >> 1) & 1) ^ 1;      // phase of chunk n - 2's release
-          if (n >= 2) ok = wait(&bars->k_empty[par], freed);
+          const int bar = n % kBars;
+          if (n >= NK) ok = wait(&bars->k_empty[(n - NK) % kBars], (n - NK) / kBars & 1);
           if (!ok) break;
-          bring(&tmap_k, sK + n % NS * Cfg::kTileBytes, &bars->k_full[par], blk);
+          bring(&tmap_k, sK + n % NK * Cfg::kTileBytes, &bars->k_full[bar], blk);
           k_out = n + 1;
-          if (n >= 2) ok = wait(&bars->v_empty[par], freed);
+          if (n >= NV) ok = wait(&bars->v_empty[(n - NV) % kBars], (n - NV) / kBars & 1);
           if (!ok) break;
           const int have = s.of.len - c * kTile;
-          uint8_t* const dst = sV + n % NS * Cfg::kTileBytes;
+          uint8_t* const dst = sV + n % NV * Cfg::kTileBytes;
           if (have >= kTile) {
-            bring(&tmap_v, dst, &bars->v_full[par], blk);
+            bring(&tmap_v, dst, &bars->v_full[bar], blk);
             v_out = n + 1;
           } else {
             // the prefix's last entries: a zero weight does not silence a NaN behind them, so those rows are cleared
@@ -353,7 +401,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->v_full[par]);
+            if (lane == 0) mbar_arrive(&bars->v_full[bar]);
           }
         }
       }
@@ -361,14 +409,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     // nothing may still be landing in shared memory when the CTA ends
     if (!ok && lane == 0) {
       if constexpr (kE4M3) {
-        for (int r = max(0, k_out - NR); r < k_out; ++r) mbar_wait_drain(&bars->raw_full[r % NR], (r / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+        for (int j = max(0, k_out - NR); j < k_out; ++j) mbar_wait_drain(&bars->raw_full[0][j % NR], (j / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+        for (int j = max(0, v_out - NR); j < v_out; ++j) mbar_wait_drain(&bars->raw_full[1][j % NR], (j / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
       } else {
-        for (int j = max(0, k_out - 2); j < k_out; ++j) mbar_wait_drain(&bars->k_full[j & 1], (j >> 1) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
-        for (int j = max(0, v_out - 2); j < v_out; ++j) mbar_wait_drain(&bars->v_full[j & 1], (j >> 1) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+        for (int j = max(0, k_out - NK); j < k_out; ++j) mbar_wait_drain(&bars->k_full[j % kBars], j / kBars & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+        for (int j = max(0, v_out - NV); j < v_out; ++j) mbar_wait_drain(&bars->v_full[j % kBars], j / kBars & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
       }
     }
   } else if (warp == 3) {
-    // ---------------- loader of Q ----------------
+    // ---------------- loader of Q, which tells the other roles what a segment is ----------------
+    if constexpr (kE4M3) give_registers<Cfg::kCtrlRegs>();
     const uint64_t pol_q = l2_policy_evict_first();
     const uint32_t q_bytes = static_cast<uint32_t>(KH) * 128 * G * p.tile_tokens;
     bool ok = true;
@@ -377,6 +427,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (segs > 0) ok = __all_sync(0xffffffffu, mbar_wait_parked(&bars->q_empty, (segs - 1) & 1, abort_flag, p.hdr, SITE_PREFIX_Q, limit));
       if (!ok) break;
       if (lane == 0) {
+        bars->brief[segs & 1] = Brief{s.unit, s.n0, s.c1 - s.c0, s.of.len - s.c0 * kTile, s.tokens, s.dual ? 1 : 0, s.group, s.g, s.c0, s.of.len};
         mbar_arrive_expect_tx(&bars->q_full, (s.dual ? 2 : 1) * q_bytes);
         for (int x = 0; x < (s.dual ? 2 : 1); ++x)
           for (int c = 0; c < KH; ++c)
@@ -385,284 +436,403 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       __syncwarp();
       ++segs;
     } while (advance(s, at));
-    if (lane == 0) mbar_wait_drain(&bars->q_full, (segs - 1) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
-  } else if (warp < kCtrlWarps) {
+    // the end of the share: nothing more to come
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_parked(&bars->q_empty, (segs - 1) & 1, abort_flag, p.hdr, SITE_PREFIX_Q, limit));
+    if (lane == 0) {
+      mbar_wait_drain(&bars->q_full, (segs - 1) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+      if (ok) {
+        bars->brief[segs & 1].chunks = 0;
+        mbar_arrive(&bars->q_full);
+      }
+    }
+  } else if (warp < 3) {
     // ---------------- issuer of one row tile ----------------
-    const int x = warp - 1;
-    constexpr uint32_t idesc_s = umma_idesc_bf16_f32(kTile, kTile);
+    // One lane issues a tile's contractions, so that they execute in the order they are issued in: O += P V of a step, then S of the step
+    // that takes P's place.  The whole warp walks the loop, with values that the compiler can see to be the same in every lane (a shuffle
+    // from lane 0), so that descriptors live in uniform registers: in a branch of one lane a contraction took twice as long to
+    // issue.  What is between two contractions is one warp's chain of dependent instructions, some ten cycles each: ring positions are
+    // carried along, not worked out.
+    if constexpr (kE4M3) give_registers<Cfg::kCtrlRegs>();
+    const int x = __shfl_sync(0xffffffffu, warp, 0) - 1;
+    // 8-bit pages: Q and K are fp16 (formats 0), P and V bf16
+    constexpr uint32_t idesc_s = umma_idesc_bf16_f32(kTile, kStep) & ~(kE4M3 ? (1u << 7) | (1u << 10) : 0u);
     constexpr uint32_t idesc_o = umma_idesc_bf16_f32(kTile, D) | (1u << 16);    // B (V) is MN-major
-    const uint32_t s_tmem = tmem_base + x * kTile, o_tmem = tmem_base + 256 + x * D;
-    bool ok = true;
-    int segs = 0, o_segs = 0;                             // segments before this one; those in which this tile had chunks
-    int pn = 0, turns = 0;
-    int issued = 0;
+    constexpr uint64_t kHalfTile = kStep * 128 >> 4;      // from a tile's first 64 entries to its second, in a descriptor's units
+    constexpr uint64_t kTileStep = Cfg::kTileBytes >> 4, kBlockStep = kHalfBytes >> 4;
+    const bool leader = elect_one();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 256 + x * D;
+    const uint64_t q_desc = umma_desc_k_sw128(smem_u32(sQ)), k_desc = umma_desc_k_sw128(smem_u32(sK)),
+                   v_desc = umma_desc_mn_sw128(smem_u32(sV), kHalfBytes);
+    bool ok = true, issued = false, again = false;        // again: the tile has had a segment with chunks
+    uint32_t q_phase = 0, p_phase = 0, o_phase = 0;       // (p_phase: the same for both buffers, they alternate)
     auto wait = [&](uint64_t* bar, uint32_t parity, int site) -> bool {
       return __all_sync(0xffffffffu, mbar_wait_nap(bar, parity, abort_flag, p.hdr, site, limit));
     };
-    do {
-      const int nk = s.chunks_of(x);
-      const uint32_t q_addr = smem_u32(sQ + (s.dual ? x : 0) * Cfg::kTileBytes);
-      auto releases = [&](uint64_t* bar) {                // a stage is free when both issuers have released it
-        tc_commit(bar);
-        if (!s.dual) tc_commit(bar);
-      };
-      ok = wait(&bars->q_full, segs & 1, SITE_PREFIX_Q);
-      for (int j = 0; nk > 0 && j <= nk && ok; ++j) {
-        if (s.dual) {
-          if (x == 0 && turns > 0) ok = wait(&bars->turn[0], (turns - 1) & 1, SITE_PREFIX_TURN);
-          if (x == 1) ok = wait(&bars->turn[1], turns & 1, SITE_PREFIX_TURN);
-          ++turns;
-        }
-        // V's contraction does not wait for the next K: where K and V have one tile each, the next K is widened behind the V that takes
-        // this one's place
-        if (ok && j > 0) {
-          const int n = s.chunk(x, j - 1);
-          ok = wait(&bars->v_full[n & 1], (n >> 1) & 1, SITE_PREFIX_V);
-          if (ok) ok = wait(&bars->p_full[x], pn & 1, SITE_PREFIX_P);
-          ++pn;
-          if (ok && j == 1 && o_segs > 0) ok = wait(&bars->o_free[x], (o_segs - 1) & 1, SITE_PREFIX_O);
-        }
-        if (!ok) break;
-        tc_fence_after_sync();
-        if (j > 0) {                                      // O (+)= P V
-          const int n = s.chunk(x, j - 1), st = n % NS;
-          const uint64_t b0 = umma_desc_mn_sw128(smem_u32(sV + st * Cfg::kTileBytes), kHalfBytes);
+    while (true) {
+      ok = wait(&bars->q_full, q_phase, SITE_PREFIX_Q);
+      if (!ok) break;
+      const Brief& shared = bars->brief[q_phase];
+      Brief br;
+      br.chunks = __shfl_sync(0xffffffffu, shared.chunks, 0);
+      br.n0 = __shfl_sync(0xffffffffu, shared.n0, 0);
+      br.dual = kOne ? 0 : __shfl_sync(0xffffffffu, shared.dual, 0);
+      if (br.chunks == 0) break;
+      if (kE4M3) ok = wait(&bars->q_wide, q_phase, SITE_PREFIX_Q);
+      q_phase ^= 1;
+      const int chunks = br.chunks_of(x), stride = br.dual ? 1 : 2;
+      const uint64_t a0 = q_desc + (br.dual ? x : 0) * kTileStep;
+      int n = br.chunk(x, 0), k_at = n % NK, v_at = n % NV, before = 0;   // the chunk whose S is next; its tiles; the one before it
+      int v_before = 0;
+      for (int j = 0; j <= chunks && chunks > 0 && ok; ++j) {
+        uint64_t* const k_full = &bars->k_full[n % kBars];
+        uint64_t* const v_full = &bars->v_full[before % kBars];
+        const uint32_t k_phase = n / kBars & 1, v_phase = before / kBars & 1;
+        const uint64_t kb = k_desc + k_at * kTileStep, vb = v_desc + v_before * kTileStep;
 #pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)         // 16 entries = 8 packed columns of P, 2048 bytes of V per step
-            if (elect_one())
-              tc_mma_bf16_ts(o_tmem, s_tmem + (kk >> 2) * 64 + (kk & 3) * 8, b0 + static_cast<uint64_t>(kk * (2048 >> 4)), idesc_o,
-                             (j > 1 || kk > 0) ? 1u : 0u);
-          if (elect_one()) releases(&bars->v_empty[n & 1]);
-          issued = 1;
-        }
-        if (j < nk) {                                     // S = Q K^T
-          const int n = s.chunk(x, j), st = n % NS;
-          ok = wait(&bars->k_full[n & 1], (n >> 1) & 1, SITE_PREFIX_K);
-          if (!ok) break;
-          tc_fence_after_sync();
-          const uint64_t a0 = umma_desc_k_sw128(q_addr), b0 = umma_desc_k_sw128(smem_u32(sK + st * Cfg::kTileBytes));
+        for (int h = 0; h < 2; ++h) {
+          if (j > 0) {                                    // O (+)= P V of the chunk before
+            if (h == 0) {
+              ok = wait(v_full, v_phase, SITE_PREFIX_V);
+              if (ok && j == 1 && again) {
+                ok = wait(&bars->o_free[x], o_phase, SITE_PREFIX_O);
+                o_phase ^= 1;
+              }
+            }
+            ok = ok && wait(&bars->p_full[x][h], p_phase, SITE_PREFIX_P);
+            if (!ok) break;
+            tc_fence_after_sync();
+            if (leader) {
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {           // 64-element block kk / 4, 32 bytes per step inside it
-            const uint64_t step = static_cast<uint64_t>(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
-            if (elect_one()) tc_mma_bf16(s_tmem, a0 + step, b0 + step, idesc_s, kk > 0 ? 1u : 0u);
+              for (int kk = 0; kk < kStep / 16; ++kk)     // 16 entries = 8 packed columns of P, 2048 bytes of V
+                tc_mma_bf16_ts(o_tmem, s_tmem + h * kStep + kk * 8, vb + h * kHalfTile + static_cast<uint64_t>(kk * (2048 >> 4)), idesc_o,
+                               (j > 1 || h > 0 || kk > 0) ? 1u : 0u);
+              tc_commit(&bars->o_step[x]);
+              if (h == 1) {                               // a tile is free when both row tiles have released it
+                tc_commit(&bars->v_empty[before % kBars]);
+                if (!br.dual) tc_commit(&bars->v_empty[before % kBars]);
+                if (j == chunks) tc_commit(&bars->o_done[x]);
+              }
+            }
+            __syncwarp();
           }
-          if (elect_one()) {
-            releases(&bars->k_empty[n & 1]);
-            if (!(x == 0 && n == p.skip_commit)) tc_commit(&bars->s_full[x]);     // (test hook: a completion that is never signalled)
+          if (j < chunks) {                               // S = Q K^T
+            if (h == 0) {
+              ok = wait(k_full, k_phase, SITE_PREFIX_K);
+              if (!ok) break;
+              tc_fence_after_sync();
+              issued = true;
+            }
+            if (leader) {
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {       // 64-element block kk / 4, 32 bytes per step inside it
+                const uint64_t step = (kk >> 2) * kBlockStep + (kk & 3) * 2;
+                tc_mma_bf16(s_tmem + h * kStep, a0 + step, kb + h * kHalfTile + step, idesc_s, kk > 0 ? 1u : 0u);
+              }
+              if (!(x == 0 && n == p.skip_commit)) tc_commit(&bars->s_full[x][h]);    // (test hook: a completion that is never signalled)
+              if (h == 1) {
+                tc_commit(&bars->k_empty[n % kBars]);
+                if (!br.dual) tc_commit(&bars->k_empty[n % kBars]);
+              }
+            }
+            __syncwarp();
           }
-          issued = 1;
         }
-        if (s.dual && elect_one()) mbar_arrive(&bars->turn[x ^ 1]);
+        if (j > 0) p_phase ^= 1;
+        before = n;
+        v_before = v_at;
+        n += stride;
+        k_at = NK == 1 ? 0 : n % NK;
+        v_at += stride;
+        if (v_at >= NV) v_at -= NV;
       }
       if (!ok) break;
-      if (elect_one()) {
-        if (nk > 0) { tc_commit(&bars->o_done[x]); tc_commit(&bars->q_empty); }
-        else mbar_arrive(&bars->q_empty);
+      if (leader) {
+        if (chunks > 0) tc_commit(&bars->q_empty); else mbar_arrive(&bars->q_empty);
       }
-      if (nk > 0) ++o_segs;
-      ++segs;
-    } while (advance(s, at));
+      __syncwarp();
+      again = again || chunks > 0;
+    }
     // every contraction issued has finished before tensor memory is released
     if (issued) {
-      if (elect_one()) tc_commit(&bars->drained[x]);
+      if (leader) tc_commit(&bars->drained[x]);
       __syncwarp();
       mbar_wait_drain(&bars->drained[x], 0, p.hdr, SITE_PREFIX_DRAIN, limit);
     }
   } else if (warp < kCtrlWarps + 2 * kSoftmaxWarps) {
-    // ---------------- softmax: eight warps per row tile, two threads per row, 64 entries of the chunk each ----------------
+    // ---------------- softmax: four warps per row tile, a thread per row ----------------
+    if constexpr (kE4M3) take_registers<Cfg::kSoftmaxRegs>();
     const int gw = warp - kCtrlWarps;
-    const int x = gw >> 3, g8 = gw & 7;                   // row tile; warp of the tile
-    const int quarter = warp & 3, half = g8 >> 2;         // a tile's warps cover the four lane quarters twice
+    const int x = gw >> 2, quarter = gw & 3;              // row tile; lane quarter (warp % 4: the control warps are four)
     const int r = quarter * 32 + lane;                    // row of the tile = tensor-memory lane
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-    const uint32_t s_addr = lane_addr + x * kTile + half * 64;         // this thread's 64 S columns; P goes into the first 32
-    const uint32_t o_addr = lane_addr + 256 + x * D + half * (D / 2);  // this thread's D / 2 columns of O
-    float* const xch = xch_all + x * (2 * 2 * kTile);
-    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + x * 4 + quarter) : "memory"); };
-    constexpr int HN = kTile / 2;
+    const uint32_t s_addr = lane_addr + x * kTile, o_addr = lane_addr + 256 + x * D;
     bool ok = true;
-    int sn = 0, o_segs = 0;                               // this tile's chunks, and segments with chunks, so far
-    do {
-      const int nk = s.chunks_of(x), rows = s.rows_of(p, x);
-      const bool active = quarter * 32 < rows;            // (uniform for the two warps of a lane quarter)
-      const long long piece = static_cast<long long>(s.unit) + blockIdx.x;
-      float2* const ml = p.part_ml + (piece * 2 + x) * p.tile_rows;
-      if (!active) {
+    int sn = 0, o_segs = 0, segs = 0;                     // this tile's steps, its segments with steps, and all segments so far
+    while (ok) {
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars->q_full, segs & 1, abort_flag, p.hdr, SITE_PREFIX_Q, limit));
+      if (!ok) break;
+      const Brief& br = bars->brief[segs & 1];
+      if (br.chunks == 0) break;
+      const int dual = kOne ? 0 : br.dual, steps = 2 * br.chunks_of(x), n_first = br.chunk(x, 0), n_step = dual ? 1 : 2;
+      const int tokens = dual ? (x == 0 ? p.tile_tokens : br.tokens - p.tile_tokens) : br.tokens, rows = tokens * G;
+      int seen = br.seen - (n_first - br.n0) * kTile;     // entries from the step's first one to the prefix's end
+      const long long piece = static_cast<long long>(br.unit) + blockIdx.x;
+      ++segs;
+      if (quarter * 32 >= rows) {
         // no rows: the warp only keeps step (nobody may run ahead of a barrier by two phases)
-        for (int j = 0; j < nk; ++j, ++sn) {
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->s_full[x], sn & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit));
-          if (ok && lane == 0) mbar_arrive(&bars->p_full[x]);
+        for (int i = 0; i < steps && ok; ++i, ++sn) {
+          ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->s_full[x][sn & 1], (sn >> 1) & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit));
+          if (ok && lane == 0) mbar_arrive(&bars->p_full[x][sn & 1]);
         }
-        if (nk > 0) {
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->o_done[x], o_segs & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit));
+        if (steps > 0 && ok) {
+          ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->o_done[x], o_segs & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit));
           if (ok && lane == 0) mbar_arrive(&bars->o_free[x]);
           ++o_segs;
         }
         continue;
       }
-      float m_ref = -INFINITY, l = 0.0f;                  // the reference is the same in both threads of a row; l is this half's
-      // Both warps of a pair walk every chunk and meet at the pair's barrier once per chunk whatever happens: a warp whose
-      // wait gave up skips the work of the chunk, never the barrier.
-      for (int j = 0; j < nk; ++j, ++sn) {
-        const int buf = sn & 1;
-        if (ok) ok = mbar_wait_bounded(&bars->s_full[x], sn & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit);
+      float by_row = p.scale_log2;                        // what a logit is multiplied by
+      if (kE4M3) {
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars->q_wide, (segs - 1) & 1, abort_flag, p.hdr, SITE_PREFIX_Q, limit));
+        if (!ok) break;
+        by_row *= __uint_as_float(pow2_bits(-row_shift[(dual ? x : 0) * kTile + r]));
+      }
+      float m_ref = -INFINITY, l = 0.0f;
+      for (int i = 0; i < steps; ++i, ++sn) {
+        const int h = i & 1, n = n_first + n_step * (i >> 1);         // (a segment's steps are even in number: sn & 1 == h)
+        ok = mbar_wait_bounded(&bars->s_full[x][h], (sn >> 1) & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit);
+        if (kE4M3 && ok) ok = mbar_wait_bounded(&bars->k_full[n % kBars], n / kBars & 1, abort_flag, p.hdr, SITE_PREFIX_K, limit);   // the scales (long there)
         ok = __all_sync(0xffffffffu, ok);
-        const int c = s.c0 + s.chunk(x, j) - s.n0;
-        const int seen = s.of.len - c * kTile - half * HN; // entries of this half
-        const bool tail = seen < HN;
-        float half_max = -INFINITY;
-        if (ok) {
-          tc_fence_after_sync();
+        if (!ok) break;
+        tc_fence_after_sync();
+        float v[kStep / 32][32];
+        float f[kE4M3 ? kStep / 16 : 1];                  // what 16 logits (of one page) are multiplied by
+        float most = -INFINITY;
+        f[0] = by_row;
 #pragma unroll
-          for (int cc = 0; cc < HN / 32; ++cc) {
-            float v[32];
-            tmem_ld_32x32(s_addr + cc * 32, v);
-            if (tail) {
+        for (int c = 0; c < kStep / 32; ++c) tmem_ld_32x32(s_addr + h * kStep + c * 32, v[c]);
+        if (seen < kStep) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = cc * 32 + i < seen ? v[i] : -INFINITY;
-            }
-            float mx[4] = {v[0], v[1], v[2], v[3]};
+          for (int c = 0; c < kStep / 32; ++c)
 #pragma unroll
-            for (int i = 4; i < 32; i += 4) {
-              mx[0] = fmaxf(mx[0], v[i]); mx[1] = fmaxf(mx[1], v[i + 1]); mx[2] = fmaxf(mx[2], v[i + 2]); mx[3] = fmaxf(mx[3], v[i + 3]);
-            }
-            half_max = fmaxf(half_max, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
-          }
+            for (int e = 0; e < 32; ++e) v[c][e] = c * 32 + e < seen ? v[c][e] : -INFINITY;
         }
-        xch[(buf * 2 + half) * kTile + r] = half_max;
-        pair_sync();
-        if (!ok) continue;
-        const float most = fmaxf(half_max, xch[(buf * 2 + (half ^ 1)) * kTile + r]) * p.scale_log2;     // the scale is positive
-        const bool move = most > m_ref + kSlackLog2;
-        const float alpha = move ? ex2(m_ref - most) : 1.0f;        // 0 at a row's first logits
-        if (move) { m_ref = most; l *= alpha; }
-        if (j >= 1 && __any_sync(0xffffffffu, move)) {
-          // O is complete up to the chunk before: the contraction that added it was issued before this chunk's S, by the same thread
+        seen -= h == 0 ? kStep : (n_step * 2 - 1) * kStep;
 #pragma unroll
-          for (int cc = 0; cc < D / 64; ++cc) {
-            float o[32];
-            tmem_ld_32x32(o_addr + cc * 32, o);
+        for (int c = 0; c < kStep / 32; ++c)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] *= alpha;
-            tmem_st_32x32(o_addr + cc * 32, o);
+          for (int z = 0; z < 2; ++z) {
+            // positive, so that masked logits stay -infinity
+            if (kE4M3) f[c * 2 + z] = fmaxf(by_row * page_scale[n % kBars * 8 + ((h * kStep + c * 32 + z * 16) >> p.c.page_log2)], 1.17549435e-38f);
+            float mx[2] = {v[c][z * 16], v[c][z * 16 + 1]};
+#pragma unroll
+            for (int e = 2; e < 16; e += 2) { mx[0] = fmaxf(mx[0], v[c][z * 16 + e]); mx[1] = fmaxf(mx[1], v[c][z * 16 + e + 1]); }
+            most = fmaxf(most, fmaxf(mx[0], mx[1]) * f[kE4M3 ? c * 2 + z : 0]);
           }
-          tmem_wait_st();
+        // the reference moves only when the step's maximum is far above it (or at a row's first logits)
+        const bool move = most > m_ref + kSlackLog2;
+        if (__any_sync(0xffffffffu, move)) {
+          const float alpha = move ? ex2(m_ref - most) : 1.0f;
+          if (move) { m_ref = most; l *= alpha; }
+          if (i >= 1) {
+            // The step before this one may still be on its way into O.  (The one before that is in it: S of this step was issued behind it.  So
+            // the barrier is at this phase or through with it, never further.)
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars->o_step[x], (sn - 1) & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit));
+            if (!ok) break;
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              float o[16];
+              tmem_ld_32x16(o_addr + c * 16, o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] *= alpha;
+              tmem_st_32x16(o_addr + c * 16, o);
+            }
+          }
         }
         const float neg_ref = m_ref == -INFINITY ? 0.0f : -m_ref;   // nothing seen yet: every weight is 2^-inf
-        float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float ls[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int cc = 0; cc < HN / 32; ++cc) {
-          float v[32];
-          tmem_ld_32x32(s_addr + cc * 32, v);
-          if (tail) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = cc * 32 + i < seen ? v[i] : -INFINITY;
-          }
+        for (int c = 0; c < kStep / 32; ++c) {
           float packed[16];
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float e0 = ex2(fmaf(v[i], p.scale_log2, neg_ref));
-            const float e1 = ex2(fmaf(v[i + 1], p.scale_log2, neg_ref));
-            ls[i & 2] += e0;
-            ls[(i & 2) + 1] += e1;
-            packed[i / 2] = __uint_as_float(pack16<false>(e0, e1));
+          for (int e = 0; e < 32; e += 2) {
+            const float by = f[kE4M3 ? (c * 32 + e) / 16 : 0];
+            const float e0 = ex2(fmaf(v[c][e], by, neg_ref));
+            const float e1 = ex2(fmaf(v[c][e + 1], by, neg_ref));
+            ls[0] += e0;
+            ls[1] += e1;
+            packed[e / 2] = __uint_as_float(pack16<false>(e0, e1));
           }
-          tmem_st_32x16(s_addr + cc * 16, packed);
+          tmem_st_32x16(s_addr + h * kStep + c * 16, packed);
         }
-        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        l += ls[0] + ls[1];
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->p_full[x]);
+        if (lane == 0) mbar_arrive(&bars->p_full[x][h]);
       }
-      if (nk == 0) {
-        if (half == 0 && r < rows) ml[r] = make_float2(-INFINITY, 0.0f);
+      if (!ok) break;
+      // ---- the segment's piece: columns of O by rows, so that a warp's stores are whole lines ----
+      float2* const ml = p.part_ml + (piece * 2 + x) * p.tile_rows + r;
+      if (steps == 0) {
+        if (r < rows) *ml = make_float2(-INFINITY, 0.0f);
         continue;
       }
-      // ---- the segment's piece: columns of O by rows, so that a warp's stores are whole lines ----
-      {
-        const int buf = sn & 1;                           // the exchange buffer that the last chunk did not use
-        xch[(buf * 2 + half) * kTile + r] = l;
-        pair_sync();
-        l += xch[(buf * 2 + (half ^ 1)) * kTile + r];
-        pair_sync();                                      // the next segment's first chunk uses that buffer again
-        if (ok) ok = mbar_wait_bounded(&bars->o_done[x], o_segs & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit);
-        ok = __all_sync(0xffffffffu, ok);
-        ++o_segs;
-        if (!ok) continue;
-        tc_fence_after_sync();
-        if (half == 0 && r < rows) ml[r] = make_float2(m_ref, l);
-        float* const po = p.part_o + ((piece * 2 + x) * D + half * (D / 2)) * p.tile_rows + r;
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars->o_done[x], o_segs & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit));
+      ++o_segs;
+      if (!ok) break;
+      tc_fence_after_sync();
+      if (r < rows) __stcg(ml, make_float2(m_ref, l));
+      int apart = p.tile_rows;
+      asm volatile("" : "+r"(apart));                     // (multiples of it are not worth a register each all through the loop above)
+      float* po = p.part_o + (piece * 2 + x) * D * p.tile_rows + r;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float o[32];
+        tmem_ld_32x32(o_addr + c * 32, o);
+        if (r < rows) {
 #pragma unroll
-        for (int cc = 0; cc < D / 64; ++cc) {
-          float o[32];
-          tmem_ld_32x32(o_addr + cc * 32, o);
-          if (r < rows) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) __stcg(po + static_cast<long long>(cc * 32 + i) * p.tile_rows, o[i]);
-          }
+          for (int e = 0; e < 32; ++e) __stcg(po + static_cast<long long>(e) * apart, o[e]);
         }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->o_free[x]);
+        po += 32ll * apart;
       }
-    } while (advance(s, at));
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->o_free[x]);
+    }
   } else {
-    // ---------------- widening: codes to bf16 tiles ----------------
+    // ---------------- widening (8-bit pages): Q and K to fp16, V to bf16 ----------------
     if constexpr (kE4M3) {
-      const int w = warp - kCtrlWarps - 2 * kSoftmaxWarps;               // rows 32 w .. of every tile
+      give_registers<Cfg::kWideRegs>();
+      const int w = warp - kCtrlWarps - 2 * kSoftmaxWarps;
       bool ok = true;
-      int n = 0;
+      int n = 0, segs = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity, int site) -> bool {
         return __all_sync(0xffffffffu, mbar_wait_nap(bar, parity, abort_flag, p.hdr, site, limit));
       };
-      // scales of page `lane` of a chunk
-      auto scales_of = [&](const Segment& y, int c) -> float2 {
-        const int blk = block_of(y, c, lane);
-        return blk < 0 ? make_float2(0.0f, 0.0f) : make_float2(__ldcg(p.c.k_scales + blk), __ldcg(p.c.v_scales + blk));
+      const int kv = w >= kWideKWarps, first = kv ? (w - kWideKWarps) * (kTile / kWideVWarps) : w * (kTile / kWideKWarps);   // K or V; first row of every tile
+      const float* const scales = kv ? p.c.v_scales : p.c.k_scales;
+      // block of page `lane` of the prefix's chunk c, and its scale
+      auto block_in = [&](const Brief& y, int c) -> int {
+        const int key = c * kTile + (lane << p.c.page_log2);
+        if (lane >= pages || key >= y.len) return -1;
+        const long long blk = pool_block(__ldcg(p.table + static_cast<size_t>(y.group) * p.max_pages + (key >> p.c.page_log2)), p.c.n_pages, Hkv, y.g);
+        return blk < 0 ? y.g : static_cast<int>(blk);     // page 0 instead, as the loader takes it
       };
-      constexpr int kPieces = D / 16;                     // 16-byte pieces of a row
+      auto scale_in = [&](int blk) -> float { return blk < 0 ? 0.0f : __ldcg(scales + blk); };
+      constexpr int kPieces = D / 16;                     // 16-byte pieces of a row of codes
       constexpr int kRowsAt = 32 / kPieces;               // rows of a warp's step
       // Eight lanes (what shared memory serves at a time) take four pieces of one column block of two neighbouring rows: the
       // swizzle puts their 16-byte stores into eight different places of a line.
       const int c4 = lane & 3, block = D == 128 ? (lane >> 3) & 1 : 0;
       const int row_in = ((lane >> 2) & 1) + (D == 128 ? (lane >> 4) * 2 : (lane >> 3) * 2);
-      do {
-        float2 next = scales_of(s, s.c0);
-        for (int c = s.c0; c < s.c1 && ok; ++c, ++n) {
-          const float2 sc = next;
-          if (c + 1 < s.c1) next = scales_of(s, c + 1);
-          const int have = s.of.len - c * kTile;
-          for (int kv = 0; kv < 2; ++kv) {
-            const int raw = 2 * n + kv, slot = raw % NR;
-            ok = wait(&bars->raw_full[slot], (raw / NR) & 1, SITE_PREFIX_RAW);
-            const int gone = n - NS;                      // the chunk whose tile this one takes
-            if (ok && gone >= 0) ok = wait(kv ? &bars->v_empty[gone & 1] : &bars->k_empty[gone & 1], (gone >> 1) & 1, SITE_PREFIX_RAW);
-            if (!ok) break;
-            const uint8_t* const src = sRaw + slot * Cfg::kRawBytes;
-            uint8_t* const dst = (kv ? sV : sK) + n % NS * Cfg::kTileBytes + block * kHalfBytes;
+      while (true) {
+        // ---- Q: bf16 to fp16 in place, a thread per row, after a power-of-two shift that brings the row's largest element to [2^14, 2^15):
+        // exact down to 2^-28 of it, and what is smaller is off by at most 2^-39 of the largest ----
+        ok = wait(&bars->q_full, segs & 1, SITE_PREFIX_Q);
+        if (!ok) break;
+        const Brief br = bars->brief[segs & 1];
+        if (br.chunks == 0) break;
+        // (page, then scale: a chain of two loads, each started a chunk before the other needs it)
+        float next = scale_in(block_in(br, br.c0));
+        int next_block = block_in(br, br.c0 + 1);
+        {
+          const int tile = w >> 2, row = (w & 3) * 32 + lane;         // (the first eight warps)
+          if (tile == 0 || (!kOne && tile == 1 && br.dual)) {
+            uint8_t* const at_row = sQ + tile * Cfg::kTileBytes + row * 128;
+            float m = 0.0f;
 #pragma unroll 4
-            for (int y = 0; y < 32 / kRowsAt; ++y) {
-              const int r = w * 32 + y * kRowsAt + row_in;
-              const float f = __shfl_sync(0xffffffffu, kv ? sc.y : sc.x, (w * 32 + y * kRowsAt) >> p.c.page_log2);
-              uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-              if (r < have) {                             // behind the prefix's end: zeros
-                const uint4 v = *reinterpret_cast<const uint4*>(src + r * D + (block * 4 + c4) * 16);
-                a = widen8(v.x, v.y, f);
-                b = widen8(v.z, v.w, f);
+            for (int i = 0; i < D / 8; ++i) {
+              const uint4 q = *reinterpret_cast<const uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
+              const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float lo, hi;
+                unpack16<false>(qw[e], lo, hi);
+                m = fmaxf(m, fmaxf(fabsf(lo), fabsf(hi)));
               }
-              *reinterpret_cast<uint4*>(dst + r * 128 + (((2 * c4) ^ (r & 7)) << 4)) = a;
-              *reinterpret_cast<uint4*>(dst + r * 128 + (((2 * c4 + 1) ^ (r & 7)) << 4)) = b;
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-              mbar_arrive(kv ? &bars->v_full[n & 1] : &bars->k_full[n & 1]);
-              mbar_arrive(&bars->raw_empty[slot]);
+            int up = m > 0.0f ? 14 - scale_log2(__float_as_uint(m)) : 0;
+            up = up > 120 ? 120 : up;                     // of a subnormal row; otherwise within [-113, 120] as it stands
+            const float f = __uint_as_float(pow2_bits(up));
+            row_shift[tile * kTile + row] = static_cast<int8_t>(up);
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+              uint4* const here = reinterpret_cast<uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
+              const uint4 q = *here;
+              uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float lo, hi;
+                unpack16<false>(qw[e], lo, hi);
+                qw[e] = pack16<true>(lo * f, hi * f);
+              }
+              *here = make_uint4(qw[0], qw[1], qw[2], qw[3]);
             }
           }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && w < 8) mbar_arrive(&bars->q_wide);
         }
-      } while (ok && advance(s, at));
+        ++segs;
+        for (int c = br.c0; c < br.c0 + br.chunks && ok; ++c, ++n) {
+          const float sc = next;
+          next = scale_in(next_block);
+          next_block = block_in(br, c + 2);
+          const int have = br.len - c * kTile;
+          const int slot = n % NR, gone = n - (kv ? NV : NK);         // gone: the chunk whose tile this one takes
+          ok = wait(&bars->raw_full[kv][slot], (n / NR) & 1, SITE_PREFIX_RAW);
+          if (ok && gone >= 0) ok = wait(kv ? &bars->v_empty[gone % kBars] : &bars->k_empty[gone % kBars], gone / kBars & 1, SITE_PREFIX_RAW);
+          if (!ok) break;
+          const uint8_t* const src = sRaw + (kv * NR + slot) * Cfg::kRawBytes + (first + row_in) * D + (block * 4 + c4) * 16;
+          uint8_t* const tile = (kv ? sV + n % NV * Cfg::kTileBytes : sK + n % NK * Cfg::kTileBytes) + block * kHalfBytes;
+          // row y * kRowsAt + row_in of the warp's: where its two 16-byte pieces go
+          auto put = [&](int y, const uint4& a, const uint4& b) {
+            const int r = first + y * kRowsAt + row_in;
+            *reinterpret_cast<uint4*>(tile + r * 128 + (((2 * c4) ^ (r & 7)) << 4)) = a;
+            *reinterpret_cast<uint4*>(tile + r * 128 + (((2 * c4 + 1) ^ (r & 7)) << 4)) = b;
+          };
+          if (kv == 0) {
+            if (first == 0 && lane < 8) page_scale[n % kBars * 8 + lane] = sc;
+#pragma unroll 2
+            for (int y = 0; y < kTile / kWideKWarps / kRowsAt; ++y) {      // (what lies behind the prefix's end is masked)
+              const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+              put(y, widen8_half(q.x, q.y), widen8_half(q.z, q.w));
+            }
+          } else {
+            constexpr int kSteps = kTile / kWideVWarps / kRowsAt;
+            const float f = __shfl_sync(0xffffffffu, sc, first >> p.c.page_log2);      // the warp's 16 rows are one page's
+            // 2^120 f in one factor, unless that is too large for one
+            const bool two = f > 128.0f;
+            const uint32_t up = __byte_perm(__float_as_uint(two ? 1.329227995784916e36f : f * 1.329227995784916e36f), 0, 0x3232);
+            const uint32_t times = __byte_perm(__float_as_uint(two ? f : 1.0f), 0, 0x3232);
+            uint32_t odd = 0;
+#pragma unroll 2
+            for (int y = 0; y < kSteps; ++y) {
+              const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+              put(y, widen8_bf16(q.x, q.y, up, times, odd), widen8_bf16(q.z, q.w, up, times, odd));
+            }
+            // NaN among the codes, or the prefix's end among the rows: those again
+            if (__any_sync(0xffffffffu, (odd & 0x7fff7fffu) != 0) || have < kTile) {
+#pragma unroll 1
+              for (int y = 0; y < kSteps; ++y) {
+                uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+                if (first + y * kRowsAt + row_in >= have) q = make_uint4(0u, 0u, 0u, 0u);       // behind the end: zeros
+                put(y, widen8_any(q.x, q.y, f), widen8_any(q.z, q.w, f));
+              }
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(kv ? &bars->v_full[n % kBars] : &bars->k_full[n % kBars]);
+            mbar_arrive(&bars->raw_empty[kv][slot]);
+          }
+        }
+        if (!ok) break;
+      }
     }
   }
 
@@ -677,7 +847,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 
 // Joins a query row's pieces and the attention over its own entries.  A warp takes 32 rows (lane = row; the pieces hold columns by rows)
 // and 8 columns; blockIdx: (32 rows, KV head, 32 columns).
-template <int D>
+template <int D, bool kE4M3>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const PrefixParams p) {
   __shared__ long long chunk0[kMaxPrefixes + 1];          // chunks and units of the prefixes before
   __shared__ int unit0[kMaxPrefixes + 1];
@@ -774,7 +944,8 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const PrefixParams p)
         const size_t tile = both == 2 ? s : 2 * s;        // tiles of a piece lie side by side
         v[k] = __ldcg(ml + tile * step_ml);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[k][i] = __ldcg(po + tile * step_o + static_cast<size_t>(i) * p.tile_rows);
+        for (int i = 0; i < 8; ++i)                        // (8-bit pages: columns 1 and 2 of four have changed places)
+          o[k][i] = __ldcg(po + tile * step_o + static_cast<size_t>(kE4M3 && ((i ^ (i >> 1)) & 1) ? i ^ 3 : i) * p.tile_rows);
       }
     }
 #pragma unroll
@@ -798,15 +969,15 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const PrefixParams p)
 
 namespace {
 
-template <int D, bool kE4M3>
+template <int D, bool kE4M3, bool kOne>
 cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t stream, int* launches) {
-  using Cfg = PrefixCfg<D, kE4M3>;
+  using Cfg = PrefixCfg<D, kE4M3, kOne>;
   static PerDeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(prefix_attn_kernel<D, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+    e = cudaFuncSetAttribute(prefix_attn_kernel<D, kE4M3, kOne>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
     if (e != cudaSuccess) return e;
     configured.set(dev);
   }
@@ -819,24 +990,30 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
   fill_pdl_attribute(&attr[0]);
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, prefix_attn_kernel<D, kE4M3>, tq, tk, tv, p);
+  e = cudaLaunchKernelEx(&cfg, prefix_attn_kernel<D, kE4M3, kOne>, tq, tk, tv, p);
   if (e != cudaSuccess) return e;
   ++*launches;
   const long long rows = static_cast<long long>(p.c.batch) * p.q_len * p.group;
   cfg.gridDim = dim3(static_cast<unsigned>((rows + 31) / 32), p.c.n_kv_heads, D / 32);
   cfg.blockDim = dim3(128);
   cfg.dynamicSmemBytes = 0;
-  e = cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D>, p);
+  e = cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, kE4M3>, p);
   if (e == cudaSuccess) ++*launches;
   return e;
+}
+
+template <int D, bool kE4M3>
+cudaError_t launch_d(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t stream, int* launches) {
+  if (static_cast<long long>(p.c.batch) * p.q_len <= p.tile_tokens) return launch_t<D, kE4M3, true>(tq, tk, tv, p, stream, launches);
+  return launch_t<D, kE4M3, false>(tq, tk, tv, p, stream, launches);
 }
 
 }  // namespace
 
 cudaError_t launch_prefix_attn(const CUtensorMap& tmap_q, const CUtensorMap& tmap_k, const CUtensorMap& tmap_v, const PrefixParams& p,
                                int head_dim, bool e4m3, cudaStream_t stream, int* launches) {
-  if (head_dim == 128) return e4m3 ? launch_t<128, true>(tmap_q, tmap_k, tmap_v, p, stream, launches) : launch_t<128, false>(tmap_q, tmap_k, tmap_v, p, stream, launches);
-  if (head_dim == 64) return e4m3 ? launch_t<64, true>(tmap_q, tmap_k, tmap_v, p, stream, launches) : launch_t<64, false>(tmap_q, tmap_k, tmap_v, p, stream, launches);
+  if (head_dim == 128) return e4m3 ? launch_d<128, true>(tmap_q, tmap_k, tmap_v, p, stream, launches) : launch_d<128, false>(tmap_q, tmap_k, tmap_v, p, stream, launches);
+  if (head_dim == 64) return e4m3 ? launch_d<64, true>(tmap_q, tmap_k, tmap_v, p, stream, launches) : launch_d<64, false>(tmap_q, tmap_k, tmap_v, p, stream, launches);
   return cudaErrorInvalidValue;
 }
 
