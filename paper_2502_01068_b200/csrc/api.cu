@@ -1210,7 +1210,7 @@ int check_eviction(const fastkv_paged_cache* c, const fastkv_eviction* v) {
 size_t evict_bytes(const fastkv_paged_cache& c, const fastkv_eviction& v) {
   // a call that can cut nothing plans nothing
   const size_t pairs = v.max_len > v.limit ? static_cast<size_t>(c.batch) * c.n_kv_heads : 0;
-  return round_up(sizeof(WorkspaceHeader) + pairs * evict_plan_words(v.keep, v.window) * sizeof(int), 256);
+  return round_up(sizeof(WorkspaceHeader) + pairs * evict_plan_words(v.keep, v.window, c.page_size) * sizeof(int), 256);
 }
 }  // namespace
 
@@ -1250,6 +1250,7 @@ int fastkv_paged_evict(const fastkv_paged_cache* cache, const fastkv_eviction* e
   p.row_bytes = c.head_dim * (c.format == FASTKV_CACHE_E4M3 ? 1 : 2);
   p.lens = lens; p.new_lens = new_lens; p.weights = weights; p.ids = ids; p.new_weights = new_weights; p.new_ids = new_ids; p.stride = stride;
   p.plan = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
+  p.plan_words = evict_plan_words(p.keep, p.window, c.page_size);
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
   cudaError_t e;
   {

@@ -128,12 +128,17 @@ struct EvictParams {
   float* new_weights;
   int* new_ids;               // null with ids
   long long stride;
-  int* plan;                  // [B][Hkv][evict_plan_words]
+  int* plan;                  // [B][Hkv][plan_words]
+  long long plan_words;
   WorkspaceHeader* hdr;
 };
 // A (sequence, KV head)'s plan: how many of the first keep - window slots keep their entry; for each of those slots -1 or the
-// number of the entry that moves in; the slots of the kept candidates by rank (written from the first that moves on).
-inline long long evict_plan_words(int keep, int window) { return (2ll * (keep - window) + 1 + 3) / 4 * 4; }
+// number of the entry that moves in; the slots of the kept candidates by rank (written from the first that moves on); the free slots;
+// how many of them are before each page.
+inline long long evict_plan_words(int keep, int window, int page_size) {
+  const long long m = keep - window;
+  return (3 * m + 1 + m / page_size + 1 + 3) / 4 * 4;
+}
 cudaError_t launch_evict_plan(const EvictParams& p, cudaStream_t stream);
 cudaError_t launch_evict_move(const EvictParams& p, bool e4m3, cudaStream_t stream);
 

@@ -49,16 +49,22 @@ struct PlanView {
   int* kept_below;                 // kept candidates in slots below m
   int* hole;                       // [m]: -1, or the slot's number among the free ones
   int* from;                       // [m]: slot of the kept candidate of rank r, written for those in slots >= m
+  int* free_slot;                  // [m]: the free slots in ascending order
+  int* page_first;                 // [pages below m, + 1]: free slots before the page
 };
 __device__ __forceinline__ PlanView plan_of(const EvictParams& p, int b, int g) {
   const int m = p.keep - p.window;
-  int* base = p.plan + (static_cast<long long>(b) * p.c.n_kv_heads + g) * ((2ll * m + 4) / 4 * 4);
-  return {base, base + 1, base + 1 + m};
+  int* base = p.plan + (static_cast<long long>(b) * p.c.n_kv_heads + g) * p.plan_words;
+  return {base, base + 1, base + 1 + m, base + 1 + 2ll * m, base + 1 + 3ll * m};
 }
+
+// Copies of the digit histogram, so that the lanes of a warp seldom meet on one counter: all 32 in blocks of 1024 threads, which sum them
+// quickly; 8 in blocks of 256, where summing (and clearing) 32 cost more than the meetings (2304 candidates: 12.8 us and 7).
+template <int THREADS> constexpr int kCopies = THREADS >= 1024 ? 32 : 8;
 
 template <int THREADS>
 struct alignas(16) PlanShared {
-  int hist[kBins * 32];            // lane-private digit counters: hist[bin * 32 + lane]
+  int hist[kBins * kCopies<THREADS>];      // hist[bin * copies + lane % copies]
   int total_hist[2][kBins];        // the cluster's histogram of a pass (every CTA adds into it), double-buffered by pass parity
   int warp_tot[2][THREADS / 32];
   alignas(8) int counts[8][2];     // per CTA of the cluster: (#above threshold, #equal to it)
@@ -67,11 +73,12 @@ struct alignas(16) PlanShared {
 
 }  // namespace
 
-// Every thread owns consecutive candidates of its CTA's chunk, so slot order is thread order.  ITEMS > 0: the candidates stay in
-// registers for all passes; ITEMS == 0: any number, read again for every pass.
+// A warp owns consecutive candidates of its CTA's chunk, 32 a row, a lane each: slot order is warp, row, lane, and what comes before a
+// candidate in its row is a ballot's.  ITEMS > 0: up to so many rows stay in registers for all passes; ITEMS == 0: any number, read again for
+// every pass.
 template <int CLUSTER, int ITEMS, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParams p) {
-  constexpr int kWarps = THREADS / 32, kPerBin = THREADS / kBins;
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_plan_kernel(const EvictParams p) {
+  constexpr int kWarps = THREADS / 32, kPerBin = THREADS / kBins, kCopy = kCopies<THREADS>;
   static_assert(THREADS % kBins == 0 && kPerBin >= 1 && kPerBin <= 4, "256, 512 or 1024 threads");
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ PlanShared<THREADS> sh;
@@ -80,9 +87,13 @@ __global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParam
   const int rank = static_cast<int>(cluster.block_rank());
   const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-  for (int i = tid; i < 2 * kBins; i += THREADS) (&sh.total_hist[0][0])[i] = 0;
-  for (int i = tid; i < kBins * 32; i += THREADS) sh.hist[i] = 0;
-  cluster.sync();                  // nobody adds into a histogram that is not cleared yet
+  auto everybody = [&]() {         // a barrier of the cluster
+    if constexpr (CLUSTER == 1) __syncthreads(); else cluster.sync();
+  };
+  if (CLUSTER > 1)
+    for (int i = tid; i < 2 * kBins; i += THREADS) (&sh.total_hist[0][0])[i] = 0;
+  for (int i = tid; i < kBins * kCopy; i += THREADS) sh.hist[i] = 0;
+  everybody();                     // nobody adds into a histogram that is not cleared yet
   pdl_launch_dependents();
   pdl_wait();
   bool ok;
@@ -97,26 +108,36 @@ __global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParam
 
   const int chunk = ((n + CLUSTER - 1) / CLUSTER + 3) & ~3;
   const int c_begin = min(n, rank * chunk), c_end = min(n, c_begin + chunk);
-  const int per = CACHED ? ITEMS : (chunk + THREADS - 1) / THREADS;
-  const int t_begin = min(c_end, c_begin + tid * per), t_end = min(c_end, t_begin + per);
-  const int n_mine = t_end - t_begin;
+  const int n_rows = (c_end - c_begin + THREADS - 1) / THREADS;             // of a warp; at most ITEMS
+  const int first = c_begin + warp * n_rows * 32 + lane;                    // this lane's candidate of the warp's first row
+  const int end = c_begin + min(c_end - c_begin, (warp + 1) * n_rows * 32);
 
   uint32_t key[R];
   uint32_t live = 0;               // bit r: candidate r exists and still matches the threshold's prefix
   if (CACHED) {
-    const float* mine = S + t_begin;
-    if (n_mine == R && R % 4 == 0 && (reinterpret_cast<uintptr_t>(mine) & 15u) == 0) {
+    float w[R];                    // (all loads first, whatever the row: in a branch each would wait for the one before)
 #pragma unroll
-      for (int r = 0; r < R; r += 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(mine + r));
-        key[r] = rank_key(v.x); key[r + 1] = rank_key(v.y); key[r + 2] = rank_key(v.z); key[r + 3] = rank_key(v.w);
-      }
-    } else {
+    for (int r = 0; r < R; ++r) w[r] = __ldg(S + max(min(first + r * 32, end - 1), 0));
 #pragma unroll
-      for (int r = 0; r < R; ++r) key[r] = r < n_mine ? rank_key(__ldg(mine + r)) : 0u;
+    for (int r = 0; r < R; ++r) {
+      const bool there = r < n_rows && first + r * 32 < end;
+      key[r] = there ? rank_key(w[r]) : 0u;
+      live |= (there ? 1u : 0u) << r;
     }
-    live = n_mine >= 32 ? 0xffffffffu : ((1u << n_mine) - 1u);
   }
+  // every row of the warp: f(candidate, whether this lane has one, its key)
+  auto rows = [&](auto&& f) {
+    if constexpr (CACHED) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (r < n_rows) f(first + r * 32, first + r * 32 < end, key[r]);
+    } else {
+      for (int r = 0; r < n_rows; ++r) {
+        const int i = first + r * 32;
+        f(i, i < end, i < end ? rank_key(__ldg(S + i)) : 0u);
+      }
+    }
+  };
 
   uint32_t tau = 0;
   int k_rem = m;
@@ -127,33 +148,35 @@ __global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParam
         if (live != 0) {
 #pragma unroll
           for (int r = 0; r < R; ++r)
-            if ((live >> r) & 1u) atomicAdd(&sh.hist[((key[r] >> shift) & 0xFFu) * 32 + lane], 1);
+            if ((live >> r) & 1u) atomicAdd(&sh.hist[((key[r] >> shift) & 0xFFu) * kCopy + lane % kCopy], 1);
         }
       } else {
-        for (int i = t_begin; i < t_end; ++i) {
-          const uint32_t u = rank_key(__ldg(S + i));
-          if (pass == 0 || ((u ^ tau) >> (shift + 8)) == 0) atomicAdd(&sh.hist[((u >> shift) & 0xFFu) * 32 + lane], 1);
-        }
+        rows([&](int, bool there, uint32_t u) {
+          if (there && (pass == 0 || ((u ^ tau) >> (shift + 8)) == 0)) atomicAdd(&sh.hist[((u >> shift) & 0xFFu) * kCopy + lane % kCopy], 1);
+        });
       }
       __syncthreads();
       {
-        // kPerBin threads per bin, each sums (and clears for the next pass) its share of the 32 lane counters
+        // kPerBin threads per bin, each sums (and clears for the next pass) its share of the copies
         const int bin = tid / kPerBin, part = tid % kPerBin;
         int sum = 0;
 #pragma unroll
-        for (int i = 0; i < 32 / kPerBin; ++i) {
-          int* c = &sh.hist[bin * 32 + ((part * (32 / kPerBin) + i + bin) & 31)];
-          sum += *c;
-          *c = 0;
+        for (int i = 0; i < kCopy / kPerBin; i += 4) {        // (the start is rotated by bin: neighbours use different banks)
+          int4* c = reinterpret_cast<int4*>(&sh.hist[bin * kCopy + ((part * (kCopy / kPerBin) + i + 4 * bin) & (kCopy - 1))]);
+          const int4 v = *c;
+          sum += (v.x + v.y) + (v.z + v.w);
+          *c = make_int4(0, 0, 0, 0);
         }
         if (kPerBin >= 2) sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         if (kPerBin >= 4) sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (part == 0 && sum != 0) {
+        if (CLUSTER == 1) {
+          if (part == 0) sh.total_hist[pass & 1][bin] = sum;
+        } else if (part == 0 && sum != 0) {
 #pragma unroll
           for (int r = 0; r < CLUSTER; ++r) atomicAdd(cluster.map_shared_rank(&sh.total_hist[pass & 1][bin], r), sum);
         }
       }
-      cluster.sync();
+      everybody();
       if (warp == 0) {
         // 8 bins per lane, highest bins first: lane 0 owns bins 255..248
         int cnt[8], tot = 0;
@@ -182,7 +205,7 @@ __global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParam
         }
       }
       __syncthreads();
-      if (tid < kBins) sh.total_hist[pass & 1][tid] = 0;   // for the pass after next; nobody adds into it before the next barrier
+      if (CLUSTER > 1 && tid < kBins) sh.total_hist[pass & 1][tid] = 0;   // for the pass after next; nobody adds into it before the next barrier
       const uint32_t digit = static_cast<uint32_t>(sh.digit);
       tau |= digit << shift;
       k_rem = sh.k_rem;
@@ -196,79 +219,66 @@ __global__ void __launch_bounds__(THREADS, 1) evict_plan_kernel(const EvictParam
   }
   // tau: image of the smallest weight that stays; need_eq: how many candidates equal to it do
   const int need_eq = m > 0 ? k_rem : 0;
-  int n_gt = 0, n_eq = 0;
+  int n_gt = 0, n_eq = 0;          // of the warp
   if (m > 0) {
-    if (CACHED) {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        n_gt += (r < n_mine && key[r] > tau) ? 1 : 0;
-        n_eq += (r < n_mine && key[r] == tau) ? 1 : 0;
-      }
-    } else {
-      for (int i = t_begin; i < t_end; ++i) {
-        const uint32_t u = rank_key(__ldg(S + i));
-        n_gt += (u > tau) ? 1 : 0;
-        n_eq += (u == tau) ? 1 : 0;
-      }
-    }
+    rows([&](int, bool there, uint32_t u) {
+      n_gt += __popc(__ballot_sync(0xffffffffu, there && u > tau));
+      n_eq += __popc(__ballot_sync(0xffffffffu, there && u == tau));
+    });
   }
-  // exclusive scans in thread order: within the warp, over the warps, over the cluster's CTAs
-  int gt_incl = n_gt, eq_incl = n_eq;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int va = __shfl_up_sync(0xffffffffu, gt_incl, o), ve = __shfl_up_sync(0xffffffffu, eq_incl, o);
-    if (lane >= o) { gt_incl += va; eq_incl += ve; }
-  }
-  if (lane == 31) { sh.warp_tot[0][warp] = gt_incl; sh.warp_tot[1][warp] = eq_incl; }
+  // before this warp's: scans over the CTA's warps and over the cluster's CTAs
+  if (lane == 0) { sh.warp_tot[0][warp] = n_gt; sh.warp_tot[1][warp] = n_eq; }
   __syncthreads();
-  if (warp == 0) {
-    int a = lane < kWarps ? sh.warp_tot[0][lane] : 0, e = lane < kWarps ? sh.warp_tot[1][lane] : 0;
-    const int a0 = a, e0 = e;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int va = __shfl_up_sync(0xffffffffu, a, o), ve = __shfl_up_sync(0xffffffffu, e, o);
-      if (lane >= o) { a += va; e += ve; }
-    }
-    if (lane < kWarps) { sh.warp_tot[0][lane] = a - a0; sh.warp_tot[1][lane] = e - e0; }
-    const int a_tot = __shfl_sync(0xffffffffu, a, 31), e_tot = __shfl_sync(0xffffffffu, e, 31);
-    if (lane < CLUSTER) *reinterpret_cast<int2*>(cluster.map_shared_rank(&sh.counts[rank][0], lane)) = make_int2(a_tot, e_tot);
+  int gt_before = 0, eq_before = 0, gt_cta = 0, eq_cta = 0;
+  {
+    const int a0 = lane < kWarps ? sh.warp_tot[0][lane] : 0, e0 = lane < kWarps ? sh.warp_tot[1][lane] : 0;
+    gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? a0 : 0);
+    eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? e0 : 0);
+    gt_cta = __reduce_add_sync(0xffffffffu, a0);
+    eq_cta = __reduce_add_sync(0xffffffffu, e0);
   }
-  __syncthreads();
-  const int gt_excl = sh.warp_tot[0][warp] + gt_incl - n_gt, eq_excl = sh.warp_tot[1][warp] + eq_incl - n_eq;
-  cluster.sync();
-  int eq_before = 0, kept_before = 0;
+  int kept_ctas = 0, eq_ctas = 0;  // kept candidates, and candidates equal to tau, of the CTAs before
+  if constexpr (CLUSTER > 1) {
+    if (warp == 0 && lane < CLUSTER) *reinterpret_cast<int2*>(cluster.map_shared_rank(&sh.counts[rank][0], lane)) = make_int2(gt_cta, eq_cta);
+    cluster.sync();
 #pragma unroll
-  for (int r = 0; r < CLUSTER; ++r) {
-    if (r < rank) {
-      kept_before += sh.counts[r][0] + max(0, min(sh.counts[r][1], need_eq - eq_before));
-      eq_before += sh.counts[r][1];
+    for (int r = 0; r < CLUSTER; ++r) {
+      if (r < rank) {
+        kept_ctas += sh.counts[r][0] + max(0, min(sh.counts[r][1], need_eq - eq_ctas));
+        eq_ctas += sh.counts[r][1];
+      }
     }
   }
-  int eq_rank = eq_before + eq_excl;                       // rank of this thread's first candidate equal to tau
-  int pos = kept_before + gt_excl + min(eq_rank, need_eq) - min(eq_before, need_eq);    // kept candidates before it
-  auto place = [&](int i, uint32_t u) {
-    const bool is_eq = u == tau && m > 0;
-    const bool kept = m > 0 && (u > tau || (is_eq && eq_rank < need_eq));
-    if (i == m) *plan.kept_below = pos;
-    if (i < m) plan.hole[i] = kept ? -1 : i - pos;
-    else if (kept) plan.from[pos] = i;
-    pos += kept ? 1 : 0;
-    eq_rank += is_eq ? 1 : 0;
-  };
-  if (CACHED) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (r < n_mine) place(t_begin + r, key[r]);
-  } else {
-    for (int i = t_begin; i < t_end; ++i) place(i, rank_key(__ldg(S + i)));
-  }
+  int eq_rank = eq_ctas + eq_before;                       // of the warp's next candidate equal to tau
+  int pos = kept_ctas + gt_before + min(eq_rank, need_eq) - min(eq_ctas, need_eq);      // kept candidates before the warp's next row
+  const uint32_t below = (1u << lane) - 1u;
+  rows([&](int i, bool there, uint32_t u) {
+    const bool eq = there && u == tau && m > 0;
+    const uint32_t all_eq = __ballot_sync(0xffffffffu, eq);
+    const bool kept = there && m > 0 && (u > tau || (eq && eq_rank + __popc(all_eq & below) < need_eq));
+    const uint32_t all_kept = __ballot_sync(0xffffffffu, kept);
+    const int at = pos + __popc(all_kept & below);         // kept candidates before this one
+    if (there) {
+      if (i <= m && (i & ((1 << p.c.page_log2) - 1)) == 0) plan.page_first[i >> p.c.page_log2] = i - at;
+      if (i == m) *plan.kept_below = at;
+      if (i < m) {
+        plan.hole[i] = kept ? -1 : i - at;
+        if (!kept) plan.free_slot[i - at] = i;
+      } else if (kept) {
+        plan.from[at] = i;
+      }
+    }
+    pos += __popc(all_kept);
+    eq_rank += __popc(all_eq);
+  });
   // (limit >= keep, so there are more candidates than m, and slot m is one of them)
 }
 
 namespace {
 
-constexpr int kMoveThreads = 512, kMoveWarps = kMoveThreads / 32;
 constexpr int kRoundRows = 128;            // rows of a round that a CTA holds in shared memory: one page at most, or several
+constexpr int kHeld = 2;                    // 8-bit pages: free slots that a lane holds at a time
+constexpr int kOwnPages = 16;              // 8-bit pages that a warp takes at a time, at most
 
 __device__ __forceinline__ uint32_t recode2(uint32_t w, float f) {        // two codes times f <= 1, rounded to nearest even
   uint32_t h;
@@ -279,22 +289,36 @@ __device__ __forceinline__ uint32_t recode2(uint32_t w, float f) {        // two
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi * f), "f"(lo * f));
   return r;
 }
+// Sixteen codes times f <= 1, a power of two.  Conversions are slow (an SM does 16 a cycle, and two codes take two of them), so four codes
+// that are all normal numbers before and after, and not NaN, have their exponents lowered in one subtraction.
 __device__ __forceinline__ uint4 recode16(uint4 v, float f) {
   if (f == 1.0f) return v;
+  const uint32_t bits = __float_as_uint(f);
+  const int down = 127 - static_cast<int>(bits >> 23);                    // f = 2^-down
+  const bool plain = (bits & 0x7fffffu) == 0u && down > 0 && down < 14;
+  const uint32_t by = static_cast<uint32_t>(plain ? down : 0) * 0x08080808u;
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = recode2(w[i] & 0xffffu, f) | (recode2(w[i] >> 16, f) << 16);
+  for (int i = 0; i < 4; ++i) {
+    // every byte: the exponent is above `down` (the sum stays at 0x80 or above), and the code is not all ones
+    const uint32_t above = ((w[i] & 0x78787878u) | 0x80808080u) - by - 0x08080808u, nan = (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+    if (plain && (above & ~nan & 0x80808080u) == 0x80808080u) w[i] -= by;
+    else w[i] = recode2(w[i] & 0xffffu, f) | (recode2(w[i] >> 16, f) << 16);
+  }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 }  // namespace
 
 // blockIdx.y: K, V, or weights and ids; blockIdx.z: (sequence, KV head); blockIdx.x: CTA of the cluster.
-template <bool kE4M3, int kRowBytes>
-__global__ void __launch_bounds__(kMoveThreads, 1) evict_move_kernel(const EvictParams p) {
+template <bool kE4M3, int kRowBytes, int kMoveThreads>
+__global__ void __launch_bounds__(kMoveThreads, 1024 / kMoveThreads) evict_move_kernel(const EvictParams p) {
+  constexpr int kMoveWarps = kMoveThreads / 32;
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int kLanesPerRow = kRowBytes / 16, kRowsPerWarp = 32 / kLanesPerRow;
-  __shared__ __align__(16) uint8_t stage[kRoundRows * kRowBytes];
+  // rows of a round; before the rounds, the warps' lists of moves
+  constexpr int kStageBytes = kRoundRows * kRowBytes, kListBytes = kMoveWarps * 32 * 16;
+  __shared__ __align__(16) uint8_t stage[kStageBytes > kListBytes ? kStageBytes : kListBytes];
   __shared__ float scale_from[kRoundRows], page_scale[kRoundRows / 16];
   const int CL = gridDim.x, rank = blockIdx.x, kind = blockIdx.y;
   const int b = blockIdx.z / p.c.n_kv_heads, g = blockIdx.z - b * p.c.n_kv_heads;
@@ -341,84 +365,152 @@ __global__ void __launch_bounds__(kMoveThreads, 1) evict_move_kernel(const Evict
 
   // ---- pages that lie below m: free slots take their entries ----
   const int m0 = m & ~mask;
-  const int span = P < 32 ? P : 32;                  // slots of a warp's step; 8-bit pages go by whole pages
-  const int gw = rank * kMoveWarps + warp, n_warps = CL * kMoveWarps;
-  const int unit = kE4M3 ? P : span;                 // slots a warp takes at a time
-  for (int u0 = gw * unit; u0 < m0; u0 += n_warps * unit) {
-    const int to_blk = block_at(u0);
-    if (to_blk < 0) continue;
-    float own = 1.0f, now = 1.0f;                    // 8-bit pages: the page's scale, before and after
-    bool again = false;                              // what stays has to be encoded again
-    if (kE4M3) {
-      own = scales[to_blk];
-      float most = 0.0f;
-      bool stays = false, comes = false;
-      for (int s0 = 0; s0 < P; s0 += 32) {
-        if (s0 + lane < P) {
-          const int j = u0 + s0 + lane, o = origin(j);
-          if (o == j) {
-            stays = true;
-          } else {
-            const int blk = block_at(o);
-            if (blk >= 0) { most = fmaxf(most, scales[blk]); comes = true; }
-          }
-        }
-      }
-#pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      stays = __any_sync(0xffffffffu, stays);
-      comes = __any_sync(0xffffffffu, comes);
-      if (!comes) continue;
-      now = stays ? fmaxf(own, most) : most;
-      again = stays && now != own;
+  const int gw = warp * CL + rank, n_warps = CL * kMoveWarps;
+  // Rows that the lanes name (from `from`, null: none, to `to`, in 8 bits times f) move, several at a time: the warp's list of them lies in
+  // shared memory, and a group of lanes takes every kRowsPerWarp-th.
+  struct Move { const uint8_t* from; uint8_t* to; };
+  static_assert(sizeof(Move) == 16, "what the lists have room for");
+  Move* const moves = reinterpret_cast<Move*>(stage) + warp * 32;
+  __shared__ float move_scale[kMoveWarps][kE4M3 ? 32 : 1];
+  auto move_rows = [&](const uint8_t* from, uint8_t* to, float f) {
+    const unsigned have = __ballot_sync(0xffffffffu, from != nullptr);
+    if (from != nullptr) {
+      const int at = __popc(have & ((1u << lane) - 1u));
+      moves[at] = {from, to};
+      if (kE4M3) move_scale[warp][at] = f;
     }
-    for (int s0 = 0; s0 < unit; s0 += 32) {
-      // this lane's slot: where its row comes from
-      const int j = u0 + s0 + lane;
-      int o = -1, blk = -1;
-      float f = 1.0f;
-      if (s0 + lane < unit) {
-        o = origin(j);
-        if (o == j && !again) o = -1;
-        if (o >= 0) {
-          blk = block_at(o);
-          if (kE4M3 && blk >= 0) f = scales[blk] / now;
-        }
+    __syncwarp();
+    const int n = __popc(have);
+    constexpr int kAhead = 4;                        // loads of a lane in flight: more cost the warps that hide the rest (8: 74 -> 97 us, four of 26214)
+    for (int i0 = sub; i0 < n; i0 += kAhead * kRowsPerWarp) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        const int i = i0 + x * kRowsPerWarp;
+        if (i < n) v[x] = *reinterpret_cast<const uint4*>(moves[i].from + piece * 16);
       }
-      unsigned todo = __ballot_sync(0xffffffffu, blk >= 0);
-      constexpr int kAhead = 4;                      // loads of a lane in flight
-      while (todo != 0) {
-        uint4 v[kAhead];
-        int to[kAhead];
-        float by[kAhead];
 #pragma unroll
-        for (int x = 0; x < kAhead; ++x) {
-          // the next rows of the step, one for each group of lanes
-          int who = -1;
-#pragma unroll
-          for (int y = 0; y < kRowsPerWarp; ++y) {
-            const int first = __ffs(todo) - 1;
-            if (y == sub) who = first;
-            if (first >= 0) todo &= todo - 1;
-          }
-          const int from = __shfl_sync(0xffffffffu, o, max(who, 0)), fb = __shfl_sync(0xffffffffu, blk, max(who, 0));
-          by[x] = __shfl_sync(0xffffffffu, f, max(who, 0));
-          to[x] = who;
-          if (who >= 0) v[x] = *reinterpret_cast<const uint4*>(row_at(fb, from) + piece * 16);
-        }
-#pragma unroll
-        for (int x = 0; x < kAhead; ++x)
-          if (to[x] >= 0)
-            *reinterpret_cast<uint4*>(row_at(to_blk, u0 + s0 + to[x]) + piece * 16) = kE4M3 ? recode16(v[x], by[x]) : v[x];
+      for (int x = 0; x < kAhead; ++x) {
+        const int i = i0 + x * kRowsPerWarp;
+        if (i < n) *reinterpret_cast<uint4*>(moves[i].to + piece * 16) = kE4M3 ? recode16(v[x], move_scale[warp][i]) : v[x];
       }
     }
-    if (kE4M3) {
+    __syncwarp();
+  };
+  if constexpr (!kE4M3) {
+    // Free slots in any order, an even share of them a warp, 64 at a time: a move is found by three loads that wait for one another, so several of them at once.
+    const int n_free = plan.page_first[m0 >> p.c.page_log2];
+    const int share = (n_free + n_warps - 1) / n_warps, end = min(n_free, (gw + 1) * share);
+    for (int h0 = gw * share; h0 < end; h0 += 64) {
+      int dst[2], src[2];
+      const uint8_t* from[2];
+      uint8_t* to[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int h = min(h0 + z * 32 + lane, end - 1);
+        dst[z] = plan.free_slot[h];
+        src[z] = plan.from[kept_below + h];
+      }
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int dst_blk = block_at(dst[z]), src_blk = block_at(src[z]);
+        const bool there = h0 + z * 32 + lane < end && dst_blk >= 0 && src_blk >= 0;
+        from[z] = there ? row_at(src_blk, src[z]) : nullptr;
+        to[z] = there ? row_at(dst_blk, dst[z]) : nullptr;
+      }
+#pragma unroll
+      for (int z = 0; z < 2; ++z) move_rows(from[z], to[z], 1.0f);
+    }
+  } else {
+    // A warp takes several pages whole: first every page's new scale, and which of its slots are free, then the rows.
+    __shared__ unsigned most_of[kMoveWarps][kOwnPages], free_of[kMoveWarps][kOwnPages][4];
+    const int n_pages = m0 >> p.c.page_log2;
+    // an even share, but no more than have some 64 free slots together: those stay in the lanes' registers
+    const int share = n_pages == 0 ? 1 : static_cast<int>(32ll * kHeld * n_pages / max(plan.page_first[n_pages], 1));
+    const int per = min(min(kOwnPages, (n_pages + n_warps - 1) / n_warps), max(share, 1));
+    for (int pa = gw * per; pa < n_pages; pa += n_warps * per) {
+      const int pb = min(pa + per, n_pages);
+      const int first = plan.page_first[pa + min(lane, pb - pa)];            // of page pa + lane, and behind the last
+      const int ha = __shfl_sync(0xffffffffu, first, 0), hb = __shfl_sync(0xffffffffu, first, pb - pa);
+      if (ha == hb) continue;
+      const int n_own = __shfl_down_sync(0xffffffffu, first, 1) - first;     // free slots of page pa + lane
+      if (lane < kOwnPages) {
+        most_of[warp][lane] = 0u;
+        for (int z = 0; z < 4; ++z) free_of[warp][lane][z] = 0u;
+      }
+      int own_blk = -1;
+      float own = 1.0f;
+      if (pa + lane < pb && n_own > 0) {
+        own_blk = block_at((pa + lane) << p.c.page_log2);
+        if (own_blk >= 0) own = scales[own_blk];
+      }
       __syncwarp();
-      if (lane == 0 && now != own) scales[to_blk] = now;
+      // kHeld free slots of the warp's pages a lane, from h0 on: three loads that wait for one another, so several of them at once
+      int src[kHeld], dst[kHeld], src_blk[kHeld];
+      float was[kHeld];
+      auto take = [&](int h0) {
+#pragma unroll
+        for (int z = 0; z < kHeld; ++z) {
+          const int h = min(h0 + z * 32 + lane, hb - 1);
+          dst[z] = plan.free_slot[h];
+          src[z] = plan.from[kept_below + h];
+        }
+#pragma unroll
+        for (int z = 0; z < kHeld; ++z) src_blk[z] = block_at(src[z]);
+#pragma unroll
+        for (int z = 0; z < kHeld; ++z) was[z] = scales[max(src_blk[z], 0)];
+      };
+      for (int h0 = ha; h0 < hb; h0 += 32 * kHeld) {
+        take(h0);
+#pragma unroll
+        for (int z = 0; z < kHeld; ++z) {
+          if (h0 + z * 32 + lane < hb) {
+            const int pg = (dst[z] >> p.c.page_log2) - pa, slot = dst[z] & mask;
+            atomicOr(&free_of[warp][pg][slot >> 5], 1u << (slot & 31));
+            if (src_blk[z] >= 0) atomicMax(&most_of[warp][pg], __float_as_uint(was[z]));     // (positive: their bits compare alike)
+          }
+        }
+      }
+      __syncwarp();
+      // lane = page: the new scale, and what becomes of the entries that stay
+      float now = own;
+      bool again = false;
+      if (own_blk >= 0) {
+        const float most = __uint_as_float(most_of[warp][lane]);
+        const bool stays = n_own < P;
+        now = stays ? fmaxf(own, most) : most > 0.0f ? most : own;
+        again = stays && now != own;
+      }
+      for (unsigned pages = __ballot_sync(0xffffffffu, again); pages != 0; pages &= pages - 1) {
+        const int pg = __ffs(pages) - 1, blk = __shfl_sync(0xffffffffu, own_blk, pg);
+        const float f = __shfl_sync(0xffffffffu, own, pg) / __shfl_sync(0xffffffffu, now, pg);
+        for (int r0 = 0; r0 < P; r0 += 32) {
+          const int r = r0 + lane;
+          const bool mine = r < P && ((free_of[warp][pg][r0 >> 5] >> lane) & 1u) == 0;
+          uint8_t* const at = mine ? row_at(blk, r) : nullptr;
+          move_rows(at, at, f);
+        }
+      }
+      for (int h0 = ha; h0 < hb; h0 += 32 * kHeld) {
+        if (hb - ha > 32 * kHeld) take(h0);          // (otherwise the lanes still hold them)
+#pragma unroll
+        for (int z = 0; z < kHeld; ++z) {
+          if (h0 + z * 32 >= hb) break;              // (uniform)
+          const bool there = h0 + z * 32 + lane < hb;
+          const int pg = there ? (dst[z] >> p.c.page_log2) - pa : 0;
+          const int dst_blk = __shfl_sync(0xffffffffu, own_blk, pg);
+          const float to = __shfl_sync(0xffffffffu, now, pg);
+          const bool moves_on = there && dst_blk >= 0 && src_blk[z] >= 0;
+          move_rows(moves_on ? row_at(src_blk[z], src[z]) : nullptr, moves_on ? row_at(dst_blk, dst[z]) : nullptr, was[z] / to);
+        }
+      }
+      if (own_blk >= 0 && now != own) scales[own_blk] = now;
+      __syncwarp();                                  // the masks are free again
     }
   }
 
   // ---- the pages from m on, in rounds of kRoundRows slots a CTA ----
+  __syncthreads();                                   // the lists have been read
   for (int r0 = m0; r0 < p.keep; r0 += CL * kRoundRows) {
     const int j0 = r0 + rank * kRoundRows, rows = max(0, min(kRoundRows, p.keep - j0));
     constexpr int kGroups = kMoveThreads / kLanesPerRow;
@@ -430,10 +522,12 @@ __global__ void __launch_bounds__(kMoveThreads, 1) evict_move_kernel(const Evict
     }
     __syncthreads();
     if (kE4M3) {
-      for (int q = tid; q * P < rows; q += kMoveThreads) {
-        float most = 0.0f;
-        for (int i = q * P; i < min(rows, (q + 1) * P); ++i) most = fmaxf(most, scale_from[i]);
-        page_scale[q] = most;
+      // the largest scale of each page's rows (positive: their bits compare alike)
+      if (tid < kRoundRows / 16) page_scale[tid] = 0.0f;
+      __syncthreads();
+      if (tid < rows) {
+        const float most = scale_from[tid];
+        if (most > 0.0f) atomicMax(reinterpret_cast<unsigned*>(&page_scale[tid >> p.c.page_log2]), __float_as_uint(most));
       }
     }
     cluster.sync();                                  // everybody has read the round
@@ -479,26 +573,27 @@ cudaError_t launch_plan_t(const EvictParams& p, cudaStream_t stream) {
 
 cudaError_t launch_evict_plan(const EvictParams& p, cudaStream_t stream) {
   const int n = p.max_len - p.window;                // the most candidates
-  if (n <= 4 * 256) return launch_plan_t<1, 4, 256>(p, stream);
-  if (n <= 16 * 256) return launch_plan_t<1, 16, 256>(p, stream);
-  if (n <= 2 * 16 * 256) return launch_plan_t<2, 16, 256>(p, stream);
-  if (n <= 4 * 16 * 256) return launch_plan_t<4, 16, 256>(p, stream);
-  if (n <= 8 * 4 * 1024) return launch_plan_t<8, 4, 1024>(p, stream);
+  // short sequences: a CTA each, of 512 threads as long as all of them run at once, else of 256
+  if (n <= 16 * 256) {
+    if (static_cast<long long>(p.c.batch) * p.c.n_kv_heads <= 2 * 148) return n <= 2 * 512 ? launch_plan_t<1, 2, 512>(p, stream) : launch_plan_t<1, 8, 512>(p, stream);
+    return n <= 4 * 256 ? launch_plan_t<1, 4, 256>(p, stream) : launch_plan_t<1, 16, 256>(p, stream);
+  }
+  // longer ones: clusters of CTAs of 512 threads and up to 16 candidates a thread, as small as the length allows when there are many
+  const long long pairs = static_cast<long long>(p.c.batch) * p.c.n_kv_heads;
+  if (n <= 2 * 16 * 512) return pairs * 4 <= 148 ? launch_plan_t<4, 8, 512>(p, stream) : launch_plan_t<2, 16, 512>(p, stream);
+  if (n <= 4 * 16 * 512) return pairs * 8 <= 148 ? launch_plan_t<8, 8, 512>(p, stream) : launch_plan_t<4, 16, 512>(p, stream);
+  if (n <= 8 * 16 * 512) return launch_plan_t<8, 16, 512>(p, stream);
   if (n <= 8 * 16 * 1024) return launch_plan_t<8, 16, 1024>(p, stream);
   return launch_plan_t<8, 0, 1024>(p, stream);
 }
 
 namespace {
 
-template <bool kE4M3, int kRowBytes>
-cudaError_t launch_move_t(const EvictParams& p, cudaStream_t stream) {
-  // CTAs of a cluster: as many as keep all SMs busy with few pairs
-  const long long pairs = static_cast<long long>(p.c.batch) * p.c.n_kv_heads;
-  int cl = 8;
-  while (cl > 1 && (pairs * 2 * cl > 4 * 148 || cl * kRoundRows >= 4 * p.keep)) cl /= 2;
+template <bool kE4M3, int kRowBytes, int kThreads>
+cudaError_t launch_move_t(const EvictParams& p, int cl, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cl, 3, static_cast<unsigned>(pairs));
-  cfg.blockDim = dim3(kMoveThreads);
+  cfg.gridDim = dim3(cl, 3, static_cast<unsigned>(p.c.batch * p.c.n_kv_heads));
+  cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -508,15 +603,25 @@ cudaError_t launch_move_t(const EvictParams& p, cudaStream_t stream) {
   fill_pdl_attribute(&attr[1]);
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, evict_move_kernel<kE4M3, kRowBytes>, p);
+  return cudaLaunchKernelEx(&cfg, evict_move_kernel<kE4M3, kRowBytes, kThreads>, p);
+}
+
+template <bool kE4M3, int kRowBytes>
+cudaError_t launch_move_r(const EvictParams& p, cudaStream_t stream) {
+  // CTAs of a cluster: as many as keep all SMs busy with few pairs; where even eight leave SMs with one CTA or none, large ones
+  const long long pairs = static_cast<long long>(p.c.batch) * p.c.n_kv_heads;
+  int cl = 8;
+  while (cl > 1 && (pairs * 2 * cl > 4 * 148 || cl * kRoundRows >= 4 * p.keep)) cl /= 2;
+  if (cl == 8 && pairs * 2 * cl <= 148) return launch_move_t<kE4M3, kRowBytes, 1024>(p, cl, stream);
+  return launch_move_t<kE4M3, kRowBytes, 256>(p, cl, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_evict_move(const EvictParams& p, bool e4m3, cudaStream_t stream) {
-  if (p.row_bytes == 256) return launch_move_t<false, 256>(p, stream);
-  if (p.row_bytes == 128) return e4m3 ? launch_move_t<true, 128>(p, stream) : launch_move_t<false, 128>(p, stream);
-  if (p.row_bytes == 64) return launch_move_t<true, 64>(p, stream);
+  if (p.row_bytes == 256) return launch_move_r<false, 256>(p, stream);
+  if (p.row_bytes == 128) return e4m3 ? launch_move_r<true, 128>(p, stream) : launch_move_r<false, 128>(p, stream);
+  if (p.row_bytes == 64) return launch_move_r<true, 64>(p, stream);
   return cudaErrorInvalidValue;
 }
 

@@ -12,7 +12,12 @@
 // step's in flight while this one is computed; no shared memory, no barrier, and every CTA an even share of all entries.
 //   S [16 entries x 8 rows] = K Q^T: A = K rows, B = the query rows; a lane holds 2 entries x 2 rows, and the sum over rows ends
 //   with two shuffles.  Each entry belongs to one lane: no atomics, and the order of the sums is fixed.
-// 8-bit codes widen exactly to bf16 in registers; K's scale multiplies the logits.  Logits, exponentials and sums are fp32.
+// 8-bit codes widen exactly to fp16 in registers, one conversion for two of them (an SM does 16 of those a cycle, and two for a pair,
+// through bf16, were what bounded the kernel: 118 us for the ragged 16 x 500 to 40000 with four query tokens).  The queries go into
+// fp16 after a power-of-two shift per row that brings the row's largest element to [2^14, 2^15): exact down to 2^-28 of it, and what is
+// smaller is off by at most 2^-39 of the largest.  K's scale and the shift multiply the logits.  Logits, exponentials and sums are fp32.
+#include <type_traits>
+
 #include "paged.cuh"
 #include "paged_mma.cuh"
 
@@ -21,19 +26,11 @@ namespace fastkv {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kLoads = 8;                 // 16-byte loads of a lane per step: 4 KB a warp
-
-// Four codes as bf16 pairs: exact (4 bits of a code's significand against 8, and every exponent).
-__device__ __forceinline__ void widen_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  float a, b;
-  unpack16<true>(widen_lo(w), a, b);
-  lo = pack16<false>(a, b);
-  unpack16<true>(widen_hi(w), a, b);
-  hi = pack16<false>(a, b);
-}
 
 template <int D, bool kE4M3>
 struct WeightsCfg {
+  // 16-byte loads of a lane per step: 4 KB a warp, in 8 bits 2 KB (with 4 KB the two steps do not fit the registers next to the queries)
+  static constexpr int kLoads = kE4M3 ? 4 : 8;
   static constexpr int kRowBytes = D * (kE4M3 ? 1 : 2);
   static constexpr int kPieces = kRowBytes / 64;         // loads of a row by its four lanes
   static constexpr int kTiles = kLoads / (2 * kPieces);  // 16-entry tiles of a step
@@ -54,7 +51,7 @@ __device__ __forceinline__ int entries_of(const PagedWeightsParams& p, int b) {
 template <int D, bool kE4M3, int NT>
 __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedWeightsParams p) {
   using Cfg = WeightsCfg<D, kE4M3>;
-  constexpr int KS = D / 16, kTiles = Cfg::kTiles, kPieces = Cfg::kPieces, kLog2 = Cfg::kChunkLog2;
+  constexpr int KS = D / 16, kTiles = Cfg::kTiles, kLoads = Cfg::kLoads, kPieces = Cfg::kPieces, kLog2 = Cfg::kChunkLog2;
   constexpr int kHeld = NT > 0 ? NT : 2;       // tiles of 8 query rows at a time
   __shared__ long long scratch[kWarps];
   __shared__ int s_first;
@@ -175,8 +172,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
   // ---- query fragments: row quad of each tile of 8, 16-byte pieces in the order K's come in ----
   uint32_t qf[kHeld][2 * KS];
   float lse[kHeld][2];                          // of rows 2c, 2c + 1
+  float shift[kHeld][2];                        // 8-bit pages: what a logit is multiplied by besides the scales
   int sees[kHeld][2];                           // entries the row sees; 0 for rows that are not there or saw nothing
-  auto take_rows = [&](const Place& x, int nt, uint32_t (&f)[2 * KS], float (&l)[2], int (&n)[2]) {
+  auto take_rows = [&](const Place& x, int nt, uint32_t (&f)[2 * KS], float (&l)[2], float (&by)[2], int (&n)[2]) {
     const int r = nt * 8 + quad, i = r / G, h = x.g * G + r - i * G;
     const uint16_t* src = p.q + ((static_cast<size_t>(x.b) * T + i) * p.n_q_heads + h) * D;
 #pragma unroll
@@ -196,29 +194,61 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
         f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
       }
     }
+    int up = 0;
+    if constexpr (kE4M3) {
+      float m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 2 * KS; ++i) {
+        float lo, hi;
+        unpack16<false>(f[i], lo, hi);
+        m = fmaxf(m, fmaxf(fabsf(lo), fabsf(hi)));
+      }
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      up = m > 0.0f ? 14 - scale_log2(__float_as_uint(m)) : 0;
+      up = up > 120 ? 120 : up;                 // of a subnormal row; otherwise within [-113, 120] as it stands
+      const float times = __uint_as_float(pow2_bits(up));
+#pragma unroll
+      for (int i = 0; i < 2 * KS; ++i) {
+        float lo, hi;
+        unpack16<false>(f[i], lo, hi);
+        f[i] = pack16<true>(lo * times, hi * times);
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      if constexpr (kE4M3) by[e] = __uint_as_float(pow2_bits(-__shfl_sync(0xffffffffu, up, (2 * c + e) * 4)));
       const int s = nt * 8 + 2 * c + e, si = s / G, sh = x.g * G + s - si * G;
-      l[e] = s < p.rows ? __ldg(p.lse + (static_cast<size_t>(x.b) * T + si) * p.n_q_heads + sh) : -INFINITY;
-      n[e] = l[e] == -INFINITY ? 0 : max(x.len - (T - 1 - si), 0);
+      l[e] = s < p.rows ? __ldg(p.lse + (static_cast<size_t>(x.b) * T + si) * p.n_q_heads + sh) : INFINITY;
+      n[e] = s >= p.rows || l[e] == -INFINITY ? 0 : max(x.len - (T - 1 - si), 0);
     }
   };
 
-  int have_b = -1, have_g = -1;
+  int have_b = -1, have_g = -1, all_see = 0;
+  // the fewest entries that a row sees which is there
+  auto least = [&]() -> int {
+    int n = 0x7fffffff;
+#pragma unroll
+    for (int nt = 0; nt < kHeld; ++nt) n = min(n, min(lse[nt][0] == INFINITY ? n : sees[nt][0], lse[nt][1] == INFINITY ? n : sees[nt][1]));
+    return __reduce_min_sync(0xffffffffu, n);
+  };
   auto compute = [&](const Place& x, const Step& s) {
     const int key0 = (x.c << kLog2) + warp * Cfg::kStep;
     if (NT > 0 && (x.b != have_b || x.g != have_g)) {
       have_b = x.b;
       have_g = x.g;
 #pragma unroll
-      for (int nt = 0; nt < kHeld; ++nt) take_rows(x, nt, qf[nt], lse[nt], sees[nt]);
+      for (int nt = 0; nt < kHeld; ++nt) take_rows(x, nt, qf[nt], lse[nt], shift[nt], sees[nt]);
+      all_see = least();
     }
     if (key0 >= x.len) return;
     float sum[kTiles][2];
 #pragma unroll
     for (int y = 0; y < kTiles; ++y) sum[y][0] = sum[y][1] = 0.0f;
-    // the rows of kHeld tiles: K's fragments (widened once) serve them all
-    auto draw = [&]() {
+    // the rows of kHeld tiles: K's fragments (widened once) serve them all.  kAll: every row that is there sees the whole step (rows that
+    // are not there have an lse of +infinity).
+    auto draw = [&](auto all_) {
+      constexpr bool kAll = decltype(all_)::value;
 #pragma unroll
       for (int y = 0; y < kTiles; ++y) {
         float d[kHeld][4];
@@ -229,12 +259,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
           if constexpr (kE4M3) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-              uint32_t a0, a1, a2, a3;
-              widen_bf16(av[w], a0, a2);
-              widen_bf16(ev[w], a1, a3);
+              const uint32_t a0 = widen_lo(av[w]), a1 = widen_lo(ev[w]), a2 = widen_hi(av[w]), a3 = widen_hi(ev[w]);
 #pragma unroll
               for (int nt = 0; nt < kHeld; ++nt)
-                mma16<false>(d[nt], j == 0 && w == 0, a0, a1, a2, a3, qf[nt][8 * j + 2 * w], qf[nt][8 * j + 2 * w + 1]);
+                mma16<true>(d[nt], j == 0 && w == 0, a0, a1, a2, a3, qf[nt][8 * j + 2 * w], qf[nt][8 * j + 2 * w + 1]);
             }
           } else {
 #pragma unroll
@@ -246,23 +274,25 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
         }
         const float k = p.scale * (kE4M3 ? __shfl_sync(0xffffffffu, s.scale, y) : 1.0f);
 #pragma unroll
-        for (int nt = 0; nt < kHeld; ++nt)
+        for (int nt = 0; nt < kHeld; ++nt) {
+          const float by[2] = {kE4M3 ? k * shift[nt][0] : k, kE4M3 ? k * shift[nt][1] : k};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             // what a row does not see must not reach the sum, NaN included
-            const float w = ex2(fmaf(d[nt][e], k, -lse[nt][e & 1]) * 1.4426950408889634f);
-            if (key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[y][e >> 1] += w;
+            const float w = ex2(fmaf(d[nt][e], by[e & 1], -lse[nt][e & 1]) * 1.4426950408889634f);
+            if (kAll || key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[y][e >> 1] += w;
           }
+        }
       }
     };
     if constexpr (NT > 0) {
-      draw();
+      if (key0 + Cfg::kStep <= all_see) draw(std::true_type{}); else draw(std::false_type{});
     } else {
 #pragma unroll 1
       for (int nt = 0; nt * 8 < p.rows; nt += kHeld) {
 #pragma unroll
-        for (int z = 0; z < kHeld; ++z) take_rows(x, nt + z, qf[z], lse[z], sees[z]);
-        draw();
+        for (int z = 0; z < kHeld; ++z) take_rows(x, nt + z, qf[z], lse[z], shift[z], sees[z]);
+        draw(std::false_type{});
       }
     }
 #pragma unroll
@@ -284,25 +314,37 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     }
   };
 
-  // ---- the stream: one step's rows in flight while another is computed, the pages of the one after being looked up ----
-  Step now, then;
-  Place cur = at, ahead = at, far = at;
-  int blk = blocks(cur);
-  load(cur, blk, now);
-  long long left = u_end - u;                   // units from `cur` on
-  if (left > 1) { ahead = next(cur); blk = blocks(ahead); }
-  while (left > 0) {
-    int blk_far = -1;
-    if (left > 1) {
-      load(ahead, blk, then);
-      if (left > 2) { far = next(ahead); blk_far = blocks(far); }
+  // ---- the stream: two steps' rows in flight or being computed, the pages of the one after being looked up.  Two buffers that take
+  // turns, not one that is copied: a copy would wait for the loads. ----
+  Step even, odd;
+  Place at_even = at, at_odd = at, far = at;
+  long long left = u_end - u;                   // units from the next one to compute on
+  load(at_even, blocks(at_even), even);
+  if (left > 1) {
+    at_odd = next(at_even);
+    load(at_odd, blocks(at_odd), odd);
+  }
+  int blk = -1;
+  if (left > 2) {
+    far = next(at_odd);
+    blk = blocks(far);
+  }
+  // computes x and starts the loads of what is two units ahead into its place
+  auto turn = [&](Place& x, Step& s) {
+    compute(x, s);
+    if (left > 2) {
+      x = far;
+      load(x, blk, s);
+      if (left > 3) {
+        far = next(far);
+        blk = blocks(far);
+      }
     }
-    compute(cur, now);
-    now = then;
-    cur = ahead;
-    ahead = far;
-    blk = blk_far;
     --left;
+  };
+  while (left > 0) {
+    turn(at_even, even);
+    if (left > 0) turn(at_odd, odd);
   }
 }
 

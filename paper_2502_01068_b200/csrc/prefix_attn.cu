@@ -845,126 +845,189 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   pdl_wait();                                             // who waits for this kernel waits for the one before it, too
 }
 
-// Joins a query row's pieces and the attention over its own entries.  A warp takes 32 rows (lane = row; the pieces hold columns by rows)
-// and 8 columns; blockIdx: (32 rows, KV head, 32 columns).
+// Joins a query row's pieces and the attention over its own entries.  A block takes 32 rows (lane = row; the pieces hold columns by rows)
+// and 16 columns; its warps share the pieces out and meet once in shared memory.  All of it is latency: every load that can be is in
+// flight before the first is used, and up to 32 prefixes are scanned without a barrier.
+constexpr int kMergeWarps = 8, kMergeCols = 16;
 template <int D, bool kE4M3>
-__global__ void __launch_bounds__(128) prefix_merge_kernel(const PrefixParams p) {
-  __shared__ long long chunk0[kMaxPrefixes + 1];          // chunks and units of the prefixes before
-  __shared__ int unit0[kMaxPrefixes + 1];
-  __shared__ long long scratch[4], scratch_u[4];
+__global__ void __launch_bounds__(32 * kMergeWarps, 3) prefix_merge_kernel(const PrefixParams p) {
+  constexpr int kMergeThreads = 32 * kMergeWarps;
+  __shared__ float acc_of[kMergeWarps][32][kMergeCols + 1];
+  __shared__ float2 ml_of[kMergeWarps][32];
+  __shared__ long long chunk0[kMaxPrefixes];              // chunks and units of the prefixes before (more than 32 of them)
+  __shared__ int unit0[kMaxPrefixes];
+  __shared__ long long scratch[kMergeWarps], scratch_u[kMergeWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len, n = p.n_prefixes;
   pdl_launch_dependents();
+  // (what is read here was there before the kernel before this one began)
+  const bool few = n <= 32;                               // then every warp scans the prefixes for itself, a lane each
+  long long total, before = 0, before_u = 0;              // of prefix `lane` (few), or of the block's scan
+  Group mine_of = {};
+  int first_seq = 0x7fffffff;
   {
-    const int per = (n + 127) / 128, i0 = min(t * per, n), i1 = min(i0 + per, n);
+    const int threads = few ? 32 : kMergeThreads, at = few ? lane : t;
+    const int per = few ? 1 : (n + threads - 1) / threads, i0 = min(at * per, n), i1 = min(i0 + per, n);
     long long mine = 0, units = 0;
     for (int i = i0; i < i1; ++i) {
       const Group g = group_of(p, i);
+      if (few) { mine_of = g; first_seq = p.cu_seqs != nullptr ? __ldcg(p.cu_seqs + i) : 0; }
       units += static_cast<long long>(g.pairs) * Hkv;
       mine += static_cast<long long>(g.pairs) * Hkv * g.chunks;
     }
-    long long before = mine, before_u = units;
+    before = mine;
+    before_u = units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, before, o), z = __shfl_up_sync(0xffffffffu, before_u, o);
       if (lane >= o) { before += y; before_u += z; }
     }
-    if (lane == 31) { scratch[warp] = before; scratch_u[warp] = before_u; }
-    __syncthreads();
+    long long all = __shfl_sync(0xffffffffu, before, 31), all_u = __shfl_sync(0xffffffffu, before_u, 31);
+    if (!few) {
+      if (lane == 31) { scratch[warp] = before; scratch_u[warp] = before_u; }
+      __syncthreads();
+      all = all_u = 0;
+      for (int w = 0; w < kMergeWarps; ++w) {
+        if (w < warp) { before += scratch[w]; before_u += scratch_u[w]; }
+        all += scratch[w];
+        all_u += scratch_u[w];
+      }
+    }
     before -= mine;
     before_u -= units;
-    for (int w = 0; w < warp; ++w) { before += scratch[w]; before_u += scratch_u[w]; }
-    for (int i = i0; i < i1; ++i) {
-      const Group g = group_of(p, i);
-      chunk0[i] = before;
-      unit0[i] = static_cast<int>(before_u);
-      before += static_cast<long long>(g.pairs) * Hkv * g.chunks;
-      before_u += static_cast<long long>(g.pairs) * Hkv;
-      if (i == n - 1) { chunk0[n] = before; unit0[n] = static_cast<int>(min(before_u, 0x7fffffffll)); }
+    if (!few) {
+      long long c = before, z = before_u;
+      for (int i = i0; i < i1; ++i) {
+        const Group g = group_of(p, i);
+        chunk0[i] = c;
+        unit0[i] = static_cast<int>(z);
+        c += static_cast<long long>(g.pairs) * Hkv * g.chunks;
+        z += static_cast<long long>(g.pairs) * Hkv;
+      }
+      __syncthreads();
     }
-    __syncthreads();
+    total = all_u > p.max_units ? 0 : all;
   }
-  const long long total = unit0[n] > p.max_units ? 0 : chunk0[n];
-  const int R = blockIdx.x * 32 + lane, g = blockIdx.y, col = blockIdx.z * 32 + warp * 8;
-  const int token = R / G, b = token / T, h = g * G + R - token * G;
-  const bool there = b < p.c.batch;
+  const int rows = p.c.batch * T * G;                     // of a KV head
+  const int R = blockIdx.x * 32 + lane, g = blockIdx.y, col0 = blockIdx.z * kMergeCols;
+  const int token = R / G, b = token / T;
   // ---- this row's pieces: `count` of them from `piece` on, and the same rows' other half of the chunks where one tile took both ----
   int count = 0, both = 1;
   const float2* ml = p.part_ml;
   const float* po = p.part_o;
-  if (there && total > 0) {
-    int lo = 0, hi = n;                                   // the last prefix that starts at or before b
-    if (p.cu_seqs != nullptr)
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldcg(p.cu_seqs + mid) <= b) lo = mid; else hi = mid;
-      }
-    const Group gr = group_of(p, lo);
+  int lo = 0;                                             // the last prefix that starts at or before the row's sequence
+  Group gr;
+  long long chunk_at, unit_at;
+  if (few) {
+    for (int i = 1; i < n; ++i)
+      if (__shfl_sync(0xffffffffu, first_seq, i) <= b) lo = i;
+    gr.seq0 = __shfl_sync(0xffffffffu, mine_of.seq0, lo);
+    gr.tokens = __shfl_sync(0xffffffffu, mine_of.tokens, lo);
+    gr.chunks = __shfl_sync(0xffffffffu, mine_of.chunks, lo);
+    gr.pairs = __shfl_sync(0xffffffffu, mine_of.pairs, lo);
+    chunk_at = __shfl_sync(0xffffffffu, before, lo);
+    unit_at = __shfl_sync(0xffffffffu, before_u, lo);
+  } else {
+    int hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldcg(p.cu_seqs + mid) <= b) lo = mid; else hi = mid;
+    }
+    gr = group_of(p, lo);
+    chunk_at = chunk0[lo];
+    unit_at = unit0[lo];
+  }
+  if (R < rows && total > 0) {
     const int in = token - gr.seq0 * T;
     if (in >= 0 && in < gr.tokens && gr.pairs > 0) {
       const int pair = in / (2 * p.tile_tokens), rest = in - pair * 2 * p.tile_tokens;
       const bool dual = min(gr.tokens - pair * 2 * p.tile_tokens, 2 * p.tile_tokens) > p.tile_tokens;
       const int tile = rest / p.tile_tokens, row = (rest - tile * p.tile_tokens) * G + R - token * G;
-      const long long unit = static_cast<long long>(g) * gr.pairs + pair, q0 = chunk0[lo] + unit * gr.chunks, q1 = q0 + gr.chunks;
+      const long long unit = static_cast<long long>(g) * gr.pairs + pair, q0 = chunk_at + unit * gr.chunks, q1 = q0 + gr.chunks;
       const int ctas = sharing_ctas(p, total);
       const int ca = static_cast<int>(((q0 + 1) * ctas - 1) / total), cb = static_cast<int>((q1 * ctas - 1) / total);
-      const long long piece = unit0[lo] + unit + ca;
-      count = cb - ca + 1;
+      const long long piece = unit_at + unit + ca;
       both = dual ? 1 : 2;
+      count = (cb - ca + 1) * both;
       ml += (piece * 2 + tile) * p.tile_rows + row;
-      po += ((piece * 2 + tile) * D + col) * p.tile_rows + row;
+      po += ((piece * 2 + tile) * D + col0) * p.tile_rows + row;
     }
   }
+  const int most = __reduce_max_sync(0xffffffffu, count);
   pdl_wait();
-  const int most = __reduce_max_sync(0xffffffffu, count * both);
-  float M = -INFINITY, L = 0.0f, acc[8];
+  float M = -INFINITY, L = 0.0f, acc[kMergeCols];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-  auto join = [&](float m, float l, const float (&o)[8]) {
-    if (l == 0.0f) return;                                // nothing seen; NaN stays
-    const float top = fmaxf(M, m), ref = top == -INFINITY ? 0.0f : top;
-    const float a = ex2(M - ref), w = ex2(m - ref);
-    M = top;
-    L = fmaf(L, a, l * w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = fmaf(acc[i], a, o[i] * w);
-  };
+  for (int i = 0; i < kMergeCols; ++i) acc[i] = 0.0f;
   const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D) * p.tile_rows;
-  constexpr int kAhead = 4;
-  for (int s0 = 0; s0 < most; s0 += kAhead) {
+  constexpr int kAhead = 2;
+  for (int s0 = warp; s0 < most; s0 += kAhead * kMergeWarps) {
     float2 v[kAhead];
-    float o[kAhead][8];
+    float o[kAhead][kMergeCols];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int s = s0 + k;
+      const int s = s0 + k * kMergeWarps;
       v[k] = make_float2(-INFINITY, 0.0f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[k][i] = 0.0f;
-      if (s < count * both) {
+      if (s < count) {
         const size_t tile = both == 2 ? s : 2 * s;        // tiles of a piece lie side by side
         v[k] = __ldcg(ml + tile * step_ml);
+        const float* at = po + tile * step_o;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)                        // (8-bit pages: columns 1 and 2 of four have changed places)
-          o[k][i] = __ldcg(po + tile * step_o + static_cast<size_t>(kE4M3 && ((i ^ (i >> 1)) & 1) ? i ^ 3 : i) * p.tile_rows);
+        for (int i = 0; i < kMergeCols; ++i, at += p.tile_rows) o[k][i] = __ldcg(at);
       }
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) join(v[k].x, v[k].y, o[k]);
+    for (int k = 0; k < kAhead; ++k) {
+      if (v[k].y == 0.0f) continue;                       // nothing seen; NaN stays
+      const float top = fmaxf(M, v[k].x), ref = top == -INFINITY ? 0.0f : top;
+      const float a = ex2(M - ref), w = ex2(v[k].x - ref);
+      M = top;
+      L = fmaf(L, a, v[k].y * w);
+#pragma unroll
+      for (int i = 0; i < kMergeCols; ++i) acc[i] = fmaf(acc[i], a, o[k][i] * w);
+    }
   }
+  ml_of[warp][lane] = make_float2(M, L);
+#pragma unroll
+  for (int i = 0; i < kMergeCols; ++i) acc_of[warp][lane][i] = acc[i];
+  // ---- now a thread for two columns of a row; its own entries' attention joins last ----
+  constexpr int kPairs = kMergeCols / 2;
+  const int r = t / kPairs, c = t % kPairs * 2, R2 = blockIdx.x * 32 + r;
+  const int token2 = R2 / G, h2 = g * G + R2 - token2 * G;
+  const bool there = R2 < rows;
+  const size_t at = static_cast<size_t>(token2) * p.n_q_heads + h2;
+  float own = -INFINITY;
+  float2 y = make_float2(0.0f, 0.0f);
+  if (there) {
+    own = __ldcg(p.own_lse + at);
+    y = __ldcg(reinterpret_cast<const float2*>(p.own_out + at * D + col0 + c));
+  }
+  __syncthreads();
+  const float own_m = own * 1.4426950408889634f, own_l = own == -INFINITY ? 0.0f : 1.0f;
+  float top = own_m;
+#pragma unroll
+  for (int w = 0; w < kMergeWarps; ++w) top = fmaxf(top, ml_of[w][r].x);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  float2 out = make_float2(0.0f, 0.0f);
+  auto join = [&](float m, float l, float x0, float x1) {
+    if (l == 0.0f) return;
+    const float w = ex2(m - ref);
+    sum = fmaf(l, w, sum);
+    out.x = fmaf(x0, w, out.x);
+    out.y = fmaf(x1, w, out.y);
+  };
+  // 8-bit pages: columns 1 and 2 of four have changed places
+  const int c0 = kE4M3 && (c & 2) ? c - 1 : c, c1 = kE4M3 && !(c & 2) ? c + 2 : c + 1;
+#pragma unroll
+  for (int w = 0; w < kMergeWarps; ++w) {
+    const float2 x = ml_of[w][r];
+    join(x.x, x.y, acc_of[w][r][c0], acc_of[w][r][c1]);
+  }
+  join(own_m, own_l, y.x, y.y);
   if (!there) return;
-  const size_t at = static_cast<size_t>(token) * p.n_q_heads + h;
-  {
-    const float own = __ldcg(p.own_lse + at);
-    const float4 y0 = __ldcg(reinterpret_cast<const float4*>(p.own_out + at * D + col)), y1 = __ldcg(reinterpret_cast<const float4*>(p.own_out + at * D + col + 4));
-    const float o[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
-    join(own * 1.4426950408889634f, own == -INFINITY ? 0.0f : 1.0f, o);
-  }
-  const float f = L != 0.0f ? 1.0f / L : 0.0f;
-  uint4 w;
-  w.x = pack16<false>(acc[0] * f, acc[1] * f); w.y = pack16<false>(acc[2] * f, acc[3] * f);
-  w.z = pack16<false>(acc[4] * f, acc[5] * f); w.w = pack16<false>(acc[6] * f, acc[7] * f);
-  *reinterpret_cast<uint4*>(p.out + at * D + col) = w;
-  if (p.lse != nullptr && col == 0) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  const float f = sum != 0.0f ? 1.0f / sum : 0.0f;
+  *reinterpret_cast<uint32_t*>(p.out + at * D + col0 + c) = pack16<false>(out.x * f, out.y * f);
+  if (p.lse != nullptr && col0 + c == 0) p.lse[at] = sum != 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 namespace {
@@ -994,8 +1057,8 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
   if (e != cudaSuccess) return e;
   ++*launches;
   const long long rows = static_cast<long long>(p.c.batch) * p.q_len * p.group;
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + 31) / 32), p.c.n_kv_heads, D / 32);
-  cfg.blockDim = dim3(128);
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + 31) / 32), p.c.n_kv_heads, D / kMergeCols);
+  cfg.blockDim = dim3(32 * kMergeWarps);
   cfg.dynamicSmemBytes = 0;
   e = cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, kE4M3>, p);
   if (e == cudaSuccess) ++*launches;

@@ -57,7 +57,7 @@ def test_evict_refuses():
 def test_evict_workspace():
     size = lambda **kw: B.fastkv_paged_evict_workspace_bytes(plain(n_kv_heads=8, batch=3), B.make_eviction(**kw))  # noqa: E731
     assert size(keep=100, max_len=100) == 256 and size(keep=100, limit=200, max_len=150) == 256           # nothing to cut
-    assert 256 + 24 * 4 * (2 * 92 + 1) <= size(keep=100, max_len=101) <= 256 + 24 * 4 * (2 * 92 + 4) + 255
+    assert 256 + 24 * 4 * (2 * 92 + 1) <= size(keep=100, max_len=101) <= 256 + 24 * 4 * (4 * 92 + 4) + 255
     assert size(keep=100, window=100, max_len=1000) <= 256 + 24 * 16 + 255
     assert size(keep=2 ** 31 - 1, window=0, max_len=2 ** 31 - 1) == 256
 
