@@ -1079,8 +1079,9 @@ int check_prefix(const fastkv_paged_cache* c, const fastkv_prefix* x, const fast
   lay->bytes = off;
   return FASTKV_OK;
 }
-// A pool for tiles of 128 entries, a page's rows at a time: bf16 in swizzled boxes of 64 columns, codes as they are.
-int encode_prefix_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base) {
+// A pool for tiles of 128 entries, a page's rows at a time: boxes of 64 bf16 columns, or of whole rows of codes; swizzled where the tensor
+// cores read them.
+int encode_prefix_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void* base, bool swizzled) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const bool e4m3 = c.format == FASTKV_CACHE_E4M3;
@@ -1089,7 +1090,8 @@ int encode_prefix_pool(CUtensorMap* map, const fastkv_paged_cache& c, const void
   cuuint64_t strides[2] = {row, row * c.page_size};
   cuuint32_t box[3] = {static_cast<cuuint32_t>(e4m3 ? c.head_dim : 64), static_cast<cuuint32_t>(c.page_size), 1}, estr[3] = {1, 1, 1};
   CUresult r = fn(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE : e4m3 && c.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(FASTKV_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
   return FASTKV_OK;
@@ -1138,7 +1140,8 @@ int fastkv_prefix_attn(const fastkv_paged_cache* cache, const fastkv_prefix* pre
   const long long tokens = static_cast<long long>(c.batch) * query->q_len;
   if ((rc = encode_bf16_3d(&tmap_q, q, c.head_dim, query->n_q_heads, tokens, c.head_dim, static_cast<long long>(query->n_q_heads) * c.head_dim,
                            p.group, lay.tile_tokens)) ||
-      (rc = encode_prefix_pool(&tmap_k, c, c.k_pages)) || (rc = encode_prefix_pool(&tmap_v, c, c.v_pages)))
+      (rc = encode_prefix_pool(&tmap_k, c, c.k_pages, true)) ||
+      (rc = encode_prefix_pool(&tmap_v, c, c.v_pages, c.format == FASTKV_CACHE_BF16)))
     return rc;
   if ((rc = enqueue_paged_attn(c, *query, lay.own, lens, q, own_out, own_lse, workspace, stream_))) return rc;
   cudaError_t e;

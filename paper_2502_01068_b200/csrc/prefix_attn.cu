@@ -19,7 +19,8 @@
 //   softmax    four warps per row tile, a thread per row, which holds most of the chunk's 128 logits in registers: online softmax in log2
 //              units with a lazily raised reference; P goes back, in bf16, into the first half of the row's S columns.
 // With more than 128 rows the two tiles hold different rows and take every chunk, their contractions alternating.  With 128 or fewer
-// both work on the same rows and take every other chunk: one's softmax runs under the other's contractions.
+// both work on the same rows and take every other chunk: one's softmax runs under the other's contractions.  With 64 or fewer the second
+// tile's rows are its last 64 (its descriptor of Q starts 64 rows early), so that the two tiles' softmax warps are on different schedulers.
 // Tensor memory (512 columns): S (and P inside it) of tile A at 0, of tile B at 128; O of A at 256, of B at 256 + d.
 //
 // P is rounded to bf16 (2^-9 of each weight, of either sign): that is what the output is rounded to; the row sums take it unrounded.
@@ -38,7 +39,7 @@ constexpr int kTile = 128;                     // rows of a tile, entries of a c
 constexpr int kStep = 64;                      // entries of a softmax step: half a chunk, so that a tile's S has two buffers
 constexpr int kCtrlWarps = 4;                  // loader of K and V, issuer of tile A, issuer of tile B, loader of Q
 constexpr int kSoftmaxWarps = 4;               // per tile
-constexpr int kWideKWarps = 4, kWideVWarps = 8, kWideWarps = kWideKWarps + kWideVWarps;
+constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two terms, V to bf16
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
 constexpr float kSlackLog2 = 8.0f;
 
@@ -47,27 +48,31 @@ template <int D, bool kE4M3, bool kOne>
 struct PrefixCfg {
   static constexpr int KH = D / 64;
   static constexpr int kTileBytes = KH * kHalfBytes;
-  // Tiles of Q, K and V, and in 8 bits the raw chunks of K and of V.  V waits for the softmax: two tiles of V in bf16 leave a load less time
-  // than memory takes.
-  static constexpr int kQTiles = kOne ? 1 : 2, kKTiles = kE4M3 ? (D == 128 && !kOne ? 1 : 2) : (kOne ? 3 : 2), kVTiles = kE4M3 ? 2 : 3;
+  // Tiles of Q, K and V, and in 8 bits V's raw chunks.  V waits for the softmax: two tiles of V in bf16 leave a load less time than memory
+  // takes.
   static constexpr int kRawBytes = kTile * D;                              // codes of a chunk's K or V
-  static constexpr int kRaw = kE4M3 ? (D == 128 ? 2 : 4) : 1;              // raw chunks of each (none in bf16)
+  static constexpr int kKBytes = kE4M3 ? kRawBytes : kTileBytes;
+  static constexpr int kQTiles = kOne ? 1 : 2, kKTiles = kE4M3 ? (D == 128 && !kOne ? 3 : 4) : (kOne ? 3 : 2), kVTiles = kE4M3 ? 2 : 3;
+  static constexpr int kRaw = kE4M3 ? (D == 128 && !kOne ? 3 : 4) : 1;     // raw chunks of V (none in bf16)
   static constexpr int kWarps = kCtrlWarps + 2 * kSoftmaxWarps + (kE4M3 ? kWideWarps : 0);
   static constexpr int kThreads = 32 * kWarps;
   // behind the tiles: the scan of the prefixes, rows' shifts, pages' scales, barriers
-  static constexpr int kScanBytes = 512, kExtra = kScanBytes + 2 * kTile + 128 + 896;
-  static constexpr int kSmem = (kQTiles + kKTiles + kVTiles) * kTileBytes + (kE4M3 ? 2 * kRaw * kRawBytes : 0) + kExtra;
+  static constexpr int kScanBytes = 512, kExtra = kScanBytes + 2 * kTile + 256 + 896;
+  static constexpr int kSmem = (kQTiles + kVTiles) * kTileBytes + kKTiles * kKBytes + (kE4M3 ? kRaw * kRawBytes : 0) + kExtra;
   static_assert(kWarps <= 32 && kSmem <= 232448, "shared memory of a CTA");
-  // 8-bit pages: the launch's 80 registers a thread go 40 to the control warps, 112 to the softmax warps and 72 to the widening ones.
-  static constexpr int kLaunchRegs = 80, kCtrlRegs = 40, kSoftmaxRegs = 112, kWideRegs = 72;
-  static_assert(kCtrlRegs + 2 * kSoftmaxRegs + 3 * kWideRegs <= 6 * kLaunchRegs, "the warpgroups' shares are within what the CTA was launched with");
+  // 8-bit pages: the launch's 96 registers a thread go 40 to the control warps, 120 to the softmax warps and 96 to the widening ones.
+  static constexpr int kLaunchRegs = 96, kCtrlRegs = 40, kSoftmaxRegs = 120, kWideRegs = 96;
+  static_assert(kCtrlRegs + 2 * kSoftmaxRegs + 2 * kWideRegs <= 5 * kLaunchRegs, "the warpgroups' shares are within what the CTA was launched with");
 };
 
-// Chunks are numbered along a CTA's share.  Chunk n's K and V are in tiles n % kKTiles and n % kVTiles, their barriers are number n % 4: no
-// fewer than chunks in flight, and a barrier serves chunks of one parity, so that a row tile that takes every other chunk has
-// barriers of its own and waits on each in order (one that waited for a phase two ahead would be answered by the phase before).  The
-// two issuers start every segment together, when all earlier chunks have been used.
-constexpr int kBars = 4;
+// Chunks are numbered along a CTA's share.  Chunk n's K and V are in tiles n % kKTiles and n % kVTiles, their barriers are number n % 8.
+// A wait for a phase that is two ahead of its barrier, or two behind, would be answered wrongly.  So a barrier serves chunks of one
+// parity (a row tile that takes every other chunk has barriers of its own and waits on each in order), the two issuers start every
+// segment together, when all earlier chunks have been used, and the eighth chunk behind one is not loaded before the softmax has it
+// behind itself (the fourth may be).
+constexpr int kBars = 8;
+// K's scales of a chunk's pages: the softmax may still read a chunk's when the fourth behind it is loaded, never when the eighth is.
+constexpr int kScaleSlots = 8;
 
 // What the roles have to know of a segment; the loader of Q leaves it with Q.
 struct Brief {
@@ -78,13 +83,15 @@ struct Brief {
   __device__ __forceinline__ int skip(int x) const { return dual ? 0 : (n0 ^ x) & 1; }
   __device__ __forceinline__ int chunks_of(int x) const { return dual ? chunks : (chunks + 1 - skip(x)) >> 1; }
   __device__ __forceinline__ int chunk(int x, int j) const { return n0 + (dual ? j : skip(x) + 2 * j); }
+  // rows of tile x that come before the unit's first
+  __device__ __forceinline__ int ahead(int x, int group) const { return x == 1 && !dual && tokens * group <= 64 ? 64 : 0; }
 };
 
 template <int NR>
 struct PrefixBarriers {
   uint64_t q_full, q_empty, q_wide, v_tail;
   uint64_t k_full[kBars], k_empty[kBars], v_full[kBars], v_empty[kBars];
-  uint64_t raw_full[2][NR], raw_empty[2][NR];  // K, V
+  uint64_t raw_full[NR], raw_empty[NR];        // 8-bit pages: V's codes
   uint64_t s_full[2][2], p_full[2][2];         // per tile and buffer: S is there; every softmax warp has stored its part of P
   uint64_t o_step[2];                          // per tile: O has the next step's product
   uint64_t o_done[2], o_free[2];               // per tile: a segment's O is complete; the softmax warps have read it
@@ -132,6 +139,31 @@ struct Segment {
   }
 };
 
+// Two floats to a pair of e4m3 codes, to nearest even (`lo` in the low byte).
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// D[tmem] (+)= A[smem] * B[smem]^T, e4m3 x e4m3 -> fp32, 32 elements of the contraction, issued by one thread.
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// K-major operand tile in rows of 64 bytes with the 64-byte swizzle: groups of 8 rows are 512 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_k_sw64(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(1) << 16;
+  d |= static_cast<uint64_t>(512 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(4) << 61;                            // layout: SWIZZLE_64B
+  return d;
+}
 // Eight codes as fp16: one conversion for two of them, of which an SM does 16 a cycle.
 __device__ __forceinline__ uint4 widen8_half(uint32_t a, uint32_t b) { return make_uint4(widen_lo(a), widen_hi(a), widen_lo(b), widen_hi(b)); }
 
@@ -179,17 +211,17 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   using Cfg = PrefixCfg<D, kE4M3, kOne>;
   constexpr int NK = Cfg::kKTiles, NV = Cfg::kVTiles, NR = Cfg::kRaw, KH = Cfg::KH, kThreads = Cfg::kThreads, kWarps = Cfg::kWarps;
   extern __shared__ __align__(1024) uint8_t smem[];       // the tiles need 1024-byte alignment (128-byte swizzle atoms)
-  uint8_t* const sQ = smem;                               // one or two row tiles
-  uint8_t* const sK = sQ + Cfg::kQTiles * Cfg::kTileBytes;
-  uint8_t* const sV = sK + NK * Cfg::kTileBytes;
+  uint8_t* const sK = smem;
+  uint8_t* const sQ = sK + NK * Cfg::kKBytes;             // one or two row tiles
+  uint8_t* const sV = sQ + Cfg::kQTiles * Cfg::kTileBytes;
   uint8_t* const sRaw = sV + NV * Cfg::kTileBytes;
   // 8-bit pages: the power of two that a row of Q was shifted by, and K's scales of a chunk's pages
-  long long* const scan = reinterpret_cast<long long*>(sRaw + (kE4M3 ? 2 * NR * Cfg::kRawBytes : 0));
+  long long* const scan = reinterpret_cast<long long*>(sRaw + (kE4M3 ? NR * Cfg::kRawBytes : 0));
   int8_t* const row_shift = reinterpret_cast<int8_t*>(scan) + Cfg::kScanBytes;                    // [tile][row]
-  float* const page_scale = reinterpret_cast<float*>(row_shift + 2 * kTile);                      // [kBars][8]
+  float* const page_scale = reinterpret_cast<float*>(row_shift + 2 * kTile);                      // [kScaleSlots][8]
   using Barriers = PrefixBarriers<NR>;
   static_assert(sizeof(Barriers) <= 896, "what is set aside for the barriers");
-  Barriers* const bars = reinterpret_cast<Barriers*>(page_scale + kBars * 8);
+  Barriers* const bars = reinterpret_cast<Barriers*>(page_scale + kScaleSlots * 8);
 
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const int Hkv = p.c.n_kv_heads, G = p.group;
@@ -205,7 +237,29 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // ---- this CTA's share ----
   long long u = 0, u_end = 0;
   Segment first;
-  {
+  if (p.n_prefixes == 1) {                                // nothing to scan
+    first.group = 0;
+    first.of = group_of(p, 0);
+    const long long total = static_cast<long long>(first.of.pairs) * Hkv * first.of.chunks;
+    const int ctas = sharing_ctas(p, total);
+    if (blockIdx.x == 0 && t == 0) {
+      if (first.of.len != __ldcg(p.lens)) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_LEN);
+      if (p.cu_seqs != nullptr) {
+        const int a = __ldcg(p.cu_seqs), b = __ldcg(p.cu_seqs + 1);
+        if (a < 0 || b < a || b > p.c.batch) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_GROUP);
+      }
+    }
+    if (static_cast<int>(blockIdx.x) < ctas) {
+      u = total * blockIdx.x / ctas;
+      u_end = total * (blockIdx.x + 1) / ctas;
+    }
+    if (u >= u_end) {                                     // nothing for this CTA (uniform)
+      pdl_wait();
+      return;
+    }
+    first.unit = static_cast<int>(u / first.of.chunks);
+    first.c0 = static_cast<int>(u - static_cast<long long>(first.unit) * first.of.chunks);
+  } else {
     const int n = p.n_prefixes;
     const int per = (n + kThreads - 1) / kThreads, i0 = min(t * per, n), i1 = min(i0 + per, n);
     long long mine = 0, units = 0;                        // chunks and units of this thread's prefixes
@@ -266,14 +320,15 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     first.of = group_of(p, first.group);
     const long long in_group = u - bars->first_chunk;
     const int unit = static_cast<int>(in_group / first.of.chunks);
-    first.g = unit / first.of.pairs;
-    first.pair = unit - first.g * first.of.pairs;
-    first.unit = bars->first_unit + unit;
+    first.unit = unit;
     first.c0 = static_cast<int>(in_group - static_cast<long long>(unit) * first.of.chunks);
-    first.c1 = static_cast<int>(min(static_cast<long long>(first.of.chunks), first.c0 + (u_end - u)));
-    first.n0 = 0;
-    first.set(p);
   }
+  first.g = first.unit / first.of.pairs;                  // (of the prefix's units, so far)
+  first.pair = first.unit - first.g * first.of.pairs;
+  if (p.n_prefixes > 1) first.unit += bars->first_unit;
+  first.c1 = static_cast<int>(min(static_cast<long long>(first.of.chunks), first.c0 + (u_end - u)));
+  first.n0 = 0;
+  first.set(p);
   // Moves on to the next segment of the share; false when there is none.
   auto advance = [&](Segment& s, long long& at) -> bool {
     at += s.c1 - s.c0;
@@ -296,14 +351,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   if (t == 0) {
     mbar_init(&bars->q_full, 1);
     mbar_init(&bars->q_empty, 2);
-    mbar_init(&bars->q_wide, 8);
+    mbar_init(&bars->q_wide, kWideWarps);
     mbar_init(&bars->v_tail, 1);
     for (int i = 0; i < kBars; ++i) {
-      mbar_init(&bars->k_full[i], kE4M3 ? kWideKWarps : 1); mbar_init(&bars->k_empty[i], 2);
-      mbar_init(&bars->v_full[i], kE4M3 ? kWideVWarps : 1); mbar_init(&bars->v_empty[i], 2);
+      mbar_init(&bars->k_full[i], 1); mbar_init(&bars->k_empty[i], 2);
+      mbar_init(&bars->v_full[i], kE4M3 ? kWideWarps : 1); mbar_init(&bars->v_empty[i], 2);
     }
-    for (int kv = 0; kv < 2; ++kv)
-      for (int i = 0; i < NR; ++i) { mbar_init(&bars->raw_full[kv][i], 1); mbar_init(&bars->raw_empty[kv][i], kv ? kWideVWarps : kWideKWarps); }
+    for (int i = 0; i < NR; ++i) { mbar_init(&bars->raw_full[i], 1); mbar_init(&bars->raw_empty[i], kWideWarps); }
     for (int i = 0; i < 2; ++i) {
       for (int h = 0; h < 2; ++h) { mbar_init(&bars->s_full[i][h], 1); mbar_init(&bars->p_full[i][h], kSoftmaxWarps); }
       mbar_init(&bars->o_step[i], 1);
@@ -332,12 +386,18 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   const int P = 1 << p.c.page_log2, pages = kTile >> p.c.page_log2;      // pages of a chunk
   Segment s = first;
   long long at = u;
-  // Block (page * Hkv + g) of page j of chunk c, -1 behind the prefix's end.
-  auto block_of = [&](const Segment& x, int c, int j) -> int {
+  // Id of page j of the chunk c of a prefix of `len` entries; kNoPage behind its end.  Whoever asks looks at the answer a chunk later: what is
+  // done with a loaded value at once waits for it.
+  constexpr int kNoPage = static_cast<int>(0x80000000u);
+  auto page_of = [&](int group, int len, int c, int j) -> int {
     const int key = c * kTile + (j << p.c.page_log2);
-    if (j >= pages || key >= x.of.len) return -1;
-    const long long blk = pool_block(__ldcg(p.table + static_cast<size_t>(x.group) * p.max_pages + (key >> p.c.page_log2)), p.c.n_pages, Hkv, x.g);
-    if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_PAGE); return x.g; }       // page 0 instead
+    return j < pages && key < len ? __ldcg(p.table + static_cast<size_t>(group) * p.max_pages + (key >> p.c.page_log2)) : kNoPage;
+  };
+  // Its block (page * Hkv + g): -1 for none, page 0 for one outside the pool.
+  auto block_of = [&](int page, int g) -> int {
+    if (page == kNoPage) return -1;
+    const long long blk = pool_block(page, p.c.n_pages, Hkv, g);
+    if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_PAGE); return g; }
     return static_cast<int>(blk);
   };
 
@@ -364,34 +424,41 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
     };
     do {
-      int next = block_of(s, s.c0, lane / kCols);
+      // (8-bit pages: page, then scale, a chain of two loads; kCols is 1 and lane = page)
+      int blk = block_of(page_of(s.group, s.of.len, s.c0, lane / kCols), s.g);
+      int next = page_of(s.group, s.of.len, s.c0 + 1, lane / kCols);
+      float scale = kE4M3 && blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f;
       for (int c = s.c0; c < s.c1 && ok; ++c, ++n) {
-        const int blk = next;
-        if (c + 1 < s.c1) next = block_of(s, c + 1, lane / kCols);
+        const int bar = n % kBars;
+        if (n >= NK) ok = wait(&bars->k_empty[(n - NK) % kBars], (n - NK) / kBars & 1);
+        if (!ok) break;
+        if (kE4M3) {
+          if (lane < 8) page_scale[n % kScaleSlots * 8 + lane] = scale;
+          __syncwarp();
+        }
+        bring(&tmap_k, sK + n % NK * Cfg::kKBytes, &bars->k_full[bar], blk);
+        k_out = n + 1;
+        const int blk_v = blk;
+        blk = block_of(next, s.g);
+        next = page_of(s.group, s.of.len, c + 2, lane / kCols);
+        scale = kE4M3 && blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f;
         if constexpr (kE4M3) {
-          for (int kv = 0; kv < 2; ++kv) {
-            const int slot = n % NR;
-            if (n >= NR) ok = wait(&bars->raw_empty[kv][slot], (n / NR - 1) & 1);
-            if (!ok) break;
-            bring(kv ? &tmap_v : &tmap_k, sRaw + (kv * NR + slot) * Cfg::kRawBytes, &bars->raw_full[kv][slot], blk);
-            (kv ? v_out : k_out) = n + 1;
-          }
-        } else {
-          const int bar = n % kBars;
-          if (n >= NK) ok = wait(&bars->k_empty[(n - NK) % kBars], (n - NK) / kBars & 1);
+          const int slot = n % NR;
+          if (n >= NR) ok = wait(&bars->raw_empty[slot], (n / NR - 1) & 1);
           if (!ok) break;
-          bring(&tmap_k, sK + n % NK * Cfg::kTileBytes, &bars->k_full[bar], blk);
-          k_out = n + 1;
+          bring(&tmap_v, sRaw + slot * Cfg::kRawBytes, &bars->raw_full[slot], blk_v);
+          v_out = n + 1;
+        } else {
           if (n >= NV) ok = wait(&bars->v_empty[(n - NV) % kBars], (n - NV) / kBars & 1);
           if (!ok) break;
           const int have = s.of.len - c * kTile;
           uint8_t* const dst = sV + n % NV * Cfg::kTileBytes;
           if (have >= kTile) {
-            bring(&tmap_v, dst, &bars->v_full[bar], blk);
+            bring(&tmap_v, dst, &bars->v_full[bar], blk_v);
             v_out = n + 1;
           } else {
             // the prefix's last entries: a zero weight does not silence a NaN behind them, so those rows are cleared
-            bring(&tmap_v, dst, &bars->v_tail, blk);
+            bring(&tmap_v, dst, &bars->v_tail, blk_v);
             ok = wait(&bars->v_tail, tails & 1);
             if (!ok) { mbar_wait_drain(&bars->v_tail, tails & 1, p.hdr, SITE_PREFIX_DRAIN, limit); break; }
             ++tails;
@@ -408,11 +475,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     } while (ok && advance(s, at));
     // nothing may still be landing in shared memory when the CTA ends
     if (!ok && lane == 0) {
+      for (int j = max(0, k_out - NK); j < k_out; ++j) mbar_wait_drain(&bars->k_full[j % kBars], j / kBars & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
       if constexpr (kE4M3) {
-        for (int j = max(0, k_out - NR); j < k_out; ++j) mbar_wait_drain(&bars->raw_full[0][j % NR], (j / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
-        for (int j = max(0, v_out - NR); j < v_out; ++j) mbar_wait_drain(&bars->raw_full[1][j % NR], (j / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
+        for (int j = max(0, v_out - NR); j < v_out; ++j) mbar_wait_drain(&bars->raw_full[j % NR], (j / NR) & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
       } else {
-        for (int j = max(0, k_out - NK); j < k_out; ++j) mbar_wait_drain(&bars->k_full[j % kBars], j / kBars & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
         for (int j = max(0, v_out - NV); j < v_out; ++j) mbar_wait_drain(&bars->v_full[j % kBars], j / kBars & 1, p.hdr, SITE_PREFIX_DRAIN, limit);
       }
     }
@@ -454,15 +520,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     // carried along, not worked out.
     if constexpr (kE4M3) give_registers<Cfg::kCtrlRegs>();
     const int x = __shfl_sync(0xffffffffu, warp, 0) - 1;
-    // 8-bit pages: Q and K are fp16 (formats 0), P and V bf16
+    // 8-bit pages: Q (its two terms) and K are e4m3 (formats 0), P and V bf16
     constexpr uint32_t idesc_s = umma_idesc_bf16_f32(kTile, kStep) & ~(kE4M3 ? (1u << 7) | (1u << 10) : 0u);
     constexpr uint32_t idesc_o = umma_idesc_bf16_f32(kTile, D) | (1u << 16);    // B (V) is MN-major
-    constexpr uint64_t kHalfTile = kStep * 128 >> 4;      // from a tile's first 64 entries to its second, in a descriptor's units
+    // from a tile's first 64 entries to its second, in a descriptor's units
+    constexpr uint64_t kHalfTile = kStep * 128 >> 4, kHalfKTile = kE4M3 ? kStep * D >> 4 : kHalfTile;
     constexpr uint64_t kTileStep = Cfg::kTileBytes >> 4, kBlockStep = kHalfBytes >> 4;
     const bool leader = elect_one();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
     const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 256 + x * D;
-    const uint64_t q_desc = umma_desc_k_sw128(smem_u32(sQ)), k_desc = umma_desc_k_sw128(smem_u32(sK)),
+    const uint64_t q_desc = umma_desc_k_sw128(smem_u32(sQ)), k_desc = kE4M3 && D == 64 ? umma_desc_k_sw64(smem_u32(sK)) : umma_desc_k_sw128(smem_u32(sK)),
                    v_desc = umma_desc_mn_sw128(smem_u32(sV), kHalfBytes);
     bool ok = true, issued = false, again = false;        // again: the tile has had a segment with chunks
     uint32_t q_phase = 0, p_phase = 0, o_phase = 0;       // (p_phase: the same for both buffers, they alternate)
@@ -477,18 +544,19 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       br.chunks = __shfl_sync(0xffffffffu, shared.chunks, 0);
       br.n0 = __shfl_sync(0xffffffffu, shared.n0, 0);
       br.dual = kOne ? 0 : __shfl_sync(0xffffffffu, shared.dual, 0);
+      br.tokens = __shfl_sync(0xffffffffu, shared.tokens, 0);
       if (br.chunks == 0) break;
       if (kE4M3) ok = wait(&bars->q_wide, q_phase, SITE_PREFIX_Q);
       q_phase ^= 1;
       const int chunks = br.chunks_of(x), stride = br.dual ? 1 : 2;
-      const uint64_t a0 = q_desc + (br.dual ? x : 0) * kTileStep;
+      const uint64_t a0 = q_desc + (br.dual ? x : 0) * kTileStep - static_cast<uint64_t>(br.ahead(x, G) * 128 >> 4);
       int n = br.chunk(x, 0), k_at = n % NK, v_at = n % NV, before = 0;   // the chunk whose S is next; its tiles; the one before it
       int v_before = 0;
       for (int j = 0; j <= chunks && chunks > 0 && ok; ++j) {
         uint64_t* const k_full = &bars->k_full[n % kBars];
         uint64_t* const v_full = &bars->v_full[before % kBars];
         const uint32_t k_phase = n / kBars & 1, v_phase = before / kBars & 1;
-        const uint64_t kb = k_desc + k_at * kTileStep, vb = v_desc + v_before * kTileStep;
+        const uint64_t kb = k_desc + k_at * static_cast<uint64_t>(Cfg::kKBytes >> 4), vb = v_desc + v_before * kTileStep;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (j > 0) {                                    // O (+)= P V of the chunk before
@@ -524,10 +592,19 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               issued = true;
             }
             if (leader) {
+              if constexpr (kE4M3) {
+                // the terms of Q: the leading one's tile, then the other's (head dimension 64: the halves of a row)
 #pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk) {       // 64-element block kk / 4, 32 bytes per step inside it
-                const uint64_t step = (kk >> 2) * kBlockStep + (kk & 3) * 2;
-                tc_mma_bf16(s_tmem + h * kStep, a0 + step, kb + h * kHalfTile + step, idesc_s, kk > 0 ? 1u : 0u);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                  const int term = kk / (D / 32), step = kk % (D / 32) * 2;             // 32 elements, 32 bytes a step
+                  tc_mma_e4m3(s_tmem + h * kStep, a0 + term * (D == 128 ? kBlockStep : 4) + step, kb + h * kHalfKTile + step, idesc_s, kk > 0 ? 1u : 0u);
+                }
+              } else {
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {     // 64-element block kk / 4, 32 bytes per step inside it
+                  const uint64_t step = (kk >> 2) * kBlockStep + (kk & 3) * 2;
+                  tc_mma_bf16(s_tmem + h * kStep, a0 + step, kb + h * kHalfTile + step, idesc_s, kk > 0 ? 1u : 0u);
+                }
               }
               if (!(x == 0 && n == p.skip_commit)) tc_commit(&bars->s_full[x][h]);    // (test hook: a completion that is never signalled)
               if (h == 1) {
@@ -564,7 +641,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if constexpr (kE4M3) take_registers<Cfg::kSoftmaxRegs>();
     const int gw = warp - kCtrlWarps;
     const int x = gw >> 2, quarter = gw & 3;              // row tile; lane quarter (warp % 4: the control warps are four)
-    const int r = quarter * 32 + lane;                    // row of the tile = tensor-memory lane
+    const int at_lane = quarter * 32 + lane;              // tensor-memory lane
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_addr = lane_addr + x * kTile, o_addr = lane_addr + 256 + x * D;
     bool ok = true;
@@ -576,10 +653,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (br.chunks == 0) break;
       const int dual = kOne ? 0 : br.dual, steps = 2 * br.chunks_of(x), n_first = br.chunk(x, 0), n_step = dual ? 1 : 2;
       const int tokens = dual ? (x == 0 ? p.tile_tokens : br.tokens - p.tile_tokens) : br.tokens, rows = tokens * G;
+      const int r = at_lane - (kOne || !dual ? br.ahead(x, G) : 0);      // row of the tile
       int seen = br.seen - (n_first - br.n0) * kTile;     // entries from the step's first one to the prefix's end
       const long long piece = static_cast<long long>(br.unit) + blockIdx.x;
       ++segs;
-      if (quarter * 32 >= rows) {
+      if (r - lane < 0 || r - lane >= rows) {
         // no rows: the warp only keeps step (nobody may run ahead of a barrier by two phases)
         for (int i = 0; i < steps && ok; ++i, ++sn) {
           ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->s_full[x][sn & 1], (sn >> 1) & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit));
@@ -624,7 +702,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             // positive, so that masked logits stay -infinity
-            if (kE4M3) f[c * 2 + z] = fmaxf(by_row * page_scale[n % kBars * 8 + ((h * kStep + c * 32 + z * 16) >> p.c.page_log2)], 1.17549435e-38f);
+            if (kE4M3) f[c * 2 + z] = fmaxf(by_row * page_scale[n % kScaleSlots * 8 + ((h * kStep + c * 32 + z * 16) >> p.c.page_log2)], 1.17549435e-38f);
             float mx[2] = {v[c][z * 16], v[c][z * 16 + 1]};
 #pragma unroll
             for (int e = 2; e < 16; e += 2) { mx[0] = fmaxf(mx[0], v[c][z * 16 + e]); mx[1] = fmaxf(mx[1], v[c][z * 16 + e + 1]); }
@@ -674,7 +752,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (lane == 0) mbar_arrive(&bars->p_full[x][h]);
       }
       if (!ok) break;
-      // ---- the segment's piece: columns of O by rows, so that a warp's stores are whole lines ----
+      // ---- the segment's piece: four columns of O by rows, so that a warp's stores are whole lines ----
       float2* const ml = p.part_ml + (piece * 2 + x) * p.tile_rows + r;
       if (steps == 0) {
         if (r < rows) *ml = make_float2(-INFINITY, 0.0f);
@@ -685,25 +763,21 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (!ok) break;
       tc_fence_after_sync();
       if (r < rows) __stcg(ml, make_float2(m_ref, l));
-      int apart = p.tile_rows;
-      asm volatile("" : "+r"(apart));                     // (multiples of it are not worth a register each all through the loop above)
-      float* po = p.part_o + (piece * 2 + x) * D * p.tile_rows + r;
+      float4* po = reinterpret_cast<float4*>(p.part_o) + (piece * 2 + x) * (D / 4) * p.tile_rows + r;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float o[32];
         tmem_ld_32x32(o_addr + c * 32, o);
-        if (r < rows) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) __stcg(po + static_cast<long long>(e) * apart, o[e]);
-        }
-        po += 32ll * apart;
+        for (int e = 0; e < 8; ++e, po += p.tile_rows)
+          if (r < rows) __stcg(po, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]));
       }
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->o_free[x]);
     }
   } else {
-    // ---------------- widening (8-bit pages): Q and K to fp16, V to bf16 ----------------
+    // ---------------- widening (8-bit pages): Q into two e4m3 terms, V's codes to bf16 ----------------
     if constexpr (kE4M3) {
       give_registers<Cfg::kWideRegs>();
       const int w = warp - kCtrlWarps - 2 * kSoftmaxWarps;
@@ -712,16 +786,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       auto wait = [&](uint64_t* bar, uint32_t parity, int site) -> bool {
         return __all_sync(0xffffffffu, mbar_wait_nap(bar, parity, abort_flag, p.hdr, site, limit));
       };
-      const int kv = w >= kWideKWarps, first = kv ? (w - kWideKWarps) * (kTile / kWideVWarps) : w * (kTile / kWideKWarps);   // K or V; first row of every tile
-      const float* const scales = kv ? p.c.v_scales : p.c.k_scales;
-      // block of page `lane` of the prefix's chunk c, and its scale
-      auto block_in = [&](const Brief& y, int c) -> int {
-        const int key = c * kTile + (lane << p.c.page_log2);
-        if (lane >= pages || key >= y.len) return -1;
-        const long long blk = pool_block(__ldcg(p.table + static_cast<size_t>(y.group) * p.max_pages + (key >> p.c.page_log2)), p.c.n_pages, Hkv, y.g);
-        return blk < 0 ? y.g : static_cast<int>(blk);     // page 0 instead, as the loader takes it
-      };
-      auto scale_in = [&](int blk) -> float { return blk < 0 ? 0.0f : __ldcg(scales + blk); };
+      const int first = w * (kTile / kWideWarps);         // the warp's 16 rows of every tile of V
+      auto scale_in = [&](int blk) -> float { return blk < 0 ? 0.0f : __ldcg(p.c.v_scales + blk); };
       constexpr int kPieces = D / 16;                     // 16-byte pieces of a row of codes
       constexpr int kRowsAt = 32 / kPieces;               // rows of a warp's step
       // Eight lanes (what shared memory serves at a time) take four pieces of one column block of two neighbouring rows: the
@@ -729,106 +795,111 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       const int c4 = lane & 3, block = D == 128 ? (lane >> 3) & 1 : 0;
       const int row_in = ((lane >> 2) & 1) + (D == 128 ? (lane >> 4) * 2 : (lane >> 3) * 2);
       while (true) {
-        // ---- Q: bf16 to fp16 in place, a thread per row, after a power-of-two shift that brings the row's largest element to [2^14, 2^15):
-        // exact down to 2^-28 of it, and what is smaller is off by at most 2^-39 of the largest ----
         ok = wait(&bars->q_full, segs & 1, SITE_PREFIX_Q);
         if (!ok) break;
         const Brief br = bars->brief[segs & 1];
         if (br.chunks == 0) break;
         // (page, then scale: a chain of two loads, each started a chunk before the other needs it)
-        float next = scale_in(block_in(br, br.c0));
-        int next_block = block_in(br, br.c0 + 1);
+        float next = scale_in(block_of(page_of(br.group, br.len, br.c0, lane), br.g));
+        int next_page = page_of(br.group, br.len, br.c0 + 1, lane);
+        // ---- Q: a thread per row, in place.  After a power-of-two shift that brings the row's largest element to [2^7, 2^8), an element is
+        // the sum of its nearest e4m3 value and the e4m3 value nearest to the rest: exact down to 2^-9 of the largest (8 bits are 4 and 4),
+        // and what is smaller is off by at most 2^-17 of the largest. ----
         {
-          const int tile = w >> 2, row = (w & 3) * 32 + lane;         // (the first eight warps)
-          if (tile == 0 || (!kOne && tile == 1 && br.dual)) {
+          const int tile = w >> 2, row = (w & 3) * 32 + lane;
+          if (tile == 0 || (!kOne && br.dual)) {
             uint8_t* const at_row = sQ + tile * Cfg::kTileBytes + row * 128;
-            float m = 0.0f;
+            auto piece_at = [&](int i) -> uint4* {        // 16 bytes, number i of the row's two lines
+              return reinterpret_cast<uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
+            };
+            uint32_t most = 0;                            // the largest element's bits (bf16, without the sign)
 #pragma unroll 4
             for (int i = 0; i < D / 8; ++i) {
-              const uint4 q = *reinterpret_cast<const uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
-              const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float lo, hi;
-                unpack16<false>(qw[e], lo, hi);
-                m = fmaxf(m, fmaxf(fabsf(lo), fabsf(hi)));
-              }
+              const uint4 q = *piece_at(i);
+              const uint32_t m = __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
+              most = max(most, max(m & 0xffffu, m >> 16));
             }
-            int up = m > 0.0f ? 14 - scale_log2(__float_as_uint(m)) : 0;
-            up = up > 120 ? 120 : up;                     // of a subnormal row; otherwise within [-113, 120] as it stands
+            int up = most > 0 ? 7 - scale_log2(most << 16) : 0;
+            up = up > 120 ? 120 : up;                     // of a subnormal row; otherwise within [-120, 120] as it stands
             const float f = __uint_as_float(pow2_bits(up));
+            const bool finite = most < 0x7f80u;
             row_shift[tile * kTile + row] = static_cast<int8_t>(up);
-#pragma unroll 4
-            for (int i = 0; i < D / 8; ++i) {
-              uint4* const here = reinterpret_cast<uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
-              const uint4 q = *here;
-              uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+            uint32_t low[D / 4];
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {            // 16 elements; their leading terms go where earlier elements were
+              const uint4 a = *piece_at(2 * i), b = *piece_at(2 * i + 1);
+              const uint32_t q[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+              uint32_t high[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                float lo, hi;
-                unpack16<false>(qw[e], lo, hi);
-                qw[e] = pack16<true>(lo * f, hi * f);
+                uint32_t hi2[2], lo2[2];
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                  float x, y, u, v;
+                  unpack16<false>(q[2 * e + z], x, y);
+                  x *= f;
+                  y *= f;
+                  hi2[z] = pack_e4m3(x, y);
+                  unpack16<true>(widen_lo(hi2[z]), u, v);
+                  lo2[z] = pack_e4m3(x - u, y - v);
+                }
+                high[e] = finite ? hi2[0] | hi2[1] << 16 : 0x7f7f7f7fu;                 // an infinite or NaN row becomes NaN
+                low[i * 4 + e] = lo2[0] | lo2[1] << 16;
               }
-              *here = make_uint4(qw[0], qw[1], qw[2], qw[3]);
+              *piece_at(i) = make_uint4(high[0], high[1], high[2], high[3]);
             }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)              // head dimension 128: the other line; 64: the line's other half
+              *piece_at((D == 128 ? 8 : 4) + i) = make_uint4(low[i * 4], low[i * 4 + 1], low[i * 4 + 2], low[i * 4 + 3]);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0 && w < 8) mbar_arrive(&bars->q_wide);
+          if (lane == 0) mbar_arrive(&bars->q_wide);
         }
         ++segs;
         for (int c = br.c0; c < br.c0 + br.chunks && ok; ++c, ++n) {
           const float sc = next;
-          next = scale_in(next_block);
-          next_block = block_in(br, c + 2);
+          next = scale_in(block_of(next_page, br.g));
+          next_page = page_of(br.group, br.len, c + 2, lane);
           const int have = br.len - c * kTile;
-          const int slot = n % NR, gone = n - (kv ? NV : NK);         // gone: the chunk whose tile this one takes
-          ok = wait(&bars->raw_full[kv][slot], (n / NR) & 1, SITE_PREFIX_RAW);
-          if (ok && gone >= 0) ok = wait(kv ? &bars->v_empty[gone % kBars] : &bars->k_empty[gone % kBars], gone / kBars & 1, SITE_PREFIX_RAW);
+          const int slot = n % NR, gone = n - NV;         // gone: the chunk whose tile this one takes
+          ok = wait(&bars->raw_full[slot], (n / NR) & 1, SITE_PREFIX_RAW);
+          if (ok && gone >= 0) ok = wait(&bars->v_empty[gone % kBars], gone / kBars & 1, SITE_PREFIX_RAW);
           if (!ok) break;
-          const uint8_t* const src = sRaw + (kv * NR + slot) * Cfg::kRawBytes + (first + row_in) * D + (block * 4 + c4) * 16;
-          uint8_t* const tile = (kv ? sV + n % NV * Cfg::kTileBytes : sK + n % NK * Cfg::kTileBytes) + block * kHalfBytes;
+          const uint8_t* const src = sRaw + slot * Cfg::kRawBytes + (first + row_in) * D + (block * 4 + c4) * 16;
+          uint8_t* const tile = sV + n % NV * Cfg::kTileBytes + block * kHalfBytes;
           // row y * kRowsAt + row_in of the warp's: where its two 16-byte pieces go
           auto put = [&](int y, const uint4& a, const uint4& b) {
             const int r = first + y * kRowsAt + row_in;
             *reinterpret_cast<uint4*>(tile + r * 128 + (((2 * c4) ^ (r & 7)) << 4)) = a;
             *reinterpret_cast<uint4*>(tile + r * 128 + (((2 * c4 + 1) ^ (r & 7)) << 4)) = b;
           };
-          if (kv == 0) {
-            if (first == 0 && lane < 8) page_scale[n % kBars * 8 + lane] = sc;
+          constexpr int kSteps = kTile / kWideWarps / kRowsAt;
+          const float f = __shfl_sync(0xffffffffu, sc, first >> p.c.page_log2);        // the warp's 16 rows are one page's
+          // 2^120 f in one factor, unless that is too large for one
+          const bool two = f > 128.0f;
+          const uint32_t up = __byte_perm(__float_as_uint(two ? 1.329227995784916e36f : f * 1.329227995784916e36f), 0, 0x3232);
+          const uint32_t times = __byte_perm(__float_as_uint(two ? f : 1.0f), 0, 0x3232);
+          uint32_t odd = 0;
 #pragma unroll 2
-            for (int y = 0; y < kTile / kWideKWarps / kRowsAt; ++y) {      // (what lies behind the prefix's end is masked)
-              const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
-              put(y, widen8_half(q.x, q.y), widen8_half(q.z, q.w));
-            }
-          } else {
-            constexpr int kSteps = kTile / kWideVWarps / kRowsAt;
-            const float f = __shfl_sync(0xffffffffu, sc, first >> p.c.page_log2);      // the warp's 16 rows are one page's
-            // 2^120 f in one factor, unless that is too large for one
-            const bool two = f > 128.0f;
-            const uint32_t up = __byte_perm(__float_as_uint(two ? 1.329227995784916e36f : f * 1.329227995784916e36f), 0, 0x3232);
-            const uint32_t times = __byte_perm(__float_as_uint(two ? f : 1.0f), 0, 0x3232);
-            uint32_t odd = 0;
-#pragma unroll 2
-            for (int y = 0; y < kSteps; ++y) {
-              const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
-              put(y, widen8_bf16(q.x, q.y, up, times, odd), widen8_bf16(q.z, q.w, up, times, odd));
-            }
-            // NaN among the codes, or the prefix's end among the rows: those again
-            if (__any_sync(0xffffffffu, (odd & 0x7fff7fffu) != 0) || have < kTile) {
+          for (int y = 0; y < kSteps; ++y) {
+            const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+            put(y, widen8_bf16(q.x, q.y, up, times, odd), widen8_bf16(q.z, q.w, up, times, odd));
+          }
+          // NaN among the codes, or the prefix's end among the rows: those again
+          if (__any_sync(0xffffffffu, (odd & 0x7fff7fffu) != 0) || have < kTile) {
 #pragma unroll 1
-              for (int y = 0; y < kSteps; ++y) {
-                uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
-                if (first + y * kRowsAt + row_in >= have) q = make_uint4(0u, 0u, 0u, 0u);       // behind the end: zeros
-                put(y, widen8_any(q.x, q.y, f), widen8_any(q.z, q.w, f));
-              }
+            for (int y = 0; y < kSteps; ++y) {
+              uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+              if (first + y * kRowsAt + row_in >= have) q = make_uint4(0u, 0u, 0u, 0u);          // behind the end: zeros
+              put(y, widen8_any(q.x, q.y, f), widen8_any(q.z, q.w, f));
             }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive(kv ? &bars->v_full[n % kBars] : &bars->k_full[n % kBars]);
-            mbar_arrive(&bars->raw_empty[kv][slot]);
+            mbar_arrive(&bars->v_full[n % kBars]);
+            mbar_arrive(&bars->raw_empty[slot]);
           }
         }
         if (!ok) break;
@@ -914,7 +985,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 3) prefix_merge_kernel(const
   // ---- this row's pieces: `count` of them from `piece` on, and the same rows' other half of the chunks where one tile took both ----
   int count = 0, both = 1;
   const float2* ml = p.part_ml;
-  const float* po = p.part_o;
+  const float4* po = reinterpret_cast<const float4*>(p.part_o);
   int lo = 0;                                             // the last prefix that starts at or before the row's sequence
   Group gr;
   long long chunk_at, unit_at;
@@ -950,7 +1021,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 3) prefix_merge_kernel(const
       both = dual ? 1 : 2;
       count = (cb - ca + 1) * both;
       ml += (piece * 2 + tile) * p.tile_rows + row;
-      po += ((piece * 2 + tile) * D + col0) * p.tile_rows + row;
+      po += ((piece * 2 + tile) * (D / 4) + col0 / 4) * p.tile_rows + row;
     }
   }
   const int most = __reduce_max_sync(0xffffffffu, count);
@@ -958,7 +1029,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 3) prefix_merge_kernel(const
   float M = -INFINITY, L = 0.0f, acc[kMergeCols];
 #pragma unroll
   for (int i = 0; i < kMergeCols; ++i) acc[i] = 0.0f;
-  const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D) * p.tile_rows;
+  const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D / 4) * p.tile_rows;
   constexpr int kAhead = 2;
   for (int s0 = warp; s0 < most; s0 += kAhead * kMergeWarps) {
     float2 v[kAhead];
@@ -970,9 +1041,12 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 3) prefix_merge_kernel(const
       if (s < count) {
         const size_t tile = both == 2 ? s : 2 * s;        // tiles of a piece lie side by side
         v[k] = __ldcg(ml + tile * step_ml);
-        const float* at = po + tile * step_o;
+        const float4* at = po + tile * step_o;
 #pragma unroll
-        for (int i = 0; i < kMergeCols; ++i, at += p.tile_rows) o[k][i] = __ldcg(at);
+        for (int i = 0; i < kMergeCols; i += 4, at += p.tile_rows) {
+          const float4 y = __ldcg(at);
+          o[k][i] = y.x; o[k][i + 1] = y.y; o[k][i + 2] = y.z; o[k][i + 3] = y.w;
+        }
       }
     }
 #pragma unroll
