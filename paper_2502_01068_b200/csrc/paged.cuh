@@ -106,7 +106,7 @@ cudaError_t launch_prefix_attn(const CUtensorMap& tmap_q, const CUtensorMap& tma
 struct PagedWeightsParams {
   PagedView c;
   int n_q_heads, group, q_len, rows;     // rows = group * q_len query rows per (sequence, KV head)
-  int ctas;                   // CTAs that share all entries, filled in by the launcher
+  int ctas, pairs_log2;       // CTAs that share all entries, and steps of a warp's unit (in pairs), filled in by the launcher
   float scale, decay;
   long long total_len;        // HOST: entries of all sequences (grid sizing)
   const int* lens;

@@ -29,14 +29,15 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 template <int D, bool kE4M3>
 struct WeightsCfg {
-  // 16-byte loads of a lane per step: 4 KB a warp, in 8 bits 2 KB (with 4 KB the two steps do not fit the registers next to the queries)
+  // 16-byte loads of a lane per step: 4 KB a warp, in 8 bits 2 KB (with 4 KB the two steps do not fit the registers next to the queries).
+  // Two steps are a pair, whose weights are read and written together; one or more pairs in a row are what a warp has of a unit, so that
+  // the walk over sequences and pages is paid for once (at one step a unit it was half of all instructions in 8 bits).
   static constexpr int kLoads = kE4M3 ? 4 : 8;
   static constexpr int kRowBytes = D * (kE4M3 ? 1 : 2);
   static constexpr int kPieces = kRowBytes / 64;         // loads of a row by its four lanes
   static constexpr int kTiles = kLoads / (2 * kPieces);  // 16-entry tiles of a step
-  static constexpr int kStep = 16 * kTiles;
-  static constexpr int kChunk = kWarps * kStep;          // entries of a CTA's step: 128, 256 or 512
-  static constexpr int kChunkLog2 = kChunk == 128 ? 7 : kChunk == 256 ? 8 : 9;
+  static constexpr int kPair = 2 * 16 * kTiles;          // entries of a pair: 32 or 64
+  static constexpr int kPairLog2 = kPair == 32 ? 5 : 6;
 };
 
 __device__ __forceinline__ int entries_of(const PagedWeightsParams& p, int b) {
@@ -51,13 +52,14 @@ __device__ __forceinline__ int entries_of(const PagedWeightsParams& p, int b) {
 template <int D, bool kE4M3, int NT>
 __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedWeightsParams p) {
   using Cfg = WeightsCfg<D, kE4M3>;
-  constexpr int KS = D / 16, kTiles = Cfg::kTiles, kLoads = Cfg::kLoads, kPieces = Cfg::kPieces, kLog2 = Cfg::kChunkLog2;
+  constexpr int KS = D / 16, kTiles = Cfg::kTiles, kLoads = Cfg::kLoads, kPieces = Cfg::kPieces;
   constexpr int kHeld = NT > 0 ? NT : 2;       // tiles of 8 query rows at a time
   __shared__ long long scratch[kWarps];
   __shared__ int s_first;
   __shared__ long long s_base;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, quad = lane >> 2, c = lane & 3;
   const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len;
+  const int span_log2 = Cfg::kPairLog2 + p.pairs_log2, log2 = span_log2 + 3;       // entries of a unit: a warp's, the CTA's
   pdl_launch_dependents();
   pdl_wait();
 
@@ -70,9 +72,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     long long mine = 0, before = 0, total;
     const int per = (B + kThreads - 1) / kThreads, b0 = min(t * per, B), b1 = min(b0 + per, B);
     if (B == 1) {
-      total = static_cast<long long>(chunk_count(entries_of(p, 0), kLog2)) * Hkv;
+      total = static_cast<long long>(chunk_count(entries_of(p, 0), log2)) * Hkv;
     } else {
-      for (int x = b0; x < b1; ++x) mine += chunk_count(entries_of(p, x), kLog2);
+      for (int x = b0; x < b1; ++x) mine += chunk_count(entries_of(p, x), log2);
       before = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
       if (before * Hkv <= u && u < (before + mine) * Hkv) {
         long long at = before;
         for (int x = b0; x < b1; ++x) {
-          const int n = chunk_count(entries_of(p, x), kLog2);
+          const int n = chunk_count(entries_of(p, x), log2);
           if (u < (at + n) * Hkv) { s_first = x; s_base = at * Hkv; break; }
           at += n;
         }
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
   Place at;
   at.b = b;
   at.len = entries_of(p, b);
-  at.n_chunks = chunk_count(at.len, kLog2);
+  at.n_chunks = chunk_count(at.len, log2);
   at.g = static_cast<int>((u - base) / at.n_chunks);
   at.c = static_cast<int>((u - base) - static_cast<long long>(at.g) * at.n_chunks);
   auto next = [&](Place x) -> Place {           // the caller knows that there is one
@@ -126,47 +128,44 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     x.g = 0;
     do {
       x.len = entries_of(p, ++x.b);
-      x.n_chunks = chunk_count(x.len, kLog2);
+      x.n_chunks = chunk_count(x.len, log2);
     } while (x.n_chunks == 0);
     return x;
   };
-  // Lane y < kTiles: block (page * Hkv + g) of tile y of the warp's step, -1 behind the end.
-  auto blocks = [&](const Place& x) -> int {
-    const int key = (x.c << kLog2) + warp * Cfg::kStep + lane * 16;
-    if (lane >= kTiles || key >= x.len) return -1;
-    const long long blk = pool_block(p.c.block_table[static_cast<size_t>(x.b) * p.c.max_pages + (key >> p.c.page_log2)], p.c.n_pages, Hkv, x.g);
-    if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_WEIGHTS_PAGE); return x.g; }      // page 0 instead
+  // Lane y: page of tile y of what the warp has of a unit, kNoPage behind the end; then its block (page * Hkv + g), -1 for none and page 0
+  // for one outside the pool.  (Two parts, since what is done with a loaded value at once waits for it.)
+  constexpr int kNoPage = static_cast<int>(0x80000000u);
+  auto first_of = [&](const Place& x) -> int { return (x.c << log2) + (warp << span_log2); };
+  auto pages_of = [&](const Place& x) -> int {
+    const int key = first_of(x) + lane * 16;
+    return lane * 16 < (1 << span_log2) && key < x.len ? __ldg(p.c.block_table + static_cast<size_t>(x.b) * p.c.max_pages + (key >> p.c.page_log2)) : kNoPage;
+  };
+  auto blocks_of = [&](const Place& x, int page) -> int {
+    if (page == kNoPage) return -1;
+    const long long blk = pool_block(page, p.c.n_pages, Hkv, x.g);
+    if (blk < 0) { raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_WEIGHTS_PAGE); return x.g; }
     return static_cast<int>(blk);
   };
-  struct Step {
-    uint4 k[kLoads];                            // [tile][half][piece]
-    float scale;                                // lane y < kTiles: K's scale of tile y
-    float old[(kTiles + 1) / 2];                // weights so far, of the entries this lane writes
-  };
-  // The entry of tile pair z that this lane writes: lanes c = 0, 1 take tile 2 z, c = 2, 3 tile 2 z + 1, each one of its halves.
-  auto my_key = [&](const Place& x, int z) -> int {
-    return (x.c << kLog2) + warp * Cfg::kStep + (2 * z + (c >> 1)) * 16 + (c & 1) * 8 + quad;
-  };
-  auto writes = [&](const Place& x, int z) -> bool { return 2 * z + (c >> 1) < kTiles && my_key(x, z) < x.len; };
+  // The entry of tile pair z of the pair of steps at `key0` that this lane writes: lanes c = 0, 1 take tile 2 z, c = 2, 3 tile 2 z + 1, each
+  // one of its halves.
+  auto my_key = [&](int key0, int z) -> int { return key0 + (2 * z + (c >> 1)) * 16 + (c & 1) * 8 + quad; };
   auto row_of = [&](const Place& x) -> float* { return p.weights + (static_cast<long long>(x.b) * Hkv + x.g) * p.stride; };
-  auto load = [&](const Place& x, int blk, Step& s) {
-    const int row = (((x.c << kLog2) + warp * Cfg::kStep) & ((1 << p.c.page_log2) - 1));
+  // K's rows of a step whose first tile is `tile` of the warp's; blk: lane y has the block of tile y
+  auto load = [&](int tile, int blk, uint4 (&k)[kLoads]) {
+    // (a warp's entries start on a multiple of their number, as pages do)
+    const int row = (warp << span_log2) + tile * 16;
 #pragma unroll
     for (int y = 0; y < kTiles; ++y) {
-      const int by = __shfl_sync(0xffffffffu, blk, y);
+      const int by = __shfl_sync(0xffffffffu, blk, tile + y);
       const int first = (row + y * 16) & ((1 << p.c.page_log2) - 1);
       const uint8_t* src = p.c.k_pages + ((static_cast<long long>(max(by, 0)) << p.c.page_log2) + first + quad) * Cfg::kRowBytes + c * 16;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j)
-          s.k[(y * 2 + h) * kPieces + j] = by < 0 ? make_uint4(0u, 0u, 0u, 0u)
+        for (int j = 0; j < kPieces; ++j)               // [tile][half][piece]
+          k[(y * 2 + h) * kPieces + j] = by < 0 ? make_uint4(0u, 0u, 0u, 0u)
               : __ldg(reinterpret_cast<const uint4*>(src + h * 8 * Cfg::kRowBytes + j * 64));
     }
-    s.scale = kE4M3 && blk >= 0 ? __ldg(p.c.k_scales + blk) : 1.0f;
-#pragma unroll
-    for (int z = 0; z < (kTiles + 1) / 2; ++z)
-      s.old[z] = writes(x, z) && my_key(x, z) < x.len - T ? row_of(x)[my_key(x, z)] : 0.0f;
   };
 
   // ---- query fragments: row quad of each tile of 8, 16-byte pieces in the order K's come in ----
@@ -232,19 +231,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     for (int nt = 0; nt < kHeld; ++nt) n = min(n, min(lse[nt][0] == INFINITY ? n : sees[nt][0], lse[nt][1] == INFINITY ? n : sees[nt][1]));
     return __reduce_min_sync(0xffffffffu, n);
   };
-  auto compute = [&](const Place& x, const Step& s) {
-    const int key0 = (x.c << kLog2) + warp * Cfg::kStep;
-    if (NT > 0 && (x.b != have_b || x.g != have_g)) {
-      have_b = x.b;
-      have_g = x.g;
+  // what the entries of the step from `key0` on draw from the lane's rows
+  auto compute = [&](const Place& x, int key0, int tile, const uint4 (&k)[kLoads], float scales, float* sum) {
 #pragma unroll
-      for (int nt = 0; nt < kHeld; ++nt) take_rows(x, nt, qf[nt], lse[nt], shift[nt], sees[nt]);
-      all_see = least();
-    }
+    for (int y = 0; y < 2 * kTiles; ++y) sum[y] = 0.0f;
     if (key0 >= x.len) return;
-    float sum[kTiles][2];
-#pragma unroll
-    for (int y = 0; y < kTiles; ++y) sum[y][0] = sum[y][1] = 0.0f;
     // the rows of kHeld tiles: K's fragments (widened once) serve them all.  kAll: every row that is there sees the whole step (rows that
     // are not there have an lse of +infinity).
     auto draw = [&](auto all_) {
@@ -254,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
         float d[kHeld][4];
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-          const uint4 a = s.k[(y * 2) * kPieces + j], e = s.k[(y * 2 + 1) * kPieces + j];
+          const uint4 a = k[(y * 2) * kPieces + j], e = k[(y * 2 + 1) * kPieces + j];
           const uint32_t av[4] = {a.x, a.y, a.z, a.w}, ev[4] = {e.x, e.y, e.z, e.w};
           if constexpr (kE4M3) {
 #pragma unroll
@@ -272,21 +263,21 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
                 mma16<false>(d[nt], j == 0 && w == 0, av[2 * w], ev[2 * w], av[2 * w + 1], ev[2 * w + 1], qf[nt][4 * j + 2 * w], qf[nt][4 * j + 2 * w + 1]);
           }
         }
-        const float k = p.scale * (kE4M3 ? __shfl_sync(0xffffffffu, s.scale, y) : 1.0f);
+        const float times = p.scale * (kE4M3 ? __shfl_sync(0xffffffffu, scales, tile + y) : 1.0f);
 #pragma unroll
         for (int nt = 0; nt < kHeld; ++nt) {
-          const float by[2] = {kE4M3 ? k * shift[nt][0] : k, kE4M3 ? k * shift[nt][1] : k};
+          const float by[2] = {kE4M3 ? times * shift[nt][0] : times, kE4M3 ? times * shift[nt][1] : times};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             // what a row does not see must not reach the sum, NaN included
             const float w = ex2(fmaf(d[nt][e], by[e & 1], -lse[nt][e & 1]) * 1.4426950408889634f);
-            if (kAll || key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[y][e >> 1] += w;
+            if (kAll || key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[2 * y + (e >> 1)] += w;
           }
         }
       }
     };
     if constexpr (NT > 0) {
-      if (key0 + Cfg::kStep <= all_see) draw(std::true_type{}); else draw(std::false_type{});
+      if (key0 + 16 * kTiles <= all_see) draw(std::true_type{}); else draw(std::false_type{});
     } else {
 #pragma unroll 1
       for (int nt = 0; nt * 8 < p.rows; nt += kHeld) {
@@ -295,56 +286,65 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
         draw(std::false_type{});
       }
     }
-#pragma unroll
-    for (int y = 0; y < kTiles; ++y)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        sum[y][h] += __shfl_xor_sync(0xffffffffu, sum[y][h], 1);
-        sum[y][h] += __shfl_xor_sync(0xffffffffu, sum[y][h], 2);
-      }
-#pragma unroll
-    for (int z = 0; z < (kTiles + 1) / 2; ++z) {
-      const int hi = 2 * z + 1 < kTiles ? 2 * z + 1 : 2 * z;
-      const float a = (c & 1) ? sum[2 * z][1] : sum[2 * z][0], d = (c & 1) ? sum[hi][1] : sum[hi][0];
-      if (writes(x, z)) {
-        const int key = my_key(x, z);
-        const float drew = c >= 2 ? d : a;
-        row_of(x)[key] = key < x.len - T ? fmaf(p.decay, s.old[z], drew) : drew;
-      }
-    }
   };
 
-  // ---- the stream: two steps' rows in flight or being computed, the pages of the one after being looked up.  Two buffers that take
+  // ---- the stream: two steps' rows in flight or being computed, the pages of the next unit being looked up.  Two buffers that take
   // turns, not one that is copied: a copy would wait for the loads. ----
-  Step even, odd;
-  Place at_even = at, at_odd = at, far = at;
-  long long left = u_end - u;                   // units from the next one to compute on
-  load(at_even, blocks(at_even), even);
-  if (left > 1) {
-    at_odd = next(at_even);
-    load(at_odd, blocks(at_odd), odd);
-  }
-  int blk = -1;
-  if (left > 2) {
-    far = next(at_odd);
-    blk = blocks(far);
-  }
-  // computes x and starts the loads of what is two units ahead into its place
-  auto turn = [&](Place& x, Step& s) {
-    compute(x, s);
-    if (left > 2) {
-      x = far;
-      load(x, blk, s);
-      if (left > 3) {
-        far = next(far);
-        blk = blocks(far);
+  const int pairs = 1 << p.pairs_log2;
+  uint4 even[kLoads], odd[kLoads];
+  int blk = blocks_of(at, pages_of(at));
+  float scales = kE4M3 && blk >= 0 ? __ldg(p.c.k_scales + blk) : 1.0f;
+  load(0, blk, even);
+  load(kTiles, blk, odd);
+  while (true) {
+    if (NT > 0 && (at.b != have_b || at.g != have_g)) {
+      have_b = at.b;
+      have_g = at.g;
+#pragma unroll
+      for (int nt = 0; nt < kHeld; ++nt) take_rows(at, nt, qf[nt], lse[nt], shift[nt], sees[nt]);
+      all_see = least();
+    }
+    const bool more = ++u < u_end;
+    Place far = at;
+    int page = kNoPage, far_blk = -1;
+    float far_scales = 1.0f;
+    if (more) {
+      far = next(at);
+      page = pages_of(far);
+    }
+#pragma unroll 1
+    for (int i = 0; i < pairs; ++i) {
+      const bool last = i + 1 == pairs;
+      const int key0 = first_of(at) + i * Cfg::kPair, tile = i * 2 * kTiles, tile_next = last ? 0 : tile + 2 * kTiles;
+      float old[kTiles];
+#pragma unroll
+      for (int z = 0; z < kTiles; ++z) old[z] = my_key(key0, z) < at.len - T ? row_of(at)[my_key(key0, z)] : 0.0f;
+      float sum[4 * kTiles];                    // [tile][half]
+      compute(at, key0, tile, even, scales, sum);
+      if (last) {
+        far_blk = blocks_of(far, page);
+        if (kE4M3 && far_blk >= 0) far_scales = __ldg(p.c.k_scales + far_blk);
+      }
+      load(tile_next, last ? far_blk : blk, even);
+      compute(at, key0 + 16 * kTiles, tile + kTiles, odd, scales, sum + 2 * kTiles);
+      load(tile_next + kTiles, last ? far_blk : blk, odd);
+#pragma unroll
+      for (int y = 0; y < 4 * kTiles; ++y) {
+        sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
+        sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
+      }
+#pragma unroll
+      for (int z = 0; z < kTiles; ++z) {
+        const float a = (c & 1) ? sum[4 * z + 1] : sum[4 * z], d = (c & 1) ? sum[4 * z + 3] : sum[4 * z + 2];
+        const int key = my_key(key0, z);
+        const float drew = c >= 2 ? d : a;
+        if (key < at.len) row_of(at)[key] = key < at.len - T ? fmaf(p.decay, old[z], drew) : drew;
       }
     }
-    --left;
-  };
-  while (left > 0) {
-    turn(at_even, even);
-    if (left > 0) turn(at_odd, odd);
+    if (!more) return;
+    at = far;
+    blk = far_blk;
+    scales = far_scales;
   }
 }
 
@@ -352,8 +352,13 @@ namespace {
 
 template <int D, bool kE4M3, int NT>
 cudaError_t launch_nt(PagedWeightsParams& p, cudaStream_t stream) {
-  // CTAs: what is resident at once (two per SM), or one for every chunk of a short call
-  const long long chunks = (p.total_len >> WeightsCfg<D, kE4M3>::kChunkLog2) + p.c.batch;
+  // CTAs: what is resident at once (two per SM), or one for every unit of a short call.  Units: four pairs a warp as long as there are
+  // sixteen for every CTA, so that the uneven last one costs little; fewer pairs in shorter calls.
+  constexpr int kLog2 = WeightsCfg<D, kE4M3>::kPairLog2 + 3;
+  const long long pairs = p.total_len * p.c.n_kv_heads >> kLog2;
+  p.pairs_log2 = 0;
+  while (p.pairs_log2 < 2 && pairs >> (p.pairs_log2 + 1) >= 16ll * 2 * 148) ++p.pairs_log2;
+  const long long chunks = (p.total_len >> (kLog2 + p.pairs_log2)) + p.c.batch;
   p.ctas = static_cast<int>(min(chunks * p.c.n_kv_heads, 2ll * 148));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.ctas));

@@ -802,60 +802,58 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         // (page, then scale: a chain of two loads, each started a chunk before the other needs it)
         float next = scale_in(block_of(page_of(br.group, br.len, br.c0, lane), br.g));
         int next_page = page_of(br.group, br.len, br.c0 + 1, lane);
-        // ---- Q: a thread per row, in place.  After a power-of-two shift that brings the row's largest element to [2^7, 2^8), an element is
+        // ---- Q: two threads per row, in place.  After a power-of-two shift that brings the row's largest element to [2^7, 2^8), an element is
         // the sum of its nearest e4m3 value and the e4m3 value nearest to the rest: exact down to 2^-9 of the largest (8 bits are 4 and 4),
         // and what is smaller is off by at most 2^-17 of the largest. ----
-        {
-          const int tile = w >> 2, row = (w & 3) * 32 + lane;
-          if (tile == 0 || (!kOne && br.dual)) {
-            uint8_t* const at_row = sQ + tile * Cfg::kTileBytes + row * 128;
-            auto piece_at = [&](int i) -> uint4* {        // 16 bytes, number i of the row's two lines
-              return reinterpret_cast<uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
-            };
-            uint32_t most = 0;                            // the largest element's bits (bf16, without the sign)
-#pragma unroll 4
-            for (int i = 0; i < D / 8; ++i) {
-              const uint4 q = *piece_at(i);
-              const uint32_t m = __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
-              most = max(most, max(m & 0xffffu, m >> 16));
-            }
-            int up = most > 0 ? 7 - scale_log2(most << 16) : 0;
-            up = up > 120 ? 120 : up;                     // of a subnormal row; otherwise within [-120, 120] as it stands
-            const float f = __uint_as_float(pow2_bits(up));
-            const bool finite = most < 0x7f80u;
-            row_shift[tile * kTile + row] = static_cast<int8_t>(up);
-            uint32_t low[D / 4];
+        for (int tile = 0; tile < (!kOne && br.dual ? 2 : 1); ++tile) {
+          const int row = w * 16 + (lane >> 1), half = lane & 1;
+          uint8_t* const at_row = sQ + tile * Cfg::kTileBytes + row * 128;
+          auto piece_at = [&](int i) -> uint4* {          // 16 bytes, number i of the row's lines (one or two)
+            return reinterpret_cast<uint4*>(at_row + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4));
+          };
+          uint32_t q[D / 4];                              // half a row
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {            // 16 elements; their leading terms go where earlier elements were
-              const uint4 a = *piece_at(2 * i), b = *piece_at(2 * i + 1);
-              const uint32_t q[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-              uint32_t high[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                uint32_t hi2[2], lo2[2];
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                  float x, y, u, v;
-                  unpack16<false>(q[2 * e + z], x, y);
-                  x *= f;
-                  y *= f;
-                  hi2[z] = pack_e4m3(x, y);
-                  unpack16<true>(widen_lo(hi2[z]), u, v);
-                  lo2[z] = pack_e4m3(x - u, y - v);
-                }
-                high[e] = finite ? hi2[0] | hi2[1] << 16 : 0x7f7f7f7fu;                 // an infinite or NaN row becomes NaN
-                low[i * 4 + e] = lo2[0] | lo2[1] << 16;
-              }
-              *piece_at(i) = make_uint4(high[0], high[1], high[2], high[3]);
-            }
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)              // head dimension 128: the other line; 64: the line's other half
-              *piece_at((D == 128 ? 8 : 4) + i) = make_uint4(low[i * 4], low[i * 4 + 1], low[i * 4 + 2], low[i * 4 + 3]);
+          for (int i = 0; i < D / 16; ++i) {
+            const uint4 v = *piece_at(half * (D / 16) + i);
+            q[4 * i] = v.x; q[4 * i + 1] = v.y; q[4 * i + 2] = v.z; q[4 * i + 3] = v.w;
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->q_wide);
+          uint32_t most = 0;                              // the largest element's bits (bf16, without the sign)
+#pragma unroll
+          for (int i = 0; i < D / 4; ++i) most = __vmaxu2(most, q[i] & 0x7fff7fffu);
+          most = max(most & 0xffffu, most >> 16);
+          most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));                      // (and nobody of the warp reads elements any more)
+          int up = most > 0 ? 7 - scale_log2(most << 16) : 0;
+          up = up > 120 ? 120 : up;                       // of a subnormal row; otherwise within [-120, 120] as it stands
+          const float f = __uint_as_float(pow2_bits(up));
+          const bool finite = most < 0x7f80u;
+          if (half == 0) row_shift[tile * kTile + row] = static_cast<int8_t>(up);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {              // 16 elements
+            uint32_t high[4], low[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t hi2[2], lo2[2];
+#pragma unroll
+              for (int z = 0; z < 2; ++z) {
+                float x, y, u, v;
+                unpack16<false>(q[8 * i + 2 * e + z], x, y);
+                x *= f;
+                y *= f;
+                hi2[z] = pack_e4m3(x, y);
+                unpack16<true>(widen_lo(hi2[z]), u, v);
+                lo2[z] = pack_e4m3(x - u, y - v);
+              }
+              high[e] = finite ? hi2[0] | hi2[1] << 16 : 0x7f7f7f7fu;                   // an infinite or NaN row becomes NaN
+              low[e] = lo2[0] | lo2[1] << 16;
+            }
+            // the leading terms, and in the row's other line (head dimension 64: its line's other half) the rests
+            *piece_at(half * (D / 32) + i) = make_uint4(high[0], high[1], high[2], high[3]);
+            *piece_at(D / 16 + half * (D / 32) + i) = make_uint4(low[0], low[1], low[2], low[3]);
+          }
         }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->q_wide);
         ++segs;
         for (int c = br.c0; c < br.c0 + br.chunks && ok; ++c, ++n) {
           const float sc = next;
