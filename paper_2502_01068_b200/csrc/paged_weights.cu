@@ -114,22 +114,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
   }
 
   // A warp's place in the share: sequence, KV head, chunk of it.
-  struct Place { int b, g, c, n_chunks, len; };
+  struct Place { int b, g, c, len; };
   Place at;
   at.b = b;
   at.len = entries_of(p, b);
-  at.n_chunks = chunk_count(at.len, log2);
-  at.g = static_cast<int>((u - base) / at.n_chunks);
-  at.c = static_cast<int>((u - base) - static_cast<long long>(at.g) * at.n_chunks);
+  {
+    const int n = chunk_count(at.len, log2);
+    at.g = static_cast<int>((u - base) / n);
+    at.c = static_cast<int>((u - base) - static_cast<long long>(at.g) * n);
+  }
+  int left = static_cast<int>(u_end - u);       // units of the share that are not done
   auto next = [&](Place x) -> Place {           // the caller knows that there is one
-    if (++x.c < x.n_chunks) return x;
+    if (++x.c < chunk_count(x.len, log2)) return x;
     x.c = 0;
     if (++x.g < Hkv) return x;
     x.g = 0;
-    do {
-      x.len = entries_of(p, ++x.b);
-      x.n_chunks = chunk_count(x.len, log2);
-    } while (x.n_chunks == 0);
+    do { x.len = entries_of(p, ++x.b); } while (x.len == 0);
     return x;
   };
   // Lane y: page of tile y of what the warp has of a unit, kNoPage behind the end; then its block (page * Hkv + g), -1 for none and page 0
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     }
   };
 
-  int have_b = -1, have_g = -1, all_see = 0;
+  int all_see = 0;
   // the fewest entries that a row sees which is there
   auto least = [&]() -> int {
     int n = 0x7fffffff;
@@ -296,15 +296,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
   float scales = kE4M3 && blk >= 0 ? __ldg(p.c.k_scales + blk) : 1.0f;
   load(0, blk, even);
   load(kTiles, blk, odd);
+  bool fresh = true;
   while (true) {
-    if (NT > 0 && (at.b != have_b || at.g != have_g)) {
-      have_b = at.b;
-      have_g = at.g;
+    if (NT > 0 && fresh) {
 #pragma unroll
       for (int nt = 0; nt < kHeld; ++nt) take_rows(at, nt, qf[nt], lse[nt], shift[nt], sees[nt]);
       all_see = least();
     }
-    const bool more = ++u < u_end;
+    const bool more = --left > 0;
     Place far = at;
     int page = kNoPage, far_blk = -1;
     float far_scales = 1.0f;
@@ -342,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
       }
     }
     if (!more) return;
+    fresh = far.c == 0;                         // another KV head or sequence
     at = far;
     blk = far_blk;
     scales = far_scales;
@@ -357,7 +357,7 @@ cudaError_t launch_nt(PagedWeightsParams& p, cudaStream_t stream) {
   constexpr int kLog2 = WeightsCfg<D, kE4M3>::kPairLog2 + 3;
   const long long pairs = p.total_len * p.c.n_kv_heads >> kLog2;
   p.pairs_log2 = 0;
-  while (p.pairs_log2 < 2 && pairs >> (p.pairs_log2 + 1) >= 16ll * 2 * 148) ++p.pairs_log2;
+  while (p.pairs_log2 < 2 && pairs >> (p.pairs_log2 + 1) >= 6ll * 2 * 148) ++p.pairs_log2;
   const long long chunks = (p.total_len >> (kLog2 + p.pairs_log2)) + p.c.batch;
   p.ctas = static_cast<int>(min(chunks * p.c.n_kv_heads, 2ll * 148));
   cudaLaunchConfig_t cfg = {};
