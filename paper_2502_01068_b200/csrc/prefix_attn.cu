@@ -130,6 +130,12 @@ __device__ __forceinline__ int sharing_ctas(const PrefixParams& p, long long tot
   return static_cast<int>(min(static_cast<long long>(p.ctas), total));
 }
 
+// The deal.  A CTA that goes from one unit to the next spends what three chunks take on it (the output's way out, the next queries' way in:
+// 5.5 us of 1.9 a chunk), so every unit counts for its chunks and three more in front of them, which are nobody's work; with less than two
+// chunks for a CTA they would only make shares uneven, and chunks alone count.  (48 x 4 tokens over 4 prefixes, 11 chunks a CTA:
+// 38.6 us with chunks alone, 36.0 with units; 64 over one prefix of 32768, 14 chunks a CTA: 40.2 and 38.2.)
+__device__ __forceinline__ int unit_cost(const PrefixParams& p, long long chunks) { return chunks >= 2ll * p.ctas ? 3 : 0; }
+
 // A segment of a CTA's share: chunks [c0, c1) of one unit.
 struct Segment {
   int group, g, pair, c0, c1, unit;
@@ -288,12 +294,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // of its blocks let this one start: only the end of this kernel has to wait for it.
 
   // ---- this CTA's share ----
-  long long u = 0, u_end = 0;
+  long long u = 0, u_end = 0;                             // in chunks and what units cost, along all units
+  int cost;
   Segment first;
+  long long in_group;
   if (p.n_prefixes == 1) {                                // nothing to scan
     first.group = 0;
     first.of = group_of(p, 0);
-    const long long total = static_cast<long long>(first.of.pairs) * Hkv * first.of.chunks;
+    const long long units = static_cast<long long>(first.of.pairs) * Hkv;
+    cost = unit_cost(p, units * first.of.chunks);
+    const long long total = units * (first.of.chunks + cost);
     const int ctas = sharing_ctas(p, total);
     if (blockIdx.x == 0 && t == 0) {
       if (first.of.len != __ldcg(p.lens)) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_LEN);
@@ -310,8 +320,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       pdl_wait();
       return;
     }
-    first.unit = static_cast<int>(quotient(u, first.of.chunks));
-    first.c0 = static_cast<int>(u - static_cast<long long>(first.unit) * first.of.chunks);
+    in_group = u;
   } else {
     const int n = p.n_prefixes;
     const int per = (n + kThreads - 1) / kThreads, i0 = min(t * per, n), i1 = min(i0 + per, n);
@@ -345,6 +354,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       total += scan[w];
       total_u += scan[32 + w];
     }
+    cost = unit_cost(p, total);
+    total += cost * total_u;
+    before += cost * before_u;
+    mine += cost * units;
     if (total_u > p.max_units) {                          // groups that overlap: there is no room for their pieces
       if (blockIdx.x == 0 && t == 0) raise_status(p.hdr, FASTKV_ERR_DEVICE_INDEX, SITE_PREFIX_GROUP);
       total = 0;
@@ -358,7 +371,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       long long at = before, at_u = before_u;
       for (int i = i0; i < i1; ++i) {
         const Group g = group_of(p, i);
-        const long long k = static_cast<long long>(g.pairs) * Hkv * g.chunks;
+        const long long k = static_cast<long long>(g.pairs) * Hkv * (g.chunks + cost);
         if (u < at + k) { bars->first_group = i; bars->first_chunk = at; bars->first_unit = static_cast<int>(at_u); break; }
         at += k;
         at_u += static_cast<long long>(g.pairs) * Hkv;
@@ -371,32 +384,37 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     }
     first.group = bars->first_group;
     first.of = group_of(p, first.group);
-    const long long in_group = u - bars->first_chunk;
-    const int unit = static_cast<int>(quotient(in_group, first.of.chunks));
-    first.unit = unit;
-    first.c0 = static_cast<int>(in_group - static_cast<long long>(unit) * first.of.chunks);
+    in_group = u - bars->first_chunk;
+  }
+  first.unit = static_cast<int>(quotient(in_group, first.of.chunks + cost));
+  in_group -= static_cast<long long>(first.unit) * (first.of.chunks + cost);            // in the unit
+  const long long next_unit = u - in_group + first.of.chunks + cost;
+  first.c0 = static_cast<int>(max(in_group - cost, 0ll));
+  first.c1 = static_cast<int>(min(static_cast<long long>(first.of.chunks), in_group - cost + (u_end - u)));
+  if (first.c1 <= first.c0) {                             // no chunk (uniform)
+    pdl_wait();
+    return;
   }
   first.g = first.unit / first.of.pairs;                  // (of the prefix's units, so far)
   first.pair = first.unit - first.g * first.of.pairs;
   if (p.n_prefixes > 1) first.unit += bars->first_unit;
-  first.c1 = static_cast<int>(min(static_cast<long long>(first.of.chunks), first.c0 + (u_end - u)));
   first.n0 = 0;
   first.set(p);
-  // Moves on to the next segment of the share; false when there is none.
+  // Moves on to the next segment of the share, `at` where its unit starts; false when there is none.
   auto advance = [&](Segment& s, long long& at) -> bool {
-    at += s.c1 - s.c0;
     s.n0 += s.c1 - s.c0;
-    if (at >= u_end) return false;
+    if (u_end - at <= cost) return false;
     ++s.unit;
     if (++s.pair == s.of.pairs) {
       s.pair = 0;
       if (++s.g == Hkv) {
         s.g = 0;
-        do { s.of = group_of(p, ++s.group); } while (s.of.pairs == 0);                 // at < u_end: there is one
+        do { s.of = group_of(p, ++s.group); } while (s.of.pairs == 0);                 // at + cost < u_end: there is one
       }
     }
     s.c0 = 0;
-    s.c1 = static_cast<int>(min(static_cast<long long>(s.of.chunks), u_end - at));
+    s.c1 = static_cast<int>(min(static_cast<long long>(s.of.chunks), u_end - at - cost));
+    at += s.of.chunks + cost;
     s.set(p);
     return true;
   };
@@ -438,7 +456,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   const long long limit = p.wait_limit;
   const int P = 1 << p.c.page_log2, pages = kTile >> p.c.page_log2;      // pages of a chunk
   Segment s = first;
-  long long at = u;
+  long long at = next_unit;
   // Id of page j of the chunk c of a prefix of `len` entries; kNoPage behind its end.  Whoever asks looks at the answer a chunk later: what is
   // done with a loaded value at once waits for it.
   constexpr int kNoPage = static_cast<int>(0x80000000u);
@@ -1002,6 +1020,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
   const bool few = n <= 32;                               // then every warp scans the prefixes for itself, a lane each
   long long total, before = 0, before_u = 0;              // of prefix `lane` (few), or of the block's scan
   Group mine_of = {};
+  int cost;
   int first_seq = 0x7fffffff;
   {
     const int threads = few ? 32 : kMergeThreads, at = few ? lane : t;
@@ -1033,13 +1052,16 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
     }
     before -= mine;
     before_u -= units;
+    cost = unit_cost(p, all);
+    all += cost * all_u;
+    before += cost * before_u;
     if (!few) {
       long long c = before, z = before_u;
       for (int i = i0; i < i1; ++i) {
         const Group g = group_of(p, i);
         chunk0[i] = c;
         unit0[i] = static_cast<int>(z);
-        c += static_cast<long long>(g.pairs) * Hkv * g.chunks;
+        c += static_cast<long long>(g.pairs) * Hkv * (g.chunks + cost);
         z += static_cast<long long>(g.pairs) * Hkv;
       }
       __syncthreads();
@@ -1081,7 +1103,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
       const int pair = in / (2 * p.tile_tokens), rest = in - pair * 2 * p.tile_tokens;
       const bool dual = min(gr.tokens - pair * 2 * p.tile_tokens, 2 * p.tile_tokens) > p.tile_tokens;
       const int tile = rest / p.tile_tokens, row = (rest - tile * p.tile_tokens) * G + R - token * G;
-      const long long unit = static_cast<long long>(g) * gr.pairs + pair, q0 = chunk_at + unit * gr.chunks, q1 = q0 + gr.chunks;
+      const long long unit = static_cast<long long>(g) * gr.pairs + pair, q0 = chunk_at + unit * (gr.chunks + cost) + cost, q1 = q0 + gr.chunks;
       const int ctas = sharing_ctas(p, total);
       const int ca = static_cast<int>(quotient((q0 + 1) * ctas - 1, total)), cb = static_cast<int>(quotient(q1 * ctas - 1, total));
       const long long piece = unit_at + unit + ca;
