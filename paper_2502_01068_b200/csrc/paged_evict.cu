@@ -68,7 +68,7 @@ struct alignas(16) PlanShared {
   int total_hist[2][kBins];        // the cluster's histogram of a pass (every CTA adds into it), double-buffered by pass parity
   int warp_tot[2][THREADS / 32];
   alignas(8) int counts[8][2];     // per CTA of the cluster: (#above threshold, #equal to it)
-  int digit, k_rem;
+  int digit, k_rem, whole;
 };
 
 }  // namespace
@@ -199,6 +199,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_plan_kernel(con
             if (above < k_rem && k_rem <= above + cnt[i]) {
               sh.digit = 255 - (lane * 8 + i);
               sh.k_rem = k_rem - above;
+              sh.whole = cnt[i] == k_rem - above;
             }
             above += cnt[i];
           }
@@ -209,6 +210,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_plan_kernel(con
       const uint32_t digit = static_cast<uint32_t>(sh.digit);
       tau |= digit << shift;
       k_rem = sh.k_rem;
+      // All that match the prefix stay: no more digits (with zeros for them the threshold is at or below each, and those equal to it are no
+      // more than k_rem).
+      if (sh.whole) break;
       if (CACHED && live != 0) {
         uint32_t still = 0;
 #pragma unroll
@@ -277,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_plan_kernel(con
 namespace {
 
 constexpr int kRoundRows = 128;            // rows of a round that a CTA holds in shared memory: one page at most, or several
-constexpr int kHeld = 2;                    // 8-bit pages: free slots that a lane holds at a time
+constexpr int kHeld = 3;                    // 8-bit pages: free slots that a lane holds at a time (2: 75 us for four of 26214, 3: 72)
 constexpr int kOwnPages = 16;              // 8-bit pages that a warp takes at a time, at most
 
 __device__ __forceinline__ uint32_t recode2(uint32_t w, float f) {        // two codes times f <= 1, rounded to nearest even
@@ -424,10 +428,12 @@ __global__ void __launch_bounds__(kMoveThreads, 1024 / kMoveThreads) evict_move_
   } else {
     // A warp takes several pages whole: first every page's new scale, and which of its slots are free, then the rows.
     __shared__ unsigned most_of[kMoveWarps][kOwnPages], free_of[kMoveWarps][kOwnPages][4];
+    __shared__ uint8_t again_of[kMoveWarps][kOwnPages];
     const int n_pages = m0 >> p.c.page_log2;
-    // an even share, but no more than have some 64 free slots together: those stay in the lanes' registers
-    const int share = n_pages == 0 ? 1 : static_cast<int>(32ll * kHeld * n_pages / max(plan.page_first[n_pages], 1));
-    const int per = min(min(kOwnPages, (n_pages + n_warps - 1) / n_warps), max(share, 1));
+    // an even share, in as many parts as it takes for one to have no more than some 96 free slots: those stay in the lanes' registers
+    const int most_pages = min(kOwnPages, max(1, n_pages == 0 ? 1 : static_cast<int>(32ll * kHeld * n_pages / max(plan.page_first[n_pages], 1))));
+    const int parts = max(1, (n_pages + n_warps * most_pages - 1) / (n_warps * most_pages));
+    const int per = max(1, (n_pages + n_warps * parts - 1) / (n_warps * parts));
     for (int pa = gw * per; pa < n_pages; pa += n_warps * per) {
       const int pb = min(pa + per, n_pages);
       const int first = plan.page_first[pa + min(lane, pb - pa)];            // of page pa + lane, and behind the last
@@ -481,15 +487,16 @@ __global__ void __launch_bounds__(kMoveThreads, 1024 / kMoveThreads) evict_move_
         now = stays ? fmaxf(own, most) : most > 0.0f ? most : own;
         again = stays && now != own;
       }
-      for (unsigned pages = __ballot_sync(0xffffffffu, again); pages != 0; pages &= pages - 1) {
-        const int pg = __ffs(pages) - 1, blk = __shfl_sync(0xffffffffu, own_blk, pg);
+      const unsigned pages_again = __ballot_sync(0xffffffffu, again);
+      if (again) again_of[warp][__popc(pages_again & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+      __syncwarp();
+      for (int r0 = 0, rows = __popc(pages_again) << p.c.page_log2; r0 < rows; r0 += 32) {
+        const int pg = r0 + lane < rows ? again_of[warp][(r0 + lane) >> p.c.page_log2] : 0, r = (r0 + lane) & mask;
+        const int blk = __shfl_sync(0xffffffffu, own_blk, pg);
         const float f = __shfl_sync(0xffffffffu, own, pg) / __shfl_sync(0xffffffffu, now, pg);
-        for (int r0 = 0; r0 < P; r0 += 32) {
-          const int r = r0 + lane;
-          const bool mine = r < P && ((free_of[warp][pg][r0 >> 5] >> lane) & 1u) == 0;
-          uint8_t* const at = mine ? row_at(blk, r) : nullptr;
-          move_rows(at, at, f);
-        }
+        const bool mine = r0 + lane < rows && ((free_of[warp][pg][r >> 5] >> (r & 31)) & 1u) == 0;
+        uint8_t* const at = mine ? row_at(blk, r) : nullptr;
+        move_rows(at, at, f);
       }
       for (int h0 = ha; h0 < hb; h0 += 32 * kHeld) {
         if (hb - ha > 32 * kHeld) take(h0);          // (otherwise the lanes still hold them)
