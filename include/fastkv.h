@@ -317,7 +317,7 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
  * max_len of `prefix` and of `query` and total_len size the launch only.  A length beyond the table's room is cut to it, a page id
  * outside the pool reads page 0 instead, a cu_seqs that descends or leaves 0 .. batch leaves the outputs of prefixed sequences
  * unspecified; all are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
- * At most 1024 prefixes and 128 query heads per KV head.
+ * At most 1024 prefixes, 2^30 entries a row of their table and 128 query heads per KV head.
  * workspace: >= fastkv_prefix_attn_workspace_bytes, 256-byte aligned; not shared by calls that may overlap.
  */
 typedef struct fastkv_prefix {
@@ -347,7 +347,8 @@ int fastkv_prefix_attn(const fastkv_paged_cache* cache, const fastkv_prefix* pre
  * a weight, NaN and infinities included.  Products, exponentials and sums in fp32, in a fixed order.
  * max_len and total_len size the launch, as in fastkv_paged_attn.  A length beyond the block table's room or weights_stride is cut
  * to it, a page id outside the pool reads page 0 instead; both are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which
- * this call does not clear.  workspace: 256 bytes (the header), 256-byte aligned.
+ * this call does not clear.  weights_stride at most 2^30, batch * n_kv_heads at most 65535.  workspace: 256 bytes (the header),
+ * 256-byte aligned.
  */
 int fastkv_paged_weights(const fastkv_paged_cache* cache, const fastkv_query* query, const int32_t* lens, const void* q,
                          const float* lse, float decay, float* weights, int64_t weights_stride, void* workspace,
@@ -369,7 +370,7 @@ int fastkv_paged_weights(const fastkv_paged_cache* cache, const fastkv_query* qu
  * All pages a sequence of the call holds belong to it alone if it is cut.  A length below 0 or beyond max_len, stride or the block
  * table's room leaves the sequence as it is, new_lens[b] = lens[b] and nothing written to new_weights and new_ids; a page id
  * outside the pool is never dereferenced, rows that would be read from or written to it are not moved.  Both are reported in the
- * status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.
+ * status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.  stride at most 2^30, batch * n_kv_heads at most 65535.
  * workspace: >= fastkv_paged_evict_workspace_bytes, 256-byte aligned; not shared by calls that may overlap.
  */
 typedef struct fastkv_eviction {

@@ -1055,8 +1055,9 @@ int check_prefix(const fastkv_paged_cache* c, const fastkv_prefix* x, const fast
   if (!x->table || !x->lens) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: the prefix's table and lens are required");
   if (x->n_prefixes > 1 && x->cu_seqs == nullptr) return fail(FASTKV_ERR_INVALID_ARG, "prefix_attn: cu_seqs is required with more than one prefix");
   if (x->n_prefixes > kMaxPrefixes) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than %d prefixes", kMaxPrefixes);
-  if (static_cast<long long>(x->max_pages) * c->page_size > 0x7fffffffLL)
-    return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: a row of the prefixes' table holds more than 2^31 - 1 entries");
+  // (pages are looked up two chunks ahead, in 32 bits)
+  if (static_cast<long long>(x->max_pages) * c->page_size > (1ll << 30))
+    return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: a row of the prefixes' table holds more than 2^30 entries");
   const int G = q->n_q_heads / c->n_kv_heads;
   if (G > 128) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than 128 query heads per KV head");
   if (c->n_kv_heads > 65535) return fail(FASTKV_ERR_UNSUPPORTED, "prefix_attn: more than 65535 KV heads");
@@ -1163,7 +1164,8 @@ bool overlap(const void* a, const void* b, unsigned long long bytes) {
 // fp32 or int32 rows for every (sequence, KV head)
 int check_entry_rows(const char* call, const fastkv_paged_cache& c, int64_t stride) {
   if (stride < 1) return fail(FASTKV_ERR_INVALID_ARG, "%s: the stride of the weights must be >= 1", call);
-  if (stride > (1ll << 31)) return fail(FASTKV_ERR_UNSUPPORTED, "%s: weights of more than 2^31 entries a row", call);
+  // (what a unit of work has in front of or behind a row's last entry is counted in 32 bits, too)
+  if (stride > (1ll << 30)) return fail(FASTKV_ERR_UNSUPPORTED, "%s: weights of more than 2^30 entries a row", call);
   if (static_cast<long long>(c.batch) * c.n_kv_heads > 65535)
     return fail(FASTKV_ERR_UNSUPPORTED, "%s: more than 65535 (sequence, KV head) pairs", call);
   return FASTKV_OK;

@@ -34,6 +34,15 @@ def test_weights_refuses():
         assert weights_call(**kw) == B.ERR_WORKSPACE, kw
 
 
+def test_rows_of_entries_end_well_before_32_bits():
+    """A length is cut to the row, and a warp's first entry of the next unit has to be a positive number still."""
+    for call in (weights_call, evict_call):
+        assert call(stride=(1 << 30) + 1, nbytes=0) == B.ERR_UNSUPPORTED
+    assert weights_call(stride=1 << 30, nbytes=0) == B.ERR_WORKSPACE
+    far = dict(weights=1 << 40, ids=2 << 40, new_weights=3 << 40, new_ids=4 << 40)
+    assert evict_call(stride=1 << 30, nbytes=0, **far) == B.ERR_WORKSPACE
+
+
 def evict_call(c=None, ev=None, lens=0x1000, weights=0x10000, ids=0x20000, stride=64, new_weights=0x30000, new_ids=0x40000, new_lens=0x2000, ws=0x100000,
                nbytes=1 << 20):
     ev = ev or B.make_eviction(keep=16, max_len=64)

@@ -49,6 +49,14 @@ def test_refusals():
     assert B._load().fastkv_prefix_attn_workspace_bytes(c, x, q, None) == B.ERR_INVALID_ARG
 
 
+def test_rows_of_the_table_end_well_before_32_bits():
+    """Pages are looked up two chunks ahead: the entry's number has to stay positive."""
+    c = plain(n_kv_heads=2)
+    most = (1 << 30) // c.page_size
+    assert call(c=c, x=prefix(max_pages=most + 1), nbytes=0) == B.ERR_UNSUPPORTED
+    assert call(c=c, x=prefix(max_pages=most), nbytes=0) == B.ERR_WORKSPACE
+
+
 def test_workspace_holds_every_piece():
     """At most one piece for every pair of row tiles and CTA boundary, whatever the groups."""
     rng = random.Random(1)
