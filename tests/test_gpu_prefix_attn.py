@@ -268,3 +268,51 @@ def test_a_wait_that_runs_out(fmt, batch):
         out, lse, ws = call(sh, q)
         assert B.fastkv_device_status(ws) == (0, 0)
         check(sh, q, out, lse, rows=[(0, 0), (batch - 1, 0)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch,T", [(60, 4), (40, 4), (50, 2), (32, 1)])
+def test_merge_by_one_to_eight_warps(fmt, batch, T):
+    """Rows for every number of warps that share a row's pieces out, over prefixes of very different lengths: CTAs that end inside what a
+    unit counts for besides its chunks, units of one chunk, a prefix without entries and one without sequences."""
+    rng = np.random.default_rng(batch)
+    lens = [int(x) for x in rng.integers(T, 60, batch)]
+    cu = [1, 6, 7, 7 + batch // 6, batch // 2, batch // 2, batch - 2]
+    rows = [(b, int(rng.integers(T))) for b in sorted({0, 1, 5, 6, 7, batch // 2 - 1, batch // 2, batch - 3, batch - 1})]
+    run(fmt, [3000, 1, 5000, 0, 129, 2000], lens, 16, 32, 8, 128, T, cu=cu, seed=batch, rows=rows)
+    run(fmt, [3000, 1, 5000, 0, 129, 2000], lens, 32, 16, 8, 64, T, cu=cu, seed=batch, rows=rows)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_one_prefix_for_some_of_the_sequences(fmt):
+    run(fmt, [700], [9, 3, 30, 1, 17], 16, 8, 2, 128, 2, cu=[1, 4])
+    run(fmt, [40000], [9, 3, 30, 1, 17], 64, 8, 2, 128, 1, cu=[2, 5])
+    run(fmt, [700], [9, 3], 16, 8, 2, 64, 1, cu=[1, 1])
+
+
+@pytest.mark.parametrize("batch", [3, 60])
+def test_nan_and_infinite_keys_of_every_column(batch):
+    """Two row tiles share an SM (or one has it): whichever way a weight's exponential is taken, a NaN key reaches every output, a key whose
+    logits are -infinity none, one of +infinity makes its row NaN."""
+    for col in (0, 1, 2, 3, 5, 6, 7, 62, 63, 64, 100, 127, 130):
+        sh = Shared("bf16", [131], [2] * batch, 16, 1, 64, col)
+        q = torch.ones(batch, 1, 4, 64, device="cuda", dtype=torch.bfloat16)
+        page, row = sh.ptable[0, col // 16].long(), col % 16
+        keep = sh.pools.k[page, 0, row].clone()
+        for value in (float("nan"), -math.inf, math.inf):
+            sh.pools.k[page, 0, row] = keep
+            sh.pools.k[page, 0, row, 0] = value
+            out, lse, ws = call(sh, q)
+            assert B.fastkv_device_status(ws) == (0, 0)
+            if value == -math.inf:
+                without = sh.pools.k64[0].copy()
+                without[col, 0] = -1e6                    # (weighs nothing either)
+                k = np.concatenate([without, sh.pools.k64[1]])
+                v = np.concatenate([sh.pools.v64[0], sh.pools.v64[1]])
+                want, want_lse, mass, size = attention(q[0, 0].double().cpu().numpy(), np.delete(k, col, 0), np.delete(v, col, 0), 132, 0.125)
+                rel = 64 * 2.0 ** -23 * size + 2.0 ** -20
+                got = out[0, 0].double().cpu().numpy()
+                assert np.all(np.abs(got - want) <= 2.0 ** -8 * (mass + np.abs(want)) * 1.01 + 2 * rel[:, None] * mass)
+                assert np.all(np.abs(lse[0, 0].double().cpu().numpy() - want_lse) <= rel + 2.0 ** -21 * (np.abs(want_lse) + 1))
+            else:
+                assert torch.isnan(out).all() and torch.isnan(lse).all()
