@@ -1189,7 +1189,8 @@ int fastkv_paged_weights(const fastkv_paged_cache* cache, const fastkv_query* qu
   p.c = paged_view(c);
   p.n_q_heads = query->n_q_heads; p.group = query->n_q_heads / c.n_kv_heads; p.q_len = query->q_len; p.rows = p.group * p.q_len;
   p.scale = softmax_scale_of(c, *query); p.decay = decay;
-  p.total_len = query->total_len > 0 ? query->total_len : static_cast<long long>(c.batch) * query->max_len;
+  // (a row has no more than 2^30 entries, whatever the caller's bound: the launch's sizes stay within 64 bits)
+  p.total_len = std::min<long long>(query->total_len > 0 ? query->total_len : static_cast<long long>(c.batch) * query->max_len, static_cast<long long>(c.batch) << 30);
   p.lens = lens; p.q = static_cast<const uint16_t*>(q); p.lse = lse; p.weights = weights; p.stride = weights_stride;
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
   cudaError_t e;

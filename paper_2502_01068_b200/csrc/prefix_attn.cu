@@ -59,7 +59,7 @@ struct PrefixCfg {
   static constexpr int kWarps = kCtrlWarps + 2 * kSoftmaxWarps + (kE4M3 ? kWideWarps : 0);
   static constexpr int kThreads = 32 * kWarps;
   // behind the tiles: the scan of the prefixes, rows' shifts, pages' scales, barriers
-  static constexpr int kScanBytes = 512, kExtra = kScanBytes + 2 * kTile + 256 + 896;
+  static constexpr int kScanBytes = 512, kExtra = kScanBytes + 2 * kTile + 512 + 896;
   static constexpr int kSmem = (kQTiles + kVTiles) * kTileBytes + kKTiles * kKBytes + (kE4M3 ? kRaw * kRawBytes : 0) + kExtra;
   static_assert(kWarps <= 32 && kSmem <= 232448, "shared memory of a CTA");
   // 8-bit pages: the launch's 96 registers a thread go 40 to the control warps, 120 to the softmax warps and 96 to the widening ones.
@@ -73,8 +73,9 @@ struct PrefixCfg {
 // segment together, when all earlier chunks have been used, and the eighth chunk behind one is not loaded before the softmax has it
 // behind itself (the fourth may be).
 constexpr int kBars = 8;
-// K's scales of a chunk's pages: the softmax may still read a chunk's when the fourth behind it is loaded, never when the eighth is.
-constexpr int kScaleSlots = 8;
+// Scales of a chunk's pages, K's and behind them V's: the softmax may still read a chunk's when the fourth behind it is loaded, never when
+// the eighth is.
+constexpr int kScaleSlots = 8, kScales = 16;
 
 // What the roles have to know of a segment; the loader of Q leaves it with Q.
 struct Brief {
@@ -181,24 +182,22 @@ __device__ __forceinline__ uint4 widen8_half(uint32_t a, uint32_t b) { return ma
 
 // Codes as bf16 times a power of two, without conversions (two of them for a pair, with the rounding back to bf16, took twice as long):
 // a code's bits moved to bf16's places are the code times 2^-120, subnormals included, and a bf16 product brings it back, exactly.
-// Only NaN (all ones, what 480 would be) needs to be told apart: its excess over 464 stays behind in `odd`.
+// Only NaN (all ones, what 480 would be) needs to be told apart: the largest of the bits stays behind in `most`.
 __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t widen2_bf16(uint32_t em, uint32_t sign, uint32_t up, uint32_t times, uint32_t& odd) {
-  uint32_t over;
-  asm("fma.rn.relu.bf16x2 %0, %1, %2, %3;" : "=r"(over) : "r"(em), "r"(0x7b807b80u), "r"(0xc3e8c3e8u));       // em * 2^120 - 464
-  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(odd), "r"(over));
+__device__ __forceinline__ uint32_t widen2_bf16(uint32_t em, uint32_t sign, uint32_t up, uint32_t times, uint32_t& most) {
+  most = __vmaxu2(most, em);
   const uint32_t r = bf16x2_mul((sign & 0x80008000u) | em, up);
   return times == 0x3f803f80u ? r : bf16x2_mul(r, times);
 }
 // Four codes come out in the order 0, 2, 1, 3: even ones and odd ones are two masks of the word.
-__device__ __forceinline__ uint4 widen8_bf16(uint32_t a, uint32_t b, uint32_t up, uint32_t times, uint32_t& odd) {
+__device__ __forceinline__ uint4 widen8_bf16(uint32_t a, uint32_t b, uint32_t up, uint32_t times, uint32_t& most) {
   constexpr uint32_t kMask = 0x07f007f0u;
-  return make_uint4(widen2_bf16((a << 4) & kMask, a << 8, up, times, odd), widen2_bf16((a >> 4) & kMask, a, up, times, odd),
-                    widen2_bf16((b << 4) & kMask, b << 8, up, times, odd), widen2_bf16((b >> 4) & kMask, b, up, times, odd));
+  return make_uint4(widen2_bf16((a << 4) & kMask, a << 8, up, times, most), widen2_bf16((a >> 4) & kMask, a, up, times, most),
+                    widen2_bf16((b << 4) & kMask, b << 8, up, times, most), widen2_bf16((b >> 4) & kMask, b, up, times, most));
 }
 // The same, in the same order, by conversions, which know NaN.
 __device__ __forceinline__ uint4 widen8_any(uint32_t a, uint32_t b, float s) {
@@ -274,13 +273,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   uint8_t* const sQ = sK + NK * Cfg::kKBytes;             // one or two row tiles
   uint8_t* const sV = sQ + Cfg::kQTiles * Cfg::kTileBytes;
   uint8_t* const sRaw = sV + NV * Cfg::kTileBytes;
-  // 8-bit pages: the power of two that a row of Q was shifted by, and K's scales of a chunk's pages
+  // 8-bit pages: the power of two that a row of Q was shifted by, and the scales of a chunk's pages
   long long* const scan = reinterpret_cast<long long*>(sRaw + (kE4M3 ? NR * Cfg::kRawBytes : 0));
   int8_t* const row_shift = reinterpret_cast<int8_t*>(scan) + Cfg::kScanBytes;                    // [tile][row]
-  float* const page_scale = reinterpret_cast<float*>(row_shift + 2 * kTile);                      // [kScaleSlots][8]
+  float* const page_scale = reinterpret_cast<float*>(row_shift + 2 * kTile);                      // [kScaleSlots][kScales]
   using Barriers = PrefixBarriers<NR>;
   static_assert(sizeof(Barriers) <= 896, "what is set aside for the barriers");
-  Barriers* const bars = reinterpret_cast<Barriers*>(page_scale + kScaleSlots * 8);
+  Barriers* const bars = reinterpret_cast<Barriers*>(page_scale + kScaleSlots * kScales);
 
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const int Hkv = p.c.n_kv_heads, G = p.group;
@@ -498,13 +497,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       // (8-bit pages: page, then scale, a chain of two loads; kCols is 1 and lane = page)
       int blk = block_of(page_of(s.group, s.of.len, s.c0, lane / kCols), s.g);
       int next = page_of(s.group, s.of.len, s.c0 + 1, lane / kCols);
-      float scale = kE4M3 && blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f;
+      float scale = kE4M3 && blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f, scale_v = kE4M3 && blk >= 0 ? __ldcg(p.c.v_scales + blk) : 0.0f;
       for (int c = s.c0; c < s.c1 && ok; ++c, ++n) {
         const int bar = n % kBars;
         if (n >= NK) ok = wait(&bars->k_empty[(n - NK) % kBars], (n - NK) / kBars & 1);
         if (!ok) break;
         if (kE4M3) {
-          if (lane < 8) page_scale[n % kScaleSlots * 8 + lane] = scale;
+          if (lane < 8) {
+            page_scale[n % kScaleSlots * kScales + lane] = scale;
+            page_scale[n % kScaleSlots * kScales + 8 + lane] = scale_v;
+          }
           __syncwarp();
         }
         bring(&tmap_k, sK + n % NK * Cfg::kKBytes, &bars->k_full[bar], blk);
@@ -512,7 +514,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const int blk_v = blk;
         blk = block_of(next, s.g);
         next = page_of(s.group, s.of.len, c + 2, lane / kCols);
-        scale = kE4M3 && blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f;
+        if (kE4M3) {
+          scale = blk >= 0 ? __ldcg(p.c.k_scales + blk) : 0.0f;
+          scale_v = blk >= 0 ? __ldcg(p.c.v_scales + blk) : 0.0f;
+        }
         if constexpr (kE4M3) {
           const int slot = n % NR;
           if (n >= NR) ok = wait(&bars->raw_empty[slot], (n / NR - 1) & 1);
@@ -776,7 +781,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             // positive, so that masked logits stay -infinity
-            if (kE4M3) f[c * 2 + z] = fmaxf(by_row * page_scale[n % kScaleSlots * 8 + ((h * kStep + c * 32 + z * 16) >> p.c.page_log2)], 1.17549435e-38f);
+            if (kE4M3) f[c * 2 + z] = fmaxf(by_row * page_scale[n % kScaleSlots * kScales + ((h * kStep + c * 32 + z * 16) >> p.c.page_log2)], 1.17549435e-38f);
             float mx[2] = {v[c][z * 16], v[c][z * 16 + 1]};
 #pragma unroll
             for (int e = 2; e < 16; e += 2) { mx[0] = fmaxf(mx[0], v[c][z * 16 + e]); mx[1] = fmaxf(mx[1], v[c][z * 16 + e + 1]); }
@@ -872,7 +877,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         return __all_sync(0xffffffffu, mbar_wait_nap(bar, parity, abort_flag, p.hdr, site, limit));
       };
       const int first = w * (kTile / kWideWarps);         // the warp's 16 rows of every tile of V
-      auto scale_in = [&](int blk) -> float { return blk < 0 ? 0.0f : __ldcg(p.c.v_scales + blk); };
       constexpr int kPieces = D / 16;                     // 16-byte pieces of a row of codes
       constexpr int kRowsAt = 32 / kPieces;               // rows of a warp's step
       // Eight lanes (what shared memory serves at a time) take four pieces of one column block of two neighbouring rows: the
@@ -884,9 +888,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (!ok) break;
         const Brief br = bars->brief[segs & 1];
         if (br.chunks == 0) break;
-        // (page, then scale: a chain of two loads, each started a chunk before the other needs it)
-        float next = scale_in(block_of(page_of(br.group, br.len, br.c0, lane), br.g));
-        int next_page = page_of(br.group, br.len, br.c0 + 1, lane);
         // ---- Q: two threads per row, in place.  After a power-of-two shift that brings the row's largest element to [2^7, 2^8), an element is
         // the sum of its nearest e4m3 value and the e4m3 value nearest to the rest: exact down to 2^-9 of the largest (8 bits are 4 and 4),
         // and what is smaller is off by at most 2^-17 of the largest. ----
@@ -941,9 +942,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (lane == 0) mbar_arrive(&bars->q_wide);
         ++segs;
         for (int c = br.c0; c < br.c0 + br.chunks && ok; ++c, ++n) {
-          const float sc = next;
-          next = scale_in(block_of(next_page, br.g));
-          next_page = page_of(br.group, br.len, c + 2, lane);
           const int have = br.len - c * kTile;
           const int slot = n % NR, gone = n - NV;         // gone: the chunk whose tile this one takes
           ok = wait(&bars->raw_full[slot], (n / NR) & 1, SITE_PREFIX_RAW);
@@ -958,19 +956,19 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             *reinterpret_cast<uint4*>(tile + r * 128 + (((2 * c4 + 1) ^ (r & 7)) << 4)) = b;
           };
           constexpr int kSteps = kTile / kWideWarps / kRowsAt;
-          const float f = __shfl_sync(0xffffffffu, sc, first >> p.c.page_log2);        // the warp's 16 rows are one page's
+          const float f = page_scale[n % kScaleSlots * kScales + 8 + (first >> p.c.page_log2)];         // the warp's 16 rows are one page's
           // 2^120 f in one factor, unless that is too large for one
           const bool two = f > 128.0f;
           const uint32_t up = __byte_perm(__float_as_uint(two ? 1.329227995784916e36f : f * 1.329227995784916e36f), 0, 0x3232);
           const uint32_t times = __byte_perm(__float_as_uint(two ? f : 1.0f), 0, 0x3232);
-          uint32_t odd = 0;
-#pragma unroll 2
-          for (int y = 0; y < kSteps; ++y) {
-            const uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
-            put(y, widen8_bf16(q.x, q.y, up, times, odd), widen8_bf16(q.z, q.w, up, times, odd));
-          }
+          uint32_t most = 0;
+          uint4 q[kSteps];
+#pragma unroll
+          for (int y = 0; y < kSteps; ++y) q[y] = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);
+#pragma unroll
+          for (int y = 0; y < kSteps; ++y) put(y, widen8_bf16(q[y].x, q[y].y, up, times, most), widen8_bf16(q[y].z, q[y].w, up, times, most));
           // NaN among the codes, or the prefix's end among the rows: those again
-          if (__any_sync(0xffffffffu, (odd & 0x7fff7fffu) != 0) || have < kTile) {
+          if (__any_sync(0xffffffffu, (most & 0xffffu) == 0x7f0u || most >> 16 == 0x7f0u) || have < kTile) {
 #pragma unroll 1
             for (int y = 0; y < kSteps; ++y) {
               uint4 q = *reinterpret_cast<const uint4*>(src + y * kRowsAt * D);

@@ -163,3 +163,19 @@ def test_same_bits_twice_on_a_stream_and_from_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("pairs", [1, 2, 4])
+@pytest.mark.parametrize("Hq,Hkv,T", [(4, 2, 1), (6, 2, 5), (6, 2, 9)])
+def test_steps_of_a_unit(fmt, d, pairs, Hq, Hkv, T):
+    """One, two and four pairs of steps a unit (the bound on the lengths decides), with ends in every step of them; rows of one tile of
+    eight, two and more."""
+    lens = [1, 31, 32, 33, 65, 127, 128, 129, 255, 257, 0, 511, 513, 700, 1023, 1500, 2049]
+    run(fmt, lens, 16, Hq, Hkv, d, T, decay=0.5, seed=T, total_len={1: 10 ** 4, 2: 3 * 1776 * 256 // Hkv, 4: 10 ** 8}[pairs] * (2 if d == 64 else 1))
+
+
+def test_a_bound_beyond_everything():
+    run("bf16", [300, 20], 16, 4, 2, 64, seed=1, total_len=2 ** 63 - 1)
+    run("e4m3", [300, 20], 16, 4, 2, 128, seed=1, total_len=2 ** 62)
