@@ -43,7 +43,9 @@ constexpr int kCtrlWarps = 4;                  // loader of K and V, issuer of t
 constexpr int kSoftmaxWarps = 4;               // per tile
 constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two terms, V to bf16
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
-constexpr float kSlackLog2 = 8.0f;
+// A row's reference moves (which rescales its output and keeps its warp for 2000 cycles) when a logit is this far above it: weights are at
+// most 2^16 then, whatever rounds them is relative.  (8: 100 us, 16: 96, 24: 96, 8 x 131072 in 8 bits.)
+constexpr float kSlackLog2 = 16.0f;
 
 // kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
 template <int D, bool kE4M3, bool kOne>
