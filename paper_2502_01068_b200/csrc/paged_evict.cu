@@ -14,6 +14,12 @@
 // round reads lies behind everything an earlier one wrote, because the window moves down.
 // Weights and ids go to buffers of their own, so that the call may be given again, and a reader may still hold the old ones.
 //
+// What bounds it: latency.  The bytes of a cut (2304 entries to 2048: 256 rows of K and V per KV head and the weights) are few, and each row
+// is found by loads that wait for one another: slot, source, page, (scale,) row.  One B200, 8 KV heads of 128: one sequence of 2304 15 us
+// (ranking 5, an empty launch 2 each), 131072 to 13107 51 us (ranking 20: 64 CTAs, 4 us until the weights are there, 2 a digit; moving
+// 25 for 102 MB, 62 % of a copy), 64 of 2304 in 8 bits 39 us and 4 of 26214 to 13107 70 us (moving 28 and 45: rows that stay in a page whose
+// scale grows are read and written, too).  More warps on an SM (40 registers) gained nothing in 8 bits: 70 and 73 us.
+//
 // 8-bit pages: a page's entries share a scale; a page that receives entries takes the largest scale of the pages that its entries
 // come from (those that stay among them), and codes from smaller scales are encoded again, code * old / new, rounded to nearest even:
 // powers of two, so only codes that fall below 2^-6 lose bits.

@@ -10,18 +10,27 @@
 //
 // A CTA's roles:
 //   loaders    one warp: K and V tiles page by page (TMA, a box per page and 64 columns) into their rings, ahead into the next
-//              segment; one warp: a segment's Q, as soon as the one before is through with it;
-//   widening   (8-bit pages) eight warps: codes from the raw ring to 16-bit tiles in the layout that TMA would write.  K to fp16, one
-//              instruction for two codes, K's scale going onto the logits; V to bf16, times the page's scale, so that the scales of
-//              pages far apart cost a weight none of its bits.  Both exact;
-//   issuers    one warp per row tile: per chunk O += P V of the chunk before, then S = Q K^T (tcgen05.mma 128 x 128 x d, fp32 in
-//              tensor memory), in that order from one thread, so that S may overwrite the P that the contraction before has read;
-//   softmax    four warps per row tile, a thread per row, which holds most of the chunk's 128 logits in registers: online softmax in log2
-//              units with a lazily raised reference; P goes back, in bf16, into the first half of the row's S columns.
+//              segment, with the pages' scales; one warp: a segment's Q, as soon as the one before is through with it;
+//   widening   (8-bit pages) eight warps: Q into two e4m3 terms, in place; V's codes from their ring to bf16 times the page's scale, so
+//              that the scales of pages far apart cost a weight none of its bits (exact);
+//   issuers    one warp per row tile: per step of 64 entries O += P V of the chunk before, then S = Q K^T into the buffer that P is read
+//              from (tcgen05.mma 128 x 64 x d and 128 x d x 64, fp32 in tensor memory), in that order from one thread;
+//   softmax    four warps per row tile, a thread per row, which holds a step's 64 logits in registers: online softmax in log2 units with a
+//              lazily raised reference; P goes back, in bf16, into the first half of the row's S columns.
+// K of 8-bit pages is multiplied as it is stored (kind::f8f6f4), its scale goes onto the logits: widened like V it would cost the same
+// 1300 cycles a chunk again (8 x 131072: 115 us, as stored 95).
 // With more than 128 rows the two tiles hold different rows and take every chunk, their contractions alternating.  With 128 or fewer
 // both work on the same rows and take every other chunk: one's softmax runs under the other's contractions.  With 64 or fewer the second
 // tile's rows are its last 64 (its descriptor of Q starts 64 rows early), so that the two tiles' softmax warps are on different schedulers.
-// Tensor memory (512 columns): S (and P inside it) of tile A at 0, of tile B at 128; O of A at 256, of B at 256 + d.
+// Tensor memory (512 columns): S (and P inside it) of tile A at 0, of tile B at 128, two buffers of 64 each; O of A at 256, of B at 256 + d.
+//
+// What bounds it (32 query heads over 8 KV heads of 128; the kernel inside a call, one B200).  64 sequences over 32768 bf16 entries, 256 rows a
+// KV head: 38 us for 134 MB and 34 GFLOP (20.5 and 20.9 us at the rates of a copy and of a large product); a step takes 1640 cycles, of
+// which each softmax warp is busy for 1350 (the tensor pipe is active for 48 % of the kernel; 128 entries a step and one buffer of S, so that
+// softmax and products wait for one another, took 50 us when this took 43).  8 x 131072 in 8 bits, 32 rows: 80 us
+// for 269 MB: widening a chunk of V (1300 cycles) and a step's softmax by one warp (1000, twice a chunk and tile) are as long as each other;
+// four copies of the rows in a tile with a quarter of the entries each brought 6 us and cost the merge 10, a third tile of V nothing.
+// Short shares: 2 us until the first copy (lengths, barriers, tensor memory), 2 us for a segment's output.
 //
 // P is rounded to bf16 (2^-9 of each weight, of either sign): that is what the output is rounded to; the row sums take it unrounded.
 // Logits, exponentials, sums, outputs and their merge are fp32.
