@@ -121,6 +121,7 @@ cudaError_t launch_paged_weights(PagedWeightsParams& p, int head_dim, bool e4m3,
 struct EvictParams {
   PagedView c;
   int keep, limit, window, max_len, row_bytes;
+  int round_rows, stage_bytes;           // rows of a CTA's round, and what they (or the lists before them) take; filled in by the launcher
   const int* lens;
   int* new_lens;
   const float* weights;       // [B][Hkv][stride], as ids, new_weights and new_ids

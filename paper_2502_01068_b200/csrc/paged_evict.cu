@@ -17,8 +17,9 @@
 // What bounds it: latency.  The bytes of a cut (2304 entries to 2048: 256 rows of K and V per KV head and the weights) are few, and each row
 // is found by loads that wait for one another: slot, source, page, (scale,) row.  One B200, 8 KV heads of 128: one sequence of 2304 15 us
 // (ranking 5, an empty launch 2 each), 131072 to 13107 51 us (ranking 20: 64 CTAs, 4 us until the weights are there, 2 a digit; moving
-// 25 for 102 MB, 62 % of a copy), 64 of 2304 in 8 bits 39 us and 4 of 26214 to 13107 70 us (moving 28 and 45: rows that stay in a page whose
-// scale grows are read and written, too).  More warps on an SM (40 registers) gained nothing in 8 bits: 70 and 73 us.
+// 25 for 102 MB, 62 % of a copy), 64 of 2304 in 8 bits 39 us and 4 of 26214 to 13107 65 us (moving 28 and 40: rows that stay in a page whose
+// scale grows are read and written, too).  More warps on an SM (48 or 40 registers a thread) gained nothing in 8 bits: 42 and 41 us, 68 and 74
+// (39 and 69 at the time).
 //
 // 8-bit pages: a page's entries share a scale; a page that receives entries takes the largest scale of the pages that its entries
 // come from (those that stay among them), and codes from smaller scales are encoded again, code * old / new, rounded to nearest even:
@@ -286,7 +287,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_plan_kernel(con
 
 namespace {
 
-constexpr int kRoundRows = 128;            // rows of a round that a CTA holds in shared memory: one page at most, or several
+// Rows of a round that a CTA holds in shared memory are a multiple of kRowsUnit, so that pages are whole: as many as a window of the call
+// needs for one round, up to kStageMost bytes (one CTA an SM, or three).  A round waits for reads, a barrier of the cluster and writes,
+// whatever its size: 25647 entries cut to their last 17173, in 8 bits, took 111 us in 17 rounds of 128 rows a CTA, in two rounds 46.
+constexpr int kRowsUnit = 128;
+template <int THREADS> constexpr int kStageMost = THREADS >= 1024 ? 160 << 10 : 64 << 10;
 constexpr int kHeld = 3;                    // 8-bit pages: free slots that a lane holds at a time (2: 75 us for four of 26214, 3: 72)
 constexpr int kOwnPages = 16;              // 8-bit pages that a warp takes at a time, at most
 
@@ -318,6 +323,12 @@ __device__ __forceinline__ uint4 recode16(uint4 v, float f) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// 16 bytes from memory to shared memory, on their way until copies_wait().
+__device__ __forceinline__ void copy16_async(uint8_t* to, const uint8_t* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 }  // namespace
 
 // blockIdx.y: K, V, or weights and ids; blockIdx.z: (sequence, KV head); blockIdx.x: CTA of the cluster.
@@ -326,10 +337,10 @@ __global__ void __launch_bounds__(kMoveThreads, 1024 / kMoveThreads) evict_move_
   constexpr int kMoveWarps = kMoveThreads / 32;
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int kLanesPerRow = kRowBytes / 16, kRowsPerWarp = 32 / kLanesPerRow;
-  // rows of a round; before the rounds, the warps' lists of moves
-  constexpr int kStageBytes = kRoundRows * kRowBytes, kListBytes = kMoveWarps * 32 * 16;
-  __shared__ __align__(16) uint8_t stage[kStageBytes > kListBytes ? kStageBytes : kListBytes];
-  __shared__ float scale_from[kRoundRows], page_scale[kRoundRows / 16];
+  // rows of a round (before the rounds, the warps' lists of moves); their scales, or -1; the new scales of their pages
+  extern __shared__ __align__(16) uint8_t stage[];
+  float* const scale_from = reinterpret_cast<float*>(stage + p.stage_bytes);
+  float* const page_scale = scale_from + p.round_rows;
   const int CL = gridDim.x, rank = blockIdx.x, kind = blockIdx.y;
   const int b = blockIdx.z / p.c.n_kv_heads, g = blockIdx.z - b * p.c.n_kv_heads;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -522,36 +533,55 @@ __global__ void __launch_bounds__(kMoveThreads, 1024 / kMoveThreads) evict_move_
     }
   }
 
-  // ---- the pages from m on, in rounds of kRoundRows slots a CTA ----
+  // ---- the pages from m on, in rounds of some slots a CTA: a lane looks a row up, the warp copies it ----
   __syncthreads();                                   // the lists have been read
-  for (int r0 = m0; r0 < p.keep; r0 += CL * kRoundRows) {
-    const int j0 = r0 + rank * kRoundRows, rows = max(0, min(kRoundRows, p.keep - j0));
-    constexpr int kGroups = kMoveThreads / kLanesPerRow;
-    const int grp = tid / kLanesPerRow;
-    for (int i = grp; i < rows; i += kGroups) {
-      const int o = origin(j0 + i), blk = block_at(o);
-      if (blk >= 0) *reinterpret_cast<uint4*>(stage + i * kRowBytes + piece * 16) = *reinterpret_cast<const uint4*>(row_at(blk, o) + piece * 16);
-      if (piece == 0) scale_from[i] = blk < 0 ? -1.0f : kE4M3 ? scales[blk] : 1.0f;      // -1: a row that is not to be had
+  const int R = p.round_rows;
+  for (int r0 = m0; r0 < p.keep; r0 += CL * R) {
+    const int j0 = r0 + rank * R, rows = max(0, min(R, p.keep - j0));
+    for (int i0 = warp * 32; i0 < rows; i0 += kMoveThreads) {
+      const int i = i0 + lane;
+      const uint8_t* from = nullptr;
+      if (i < rows) {
+        const int o = origin(j0 + i), blk = block_at(o);
+        if (blk >= 0) from = row_at(blk, o);
+        scale_from[i] = blk < 0 ? -1.0f : kE4M3 ? scales[blk] : 1.0f;        // -1: a row that is not to be had
+      }
+#pragma unroll
+      for (int r = 0; r < 32; r += kRowsPerWarp) {
+        const unsigned long long src = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), r + sub);
+        if (src != 0) copy16_async(stage + (i0 + r + sub) * kRowBytes + piece * 16, reinterpret_cast<const uint8_t*>(src) + piece * 16);
+      }
     }
+    copies_wait();
     __syncthreads();
     if (kE4M3) {
       // the largest scale of each page's rows (positive: their bits compare alike)
-      if (tid < kRoundRows / 16) page_scale[tid] = 0.0f;
+      for (int q = tid; q * 16 < rows; q += kMoveThreads) page_scale[q] = 0.0f;
       __syncthreads();
-      if (tid < rows) {
-        const float most = scale_from[tid];
-        if (most > 0.0f) atomicMax(reinterpret_cast<unsigned*>(&page_scale[tid >> p.c.page_log2]), __float_as_uint(most));
+      for (int i = tid; i < rows; i += kMoveThreads) {
+        const float most = scale_from[i];
+        if (most > 0.0f) atomicMax(reinterpret_cast<unsigned*>(&page_scale[i >> p.c.page_log2]), __float_as_uint(most));
       }
     }
     cluster.sync();                                  // everybody has read the round
-    for (int i = grp; i < rows; i += kGroups) {
-      const int j = j0 + i;
-      if (scale_from[i] < 0.0f) continue;
-      const int blk = block_at(j);
-      if (blk < 0) continue;
-      uint4 v = *reinterpret_cast<const uint4*>(stage + i * kRowBytes + piece * 16);
-      if (kE4M3) v = recode16(v, scale_from[i] / page_scale[i >> p.c.page_log2]);
-      *reinterpret_cast<uint4*>(row_at(blk, j) + piece * 16) = v;
+    for (int i0 = warp * 32; i0 < rows; i0 += kMoveThreads) {
+      const int i = i0 + lane;
+      uint8_t* to = nullptr;
+      float f = 1.0f;
+      if (i < rows && scale_from[i] >= 0.0f) {
+        const int blk = block_at(j0 + i);
+        if (blk >= 0) to = row_at(blk, j0 + i);
+        if (kE4M3) f = scale_from[i] / page_scale[i >> p.c.page_log2];
+      }
+#pragma unroll
+      for (int r = 0; r < 32; r += kRowsPerWarp) {
+        const unsigned long long dst = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), r + sub);
+        const float by = kE4M3 ? __shfl_sync(0xffffffffu, f, r + sub) : 1.0f;
+        if (dst != 0) {
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + (i0 + r + sub) * kRowBytes + piece * 16);
+          *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dst) + piece * 16) = kE4M3 ? recode16(v, by) : v;
+        }
+      }
     }
     if (kE4M3) {
       for (int q = tid; q * P < rows; q += kMoveThreads) {
@@ -603,10 +633,26 @@ cudaError_t launch_evict_plan(const EvictParams& p, cudaStream_t stream) {
 namespace {
 
 template <bool kE4M3, int kRowBytes, int kThreads>
-cudaError_t launch_move_t(const EvictParams& p, int cl, cudaStream_t stream) {
+cudaError_t launch_move_t(EvictParams p, int cl, cudaStream_t stream) {
+  // the window and what of m's page lies below it
+  const long long rows = p.window + ((p.keep - p.window) & ((1 << p.c.page_log2) - 1)), unit = kRowsUnit;
+  const long long each = (rows + cl * unit - 1) / (cl * unit) * unit, most = kStageMost<kThreads> / kRowBytes / unit * unit;
+  p.round_rows = static_cast<int>(max(unit, min(each, most)));
+  p.stage_bytes = max(p.round_rows * kRowBytes, kThreads * 16);
+  constexpr int kMost = kStageMost<kThreads> + kStageMost<kThreads> / kRowBytes * 5;
+  static PerDeviceOnce configured;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (!configured.done(dev)) {
+    e = cudaFuncSetAttribute(evict_move_kernel<kE4M3, kRowBytes, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (e != cudaSuccess) return e;
+    configured.set(dev);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cl, 3, static_cast<unsigned>(p.c.batch * p.c.n_kv_heads));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = p.stage_bytes + p.round_rows * 5;         // (a scale a row, and one for 16 of them)
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -624,7 +670,7 @@ cudaError_t launch_move_r(const EvictParams& p, cudaStream_t stream) {
   // CTAs of a cluster: as many as keep all SMs busy with few pairs; where even eight leave SMs with one CTA or none, large ones
   const long long pairs = static_cast<long long>(p.c.batch) * p.c.n_kv_heads;
   int cl = 8;
-  while (cl > 1 && (pairs * 2 * cl > 4 * 148 || cl * kRoundRows >= 4 * p.keep)) cl /= 2;
+  while (cl > 1 && (pairs * 2 * cl > 4 * 148 || cl * kRowsUnit >= 4 * p.keep)) cl /= 2;
   if (cl == 8 && pairs * 2 * cl <= 148) return launch_move_t<kE4M3, kRowBytes, 1024>(p, cl, stream);
   return launch_move_t<kE4M3, kRowBytes, 256>(p, cl, stream);
 }
