@@ -188,3 +188,12 @@ def test_again_after_more_entries_and_from_a_graph():
         outs.append([t.clone() for t in (pools.k, pools.v, pools.ks, w2, w3)])
     for a, b in zip(*outs):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,keep,window", [([9000, 8000], 7000, 7000), ([9000], 7001, 6500), ([3000] * 30, 2500, 2500), ([700] * 40, 600, 599), ([12000], 11990, 11985)])
+def test_windows_of_several_rounds(fmt, d, lens, keep, window):
+    """Nothing but the window moves, or next to nothing: rounds of as many rows as shared memory holds, sources that overlap with what is
+    written (by 10 slots of a page, or by none), ends inside a round and a page."""
+    run(fmt, lens, keep, window, 32, 2, d, seed=keep)
