@@ -1009,18 +1009,28 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 }
 
 // Joins a query row's pieces and the attention over its own entries.  A block takes 32 rows (lane = row; the pieces hold columns by rows),
-// a warp 16 columns of them.  SPLIT: warps that share the pieces out and meet once in shared memory; 1: a warp has all of them, and the
+// a warp some columns of them.  SPLIT: warps that share the pieces out and meet once in shared memory; 1: a warp has all of them, and the
 // block every column.  All of it is latency: every load that can be is in flight before the first is used, the row's own entries are
 // what the sum starts from, and up to 32 prefixes are scanned without a barrier.
-constexpr int kMergeCols = 16, kMergeResident = 24;       // columns of a warp; warps on an SM
-template <int D, int SPLIT> constexpr int kMergeWarps = SPLIT == 1 ? D / kMergeCols : SPLIT;
+template <int D, int SPLIT>
+struct MergeCfg {
+  static constexpr int kCols = SPLIT > 8 ? 8 : 16;        // columns of a warp
+  static constexpr int kAhead = SPLIT > 8 ? 3 : 2;        // pieces whose loads are in flight
+  static constexpr int kWarps = SPLIT == 1 ? D / kCols : SPLIT;
+  static constexpr int kResident = SPLIT > 8 ? 32 : 24;   // warps on an SM
+};
 template <int D, bool kE4M3, int SPLIT>
-__global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / kMergeWarps<D, SPLIT>) prefix_merge_kernel(const PrefixParams p) {
-  constexpr int kWarps = kMergeWarps<D, SPLIT>, kMergeThreads = 32 * kWarps;
-  __shared__ float acc_of[SPLIT == 1 ? 1 : kWarps][32][kMergeCols + 1];
+__global__ void __launch_bounds__(32 * MergeCfg<D, SPLIT>::kWarps, MergeCfg<D, SPLIT>::kResident / MergeCfg<D, SPLIT>::kWarps)
+prefix_merge_kernel(const PrefixParams p) {
+  using Cfg = MergeCfg<D, SPLIT>;
+  constexpr int kWarps = Cfg::kWarps, kMergeThreads = 32 * kWarps, kMergeCols = Cfg::kCols;
+  // chunks and units of the prefixes before (more than 32 of them), later the warps' sums
+  constexpr int kSums = SPLIT == 1 ? 0 : kWarps * 32 * (kMergeCols + 1) * 4, kScan = kMaxPrefixes * 12;
+  __shared__ __align__(16) uint8_t space[kSums > kScan ? kSums : kScan];
+  auto acc_of = reinterpret_cast<float (*)[32][kMergeCols + 1]>(space);
+  long long* const chunk0 = reinterpret_cast<long long*>(space);
+  int* const unit0 = reinterpret_cast<int*>(chunk0 + kMaxPrefixes);
   __shared__ float2 ml_of[SPLIT == 1 ? 1 : kWarps][32];
-  __shared__ long long chunk0[kMaxPrefixes];              // chunks and units of the prefixes before (more than 32 of them)
-  __shared__ int unit0[kMaxPrefixes];
   __shared__ long long scratch[kWarps], scratch_u[kWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int Hkv = p.c.n_kv_heads, G = p.group, T = p.q_len, n = p.n_prefixes;
@@ -1105,6 +1115,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
     gr = group_of(p, lo);
     chunk_at = chunk0[lo];
     unit_at = unit0[lo];
+    __syncthreads();                                      // (the sums go there)
   }
   if (R < rows && total > 0) {
     const int in = token - gr.seq0 * T;
@@ -1143,7 +1154,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
     L = own == -INFINITY ? 0.0f : 1.0f;                   // (without entries its output is zeros)
   }
   const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D / 4) * p.tile_rows;
-  constexpr int kAhead = 2;
+  constexpr int kAhead = Cfg::kAhead;
   for (int s0 = sub; s0 < most; s0 += kAhead * SPLIT) {
     float2 v[kAhead];
     float o[kAhead][kMergeCols];
@@ -1192,9 +1203,9 @@ __global__ void __launch_bounds__(32 * kMergeWarps<D, SPLIT>, kMergeResident / k
     for (int i = 0; i < kMergeCols; ++i) acc_of[warp][lane][i] = acc[i];
     __syncthreads();
     // ---- now a thread for some columns of a row ----
-    constexpr int kMine = kMergeCols / SPLIT;
-    const int r = t / SPLIT, c = t % SPLIT * kMine, R2 = blockIdx.x * 32 + r;
-    if (R2 >= rows) return;
+    constexpr int kMine = SPLIT > 8 ? 2 : kMergeCols / SPLIT, kEach = kMergeCols / kMine;
+    const int r = t / kEach, c = t % kEach * kMine, R2 = blockIdx.x * 32 + r;
+    if (r >= 32 || R2 >= rows) return;
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < SPLIT; ++w) top = fmaxf(top, ml_of[w][r].x);
@@ -1253,20 +1264,25 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
   const long long rows = static_cast<long long>(p.c.batch) * p.q_len * p.group;
   cfg.dynamicSmemBytes = 0;
   // As many warps share a row's pieces out as one wave has room for: what a block does before its first load and behind its last is most
-  // of the time.  (Eight everywhere: 48 x 4 tokens, 1536 blocks in 3.5 waves, 16 us; rule: 8.7.)
-  const long long warps = (rows + 31) / 32 * p.c.n_kv_heads * (D / kMergeCols);
-  int split = 8;
-  while (split > 1 && warps * split > 148ll * kMergeResident) split /= 2;
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + 31) / 32), p.c.n_kv_heads, split == 1 ? 1 : D / kMergeCols);
+  // of the time.  (Eight everywhere: 48 x 4 tokens, 1536 blocks in 3.5 waves, 16 us; rule: 8.7.)  More than eight where a row has as many
+  // pieces (7 rows of one head over 66101 entries, 296 pieces a row: whole call 39 us with eight, 26 with 32).
+  const long long tokens = static_cast<long long>(p.c.batch) * p.q_len, row_blocks = (rows + 31) / 32 * p.c.n_kv_heads;
+  const long long units = p.c.n_kv_heads * max(static_cast<long long>(p.n_prefixes), (tokens + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens));
+  const long long pieces = (p.ctas / units + 1) * 2;      // of a row, two tiles each
   auto merge = [&](auto split_) {
     constexpr int kSplit = decltype(split_)::value;
-    cfg.blockDim = dim3(32 * kMergeWarps<D, kSplit>);
+    using Cfg = MergeCfg<D, kSplit>;
+    cfg.gridDim = dim3(static_cast<unsigned>((rows + 31) / 32), p.c.n_kv_heads, kSplit == 1 ? 1 : D / Cfg::kCols);
+    cfg.blockDim = dim3(32 * Cfg::kWarps);
     return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, kE4M3, kSplit>, p);
   };
-  e = split == 8   ? merge(std::integral_constant<int, 8>{})
-      : split == 4 ? merge(std::integral_constant<int, 4>{})
-      : split == 2 ? merge(std::integral_constant<int, 2>{})
-                   : merge(std::integral_constant<int, 1>{});
+  auto fits = [&](int split) { return row_blocks * (D / (split > 8 ? 8 : 16)) * split <= 148ll * (split > 8 ? 32 : 24); };
+  e = pieces >= 32 && fits(32)   ? merge(std::integral_constant<int, 32>{})
+      : pieces >= 16 && fits(16) ? merge(std::integral_constant<int, 16>{})
+      : fits(8)                  ? merge(std::integral_constant<int, 8>{})
+      : fits(4)                  ? merge(std::integral_constant<int, 4>{})
+      : fits(2)                  ? merge(std::integral_constant<int, 2>{})
+                                 : merge(std::integral_constant<int, 1>{});
   if (e == cudaSuccess) ++*launches;
   return e;
 }

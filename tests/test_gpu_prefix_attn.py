@@ -316,3 +316,11 @@ def test_nan_and_infinite_keys_of_every_column(batch):
                 assert np.all(np.abs(lse[0, 0].double().cpu().numpy() - want_lse) <= rel + 2.0 ** -21 * (np.abs(want_lse) + 1))
             else:
                 assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_merge_by_sixteen_and_more_warps(fmt, d):
+    """Few rows and a piece of them on every SM: 16 warps share them out, or 32."""
+    run(fmt, [20000], [5] * (40 if d == 128 else 80), 64, 8, 2, d, seed=1, rows=[(0, 0), (7, 0), (8, 0), (31, 0), (39, 0)])
+    run(fmt, [20000], [5, 1, 300], 64, 7, 1, d, T=2, seed=2)
