@@ -159,3 +159,29 @@ def test_a_step_as_a_graph(fmt):
     for x, y in zip(a.state(), b.state()):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
     assert a.lens.tolist() != [n + 12 for n in STARTS]                   # some were cut
+
+
+def test_two_loops_at_once():
+    """Two serving loops on two streams, each with pools and a workspace of its own, give what they give one after the other."""
+    def loop(dec):
+        for step in range(6):
+            dec.feed(step)
+            dec.step()
+
+    def fresh():
+        return Decoder("bf16", 64, 16, 2, 3000, seed=3), Decoder("e4m3", 128, 32, 1, 5000, seed=4)
+    alone = fresh()
+    for dec in alone:
+        loop(dec)
+    both, streams = fresh(), [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for step in range(6):
+        for dec, stream in zip(both, streams):
+            with torch.cuda.stream(stream):
+                dec.feed(step)
+                dec.step()
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        for x, y in zip(a.state(), b.state()):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        assert B.fastkv_device_status(b.ws) == (0, 0)
