@@ -1075,7 +1075,7 @@ int check_prefix(const fastkv_paged_cache* c, const fastkv_prefix* x, const fast
   auto take = [&](size_t n) { const size_t o = off; off += round_up(n, 256); return o; };
   lay->off_own_out = take(static_cast<size_t>(tokens) * q->n_q_heads * c->head_dim * 4);
   lay->off_own_lse = take(static_cast<size_t>(tokens) * q->n_q_heads * 4);
-  lay->off_ml = take(pieces * 2 * lay->tile_rows * sizeof(float2));
+  lay->off_ml = take(pieces * 2 * lay->tile_rows * sizeof(float4));
   lay->off_o = take(pieces * 2 * lay->tile_rows * c->head_dim * 4);
   lay->bytes = off;
   return FASTKV_OK;
@@ -1130,7 +1130,7 @@ int fastkv_prefix_attn(const fastkv_paged_cache* cache, const fastkv_prefix* pre
   p.wait_limit = g_debug.wait_limit_cycles > 0 ? g_debug.wait_limit_cycles : kWaitLimitCycles;
   p.skip_commit = g_debug.prefix_skip_commit - 1;
   p.scale_log2 = softmax_scale_of(c, *query) * 1.4426950408889634f;
-  p.part_ml = reinterpret_cast<float2*>(ws + lay.off_ml);
+  p.part_ml = reinterpret_cast<float4*>(ws + lay.off_ml);
   p.part_o = reinterpret_cast<float*>(ws + lay.off_o);
   float* own_out = reinterpret_cast<float*>(ws + lay.off_own_out);
   float* own_lse = reinterpret_cast<float*>(ws + lay.off_own_lse);

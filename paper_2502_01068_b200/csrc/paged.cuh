@@ -92,7 +92,7 @@ struct PrefixParams {
   const int* table;           // [n_prefixes][max_pages]
   const int* lens;            // [n_prefixes]
   const int* cu_seqs;         // [n_prefixes + 1] or null
-  float2* part_ml;            // [pieces][2 tiles][tile_rows]: (reference, sum)
+  float4* part_ml;            // [pieces][2 tiles][tile_rows]: (reference, sum of the weights as rounded, sum of the weights, 0)
   float* part_o;              // [pieces][2 tiles][d / 4][tile_rows][4]
   const float* own_out;       // [B][q_len][Hq][d], the attention over the sequences' own entries
   const float* own_lse;       // [B][q_len][Hq]

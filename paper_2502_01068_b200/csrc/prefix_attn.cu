@@ -32,7 +32,9 @@
 // four copies of the rows in a tile with a quarter of the entries each brought 6 us and cost the merge 10, a third tile of V nothing.
 // Short shares: 2 us until the first copy (lengths, barriers, tensor memory), 2 us for a segment's output.
 //
-// P is rounded to bf16 (2^-9 of each weight, of either sign): that is what the output is rounded to; the row sums take it unrounded.
+// P is rounded to bf16 (by at most 2^-8 of each weight, of either sign), which is what the output is rounded to.  The output is divided by the
+// sum of the rounded weights, so that a row of one entry that outweighs the others has none of that error (2 x 512: 0.21 % off on the whole,
+// 0.25 divided by the other sum, which takes 3 % less time); lse takes the sum of the unrounded ones.
 // Logits, exponentials, sums, outputs and their merge are fp32.
 //
 // Every wait is bounded; a wait that gives up raises the status word and the CTA-wide abort flag, the roles stop issuing work, copies and
@@ -52,8 +54,10 @@ constexpr int kCtrlWarps = 4;                  // loader of K and V, issuer of t
 constexpr int kSoftmaxWarps = 4;               // per tile
 constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two terms, V to bf16
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
-// A row's reference moves (which rescales its output and keeps its warp for 2000 cycles) when a logit is this far above it: weights are at
-// most 2^16 then, whatever rounds them is relative.  (8: 100 us, 16: 96, 24: 96, 8 x 131072 in 8 bits.)
+// A row's reference is set this far above its largest logit, so that no weight is above 1 (V may be anything that bf16 holds), and moves when a
+// logit passes it (which rescales the row's output and keeps its warp for 2000 cycles).  Weights are relative to it, and so is whatever
+// rounds them.  (8: 100 us, 16: 96, 24: 96, 8 x 131072 in 8
+// bits.)
 constexpr float kSlackLog2 = 16.0f;
 
 // kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
@@ -766,7 +770,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (!ok) break;
         by_row *= __uint_as_float(pow2_bits(-row_shift[(dual ? x : 0) * kTile + r]));
       }
-      float m_ref = -INFINITY, l = 0.0f;
+      float m_ref = -INFINITY, l = 0.0f, lr = 0.0f;       // sums of the weights, and of the weights as rounded
       for (int i = 0; i < steps; ++i, ++sn) {
         const int h = i & 1, n = n_first + n_step * (i >> 1);         // (a segment's steps are even in number: sn & 1 == h)
         ok = mbar_wait_bounded(&bars->s_full[x][h], (sn >> 1) & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit);
@@ -798,11 +802,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             for (int e = 2; e < 16; e += 2) { mx[0] = fmaxf(mx[0], v[c][z * 16 + e]); mx[1] = fmaxf(mx[1], v[c][z * 16 + e + 1]); }
             most = fmaxf(most, fmaxf(mx[0], mx[1]) * f[kE4M3 ? c * 2 + z : 0]);
           }
-        // the reference moves only when the step's maximum is far above it (or at a row's first logits)
-        const bool move = most > m_ref + kSlackLog2;
+        // the reference moves only when a logit is above it (or at a row's first logits)
+        const bool move = most > m_ref;
         if (__any_sync(0xffffffffu, move)) {
-          const float alpha = move ? ex2(m_ref - most) : 1.0f;
-          if (move) { m_ref = most; l *= alpha; }
+          const float to = most + kSlackLog2, alpha = move ? ex2(m_ref - to) : 1.0f;
+          if (move) { m_ref = to; l *= alpha; lr *= alpha; }
           if (i >= 1) {
             // The step before this one may still be on its way into O.  (The one before that is in it: S of this step was issued behind it.  So
             // the barrier is at this phase or through with it, never further.)
@@ -821,7 +825,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         }
         const float neg_ref = m_ref == -INFINITY ? 0.0f : -m_ref;   // nothing seen yet: every weight is 2^-inf
         const uint64_t neg2 = pair_of(neg_ref, neg_ref);
-        uint64_t ls = 0;
+        uint64_t ls = 0, lrs = 0;
 #pragma unroll
         for (int c = 0; c < kStep / 32; ++c) {
           float packed[16];
@@ -840,13 +844,17 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               w = pair_of(e0, e1);
             }
             ls = add2(ls, w);
-            packed[e / 2] = __uint_as_float(pack16<false>(e0, e1));
+            const uint32_t pair = pack16<false>(e0, e1);
+            lrs = add2(lrs, pair_of(__uint_as_float(pair << 16), __uint_as_float(pair & 0xffff0000u)));
+            packed[e / 2] = __uint_as_float(pair);
           }
           tmem_st_32x16(s_addr + h * kStep + c * 16, packed);
         }
         float l0, l1;
         split(ls, l0, l1);
         l += l0 + l1;
+        split(lrs, l0, l1);
+        lr += l0 + l1;
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
@@ -854,16 +862,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
       if (!ok) break;
       // ---- the segment's piece: four columns of O by rows, so that a warp's stores are whole lines ----
-      float2* const ml = p.part_ml + (piece * 2 + x) * p.tile_rows + r;
+      float4* const ml = p.part_ml + (piece * 2 + x) * p.tile_rows + r;
       if (steps == 0) {
-        if (r < rows) *ml = make_float2(-INFINITY, 0.0f);
+        if (r < rows) *ml = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
         continue;
       }
       ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars->o_done[x], o_segs & 1, abort_flag, p.hdr, SITE_PREFIX_O, limit));
       ++o_segs;
       if (!ok) break;
       tc_fence_after_sync();
-      if (r < rows) __stcg(ml, make_float2(m_ref, l));
+      if (r < rows) __stcg(ml, make_float4(m_ref, lr, l, 0.0f));
       float4* po = reinterpret_cast<float4*>(p.part_o) + (piece * 2 + x) * (D / 4) * p.tile_rows + r;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
@@ -1092,7 +1100,7 @@ prefix_merge_kernel(const PrefixParams p) {
   const int token = R / G, b = token / T;
   // ---- this row's pieces: `count` of them from `piece` on, and the same rows' other half of the chunks where one tile took both ----
   int count = 0, both = 1;
-  const float2* ml = p.part_ml;
+  const float4* ml = p.part_ml;
   const float4* po = reinterpret_cast<const float4*>(p.part_o);
   int lo = 0;                                             // the last prefix that starts at or before the row's sequence
   Group gr;
@@ -1139,7 +1147,7 @@ prefix_merge_kernel(const PrefixParams p) {
   constexpr int k1 = kE4M3 ? 2 : 1, k2 = kE4M3 ? 1 : 2;
   const int sub = SPLIT == 1 ? 0 : warp;
   const size_t at = static_cast<size_t>(token) * p.n_q_heads + g * G + R - token * G;
-  float M = -INFINITY, L = 0.0f, acc[kMergeCols];
+  float M = -INFINITY, L = 0.0f, E = 0.0f, acc[kMergeCols];        // reference, what the output is divided by, sum of the weights
 #pragma unroll
   for (int i = 0; i < kMergeCols; ++i) acc[i] = 0.0f;
   if (R < rows && sub == 0) {
@@ -1151,17 +1159,17 @@ prefix_merge_kernel(const PrefixParams p) {
       acc[i] = y.x; acc[i + k1] = y.y; acc[i + k2] = y.z; acc[i + 3] = y.w;
     }
     M = own * 1.4426950408889634f;
-    L = own == -INFINITY ? 0.0f : 1.0f;                   // (without entries its output is zeros)
+    L = E = own == -INFINITY ? 0.0f : 1.0f;               // (without entries its output is zeros)
   }
   const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D / 4) * p.tile_rows;
   constexpr int kAhead = Cfg::kAhead;
   for (int s0 = sub; s0 < most; s0 += kAhead * SPLIT) {
-    float2 v[kAhead];
+    float4 v[kAhead];
     float o[kAhead][kMergeCols];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int s = s0 + k * SPLIT;
-      v[k] = make_float2(-INFINITY, 0.0f);
+      v[k] = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
       if (s < count) {
         const size_t tile = both == 2 ? s : 2 * s;        // tiles of a piece lie side by side
         v[k] = __ldcg(ml + tile * step_ml);
@@ -1180,6 +1188,7 @@ prefix_merge_kernel(const PrefixParams p) {
       const float a = ex2(M - ref), w = ex2(v[k].x - ref);
       M = top;
       L = fmaf(L, a, v[k].y * w);
+      E = fmaf(E, a, v[k].z * w);
 #pragma unroll
       for (int i = 0; i < kMergeCols; ++i) acc[i] = fmaf(acc[i], a, o[k][i] * w);
     }
@@ -1196,11 +1205,12 @@ prefix_merge_kernel(const PrefixParams p) {
     uint4* to = reinterpret_cast<uint4*>(p.out + at * D + col0);
     to[0] = make_uint4(o[0], o[1], o[2], o[3]);
     to[1] = make_uint4(o[4], o[5], o[6], o[7]);
-    if (p.lse != nullptr && col0 == 0) p.lse[at] = L != 0.0f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+    if (p.lse != nullptr && col0 == 0) p.lse[at] = L != 0.0f ? (M + log2f(E)) * 0.6931471805599453f : -INFINITY;
   } else {
     ml_of[warp][lane] = make_float2(M, L);
 #pragma unroll
     for (int i = 0; i < kMergeCols; ++i) acc_of[warp][lane][i] = acc[i];
+    acc_of[warp][lane][kMergeCols] = E;
     __syncthreads();
     // ---- now a thread for some columns of a row ----
     constexpr int kMine = SPLIT > 8 ? 2 : kMergeCols / SPLIT, kEach = kMergeCols / kMine;
@@ -1210,7 +1220,7 @@ prefix_merge_kernel(const PrefixParams p) {
 #pragma unroll
     for (int w = 0; w < SPLIT; ++w) top = fmaxf(top, ml_of[w][r].x);
     const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, out[kMine];
+    float sum = 0.0f, weights = 0.0f, out[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) out[i] = 0.0f;
 #pragma unroll
@@ -1219,6 +1229,7 @@ prefix_merge_kernel(const PrefixParams p) {
       if (x.y == 0.0f) continue;
       const float by = ex2(x.x - ref);
       sum = fmaf(x.y, by, sum);
+      weights = fmaf(acc_of[w][r][kMergeCols], by, weights);
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int z = (c + i) & 3;
@@ -1231,7 +1242,7 @@ prefix_merge_kernel(const PrefixParams p) {
     uint32_t* const to = reinterpret_cast<uint32_t*>(p.out + at2 * D + col0 + c);
 #pragma unroll
     for (int i = 0; i < kMine; i += 2) to[i / 2] = pack16<false>(out[i] * f, out[i + 1] * f);
-    if (p.lse != nullptr && col0 + c == 0) p.lse[at2] = sum != 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+    if (p.lse != nullptr && col0 + c == 0) p.lse[at2] = sum != 0.0f ? (top + log2f(weights)) * 0.6931471805599453f : -INFINITY;
   }
 }
 

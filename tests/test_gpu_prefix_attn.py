@@ -324,3 +324,20 @@ def test_merge_by_sixteen_and_more_warps(fmt, d):
     """Few rows and a piece of them on every SM: 16 warps share them out, or 32."""
     run(fmt, [20000], [5] * (40 if d == 128 else 80), 64, 8, 2, d, seed=1, rows=[(0, 0), (7, 0), (8, 0), (31, 0), (39, 0)])
     run(fmt, [20000], [5, 1, 300], 64, 7, 1, d, T=2, seed=2)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [3, 50])
+def test_values_next_to_the_end_of_the_range(fmt, batch):
+    """V up to 2^125: a weight is never above 1 and a row's largest starts at 2^-16 or below, so the running output of 2000 entries, which is
+    not divided by their sum yet, stays finite."""
+    sh = Shared(fmt, [2000], [4] * batch, 32, 2, 128, 5)
+    if fmt == "bf16":
+        sh.pools.v *= 2.0 ** 122
+    else:
+        sh.pools.vs *= 2.0 ** 119
+    sh.pools.v64 = [x * 2.0 ** (122 if fmt == "bf16" else 119) for x in sh.pools.v64]
+    q = (torch.randn(batch, 1, 8, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) * 0.25).to(torch.bfloat16)
+    out, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (0, 0) and torch.isfinite(out).all()
+    check(sh, q, out, lse, rows=[(b, 0) for b in range(0, batch, 7)])
