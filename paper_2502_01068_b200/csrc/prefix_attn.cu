@@ -25,9 +25,9 @@
 // Tensor memory (512 columns): S (and P inside it) of tile A at 0, of tile B at 128, two buffers of 64 each; O of A at 256, of B at 256 + d.
 //
 // What bounds it (32 query heads over 8 KV heads of 128; the kernel inside a call, one B200).  64 sequences over 32768 bf16 entries, 256 rows a
-// KV head: 38 us for 134 MB and 34 GFLOP (20.5 and 20.9 us at the rates of a copy and of a large product); a step takes 1640 cycles, of
-// which each softmax warp is busy for 1350 (the tensor pipe is active for 48 % of the kernel; 128 entries a step and one buffer of S, so that
-// softmax and products wait for one another, took 50 us when this took 43).  8 x 131072 in 8 bits, 32 rows: 80 us
+// KV head: 41 us for 134 MB and 34 GFLOP (20.5 and 20.9 us at the rates of a copy and of a large product); a step takes 1700 cycles, of
+// which each softmax warp is busy for 1400 (the tensor pipe is active for 45 % of the kernel; 128 entries a step and one buffer of S, so that
+// softmax and products wait for one another, took 50 us when this took 43).  8 x 131072 in 8 bits, 32 rows: 82 us
 // for 269 MB: widening a chunk of V (1300 cycles) and a step's softmax by one warp (1000, twice a chunk and tile) are as long as each other;
 // four copies of the rows in a tile with a quarter of the entries each brought 6 us and cost the merge 10, a third tile of V nothing.
 // Short shares: 2 us until the first copy (lengths, barriers, tensor memory), 2 us for a segment's output.
@@ -56,8 +56,8 @@ constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two te
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
 // A row's reference is set this far above its largest logit, so that no weight is above 1 (V may be anything that bf16 holds), and moves when a
 // logit passes it (which rescales the row's output and keeps its warp for 2000 cycles).  Weights are relative to it, and so is whatever
-// rounds them.  (8: 100 us, 16: 96, 24: 96, 8 x 131072 in 8
-// bits.)
+// rounds them.  (8 x 131072 in
+// 8 bits, whole call, with one sum of the weights: 8 100 us, 16 96, 24 96.)
 constexpr float kSlackLog2 = 16.0f;
 
 // kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
@@ -149,7 +149,7 @@ __device__ __forceinline__ int sharing_ctas(const PrefixParams& p, long long tot
 // The deal.  A CTA that goes from one unit to the next spends what three chunks take on it (the output's way out, the next queries' way in:
 // 5.5 us of 1.9 a chunk), so every unit counts for its chunks and three more in front of them, which are nobody's work; with less than two
 // chunks for a CTA they would only make shares uneven, and chunks alone count.  (48 x 4 tokens over 4 prefixes, 11 chunks a CTA:
-// 38.6 us with chunks alone, 36.0 with units; 64 over one prefix of 32768, 14 chunks a CTA: 40.2 and 38.2.)
+// 38.6 us with chunks alone, 36.0 with units; 64 over one prefix of 32768, 14 chunks a CTA: 40.2 and 38.2; with one sum of the weights.)
 __device__ __forceinline__ int unit_cost(const PrefixParams& p, long long chunks) { return chunks >= 2ll * p.ctas ? 3 : 0; }
 
 // A segment of a CTA's share: chunks [c0, c1) of one unit.
