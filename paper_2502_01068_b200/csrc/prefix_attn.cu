@@ -56,8 +56,7 @@ constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two te
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
 // A row's reference is set this far above its largest logit, so that no weight is above 1 (V may be anything that bf16 holds), and moves when a
 // logit passes it (which rescales the row's output and keeps its warp for 2000 cycles).  Weights are relative to it, and so is whatever
-// rounds them.  (8 x 131072 in
-// 8 bits, whole call, with one sum of the weights: 8 100 us, 16 96, 24 96.)
+// rounds them.  (2^8: 100 us, 2^16: 96, 2^24: 96, 8 x 131072 in 8 bits, whole call, with one sum of the weights.)
 constexpr float kSlackLog2 = 16.0f;
 
 // kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
