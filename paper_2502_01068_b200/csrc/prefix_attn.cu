@@ -85,7 +85,9 @@ struct PrefixCfg {
 // A wait for a phase that is two ahead of its barrier, or two behind, would be answered wrongly.  So a barrier serves chunks of one
 // parity (a row tile that takes every other chunk has barriers of its own and waits on each in order), the two issuers start every
 // segment together, when all earlier chunks have been used, and the eighth chunk behind one is not loaded before the softmax has it
-// behind itself (the fourth may be).
+// behind itself (the fourth may be).  q_full and q_wide are one barrier each: the next segment's Q waits for both issuers and for every
+// softmax warp to have come to this segment (q_empty), since a tile without chunks in a segment would not hold it up, and its softmax
+// warps may still be writing the output of the one before.
 constexpr int kBars = 8;
 // Scales of a chunk's pages, K's and behind them V's: the softmax may still read a chunk's when the fourth behind it is loaded, never when
 // the eighth is.
@@ -434,7 +436,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 
   if (t == 0) {
     mbar_init(&bars->q_full, 1);
-    mbar_init(&bars->q_empty, 2);
+    mbar_init(&bars->q_empty, 2 + 2 * kSoftmaxWarps);
     mbar_init(&bars->q_wide, kWideWarps);
     mbar_init(&bars->v_tail, 1);
     for (int i = 0; i < kBars; ++i) {
@@ -750,7 +752,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       int seen = br.seen - (n_first - br.n0) * kTile;     // entries from the step's first one to the prefix's end
       const long long piece = static_cast<long long>(br.unit) + blockIdx.x;
       ++segs;
+      // what the warp needs of the segment that the next one writes over has been read: as far as it goes, the next one may come
+      auto taken = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->q_empty);
+      };
       if (r - lane < 0 || r - lane >= rows) {
+        taken();
         // no rows: the warp only keeps step (nobody may run ahead of a barrier by two phases)
         for (int i = 0; i < steps && ok; ++i, ++sn) {
           ok = __all_sync(0xffffffffu, mbar_wait_nap(&bars->s_full[x][sn & 1], (sn >> 1) & 1, abort_flag, p.hdr, SITE_PREFIX_S, limit));
@@ -769,6 +777,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (!ok) break;
         by_row *= __uint_as_float(pow2_bits(-row_shift[(dual ? x : 0) * kTile + r]));
       }
+      taken();
       float m_ref = -INFINITY, l = 0.0f, lr = 0.0f;       // sums of the weights, and of the weights as rounded
       for (int i = 0; i < steps; ++i, ++sn) {
         const int h = i & 1, n = n_first + n_step * (i >> 1);         // (a segment's steps are even in number: sn & 1 == h)

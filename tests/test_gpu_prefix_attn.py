@@ -341,3 +341,28 @@ def test_values_next_to_the_end_of_the_range(fmt, batch):
     out, lse, ws = call(sh, q)
     assert B.fastkv_device_status(ws) == (0, 0) and torch.isfinite(out).all()
     check(sh, q, out, lse, rows=[(b, 0) for b in range(0, batch, 7)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,T,longest", [(1, 1, 128), (4, 25, 128), (4, 1, 700), (4, 60, 700)])
+def test_shares_of_many_short_segments(fmt, d, G, T, longest):
+    """Hundreds of prefixes of a chunk each, or of a few: a CTA's share is a row of short segments, many of which leave one of its two row tiles
+    without chunks, and ends in one of them.  Again and again, with memory busy on another stream: the same bits."""
+    rng = np.random.default_rng(longest + T)
+    n = 400
+    sh = Shared(fmt, [int(x) for x in rng.integers(1, longest + 1, n)], [int(x) for x in rng.integers(T, T + 9, n)], 16, 8, d, 3, list(range(n + 1)))
+    q = torch.randn(n, T, 8 * G, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)).to(torch.bfloat16)
+    first, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    check(sh, q, first, lse, rows=[(b, b % T) for b in range(0, n, 13)] + [(n - 1, T - 1)])
+    side, a, b = torch.cuda.Stream(), torch.zeros(1 << 28, dtype=torch.uint8, device="cuda"), torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(40):
+            b.copy_(a)
+    for _ in range(10):
+        out, l, ws = call(sh, q)
+        assert B.fastkv_device_status(ws) == (0, 0)
+        assert torch.equal(out.view(torch.int16), first.view(torch.int16)) and torch.equal(l, lse)
+    torch.cuda.synchronize()
