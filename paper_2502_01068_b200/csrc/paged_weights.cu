@@ -221,17 +221,21 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
     for (int e = 0; e < 2; ++e) {
       if constexpr (kE4M3) by[e] = __uint_as_float(pow2_bits(-__shfl_sync(0xffffffffu, up, (2 * c + e) * 4)));
       const int s = nt * 8 + 2 * c + e, si = s / G, sh = x.g * G + s - si * G;
-      l[e] = s < p.rows ? __ldg(p.lse + (static_cast<size_t>(x.b) * T + si) * p.n_q_heads + sh) : INFINITY;
+      l[e] = s < p.rows ? __ldg(p.lse + (static_cast<size_t>(x.b) * T + si) * p.n_q_heads + sh) : 0.0f;
       n[e] = s >= p.rows || l[e] == -INFINITY ? 0 : max(x.len - (T - 1 - si), 0);
     }
   };
 
   int all_see = 0;
+  // whether row 2c + e of a tile is there (the last tile's may be padding, with queries of zeros)
+  auto is_row = [&](int nt, int e) -> bool { return nt * 8 + 2 * c + e < p.rows; };
   // the fewest entries that a row sees which is there
   auto least = [&]() -> int {
     int n = 0x7fffffff;
 #pragma unroll
-    for (int nt = 0; nt < kHeld; ++nt) n = min(n, min(lse[nt][0] == INFINITY ? n : sees[nt][0], lse[nt][1] == INFINITY ? n : sees[nt][1]));
+    for (int nt = 0; nt < kHeld; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) n = min(n, is_row(nt, e) ? sees[nt][e] : n);
     return __reduce_min_sync(0xffffffffu, n);
   };
   // what the entries of the step from `key0` on draw from the lane's rows
@@ -239,8 +243,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
 #pragma unroll
     for (int y = 0; y < 2 * kTiles; ++y) sum[y] = 0.0f;
     if (key0 >= x.len) return;
-    // the rows of kHeld tiles: K's fragments (widened once) serve them all.  kAll: every row that is there sees the whole step (rows that
-    // are not there have an lse of +infinity).
+    // the rows of kHeld tiles: K's fragments (widened once) serve them all.  kAll: every row that is there sees the whole step; those that are
+    // not are left out by selection, because a query of zeros meets an infinite key as NaN.
     auto draw = [&](auto all_) {
       constexpr bool kAll = decltype(all_)::value;
 #pragma unroll
@@ -274,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_weights_kernel(const PagedW
           for (int e = 0; e < 4; ++e) {
             // what a row does not see must not reach the sum, NaN included
             const float w = ex2(fmaf(d[nt][e], by[e & 1], -lse[nt][e & 1]) * 1.4426950408889634f);
-            if (kAll || key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[2 * y + (e >> 1)] += w;
+            if (kAll ? is_row(nt, e & 1) : key0 + y * 16 + quad + (e >> 1) * 8 < sees[nt][e & 1]) sum[2 * y + (e >> 1)] += w;
           }
         }
       }

@@ -179,3 +179,60 @@ def test_steps_of_a_unit(fmt, d, pairs, Hq, Hkv, T):
 def test_a_bound_beyond_everything():
     run("bf16", [300, 20], 16, 4, 2, 64, seed=1, total_len=2 ** 63 - 1)
     run("e4m3", [300, 20], 16, 4, 2, 128, seed=1, total_len=2 ** 62)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,T", [(2, 2, 1), (4, 1, 1), (8, 2, 1), (10, 2, 1), (8, 1, 1), (8, 2, 3), (4, 1, 4), (7, 1, 3)])
+def test_infinite_and_nan_keys(fmt, d, Hq, Hkv, T):
+    """Entries with one infinite element (bf16; NaN in both formats): logits of -infinity draw 0, those of +infinity infinity, NaN gives NaN, where
+    every row sees the step and where the last entries cut it; rows 1 to 21, tiles of eight with and without padding.  Nothing else changes."""
+    rng = np.random.default_rng(d + Hq + T)
+    n, by = 700, 1.0 / math.sqrt(d)
+    values = [float("nan")] if fmt == "e4m3" else [-math.inf, math.inf, float("nan")]
+    slots = [0, 17, 100, 255, 256, 511, 600, 697, 698, 699]
+    for signs in (1.0, None):                             # all queries meet them with one sign, or with either
+        for value in values:
+            pools = Pools(fmt, [n], [n], 16, Hkv, d, 5)
+            k64 = pools.k64[0].copy()
+            for t in slots:
+                page = int(pools.table_np[0, t // 16])
+                (pools.k if fmt == "bf16" else pools.k.view(torch.float8_e4m3fn))[page, :, t % 16, 3] = value
+                k64[t, :, 3] = value
+            q = rng.standard_normal((1, T, Hq, d))
+            q[..., 3] = 1.0 if signs else np.sign(q[..., 3])
+            q = torch.from_numpy(q).to(torch.bfloat16)
+            q64 = q.double().numpy()
+            lse = lse_of(pools, q64, [n], by)             # of the entries without them
+            old = np.exp(rng.standard_normal((1, Hkv, n))).astype(np.float32)
+            w, ws = torch.from_numpy(old).cuda(), workspace()
+            B.fastkv_paged_weights(pools.cache(), B.make_query(n_q_heads=Hq, q_len=T, max_len=n), pools.dev_lens, q.cuda(), torch.from_numpy(lse).cuda(), 0.5, w, ws)
+            assert B.fastkv_device_status(ws) == (0, 0)
+            want, slack = reference(pools, q64, lse.astype(np.float64), [n], old.astype(np.float64), 0.5, by)
+            pools.k64[0] = k64
+            with np.errstate(invalid="ignore"):
+                there, _ = reference(pools, q64, lse.astype(np.float64), [n], old.astype(np.float64), 0.5, by)
+            want[:, :, slots], slack[:, :, slots] = there[:, :, slots], 2.0 ** -22 * old[:, :, slots]
+            got = w.cpu().double().numpy()
+            finite = np.isfinite(want)
+            assert np.array_equal(np.where(finite, 0, got), np.where(finite, 0, want), equal_nan=True), (value, np.argwhere(~finite & (got != want))[:4])
+            assert np.all(np.abs(got[finite] - want[finite]) <= slack[finite])
+            if value == -math.inf and signs:              # drew nothing: the old weight's half, exactly
+                assert np.array_equal(got[0][:, slots[:-3]], old[0][:, slots[:-3]] * 0.5)
+
+
+def test_rows_of_infinite_lse():
+    """A row whose lse is +infinity draws nothing from finite logits, and has no part in what it does not see."""
+    n, d = 256, 64
+    pools = Pools("bf16", [n], [n], 16, 1, d, 1)
+    pools.k[int(pools.table_np[0, (n - 1) // 16]), 0, (n - 1) % 16, 0] = math.inf
+    q = torch.ones(1, 2, 2, d, device="cuda", dtype=torch.bfloat16)
+    lse = torch.tensor([[[math.inf, math.inf], [10.0, 11.0]]], device="cuda")
+    w, ws = torch.zeros(1, 1, n, device="cuda"), workspace()
+    B.fastkv_paged_weights(pools.cache(), B.make_query(n_q_heads=2, q_len=2, max_len=n), pools.dev_lens, q, lse, 1.0, w, ws)
+    x = w[0, 0].cpu().double().numpy()
+    logit = 0.125 * pools.k64[0][:n - 1, 0].sum(axis=-1)
+    # a logit and its difference to lse are off by at most 64 2^-23 sum |k| / 8 + 2^-22 (|x| + 11) < 2^-12
+    want = np.exp(logit - 10.0) + np.exp(logit - 11.0)
+    assert np.abs(pools.k64[0][:n - 1]).sum(axis=-1).max() < 128 and np.all(np.abs(x[:-1] - want) <= 2.0 ** -12 * want)
+    assert x[-1] == math.inf                              # of the second token's rows; the first token's do not see it
