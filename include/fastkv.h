@@ -314,6 +314,8 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
  * Accuracy: the softmax's weights of prefix entries are rounded to bf16 (and the output is divided by the sum of what they were rounded to),
  * all products, sums and the merge are fp32, lse takes the weights unrounded, with one rounding to bf16 at the end; own entries as in fastkv_paged_attn.  8-bit entries of a prefix meet the query as the sum of two e4m3 terms: elements
  * below 2^-9 of the largest of a query and head are rounded to multiples of 2^-16 of that, or finer.
+ * Sums of weighted values are divided at the end: they stay finite for values up to 2^113, and to the end of bf16's range as long as
+ * all entries of a prefix weigh no more than 2^14 times the heaviest.
  * max_len of `prefix` and of `query` and total_len size the launch only.  A length beyond the table's room is cut to it, a page id
  * outside the pool reads page 0 instead, a cu_seqs that descends or leaves 0 .. batch leaves the outputs of prefixed sequences
  * unspecified; all are reported in the status word (FASTKV_ERR_DEVICE_INDEX), which this call does not clear.

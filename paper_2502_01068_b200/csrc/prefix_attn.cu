@@ -54,10 +54,13 @@ constexpr int kCtrlWarps = 4;                  // loader of K and V, issuer of t
 constexpr int kSoftmaxWarps = 4;               // per tile
 constexpr int kWideWarps = 8;                  // 8-bit pages: Q into its two terms, V to bf16
 constexpr int kHalfBytes = kTile * 128;        // 128 rows x 64 16-bit values: one swizzled column block of a tile
-// A row's reference is set this far above its largest logit, so that no weight is above 1 (V may be anything that bf16 holds), and moves when a
-// logit passes it (which rescales the row's output and keeps its warp for 2000 cycles).  Weights are relative to it, and so is whatever
-// rounds them.  (2^8: 100 us, 2^16: 96, 2^24: 96, 8 x 131072 in 8 bits, whole call, with one sum of the weights.)
-constexpr float kSlackLog2 = 16.0f;
+// A row's reference is set kSlackLog2 + kRoomLog2 above its largest logit and moves when a logit comes nearer than kRoomLog2 (which rescales
+// the row's output and keeps its warp for 2000 cycles).  So a weight is 2^-15 at most, and what is not divided by the sum of the weights yet
+// stays finite for V of any finite bf16 as long as the entries weigh no more than 2^14 of the largest would, and for V up to 2^113 whatever
+// the entries; V of 2^-95 and above keeps its bits.  Weights are relative to the reference, and so is whatever rounds them; further away
+// than 32 their exponents would lose a bit.  (Slack of 2^8: 100 us, 2^16: 96, 2^24: 96, 8 x 131072 in 8 bits, whole call, with one sum of the
+// weights.)
+constexpr float kSlackLog2 = 16.0f, kRoomLog2 = 15.0f;
 
 // kOne: every unit has at most one tile of rows (the batch has no more), so that Q needs half the space.
 template <int D, bool kE4M3, bool kOne>
@@ -810,10 +813,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             for (int e = 2; e < 16; e += 2) { mx[0] = fmaxf(mx[0], v[c][z * 16 + e]); mx[1] = fmaxf(mx[1], v[c][z * 16 + e + 1]); }
             most = fmaxf(most, fmaxf(mx[0], mx[1]) * f[kE4M3 ? c * 2 + z : 0]);
           }
-        // the reference moves only when a logit is above it (or at a row's first logits)
-        const bool move = most > m_ref;
+        // the reference moves only when a logit comes close to it (or at a row's first logits)
+        const bool move = most > m_ref - kRoomLog2;
         if (__any_sync(0xffffffffu, move)) {
-          const float to = most + kSlackLog2, alpha = move ? ex2(m_ref - to) : 1.0f;
+          const float to = most + (kSlackLog2 + kRoomLog2), alpha = move ? ex2(m_ref - to) : 1.0f;
           if (move) { m_ref = to; l *= alpha; lr *= alpha; }
           if (i >= 1) {
             // The step before this one may still be on its way into O.  (The one before that is in it: S of this step was issued behind it.  So
@@ -1151,7 +1154,8 @@ prefix_merge_kernel(const PrefixParams p) {
   }
   const int most = __reduce_max_sync(0xffffffffu, count);
   pdl_wait();
-  // ---- the sum starts with the row's own entries (8-bit pages: the pieces' columns 1 and 2 of four have changed places) ----
+  // ---- the sum starts with the row's own entries (8-bit pages: the pieces' columns 1 and 2 of four have changed places), at half their
+  // size: next to values at the end of the range there is room for the pieces' ----
   constexpr int k1 = kE4M3 ? 2 : 1, k2 = kE4M3 ? 1 : 2;
   const int sub = SPLIT == 1 ? 0 : warp;
   const size_t at = static_cast<size_t>(token) * p.n_q_heads + g * G + R - token * G;
@@ -1164,10 +1168,10 @@ prefix_merge_kernel(const PrefixParams p) {
 #pragma unroll
     for (int i = 0; i < kMergeCols; i += 4) {
       const float4 y = __ldcg(from + i / 4);
-      acc[i] = y.x; acc[i + k1] = y.y; acc[i + k2] = y.z; acc[i + 3] = y.w;
+      acc[i] = 0.5f * y.x; acc[i + k1] = 0.5f * y.y; acc[i + k2] = 0.5f * y.z; acc[i + 3] = 0.5f * y.w;
     }
-    M = own * 1.4426950408889634f;
-    L = E = own == -INFINITY ? 0.0f : 1.0f;               // (without entries its output is zeros)
+    M = fmaf(own, 1.4426950408889634f, 1.0f);
+    L = E = own == -INFINITY ? 0.0f : 0.5f;               // (without entries its output is zeros)
   }
   const size_t step_ml = static_cast<size_t>(p.tile_rows), step_o = static_cast<size_t>(D / 4) * p.tile_rows;
   constexpr int kAhead = Cfg::kAhead;

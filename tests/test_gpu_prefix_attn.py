@@ -366,3 +366,53 @@ def test_shares_of_many_short_segments(fmt, d, G, T, longest):
         assert B.fastkv_device_status(ws) == (0, 0)
         assert torch.equal(out.view(torch.int16), first.view(torch.int16)) and torch.equal(l, lse)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch,n,heavy", [(3, 128, 3), (50, 128, 3), (3, 128, 64), (50, 300, 30), (2, 16000, 15900), (70, 16000, 15900)])
+def test_values_at_the_end_of_the_range_and_logits_that_rise(fmt, batch, n, heavy):
+    """The last entries' logits are 2^15 times the first ones' in weight, which is below what moves a row's reference, and all values of the
+    prefix are the largest of bf16 (8 bits: 224 * 2^120): their sum before the division has to stay finite."""
+    d, scale = 64, math.log(2.0)
+    sh = Shared(fmt, [n], [4] * batch, 16, 1, d, 5)
+    p = sh.pools
+    top = float(torch.finfo(torch.bfloat16).max) if fmt == "bf16" else 224.0 * 2.0 ** 120
+    pages = sh.ptable[0].long()
+    k, v = torch.zeros(n, d), torch.full((n, d), top if fmt == "bf16" else 224.0)
+    k[n - heavy:, 0] = 15.0
+    v[1::2, ::3] *= -1
+    for page0 in range(0, n, 16):
+        m, page = min(16, n - page0), pages[page0 // 16]
+        for pool, x in ((p.k, k), (p.v, v)):
+            pool[page, 0, :m] = (x[page0:page0 + m].to(torch.bfloat16) if fmt == "bf16" else x[page0:page0 + m].to(torch.float8_e4m3fn).view(torch.uint8)).cuda()
+    if fmt == "e4m3":
+        p.ks[pages], p.vs[pages] = 1.0, 2.0 ** 120
+    p.k64[0], p.v64[0] = k[:, None].double().numpy(), (v[:, None].double() * (1.0 if fmt == "bf16" else 2.0 ** 120)).numpy()
+    q = torch.zeros(batch, 1, 4, d, device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    out, lse, ws = call(sh, q, scale)
+    assert B.fastkv_device_status(ws) == (0, 0) and torch.isfinite(out).all()
+    check(sh, q, out, lse, scale, rows=[(b, 0) for b in range(0, batch, 7)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [3, 70])
+def test_own_values_at_the_end_of_the_range(fmt, batch):
+    """One's own entry weighs 2^16 times an entry of the prefix, and all values are next to the end of the range: so is the sum of both parts."""
+    n, d, scale = 16000, 64, math.log(2.0)
+    sh = Shared(fmt, [n], [1] * batch, 16, 1, d, 5)
+    p, top = sh.pools, float(torch.finfo(torch.bfloat16).max) if fmt == "bf16" else 224.0 * 2.0 ** 120
+    if fmt == "bf16":
+        p.v = torch.where(torch.isnan(p.v), p.v, torch.full_like(p.v, top))
+        p.k = torch.where(torch.isnan(p.k), p.k, torch.zeros_like(p.k))
+    else:
+        p.v = torch.where(p.v == 0x7F, p.v, torch.full_like(p.v, 0x76))                   # 224
+        p.k = torch.where(p.k == 0x7F, p.k, torch.zeros_like(p.k))
+        p.vs, p.ks = torch.full_like(p.vs, 2.0 ** 120), torch.ones_like(p.ks)
+    p.k[sh.table[:, 0].long(), 0, 0, 0] = 16.0 if fmt == "bf16" else 0x58                 # (16)
+    p.v64 = [np.full_like(x, top) for x in p.v64]
+    p.k64 = [np.zeros_like(p.k64[0])] + [np.full_like(x, 16.0) * (np.arange(d) == 0) for x in p.k64[1:]]
+    q = torch.ones(batch, 1, 4, d, device="cuda", dtype=torch.bfloat16)
+    out, lse, ws = call(sh, q, scale)
+    assert B.fastkv_device_status(ws) == (0, 0) and torch.isfinite(out).all()
+    check(sh, q, out, lse, scale, rows=[(b, 0) for b in range(0, batch, 29)])
