@@ -197,3 +197,54 @@ def test_windows_of_several_rounds(fmt, d, lens, keep, window):
     """Nothing but the window moves, or next to nothing: rounds of as many rows as shared memory holds, sources that overlap with what is
     written (by 10 slots of a page, or by none), ends inside a round and a page."""
     run(fmt, lens, keep, window, 32, 2, d, seed=keep)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page,keep,window", [(16, 100, 30), (16, 96, 0), (32, 120, 120), (64, 140, 9)])
+def test_rows_of_pages_outside_the_pool_stay_where_they_are(fmt, page, keep, window):
+    """Every row whose page and whose source's page exist moves by the rule; nothing else is written: not page 0, not the page that the table
+    named before, not the rows whose source is not to be had.  The other sequence is cut as ever."""
+    lens, Hkv, d = [200, 190], 2, 64
+    for at in range(-(-200 // page)):
+        for bad in (-1, 10 ** 6):
+            pools = Pools(fmt, lens, lens, page, Hkv, d, at + 1)
+            table = pools.table_np.copy()
+            table[0, at] = bad
+            pools.table = torch.from_numpy(table).cuda()
+            before = raw(pools)
+            rng = np.random.default_rng(at)
+            w = np.exp(rng.standard_normal((2, Hkv, 200))).astype(np.float32)
+            ev = B.make_eviction(keep=keep, window=window, max_len=200)
+            ws = torch.zeros(B.fastkv_paged_evict_workspace_bytes(pools.cache(), ev), dtype=torch.uint8, device="cuda")
+            new_w, new_lens = torch.zeros(w.shape, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+            B.fastkv_paged_evict(pools.cache(), ev, pools.dev_lens, torch.from_numpy(w).cuda(), None, new_w, None, new_lens, ws)
+            status = B.fastkv_device_status(ws)
+            after = raw(pools)
+            item = lambda t: t.view(torch.int16).numpy() if fmt == "bf16" else t.view(torch.uint8).numpy()  # noqa: E731
+            want = [item(t).copy() for t in before[:2]]
+            want_s = [None if t is None else t.numpy().copy() for t in before[2:]]
+            touched = False
+            for b, n in enumerate(lens):
+                for g in range(Hkv):
+                    o = np.array(origins(w[b, g], n, keep, window))
+                    assert np.array_equal(new_w.cpu().numpy()[b, g, :keep], w[b, g, o])
+                    to, src = table[b, np.arange(keep) // page], table[b, o // page]
+                    moves = (to >= 0) & (to < pools.n_pages) & (src >= 0) & (src < pools.n_pages)
+                    touched = touched or not moves[o != np.arange(keep)].all()
+                    j = np.flatnonzero(moves)
+                    for x in range(2):
+                        rows = item(before[x])[src[j], g, o[j] % page]
+                        if fmt == "e4m3":
+                            was = before[2 + x].numpy()[src[j], g].astype(np.float64)
+                            now = np.array([was[j // page == i // page].max() for i in j])
+                            values = before[x].view(torch.float8_e4m3fn).float().numpy().astype(np.float64)[src[j], g, o[j] % page]
+                            codes = torch.from_numpy(rn_e4m3(values * (was / now)[:, None])).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+                            rows = np.where((was == now)[:, None], rows, codes)
+                            want_s[x][to[j], g] = now
+                        want[x][to[j], g, j % page] = rows
+            for x in range(2):
+                assert np.array_equal(item(after[x]), want[x]), (at, bad, "kv"[x], np.argwhere(item(after[x]) != want[x])[:4])
+                if fmt == "e4m3":
+                    assert np.array_equal(after[2 + x].numpy(), want_s[x], equal_nan=True)
+            assert new_lens.tolist() == [keep, keep]
+            assert not touched or status == (B.ERR_DEVICE_INDEX, 46)
