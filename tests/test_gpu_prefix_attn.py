@@ -416,3 +416,27 @@ def test_own_values_at_the_end_of_the_range(fmt, batch):
     out, lse, ws = call(sh, q, scale)
     assert B.fastkv_device_status(ws) == (0, 0) and torch.isfinite(out).all()
     check(sh, q, out, lse, scale, rows=[(b, 0) for b in range(0, batch, 29)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,Hq,cu", [(64, 128, None), (4, 8, [0, 8, 0, 8, 2]), (3, 8, [8, 0, 8, 4]), (64, 8, None), (5, 4, [-3, 20, 1, 7, 3, 100])])
+def test_groups_that_overlap_stay_in_their_buffers(fmt, n, Hq, cu):
+    """Whatever cu_seqs says: nothing is written behind the workspace, the outputs and the lse, or in front of them, and sequences are all
+    there is to write to."""
+    sh = Shared(fmt, [150] * n, [3] * 8, 16, 1, 64, 3, cu=cu or [0, 8] * (n // 2) + [8])
+    cache, prefix, query = sh.cache(), sh.prefix(), B.make_query(n_q_heads=Hq, max_len=3, total_len=24)
+    q = torch.randn(8, 1, Hq, 64, device="cuda").to(torch.bfloat16)
+    size, edge = B.fastkv_prefix_attn_workspace_bytes(cache, prefix, query), 4096
+
+    def guarded(nbytes):
+        x = torch.full((nbytes + 2 * edge,), 0x5A, dtype=torch.uint8, device="cuda")
+        return x, x[edge:edge + nbytes]
+    (all_ws, ws), (all_out, out), (all_lse, lse) = guarded(size), guarded(8 * Hq * 64 * 2), guarded(8 * Hq * 4)
+    ws[:256] = 0
+    pools = [x.clone() for x in (sh.pools.k, sh.pools.v)]
+    B.fastkv_prefix_attn(cache, prefix, query, sh.dev_lens, q, out.view(torch.bfloat16), lse.view(torch.float32), ws)
+    assert B.fastkv_device_status(ws) == (B.ERR_DEVICE_INDEX, 60)
+    for x in (all_ws, all_out, all_lse):
+        assert (x[:edge] == 0x5A).all() and (x[-edge:] == 0x5A).all()
+    for x, y in zip(pools, (sh.pools.k, sh.pools.v)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
