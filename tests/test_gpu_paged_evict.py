@@ -248,3 +248,32 @@ def test_rows_of_pages_outside_the_pool_stay_where_they_are(fmt, page, keep, win
                     assert np.array_equal(after[2 + x].numpy(), want_s[x], equal_nan=True)
             assert new_lens.tolist() == [keep, keep]
             assert not touched or status == (B.ERR_DEVICE_INDEX, 46)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_pages_and_rows_beyond_32_bits(fmt):
+    """The same entries in the last pages of pools of more than 2^32 elements, weights in rows of 2^30, and a bound beyond everything: the same."""
+    lens = [300, 170]
+    small = Pools(fmt, lens, lens, 16, 2, 128, 3)
+    far = Pools(fmt, lens, lens, 16, 2, 128, 3)
+    n, last = (1 << 32) // (2 * 16 * 128) + far.n_pages, far.n_pages
+    for name in ("k", "v", "ks", "vs"):
+        x = getattr(far, name)
+        if x is not None:
+            y = torch.empty((n, *x.shape[1:]), dtype=x.dtype, device="cuda")
+            y[n - last:] = x
+            setattr(far, name, y)
+    far.table += torch.where(far.table >= 0, n - last, 0).to(torch.int32)
+    first = torch.rand(2, 2, 300, device="cuda")
+    got = []
+    for pools, stride, max_len in ((small, 300, 300), (far, 1 << 30, 2 ** 31 - 1)):
+        w, new_w = torch.empty(2, 2, stride, device="cuda"), torch.empty(2, 2, stride, device="cuda")
+        w[:, :, :300] = first
+        ev, new_lens = B.make_eviction(keep=120, window=20, max_len=max_len), torch.zeros(2, dtype=torch.int32, device="cuda")
+        ws = torch.zeros(B.fastkv_paged_evict_workspace_bytes(pools.cache(), ev), dtype=torch.uint8, device="cuda")
+        B.fastkv_paged_evict(pools.cache(), ev, pools.dev_lens, w, None, new_w, None, new_lens, ws)
+        assert B.fastkv_device_status(ws) == (0, 0) and new_lens.tolist() == [120, 120]
+        got.append([new_w[:, :, :120].clone()] + [x[-last:].clone() for x in (pools.k, pools.v, pools.ks, pools.vs) if x is not None])
+        del w, new_w
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))

@@ -236,3 +236,29 @@ def test_rows_of_infinite_lse():
     want = np.exp(logit - 10.0) + np.exp(logit - 11.0)
     assert np.abs(pools.k64[0][:n - 1]).sum(axis=-1).max() < 128 and np.all(np.abs(x[:-1] - want) <= 2.0 ** -12 * want)
     assert x[-1] == math.inf                              # of the second token's rows; the first token's do not see it
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_pages_and_rows_beyond_32_bits(fmt):
+    """The same entries in the last pages of pools of more than 2^32 elements, weights in rows of 2^30: the same bits."""
+    pools = Pools(fmt, [300, 70], [300, 70], 16, 2, 128, 3)
+    q = torch.randn(2, 1, 8, 128, device="cuda").to(torch.bfloat16)
+    lse, query, ws = torch.full((2, 1, 8), 4.0, device="cuda"), B.make_query(n_q_heads=8, max_len=300), workspace()
+    old = torch.rand(2, 2, 300, device="cuda")
+    want = old.clone()
+    B.fastkv_paged_weights(pools.cache(), query, pools.dev_lens, q, lse, 0.5, want, ws)
+    n, k = (1 << 32) // (2 * 16 * 128) + pools.n_pages, pools.k
+    pools.k = torch.empty((n, *k.shape[1:]), dtype=k.dtype, device="cuda")
+    pools.k[n - pools.n_pages:] = k
+    pools.v = pools.k                                     # (not read)
+    if fmt == "e4m3":
+        ks = pools.ks
+        pools.ks = torch.empty((n, 2), device="cuda")
+        pools.ks[n - pools.n_pages:] = ks
+        pools.vs = pools.ks
+    pools.table += torch.where(pools.table >= 0, n - pools.n_pages, 0).to(torch.int32)
+    got = torch.empty(2, 2, 1 << 30, device="cuda")
+    got[:, :, :300] = old
+    B.fastkv_paged_weights(pools.cache(), query, pools.dev_lens, q, lse, 0.5, got, ws)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    assert torch.equal(got[:, :, :300], want)

@@ -440,3 +440,41 @@ def test_groups_that_overlap_stay_in_their_buffers(fmt, n, Hq, cu):
         assert (x[:edge] == 0x5A).all() and (x[-edge:] == 0x5A).all()
     for x, y in zip(pools, (sh.pools.k, sh.pools.v)):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch,Hq,Hkv,T,lens", [(2, 8, 2, 300, [300, 512]), (3, 5, 1, 129, [700, 64, 0]), (1, 32, 8, 512, [512]), (4, 4, 4, 65, [65, 66, 64, 1])])
+def test_many_query_tokens(fmt, batch, Hq, Hkv, T, lens):
+    """A prompt's chunk behind the prefix: hundreds of query tokens, some ahead of what their sequence holds."""
+    rows = [(b, i) for b in range(batch) for i in sorted({0, 1, T // 2, T - 65, T - 2, T - 1})]
+    run(fmt, [900], lens, 32, Hq, Hkv, 128, T, seed=T, rows=rows)
+    run(fmt, [130, 257], lens, 16, Hq, Hkv, 64, T, seed=T, cu=[0, batch // 2, batch], rows=rows)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_the_most_prefixes(fmt):
+    rng = np.random.default_rng(3)
+    cu = [1] + (1 + np.cumsum(rng.integers(0, 3, 1024))).tolist()
+    run(fmt, [int(x) for x in rng.integers(0, 200, 1024)], [int(x) for x in rng.integers(0, 20, cu[-1] + 1)], 32, 4, 2, 64, cu=cu, seed=5,
+        rows=[(b, 0) for b in range(0, cu[-1] + 1, 31)] + [(cu[-1], 0)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_pages_beyond_32_bits(fmt):
+    """The same entries in the last pages of pools of more than 2^32 elements: the same bits."""
+    sh = Shared(fmt, [300, 70], [20, 9, 40], 16, 2, 128, 3, cu=[0, 2, 3])
+    q = torch.randn(3, 2, 8, 128, device="cuda").to(torch.bfloat16)
+    want, want_lse, _ = call(sh, q)
+    p = sh.pools
+    n = (1 << 32) // (2 * 16 * 128) + p.n_pages
+    for name in ("k", "v", "ks", "vs"):
+        x = getattr(p, name)
+        if x is not None:
+            far = torch.empty((n, *x.shape[1:]), dtype=x.dtype, device="cuda")
+            far[n - p.n_pages:] = x
+            setattr(p, name, far)
+    for table in (sh.ptable, sh.table):
+        table += torch.where(table >= 0, n - p.n_pages, 0).to(torch.int32)
+    out, lse, ws = call(sh, q)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
