@@ -478,3 +478,20 @@ def test_pages_beyond_32_bits(fmt):
     out, lse, ws = call(sh, q)
     assert B.fastkv_device_status(ws) == (0, 0)
     assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [3, 50])
+def test_queries_that_are_not_finite_keep_to_themselves(fmt, batch):
+    """A NaN in one head's query, an infinity in another's: their own outputs are NaN (keys of either sign meet them), all others as ever."""
+    sh = Shared(fmt, [400], [9] * batch, 16, 2, 128, 3)
+    q = torch.randn(batch, 2, 8, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(torch.bfloat16)
+    want, want_lse, _ = call(sh, q)
+    bad = q.clone()
+    bad[1, 0, 2, 7], bad[1, 1, 5, 127], bad[batch - 1, 1, 0, 0] = float("nan"), math.inf, -math.inf
+    out, lse, ws = call(sh, bad)
+    assert B.fastkv_device_status(ws) == (0, 0)
+    hit = torch.zeros(batch, 2, 8, dtype=torch.bool, device="cuda")
+    hit[1, 0, 2] = hit[1, 1, 5] = hit[batch - 1, 1, 0] = True
+    assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+    assert torch.equal(out[~hit].view(torch.int16), want[~hit].view(torch.int16)) and torch.equal(lse[~hit], want_lse[~hit])
