@@ -309,8 +309,8 @@ int fastkv_paged_attn(const fastkv_paged_cache* cache, const fastkv_query* query
  * the first and behind the last have no prefix.  cu_seqs == NULL: one prefix that all share.  prefix->lens may be 0.
  * q: bf16, dense [batch, q_len, n_q_heads, head_dim], 16-byte aligned; out: bf16, the same shape, 16-byte aligned; lse (optional): fp32
  * [batch, q_len, n_q_heads], natural log, over prefix and own entries (what fastkv_paged_weights wants for the own entries).
- * A query that sees no entry gives out 0 and lse -infinity.  NaN and infinities as in fastkv_paged_attn; what lies behind a prefix's
- * last entry in its page never reaches an output.
+ * A query that sees no entry gives out 0 and lse -infinity.  NaN and infinities as in fastkv_paged_attn, but that an infinite element of
+ * a query counts as NaN over 8-bit pages; what lies behind a prefix's last entry in its page never reaches an output.
  * Accuracy: the softmax's weights of prefix entries are rounded to bf16 (and the output is divided by the sum of what they were rounded to),
  * all products, sums and the merge are fp32, lse takes the weights unrounded, with one rounding to bf16 at the end; own entries as in fastkv_paged_attn.  8-bit entries of a prefix meet the query as the sum of two e4m3 terms: elements
  * below 2^-9 of the largest of a query and head are rounded to multiples of 2^-16 of that, or finer.

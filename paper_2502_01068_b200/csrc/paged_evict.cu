@@ -17,9 +17,10 @@
 // What bounds it: latency.  The bytes of a cut (2304 entries to 2048: 256 rows of K and V per KV head and the weights) are few, and each row
 // is found by loads that wait for one another: slot, source, page, (scale,) row.  One B200, 8 KV heads of 128: one sequence of 2304 15 us
 // (ranking 5, an empty launch 2 each), 131072 to 13107 51 us (ranking 20: 64 CTAs, 4 us until the weights are there, 2 a digit; moving
-// 25 for 102 MB, 62 % of a copy), 64 of 2304 in 8 bits 39 us and 4 of 26214 to 13107 65 us (moving 28 and 40: rows that stay in a page whose
-// scale grows are read and written, too).  More warps on an SM (48 or 40 registers a thread) gained nothing in 8 bits: 42 and 41 us, 68 and 74
-// (39 and 69 at the time).
+// 25 for 102 MB, 62 % of a copy).  In 8 bits 64 of 2304 take 84 us and 4 of 26214 to 13107 102 on pages as appends leave them, where entries that
+// stay in a page whose scale grows are read and encoded again; on pages whose scales are equal already 40 and 65 (moving 28 and 40), which is
+// what calls in a row on the same pages measure.  More warps on an SM (48 or 40 registers a thread) gained nothing in 8 bits: 42 and 41 us, 68 and
+// 74 on equal scales (39 and 69 at the time).
 //
 // 8-bit pages: a page's entries share a scale; a page that receives entries takes the largest scale of the pages that its entries
 // come from (those that stay among them), and codes from smaller scales are encoded again, code * old / new, rounded to nearest even:
