@@ -13,10 +13,10 @@
 //   S [16 entries x 8 rows] = K Q^T: A = K rows, B = the query rows; a lane holds 2 entries x 2 rows, and the sum over rows ends
 //   with two shuffles.  Each entry belongs to one lane: no atomics, and the order of the sums is fixed.
 // 32 query heads over 8 KV heads of 128, one B200: 64 sequences of 2048 bf16 entries 45 us, 250 MB at 5.5 TB/s (85 % of a copy); 16 of 500
-// to 40000 in 8 bits with four query tokens 79 to 84 us, 375 MB at 4.5 to 4.7 TB/s: there half of the issue slots are taken (products,
+// to 40000 in 8 bits with four query tokens 84 us, 375 MB at 4.5 TB/s (79 to 88 by the lengths drawn): there half of the issue slots are taken (products,
 // conversions and exponentials of 16 rows an entry) and the rest is lost to waits that four warps a scheduler, all that the registers
 // allow, do not cover.  64 sequences of 2048: one query token in 8 bits 31 us (65 % of a copy), two in bf16 46, four (16 rows) 60 in bf16, where
-// the fragments of 16 rows and two steps spill (176 bytes a thread), and 37 in 8 bits.  More than 16 rows are slow: their fragments do not stay
+// the fragments of 16 rows and two steps spill (172 bytes a thread), and 37 in 8 bits.  More than 16 rows are slow: their fragments do not stay
 // in registers and are read (in 8 bits also converted) again for every step, eight query tokens (32 rows) 109 us in bf16 and 158 in 8 bits.
 // 8-bit codes widen exactly to fp16 in registers, one conversion for two of them (an SM does 16 of those a cycle, and two for a pair,
 // through bf16, were what bounded the kernel: 118 us for the ragged batch against 109, with one step a unit both times).  The queries go into

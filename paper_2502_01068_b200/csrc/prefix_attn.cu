@@ -26,7 +26,7 @@
 //
 // What bounds it (32 query heads over 8 KV heads of 128; the kernel inside a call, one B200).  64 sequences over 32768 bf16 entries, 256 rows a
 // KV head: 41 us for 134 MB and 34 GFLOP (20.5 and 20.9 us at the rates of a copy and of a large product); a step takes 1700 cycles, of
-// which each softmax warp is busy for 1400 (the tensor pipe is active for 45 % of the kernel; 128 entries a step and one buffer of S, so that
+// which each softmax warp is busy for 1400 (the tensor pipe is active for 44 % of the kernel; 128 entries a step and one buffer of S, so that
 // softmax and products wait for one another, took 50 us when this took 43).  8 x 131072 in 8 bits, 32 rows: 82 us
 // for 269 MB: widening a chunk of V (1300 cycles) and a step's softmax by one warp (1000, twice a chunk and tile) are as long as each other;
 // four copies of the rows in a tile with a quarter of the entries each brought 6 us and cost the merge 10, a third tile of V nothing.
